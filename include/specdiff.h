@@ -405,6 +405,85 @@ size_t sd_plain_em_workspace(sd_target target, int32_t B);
 sd_status sd_run_plain_em(sd_target target, int32_t B, uint64_t seed, float* y_out, void* ws,
                           size_t ws_bytes, sd_stream stream);
 
+/* ------------------------------------------- language-model verification --
+ * The same verification for the drafts of a language model, whose target and
+ * draft laws are softmaxes of logits over a vocabulary and whose target call is
+ * attention over a cache: the paper's block verification of Gaussian steps is
+ * that of tokens with the sums over the vocabulary in closed form.  A round is
+ *   sd_latent_attention (every layer's attention of the K+1 rows of a block) ->
+ *   the caller's products -> sd_verify_tokens;
+ * a prompt goes through sd_latent_attention_expanded, and sd_token_logprobs
+ * reports what the target says of given tokens.
+ *
+ * Element types of these calls; sums, softmax statistics and workspaces are
+ * float32 or float64 whatever the type. */
+typedef enum { SD_TYPE_F32 = 0, SD_TYPE_BF16 = 1, SD_TYPE_F16 = 2 } sd_type;
+
+#define SD_MAX_TOP 32
+#define SD_MAX_VOCAB (1 << 24)
+
+/* Log-probabilities of given tokens, entropy and alternatives of `rows` rows of
+ * logits over a vocabulary of V tokens: with z = logits / temperature,
+ *   lse = log sum_x e^{z_x},  logprob[r][i] = z_{tokens[r][i]} - lse,
+ *   entropy[r] = -sum_x p_x log p_x,  p_x = e^{z_x - lse},
+ * and top_ids, top_logprob[r][0..n_top-1]: the n_top largest logits in falling
+ * order, equal ones by the lower token (tokens of logit -inf come last, with
+ * -inf; past V tokens: -1, -inf).  tokens outside [0, V) have -inf.
+ * A row whose logits are all -inf (a mask that leaves nothing): logprob and lse
+ * -inf, entropy 0.  A row with a NaN or +inf has no law: all its floats are NaN
+ * and its top_ids -1.
+ * logits: rows of V contiguous elements of `type`, row_stride >= V elements
+ * apart, aligned to their element.  tokens, logprob [rows][n_tok] (NULL with
+ * n_tok = 0); entropy, lse [rows], nullable; top_ids, top_logprob
+ * [rows][n_top] (NULL with n_top = 0).  1 <= V <= SD_MAX_VOCAB, 0 <= n_tok,
+ * 0 <= n_top <= SD_MAX_TOP, 2^-60 <= temperature <= 2^60.
+ * ws: >= sd_token_logprobs_workspace bytes, 256-byte aligned. */
+size_t sd_token_logprobs_workspace(int32_t rows, int32_t V, int32_t n_top);
+sd_status sd_token_logprobs(int32_t rows, int32_t V, sd_type type, const void* logits,
+                            int64_t row_stride, double temperature, int32_t n_tok,
+                            const int32_t* tokens, float* logprob, float* entropy, float* lse,
+                            int32_t n_top, int32_t* top_ids, float* top_logprob, void* ws,
+                            size_t ws_bytes, sd_stream stream);
+
+/* Verification of B drafted blocks of tokens (Alg. 6 block / Alg. 2 token) and
+ * the draw of the token that follows the accepted ones.  For chain b with kb[b]
+ * drafts x_1..x_{K_b} (kb is clamped to K; kb <= 0: an inactive chain), p_j and q_j
+ * the laws of draft row j-1 and target row j-1 (softmaxes of logits /
+ * temperature):
+ *   log_ratio[b][j-1] = ell_j = log q_j(x_j) - log p_j(x_j)   (0 for j > K_b);
+ *   block: log alpha_j = min(0, log alpha_{j-1} + ell_j),
+ *          v_j = sum_x max(0, alpha_j q_{j+1}(x) - p_{j+1}(x)),
+ *          h_j = v_j / (v_j + 1 - alpha_j) (1 where alpha_j = 1), h_{K_b} = alpha_{K_b},
+ *          coins eta_j < h_j, tau = 1 + max{j : c_j = 1},
+ *          log_alpha_res = log alpha_{tau-1};
+ *   token: coins eta_j < min(1, e^{ell_j}), tau = first rejected j (K_b + 1 if
+ *          none), log_alpha_res = 0.
+ * tau - 1 drafts are accepted, and token[b] is drawn from the law proportional to
+ * max(0, alpha_res q_tau - p_tau) for tau <= K_b (q_tau where that has no mass
+ * left) and from q_{K_b+1} for tau = K_b + 1: the lowest x whose cumulative sum
+ * exceeds u times the whole, in float64.
+ * eta_j = uniforms[b][j-1] and u = uniforms[b][K] (float64 in (0, 1)), or with
+ * uniforms NULL eta_j = uniform j-1 of (b, round[b], COIN) and u = ((w0 >> 6) 2^26
+ * + (w1 >> 6) + 1/2) 2^-52 of the first words of (b, round[b], USAMPLE); round
+ * is not read, and may be NULL, where uniforms are given.
+ * A draft outside [0, V), of target probability 0, or whose target or draft row
+ * has no law (a NaN or +inf) is rejected (log_ratio -inf or NaN); a draft of draft
+ * probability 0 and target probability > 0 is accepted.  token is -1 where no law
+ * is left to draw from (target row all -inf; a NaN or +inf), and for inactive
+ * chains, whose tau, log_alpha_res and coins are 0.
+ * draft [B][K][V] and target [B][K+1][V] views of `type` (rows contiguous,
+ * aligned to their element; rows past kb are not read); tokens [B][K]; tau,
+ * token, log_alpha_res [B], log_ratio [B][K]; coins [B] bitmask of c_1..c_K
+ * (nullable).  ws: >= sd_verify_tokens_workspace bytes, 256-byte aligned. */
+size_t sd_verify_tokens_workspace(int32_t B, int32_t K, int32_t V);
+sd_status sd_verify_tokens(int32_t B, int32_t K, int32_t V, sd_verify_mode mode, sd_type type,
+                           double temperature, const void* draft, sd_stride ds,
+                           const void* target, sd_stride ts, const int32_t* tokens,
+                           const int32_t* kb, const double* uniforms, const uint32_t* round,
+                           uint64_t seed, int32_t* tau, int32_t* token, float* log_alpha_res,
+                           float* log_ratio, uint64_t* coins, void* ws, size_t ws_bytes,
+                           sd_stream stream);
+
 /* ------------------------------------------------------------- profiling --
  * Per-kernel timing with HIP events recorded around every launch on the
  * launch's own stream.  sd_profile_enable(1) clears and starts collection,

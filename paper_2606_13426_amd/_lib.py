@@ -17,7 +17,9 @@ SD_FP32, SD_BF16 = 0, 1
 SD_USAMPLE_EXACT, SD_USAMPLE_PAPER = 0, 1
 SD_RESIDUAL_DECOMPOSITION, SD_RESIDUAL_REFLECTION = 0, 1
 SD_DRAFTER_FREE, SD_DRAFTER_FROZEN = 0, 1
+SD_TYPE_F32, SD_TYPE_BF16, SD_TYPE_F16 = 0, 1, 2
 SD_MAX_BLOCK = 64
+SD_MAX_TOP, SD_MAX_VOCAB = 32, 1 << 24
 TAG_INIT, TAG_DRAFT, TAG_COIN, TAG_USAMPLE, TAG_RESID, TAG_TARGET = 1, 2, 3, 4, 5, 6
 
 c_int32, c_int64, c_uint32, c_uint64 = ctypes.c_int32, ctypes.c_int64, ctypes.c_uint32, ctypes.c_uint64
@@ -96,6 +98,12 @@ SIGNATURES = [
                                    ctypes.POINTER(sd_sampler_view)]),
     ("sd_plain_em_workspace", c_size_t, [P, c_int32]),
     ("sd_run_plain_em", c_int32, [P, c_int32, c_uint64, P, P, c_size_t, P]),
+    ("sd_token_logprobs_workspace", c_size_t, [c_int32, c_int32, c_int32]),
+    ("sd_token_logprobs", c_int32, [c_int32, c_int32, c_int32, P, c_int64, c_double, c_int32, P, P, P, P, c_int32,
+                                    P, P, P, c_size_t, P]),
+    ("sd_verify_tokens_workspace", c_size_t, [c_int32, c_int32, c_int32]),
+    ("sd_verify_tokens", c_int32, [c_int32, c_int32, c_int32, c_int32, c_int32, c_double, P, S, P, S, P, P, P, P,
+                                   c_uint64, P, P, P, P, P, P, c_size_t, P]),
     ("sd_profile_enable", c_int32, [c_int32]),
     ("sd_profile_only", c_int32, [c_char_p]),
     ("sd_profile_every", c_int32, [c_int32]),
@@ -389,6 +397,111 @@ def sd_run_plain_em(target, B, seed, y_out=None, ws=None, device="cuda"):
     _check(load().sd_run_plain_em(target.handle, B, seed, _p(y_out), _p(ws), ws.numel(), _stream()),
            "sd_run_plain_em")
     return y_out
+
+
+def _type(t):
+    import torch
+    types = {torch.float32: SD_TYPE_F32, torch.bfloat16: SD_TYPE_BF16, torch.float16: SD_TYPE_F16}
+    if t.dtype not in types:
+        raise SpecDiffError(SD_EINVAL, f"unsupported element type {t.dtype}")
+    return types[t.dtype]
+
+
+def _need(cond, name, what):
+    if not cond:
+        raise SpecDiffError(SD_EINVAL, f"{name}: {what}")
+
+
+def _operands(name, dtypes, tensors):
+    """Refuses operands that are not on the current device or not of the stated type."""
+    import torch
+    dev = torch.cuda.current_device() if torch.cuda.is_available() else None
+    for what, t in tensors.items():
+        if t is None:
+            continue
+        _need(t.device.type == "cuda" and t.device.index == dev, name,
+              f"{what} is on {t.device}, not on the current GPU")
+        want = dtypes.get(what)
+        _need(want is None or t.dtype == want, name, f"{what} must be {want}, not {t.dtype}")
+
+
+def _workspace(ws, need, device):
+    import torch
+    return torch.empty(need, dtype=torch.uint8, device=device) if ws is None else ws
+
+
+def sd_token_logprobs_workspace(rows, V, n_top=0):
+    return load().sd_token_logprobs_workspace(rows, V, n_top)
+
+
+def sd_token_logprobs(logits, tokens=None, n_top=0, temperature=1.0, ws=None):
+    """logits [rows][V] (float32, bfloat16 or float16; rows contiguous); tokens [rows] or [rows][n_tok] int32.
+
+    Returns dict of device tensors lse, entropy [rows] and, where asked for, logprob (as
+    tokens) and top_ids, top_logprobs [rows][n_top].
+    """
+    import torch
+    name, i32 = "sd_token_logprobs", torch.int32
+    _need(logits.dim() == 2 and (logits.stride(1) == 1 or logits.shape[1] == 1), name, "logits must be [rows][V] with contiguous rows")
+    rows, V = logits.shape
+    _operands(name, dict(tokens=i32, ws=torch.uint8), dict(logits=logits, tokens=tokens, ws=ws))
+    n_tok = 0
+    if tokens is not None:
+        _need(tokens.dim() in (1, 2) and tokens.shape[0] == rows and tokens.is_contiguous(), name,
+              "tokens must be contiguous [rows] or [rows][n_tok]")
+        n_tok = 1 if tokens.dim() == 1 else tokens.shape[1]
+    f32 = dict(dtype=torch.float32, device=logits.device)
+    out = dict(lse=torch.empty(rows, **f32), entropy=torch.empty(rows, **f32))
+    if tokens is not None:
+        out["logprob"] = torch.empty(tokens.shape, **f32)
+    if n_top > 0:
+        out["top_ids"] = torch.empty(rows, n_top, dtype=i32, device=logits.device)
+        out["top_logprobs"] = torch.empty(rows, n_top, **f32)
+    ws = _workspace(ws, sd_token_logprobs_workspace(rows, V, n_top), logits.device)
+    _check(load().sd_token_logprobs(rows, V, _type(logits), _p(logits), logits.stride(0) if rows > 1 else V,
+                                    float(temperature), n_tok, _p(tokens), _p(out.get("logprob")),
+                                    _p(out["entropy"]), _p(out["lse"]), n_top, _p(out.get("top_ids")),
+                                    _p(out.get("top_logprobs")), _p(ws), ws.numel(), _stream()), name)
+    return out
+
+
+def sd_verify_tokens_workspace(B, K, V):
+    return load().sd_verify_tokens_workspace(B, K, V)
+
+
+def sd_verify_tokens(draft, target, tokens, kb, uniforms=None, rnd=None, seed=0, mode=SD_BLOCK, temperature=1.0,
+                     ws=None, out=None):
+    """draft [B][K][V], target [B][K+1][V] logits of one type (rows contiguous); tokens [B][K],
+    kb [B] int32; uniforms [B][K+1] float64, or rnd [B] int32/uint32 and the seed.
+
+    Returns dict of device tensors tau, token [B] int32, log_alpha_res [B], log_ratio [B][K]
+    float32, coins [B] int64.
+    """
+    import torch
+    name, i32, f32 = "sd_verify_tokens", torch.int32, torch.float32
+    _need(draft.dim() == 3 and target.dim() == 3, name, "draft and target must be [B][K][V] and [B][K+1][V]")
+    B, K, V = draft.shape
+    _need(tuple(target.shape) == (B, K + 1, V), name, "target must be [B][K+1][V]")
+    _need(draft.dtype == target.dtype, name, "draft and target must be of one type")
+    _operands(name, dict(tokens=i32, kb=i32, uniforms=torch.float64, ws=torch.uint8),
+              dict(draft=draft, target=target, tokens=tokens, kb=kb, uniforms=uniforms, rnd=rnd, ws=ws))
+    _need(tuple(tokens.shape) == (B, K) and tokens.is_contiguous(), name, "tokens must be contiguous [B][K]")
+    _need(tuple(kb.shape) == (B,) and kb.is_contiguous(), name, "kb must be contiguous [B]")
+    _need(uniforms is None or (tuple(uniforms.shape) == (B, K + 1) and uniforms.is_contiguous()), name,
+          "uniforms must be contiguous [B][K+1]")
+    _need(rnd is None or (tuple(rnd.shape) == (B,) and rnd.element_size() == 4 and rnd.is_contiguous()), name,
+          "rnd must be contiguous [B] of 32 bits")
+    if out is None:
+        out = dict(tau=torch.empty(B, dtype=i32, device=draft.device), token=torch.empty(B, dtype=i32, device=draft.device),
+                   log_alpha_res=torch.empty(B, dtype=f32, device=draft.device),
+                   log_ratio=torch.empty(B, K, dtype=f32, device=draft.device),
+                   coins=torch.empty(B, dtype=torch.int64, device=draft.device))
+    ws = _workspace(ws, sd_verify_tokens_workspace(B, K, V), draft.device)
+    _check(load().sd_verify_tokens(B, K, V, mode, _type(draft), float(temperature), _p(draft), stride3(draft),
+                                   _p(target), stride3(target), _p(tokens), _p(kb), _p(uniforms), _p(rnd), seed,
+                                   _p(out["tau"]), _p(out["token"]), _p(out["log_alpha_res"]), _p(out["log_ratio"]),
+                                   _p(out.get("coins")), _p(ws), ws.numel(), _stream()), name)
+    return out
 
 
 def sd_profile_enable(on=True):

@@ -1100,6 +1100,74 @@ sd_status sd_run_plain_em(sd_target target, int32_t B, uint64_t seed, float* y_o
   return SD_OK;
 }
 
+// ------------------------------------------- language-model verification --
+static bool type_ok(sd_type t) { return t == SD_TYPE_F32 || t == SD_TYPE_BF16 || t == SD_TYPE_F16; }
+static size_t type_size(sd_type t) { return t == SD_TYPE_F32 ? 4 : 2; }
+static bool aligned(const void* p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
+static bool temperature_ok(double t) { return t >= 0x1p-60 && t <= 0x1p60; }
+constexpr int64_t kMaxGroups = ((int64_t)1 << 31) - 1;  // workgroups of a launch
+
+size_t sd_token_logprobs_workspace(int32_t rows, int32_t V, int32_t n_top) {
+  if (rows < 1 || V < 1 || V > SD_MAX_VOCAB || n_top < 0 || n_top > SD_MAX_TOP) return 0;
+  return logprobs_ws_bytes(rows, V, n_top);
+}
+
+sd_status sd_token_logprobs(int32_t rows, int32_t V, sd_type type, const void* logits, int64_t row_stride,
+                            double temperature, int32_t n_tok, const int32_t* tokens, float* logprob, float* entropy,
+                            float* lse, int32_t n_top, int32_t* top_ids, float* top_logprob, void* ws,
+                            size_t ws_bytes, sd_stream stream) {
+  SD_CHECK_ARG(rows >= 1, "sd_token_logprobs: rows = %d < 1", rows);
+  SD_CHECK_ARG(V >= 1 && V <= SD_MAX_VOCAB, "sd_token_logprobs: V = %d not in [1, %d]", V, SD_MAX_VOCAB);
+  SD_CHECK_ARG(type_ok(type), "sd_token_logprobs: unknown type");
+  SD_CHECK_ARG(n_tok >= 0, "sd_token_logprobs: n_tok = %d < 0", n_tok);
+  SD_CHECK_ARG(n_top >= 0 && n_top <= SD_MAX_TOP, "sd_token_logprobs: n_top = %d not in [0, %d]", n_top, SD_MAX_TOP);
+  SD_CHECK_ARG(temperature_ok(temperature), "sd_token_logprobs: temperature must be in [2^-60, 2^60]");
+  SD_CHECK_ARG(logits && ws, "sd_token_logprobs: logits and ws must be non-NULL");
+  SD_CHECK_ARG(n_tok == 0 || (tokens && logprob), "sd_token_logprobs: tokens and logprob must be non-NULL with n_tok > 0");
+  SD_CHECK_ARG(n_top == 0 || (top_ids && top_logprob), "sd_token_logprobs: top_ids and top_logprob must be non-NULL with n_top > 0");
+  SD_CHECK_ARG(row_stride >= V, "sd_token_logprobs: row stride must be >= V = %d", V);
+  SD_CHECK_ARG(aligned(logits, type_size(type)), "sd_token_logprobs: logits must be aligned to their element");
+  const size_t need = logprobs_ws_bytes(rows, V, n_top);
+  SD_CHECK_ARG(ws_bytes >= need, "sd_token_logprobs: workspace %zu < %zu bytes", ws_bytes, need);
+  SD_CHECK_ARG(aligned(ws, 256), "sd_token_logprobs: workspace must be 256-byte aligned");
+  SD_CHECK_ARG(logprobs_groups(rows, V) <= kMaxGroups, "sd_token_logprobs: too many rows for one call");
+  SD_HIP(logprobs_launch(rows, V, type, logits, row_stride, temperature, n_tok, tokens, logprob, entropy, lse, n_top,
+                         top_ids, top_logprob, ws, (hipStream_t)stream));
+  return SD_OK;
+}
+
+size_t sd_verify_tokens_workspace(int32_t B, int32_t K, int32_t V) {
+  if (B < 1 || K < 1 || K > SD_MAX_BLOCK || V < 1 || V > SD_MAX_VOCAB) return 0;
+  return verify_tokens_ws_bytes(B, K, V);
+}
+
+sd_status sd_verify_tokens(int32_t B, int32_t K, int32_t V, sd_verify_mode mode, sd_type type, double temperature,
+                           const void* draft, sd_stride ds, const void* target, sd_stride ts, const int32_t* tokens,
+                           const int32_t* kb, const double* uniforms, const uint32_t* round, uint64_t seed,
+                           int32_t* tau, int32_t* token, float* log_alpha_res, float* log_ratio, uint64_t* coins,
+                           void* ws, size_t ws_bytes, sd_stream stream) {
+  SD_CHECK_ARG(B >= 1, "sd_verify_tokens: B = %d < 1", B);
+  SD_CHECK_ARG(K >= 1 && K <= SD_MAX_BLOCK, "sd_verify_tokens: K = %d not in [1, %d]", K, SD_MAX_BLOCK);
+  SD_CHECK_ARG(V >= 1 && V <= SD_MAX_VOCAB, "sd_verify_tokens: V = %d not in [1, %d]", V, SD_MAX_VOCAB);
+  SD_CHECK_ARG(mode == SD_BLOCK || mode == SD_TOKEN, "sd_verify_tokens: unknown mode");
+  SD_CHECK_ARG(type_ok(type), "sd_verify_tokens: unknown type");
+  SD_CHECK_ARG(temperature_ok(temperature), "sd_verify_tokens: temperature must be in [2^-60, 2^60]");
+  SD_CHECK_ARG(draft && target && tokens && kb && tau && token && log_alpha_res && log_ratio && ws,
+               "sd_verify_tokens: NULL pointer argument");
+  SD_CHECK_ARG(uniforms || round, "sd_verify_tokens: one of uniforms and round must be non-NULL");
+  SD_CHECK_ARG(stride_ok(ds, V, K), "sd_verify_tokens: draft stride too small for [B][K][V]");
+  SD_CHECK_ARG(stride_ok(ts, V, K + 1), "sd_verify_tokens: target stride too small for [B][K+1][V]");
+  SD_CHECK_ARG(aligned(draft, type_size(type)) && aligned(target, type_size(type)),
+               "sd_verify_tokens: draft and target must be aligned to their element");
+  const size_t need = verify_tokens_ws_bytes(B, K, V);
+  SD_CHECK_ARG(ws_bytes >= need, "sd_verify_tokens: workspace %zu < %zu bytes", ws_bytes, need);
+  SD_CHECK_ARG(aligned(ws, 256), "sd_verify_tokens: workspace must be 256-byte aligned");
+  SD_CHECK_ARG(verify_tokens_groups(B, K, V) <= kMaxGroups, "sd_verify_tokens: too many rows for one call");
+  SD_HIP(verify_tokens_launch(B, K, V, mode, type, temperature, draft, ds, target, ts, tokens, kb, uniforms, round,
+                              seed, tau, token, log_alpha_res, log_ratio, coins, ws, (hipStream_t)stream));
+  return SD_OK;
+}
+
 // ------------------------------------------------------------- profiling --
 sd_status sd_profile_enable(int32_t on) {
   std::lock_guard<std::mutex> lk(g_prof_mu);

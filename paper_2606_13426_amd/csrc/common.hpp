@@ -283,6 +283,22 @@ hipError_t philox_normals_launch(uint64_t seed, uint32_t chain, uint32_t rnd, ui
 // instructions on registers; one float per wavefront to out ([blocks][4]).
 hipError_t mfma_loop_launch(int blocks, int iters, float* out, hipStream_t s);
 
+// ----------------------------------------------- language-model verification --
+// Workgroups of the widest launch, workspace and launches of sd_token_logprobs
+// and sd_verify_tokens.
+int64_t logprobs_groups(int rows, int V);
+size_t logprobs_ws_bytes(int rows, int V, int n_top);
+hipError_t logprobs_launch(int rows, int V, sd_type type, const void* x, int64_t ld, double temperature, int n_tok,
+                           const int32_t* tokens, float* logprob, float* entropy, float* lse, int n_top,
+                           int32_t* top_ids, float* top_logprob, void* ws, hipStream_t s);
+int64_t verify_tokens_groups(int B, int K, int V);
+size_t verify_tokens_ws_bytes(int B, int K, int V);
+hipError_t verify_tokens_launch(int B, int K, int V, int mode, sd_type type, double temperature, const void* draft,
+                                sd_stride ds, const void* target, sd_stride ts, const int32_t* tokens,
+                                const int32_t* kb, const double* uniforms, const uint32_t* round, uint64_t seed,
+                                int32_t* tau, int32_t* token, float* log_alpha_res, float* log_ratio,
+                                uint64_t* coins, void* ws, hipStream_t s);
+
 inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 
 // Whether a kernel that writes a block of `bytes` of draft rows uses

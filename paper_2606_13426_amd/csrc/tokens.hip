@@ -1,0 +1,920 @@
+// Laws over a vocabulary: log-probabilities of given tokens with entropy and
+// alternatives, and the verification of drafted tokens (Alg. 6 / Alg. 2) with the
+// draw of the next one.
+//
+// All of it streams rows of logits once or twice (logits.hpp): a workgroup holds
+// a slice of a row in registers, so its maximum, sum, entropy term and largest
+// elements come from one read, and a second kernel joins a row's slices.  With
+// z = x / T and m the slice's maximum,
+//   S = sum e^{(x - m) / T},   U = sum (x - m) e^{(x - m) / T},
+// differences and exponentials in float32 (one instruction each), the sums of a
+// thread's elements too; everything across threads and slices is float64.
+#include <type_traits>
+
+#include "common.hpp"
+#include "logits.hpp"
+#include "philox.hpp"
+#include "wavered.hpp"
+
+namespace sd {
+namespace {
+
+using namespace logits;
+
+// What a slice says of its part of a row.
+struct Part {
+  double S, U;  // sums against the slice's own maximum
+  float m;      // -inf: nothing but -inf in it
+  float pad;
+};
+
+// ------------------------------------------------------------ alternatives --
+// Elements are ordered by keys: the value's bits in an order-preserving form
+// above, the complement of the position below, so equal values fall by position
+// and no two elements share a key.  0 stands for no element.
+__device__ __forceinline__ uint64_t key_of(float x, int pos) {
+  const uint32_t b = __builtin_bit_cast(uint32_t, x + 0.0f);  // -0 and 0 are equal
+  const uint32_t o = b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+  return ((uint64_t)o << 32) | (uint32_t)~pos;
+}
+__device__ __forceinline__ int key_pos(uint64_t k) { return (int)~(uint32_t)k; }
+__device__ __forceinline__ float key_value(uint64_t k) {
+  const uint32_t o = (uint32_t)(k >> 32);
+  return __builtin_bit_cast(float, o ^ ((uint32_t)((int32_t)~o >> 31) | 0x80000000u));
+}
+template <int CTRL>
+__device__ __forceinline__ uint64_t dpp(uint64_t v) {
+  return ((uint64_t)dpp32<CTRL>((uint32_t)(v >> 32)) << 32) | dpp32<CTRL>((uint32_t)v);
+}
+__device__ __forceinline__ uint64_t max64(uint64_t a, uint64_t b) { return a > b ? a : b; }
+__device__ __forceinline__ uint64_t lane_key(uint64_t v, int i) {
+  return ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), i) << 32) |
+         (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, i);
+}
+__device__ __forceinline__ uint64_t wave_max(uint64_t v) {
+  v = max64(v, dpp<kDppXor1>(v));
+  v = max64(v, dpp<kDppXor2>(v));
+  v = max64(v, dpp<kDppHalfMirror>(v));
+  v = max64(v, dpp<kDppMirror>(v));
+  v = max64(v, (uint64_t)__shfl_xor((unsigned long long)v, 16));
+  return max64(v, (uint64_t)__shfl_xor((unsigned long long)v, 32));
+}
+
+constexpr int kPool = 1024;  // candidates a workgroup orders at once
+struct TopLds {
+  uint64_t group[64];
+  uint64_t pool[kPool];
+  uint64_t bound;
+  int count;
+};
+
+// The keys of pool[0..c) in falling order to out[0..n) (fewer than n: the rest 0).
+// Every key counts those above it; c is mostly little more than n.
+__device__ __forceinline__ void write_ranked(const uint64_t* pool, int c, int n, uint64_t* out) {
+  for (int i = threadIdx.x; i < c; i += kThreads) {
+    const uint64_t k = pool[i];
+    int above = 0;
+    for (int j = 0; j < c; ++j) above += pool[j] > k;
+    if (above < n) out[above] = k;
+  }
+  for (int i = c + (int)threadIdx.x; i < n; i += kThreads) out[i] = 0;
+}
+
+// The n largest of the slice x to out[0..n) in falling order, 0 past its elements.
+// The largest keys of 64 groups of four threads give a bound: n groups hold a key
+// at or above the n-th largest of them, so the n largest elements are among those
+// not below it, which are few.  Where they do not fit the pool (an order made for
+// it) the n largest are taken one after another.
+template <class T, int E>
+__device__ void slice_top(const float (&x)[E], int slice, int a, int V, int n, TopLds& sm, uint64_t* out) {
+  const int t = threadIdx.x;
+  float best = x[0];
+#pragma unroll
+  for (int i = 1; i < E; ++i) best = fmaxf(best, x[i]);
+  int bi = 0;
+#pragma unroll
+  for (int i = E - 1; i >= 0; --i) {
+    const int pos = position<T, E>(slice, a, i);
+    if (x[i] == best && pos >= 0) bi = i;
+  }
+  const int bpos = position<T, E>(slice, a, bi);
+  const uint64_t mine = bpos >= 0 && bpos < V ? key_of(best, bpos) : 0;
+  uint64_t g = max64(mine, dpp<kDppXor1>(mine));
+  g = max64(g, dpp<kDppXor2>(g));
+  if ((t & 3) == 0) sm.group[t >> 2] = g;
+  if (t == 0) sm.count = 0;
+  __syncthreads();
+  if (t < 64) {
+    const uint64_t k = sm.group[t];
+    int above = 0;
+    for (int i = 0; i < 64; ++i) above += lane_key(k, i) > k;
+    // groups without an element share the key 0: their rank is the first of them
+    const uint64_t at = __ballot(above == n - 1);
+    const uint64_t b = at ? lane_key(k, __ffsll((unsigned long long)at) - 1) : 0;
+    if (t == 0) sm.bound = b;
+  }
+  __syncthreads();
+  const uint64_t bound = sm.bound;
+  if (mine != 0 && mine >= bound) {
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      const int pos = position<T, E>(slice, a, i);
+      if (pos < 0 || pos >= V) continue;
+      const uint64_t k = key_of(x[i], pos);
+      if (k < bound) continue;
+      const int c = atomicAdd(&sm.count, 1);
+      if (c < kPool) sm.pool[c] = k;
+    }
+  }
+  __syncthreads();
+  const int c = sm.count;
+  if (c <= kPool) {
+    write_ranked(sm.pool, c, n, out);
+    return;
+  }
+  uint64_t last = ~0ull;
+  for (int r = 0; r < n; ++r) {
+    uint64_t k = 0;
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      const int pos = position<T, E>(slice, a, i);
+      const uint64_t q = pos >= 0 && pos < V ? key_of(x[i], pos) : 0;
+      if (q < last) k = max64(k, q);
+    }
+    k = wave_max(k);
+    __syncthreads();
+    if ((t & 63) == 0) sm.group[t >> 6] = k;
+    __syncthreads();
+    k = max64(max64(sm.group[0], sm.group[1]), max64(sm.group[2], sm.group[3]));
+    if (t == 0) out[r] = k;
+    last = k;
+  }
+}
+
+// ------------------------------------------------------------------- sums --
+// Sums of a workgroup's slice: m its maximum, S and (ENT) U.
+template <class T, int E, bool ENT>
+__device__ __forceinline__ Part slice_sums(const float (&x)[E], float c, double* red, float* redm) {
+  const int t = threadIdx.x, w = t >> 6;
+  float m = x[0];
+#pragma unroll
+  for (int i = 1; i < E; ++i) m = fmaxf(m, x[i]);
+  m = (float)group_max((double)m, 64);
+  if ((t & 63) == 0) redm[w] = m;
+  __syncthreads();
+  m = fmaxf(fmaxf(redm[0], redm[1]), fmaxf(redm[2], redm[3]));
+  const float ref = m == -INFINITY ? 0.f : m;
+  float s[4] = {0.f, 0.f, 0.f, 0.f}, u[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    const float d = x[i] - ref;
+    const float e = __builtin_amdgcn_exp2f(d * c);
+    s[i & 3] += e;
+    if (ENT) u[i & 3] = __fmaf_rn(e, fmaxf(d, kLowest), u[i & 3]);
+  }
+  const double S = wave_sum((double)s[0] + s[1] + ((double)s[2] + s[3]));
+  double U = 0.0;
+  if (ENT) U = wave_sum((double)u[0] + u[1] + ((double)u[2] + u[3]));
+  if ((t & 63) == 0) {
+    red[w] = S;
+    if (ENT) red[4 + w] = U;
+  }
+  __syncthreads();
+  Part p;
+  p.S = red[0] + red[1] + (red[2] + red[3]);
+  p.U = ENT ? red[4] + red[5] + (red[6] + red[7]) : 0.0;
+  p.m = m;
+  p.pad = 0.f;
+  return p;
+}
+
+template <class T, int E>
+__global__ __launch_bounds__(kThreads) void logprobs_slice_kernel(const typename T::raw* __restrict__ x, int64_t ld,
+                                                                  int V, int S, float c, int n,
+                                                                  Part* __restrict__ parts,
+                                                                  uint64_t* __restrict__ keys) {
+  __shared__ double red[8];
+  __shared__ float redm[4];
+  __shared__ TopLds top;
+  const int64_t id = blockIdx.x;
+  const int slice = (int)(id % S);
+  const typename T::raw* p = x + (id / S) * ld;
+  const int a = lead<T>(p);
+  float v[E];
+  load_slice<T, E, true>(p, a, V, slice, v);
+  const Part r = slice_sums<T, E, true>(v, c, red, redm);
+  if (threadIdx.x == 0) parts[id] = r;
+  if (n > 0) slice_top<T, E>(v, slice, a, V, n, top, keys + id * n);
+}
+
+// One workgroup a row: the slices' sums, the given tokens and the alternatives.
+template <class T>
+__global__ __launch_bounds__(kThreads) void logprobs_join_kernel(
+    const typename T::raw* __restrict__ x, int64_t ld, int V, int S, double inv_t, int n_tok,
+    const int32_t* __restrict__ tokens, float* __restrict__ logprob, float* __restrict__ entropy,
+    float* __restrict__ lse, int n, int32_t* __restrict__ ids, float* __restrict__ tops,
+    const Part* __restrict__ parts, const uint64_t* __restrict__ keys) {
+  __shared__ double red[8];
+  __shared__ float redm[4];
+  __shared__ TopLds top;
+  __shared__ uint64_t best[SD_MAX_TOP];
+  const int t = threadIdx.x, w = t >> 6;
+  const int64_t row = blockIdx.x;
+  const Part* p = parts + row * S;
+  float m = -INFINITY;
+  for (int i = t; i < S; i += kThreads) m = fmaxf(m, p[i].m);
+  m = (float)group_max((double)m, 64);
+  if ((t & 63) == 0) redm[w] = m;
+  __syncthreads();
+  m = fmaxf(fmaxf(redm[0], redm[1]), fmaxf(redm[2], redm[3]));
+  double s = 0.0, u = 0.0;
+  for (int i = t; i < S; i += kThreads) {
+    const Part q = p[i];
+    if (q.m == -INFINITY && q.S == 0.0) continue;  // nothing in it (a NaN leaves S NaN)
+    const double d = (double)q.m - (double)m, f = exp(d * inv_t);
+    s += q.S * f;
+    u += f == 0.0 ? 0.0 : f * (q.U + d * q.S);
+  }
+  s = wave_sum(s);
+  u = wave_sum(u);
+  if ((t & 63) == 0) {
+    red[w] = s;
+    red[4 + w] = u;
+  }
+  __syncthreads();
+  s = red[0] + red[1] + (red[2] + red[3]);
+  u = red[4] + red[5] + (red[6] + red[7]);
+  const bool law = s > 0.0 && isfinite(s), none = s == 0.0;
+  const double logs = log(s);
+  auto logp = [&](float v) {
+    return law ? (float)(((double)v - (double)m) * inv_t - logs) : none ? -INFINITY : NAN;
+  };
+  if (t == 0) {
+    if (lse) lse[row] = law ? (float)((double)m * inv_t + logs) : none ? -INFINITY : NAN;
+    if (entropy) entropy[row] = law ? (float)(logs - u * inv_t / s) : none ? 0.f : NAN;
+  }
+  for (int i = t; i < n_tok; i += kThreads) {
+    const int tok = tokens[row * n_tok + i];
+    logprob[row * n_tok + i] =
+        logp(tok >= 0 && tok < V ? T::value(x[row * ld + tok]) : -INFINITY);
+  }
+  if (n == 0) return;
+  // The slices' lists are ordered: the n-th largest of their first q elements, q
+  // the least with S q >= n, bounds the n largest of all from below.
+  const uint64_t* k = keys + row * S * n;
+  const int q = (n + S - 1) / S, pool = min(S * q, kPool);
+  for (int i = t; i < pool; i += kThreads) top.pool[i] = k[(int64_t)(i / q) * n + i % q];
+  if (t == 0) {
+    top.count = 0;
+    top.bound = 0;
+  }
+  __syncthreads();
+  for (int i = t; i < pool; i += kThreads) {
+    const uint64_t me = top.pool[i];
+    int above = 0;
+    for (int j = 0; j < pool; ++j) above += top.pool[j] > me;
+    if (above == n - 1) top.bound = me;
+  }
+  __syncthreads();
+  const uint64_t bound = top.bound > 0 ? top.bound : 1;
+  __syncthreads();
+  for (int i = t; i < S; i += kThreads)
+    for (int j = 0; j < n; ++j) {
+      const uint64_t me = k[(int64_t)i * n + j];
+      if (me < bound) break;
+      const int c = atomicAdd(&top.count, 1);
+      if (c < kPool) top.pool[c] = me;
+    }
+  __syncthreads();
+  if (top.count <= kPool) {
+    write_ranked(top.pool, top.count, n, best);
+  } else {
+    // more than kPool lists, whose heads gave a weak bound: one after another
+    uint64_t last = ~0ull;
+    for (int r = 0; r < n; ++r) {
+      uint64_t me = 0;
+      for (int64_t i = t; i < (int64_t)S * n; i += kThreads)
+        if (k[i] < last) me = max64(me, k[i]);
+      me = wave_max(me);
+      __syncthreads();
+      if ((t & 63) == 0) top.group[w] = me;
+      __syncthreads();
+      last = max64(max64(top.group[0], top.group[1]), max64(top.group[2], top.group[3]));
+      if (t == 0) best[r] = last;
+    }
+  }
+  __syncthreads();
+  if (t < n) {
+    const uint64_t me = best[t];
+    const bool real = me != 0 && (law || none);
+    ids[row * n + t] = real ? key_pos(me) : -1;
+    tops[row * n + t] = law || none ? (me != 0 ? logp(key_value(me)) : -INFINITY) : NAN;
+  }
+}
+
+// ------------------------------------------------------------ verification --
+// Rows of a chain in the order the workspace holds them: target rows 0..K, then
+// draft rows 0..K-1.
+struct Rows {
+  const void *draft, *target;
+  sd_stride ds, ts;
+};
+template <class T>
+__device__ __forceinline__ const typename T::raw* row_of(const Rows& r, int b, int i, int K) {
+  return i <= K ? reinterpret_cast<const typename T::raw*>(r.target) + (int64_t)b * r.ts.chain + (int64_t)i * r.ts.row
+                : reinterpret_cast<const typename T::raw*>(r.draft) + (int64_t)b * r.ds.chain +
+                      (int64_t)(i - K - 1) * r.ds.row;
+}
+__device__ __forceinline__ int drafts(const int32_t* kb, int b, int K) { return min(max(kb[b], 0), K); }
+
+// A row's law: e^{(x - m) c} / S with c = log2(e) / T, log S in float64.  S is 0 where the row is all
+// -inf and NaN where it has no law.
+struct Law {
+  double S, logS;
+  float m, pad;
+};
+struct Mass {
+  double q, p;
+};
+
+// Sums of every valid row's slices.
+template <class T, int E>
+__global__ __launch_bounds__(kThreads) void verify_sums_kernel(Rows rows, int K, int V, int S, float c,
+                                                               const int32_t* __restrict__ kb,
+                                                               Part* __restrict__ parts) {
+  __shared__ double red[8];
+  __shared__ float redm[4];
+  const int64_t id = blockIdx.x;
+  const int slice = (int)(id % S), r = (int)(id / S), b = r / (2 * K + 1), i = r % (2 * K + 1);
+  const int n = drafts(kb, b, K);
+  if (n == 0 || (i <= K ? i > n : i - K - 1 >= n)) return;
+  const typename T::raw* p = row_of<T>(rows, b, i, K);
+  float v[E];
+  load_slice<T, E>(p, lead<T>(p), V, slice, v);
+  const Part q = slice_sums<T, E, false>(v, c, red, redm);
+  if (threadIdx.x == 0) parts[id] = q;
+}
+
+// Token verification's tau from the coins of n drafts.
+__device__ __forceinline__ int first_rejected(uint64_t cm, int n) {
+  const uint64_t rej = ~cm & (n >= 64 ? ~0ull : (1ull << n) - 1ull);
+  return rej ? __ffsll((unsigned long long)rej) : n + 1;
+}
+
+// One wavefront a chain: the rows' laws, the log-ratios, log alpha_j; with token
+// verification also the decision.
+template <class T>
+__global__ __launch_bounds__(64) void verify_join_kernel(Rows rows, int K, int V, int S, int mode, double inv_t,
+                                                         const int32_t* __restrict__ tokens,
+                                                         const int32_t* __restrict__ kb,
+                                                         const double* __restrict__ uniforms,
+                                                         const uint32_t* __restrict__ round, uint64_t seed,
+                                                         const Part* __restrict__ parts, Law* __restrict__ laws,
+                                                         double* __restrict__ la, int32_t* __restrict__ tau,
+                                                         float* __restrict__ lar, float* __restrict__ ratio,
+                                                         uint64_t* __restrict__ coins) {
+  const int b = blockIdx.x, lane = threadIdx.x;
+  const int n = drafts(kb, b, K);
+  double qx = NAN, px = NAN;  // log q_j(x_j), log p_j(x_j) of draft j = lane + 1
+  const int tok = lane < n ? tokens[(int64_t)b * K + lane] : -1;
+  const bool known = tok >= 0 && tok < V;
+  for (int i = lane; i < 2 * K + 1; i += 64) {
+    const int j = i <= K ? i : i - K - 1;
+    if (n == 0 || (i <= K ? j > n : j >= n)) continue;
+    const Part* p = parts + ((int64_t)b * (2 * K + 1) + i) * S;
+    float m = -INFINITY;
+    for (int s = 0; s < S; ++s) m = fmaxf(m, p[s].m);
+    double sum = 0.0;
+    for (int s = 0; s < S; ++s)
+      if (!(p[s].m == -INFINITY && p[s].S == 0.0)) sum += p[s].S * exp(((double)p[s].m - (double)m) * inv_t);
+    laws[(int64_t)b * (2 * K + 1) + i] = Law{sum, log(sum), m, 0.f};
+  }
+  __syncthreads();
+  if (lane < n) {
+    const Law q = laws[(int64_t)b * (2 * K + 1) + lane], p = laws[(int64_t)b * (2 * K + 1) + K + 1 + lane];
+    auto logp = [&](const Law& l, const typename T::raw* row) {
+      if (l.S == 0.0) return -(double)INFINITY;
+      if (!(l.S > 0.0) || !isfinite(l.S)) return (double)NAN;
+      return known ? ((double)T::value(row[tok]) - (double)l.m) * inv_t - l.logS : -(double)INFINITY;
+    };
+    qx = logp(q, row_of<T>(rows, b, lane, K));
+    px = logp(p, row_of<T>(rows, b, K + 1 + lane, K));
+  }
+  // log_ratio: -inf where q has nothing for the draft, whatever p has
+  const double ell = qx == -(double)INFINITY && px == px ? -(double)INFINITY : qx - px;
+  const double use = ell == ell ? ell : -(double)INFINITY;  // no law: rejected
+  double acc = 0.0, mine = 0.0;
+  for (int i = 0; i < n; ++i) {
+    const double e = __shfl(use, i);
+    acc = acc == -(double)INFINITY ? acc : fmin(0.0, acc + e);
+    if (i == lane) mine = acc;
+  }
+  if (lane < K) {
+    ratio[(int64_t)b * K + lane] = lane < n ? (float)ell : 0.f;
+    la[(int64_t)b * K + lane] = mine;
+  }
+  if (mode == SD_TOKEN || n == 0) {
+    double eta = 2.0;
+    if (lane < n) {
+      if (uniforms) {
+        eta = uniforms[(int64_t)b * (K + 1) + lane];
+      } else {
+        const uint4 w = philox((uint32_t)(lane >> 2), (uint32_t)b, round[b], TAG_COIN << 24, seed);
+        eta = uniform64(pick(w, lane & 3));
+      }
+    }
+    const uint64_t cm = __ballot(lane < n && eta < exp(fmin(0.0, use)));
+    if (lane == 0) {
+      tau[b] = n == 0 ? 0 : first_rejected(cm, n);
+      lar[b] = 0.f;
+      if (coins) coins[b] = n == 0 ? 0 : cm;
+    }
+  }
+}
+
+// The slices of v_j for j = 1..K_b - 1: rows j (0-based) of target and draft.
+template <class T, int E>
+__global__ __launch_bounds__(kThreads) void verify_excess_kernel(Rows rows, int K, int V, int S, float c,
+                                                                 const int32_t* __restrict__ kb,
+                                                                 const Law* __restrict__ laws,
+                                                                 const double* __restrict__ la,
+                                                                 double* __restrict__ excess) {
+  __shared__ double red[4];
+  const int64_t id = blockIdx.x;
+  const int slice = (int)(id % S), r = (int)(id / S), b = r / (K - 1), j = r % (K - 1) + 1;
+  if (j >= drafts(kb, b, K)) return;
+  const Law q = laws[(int64_t)b * (2 * K + 1) + j], p = laws[(int64_t)b * (2 * K + 1) + K + 1 + j];
+  // alpha q and p are products of an exponential against the row's maximum and
+  // one factor, so a factor's rounding (2^-24) is all that scales them
+  const float A = q.S == 0.0 ? 0.f : (float)(exp(la[(int64_t)b * K + j - 1]) / q.S);
+  const float B = p.S == 0.0 ? 0.f : (float)(1.0 / p.S);
+  const float mq = q.S == 0.0 ? 0.f : q.m, mp = p.S == 0.0 ? 0.f : p.m;
+  const typename T::raw *pq = row_of<T>(rows, b, j, K), *pp = row_of<T>(rows, b, K + 1 + j, K);
+  float x[E], y[E];
+  const int a = lead<T>(pq);
+  load_slice<T, E>(pq, a, V, slice, x);
+  load_slice<T, E>(pp, a, V, slice, y);
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    const float eq = __builtin_amdgcn_exp2f((x[i] - mq) * c), ep = __builtin_amdgcn_exp2f((y[i] - mp) * c);
+    const float d = __fmaf_rn(eq, A, -(ep * B));
+    s[i & 3] += d > 0.f ? d : d != d ? d : 0.f;
+  }
+  const double sum = wave_sum((double)s[0] + s[1] + ((double)s[2] + s[3]));
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) excess[((int64_t)b * K + j) * S + slice] = red[0] + red[1] + (red[2] + red[3]);
+}
+
+// One wavefront a chain: block verification's coins and tau.
+__global__ __launch_bounds__(64) void verify_decide_kernel(int K, int S, const int32_t* __restrict__ kb,
+                                                           const double* __restrict__ uniforms,
+                                                           const uint32_t* __restrict__ round, uint64_t seed,
+                                                           const double* __restrict__ la,
+                                                           const double* __restrict__ excess,
+                                                           int32_t* __restrict__ tau, float* __restrict__ lar,
+                                                           uint64_t* __restrict__ coins) {
+  const int b = blockIdx.x, lane = threadIdx.x;
+  const int n = drafts(kb, b, K);
+  if (n == 0) return;  // verify_join_kernel has written its outputs
+  double l = 0.0, h = 0.0, eta = 2.0;
+  if (lane < n) {
+    l = la[(int64_t)b * K + lane];
+    if (lane + 1 < n) {
+      double v = 0.0;
+      const double* e = excess + ((int64_t)b * K + lane + 1) * S;
+      for (int s = 0; s < S; ++s) v += e[s];
+      h = l >= 0.0 ? 1.0 : v / (v - expm1(l));
+    } else {
+      h = exp(l);
+    }
+    if (uniforms) {
+      eta = uniforms[(int64_t)b * (K + 1) + lane];
+    } else {
+      const uint4 w = philox((uint32_t)(lane >> 2), (uint32_t)b, round[b], TAG_COIN << 24, seed);
+      eta = uniform64(pick(w, lane & 3));
+    }
+  }
+  const uint64_t cm = __ballot(lane < n && eta < h);
+  const int t = cm ? 65 - __clzll((long long)cm) : 1;
+  const double res = t >= 2 ? __shfl(l, t - 2) : 0.0;
+  if (lane == 0) {
+    tau[b] = t;
+    lar[b] = (float)res;
+    if (coins) coins[b] = cm;
+  }
+}
+
+// ---------------------------------------------------------------- the draw --
+// All of it in float64: a cumulative sum over a vocabulary is compared with a
+// uniform, and the tokens' borders are as near as 1e-6 of the whole.
+template <class T>
+struct Pair {
+  const typename T::raw *q, *p;  // the target's row tau - 1, the draft's (null where every draft was accepted)
+  int iq, ip;                    // their places among the chain's rows
+  bool any;
+};
+template <class T>
+__device__ __forceinline__ Pair<T> drawn_rows(const Rows& rows, int b, int K, int n, int tau) {
+  Pair<T> r{nullptr, nullptr, tau - 1, K + tau, n > 0};
+  if (!r.any) return r;
+  r.q = row_of<T>(rows, b, tau - 1, K);
+  if (tau <= n) r.p = row_of<T>(rows, b, K + tau, K);
+  return r;
+}
+
+// e^{(x - m) / T} of one element.
+__device__ __forceinline__ double weight(float x, float m, double inv_t) {
+  return exp(((double)x - (double)m) * inv_t);
+}
+
+// Slices of the two rows' sums.
+template <class T, int E>
+__global__ __launch_bounds__(kThreads) void draw_sums_kernel(Rows rows, int K, int V, int S, double inv_t,
+                                                             const int32_t* __restrict__ kb,
+                                                             const int32_t* __restrict__ tau,
+                                                             const Law* __restrict__ laws, Mass* __restrict__ sums) {
+  __shared__ double red[8];
+  const int slice = blockIdx.x % S, b = blockIdx.x / S, t = threadIdx.x;
+  const Pair<T> r = drawn_rows<T>(rows, b, K, drafts(kb, b, K), tau[b]);
+  if (!r.any) return;
+  const int a = lead<T>(r.q);
+  double s[2] = {0.0, 0.0};
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const typename T::raw* p = h ? r.p : r.q;
+    if (!p) continue;
+    const float m = laws[(int64_t)b * (2 * K + 1) + (h ? r.ip : r.iq)].m;
+    float x[E];
+    load_slice<T, E>(p, a, V, slice, x);
+    if (m > -INFINITY)
+#pragma unroll
+      for (int i = 0; i < E; ++i) s[h] += weight(x[i], m, inv_t);
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    s[h] = wave_sum(s[h]);
+    if ((t & 63) == 0) red[4 * h + (t >> 6)] = s[h];
+  }
+  __syncthreads();
+  if (t == 0)
+    sums[blockIdx.x] = Mass{red[0] + red[1] + (red[2] + red[3]), red[4] + red[5] + (red[6] + red[7])};
+}
+
+// Inclusive sums of v over the workgroup's threads, in their order.
+__device__ __forceinline__ double block_scan(double v, double* red) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const double o = __shfl_up(v, d);
+    if (lane >= d) v += o;
+  }
+  __syncthreads();
+  if (lane == 63) red[w] = v;
+  __syncthreads();
+  for (int i = 0; i < w; ++i) v += red[i];
+  return v;
+}
+__device__ __forceinline__ double block_sum(double v, double* red) {
+  v = wave_sum(v);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  return red[0] + red[1] + (red[2] + red[3]);
+}
+// The lowest thread whose flag is set, kThreads if none.
+__device__ __forceinline__ int block_first(bool flag, int* red) {
+  const uint64_t m = __ballot(flag);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0)
+    red[threadIdx.x >> 6] = m ? (int)(threadIdx.x & ~63u) + __ffsll((unsigned long long)m) - 1 : kThreads;
+  __syncthreads();
+  return min(min(red[0], red[1]), min(red[2], red[3]));
+}
+__device__ __forceinline__ int block_last(bool flag, int* red) {
+  const uint64_t m = __ballot(flag);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0)
+    red[threadIdx.x >> 6] = m ? (int)(threadIdx.x & ~63u) + 63 - __clzll((long long)m) : -1;
+  __syncthreads();
+  return max(max(red[0], red[1]), max(red[2], red[3]));
+}
+
+// The factors of the residual law's two terms: w = max(0, A e^{(x - mq) / T} - B e^{(y - mp) / T}).
+struct Residual {
+  double A, B;
+  float mq, mp;
+};
+// Every thread of the workgroup takes part and gets the same bits.
+template <class T>
+__device__ __forceinline__ Residual residual_of(const Pair<T>& r, int b, int K, int S, int mode, int tau,
+                                                const Law* __restrict__ laws, const double* __restrict__ la,
+                                                const Mass* __restrict__ sums, double* red) {
+  double q = 0.0, p = 0.0;
+  for (int i = threadIdx.x; i < S; i += kThreads) {
+    q += sums[(int64_t)b * S + i].q;
+    p += sums[(int64_t)b * S + i].p;
+  }
+  q = block_sum(q, red);
+  p = block_sum(p, red);
+  const double res = mode == SD_BLOCK && tau >= 2 ? la[(int64_t)b * K + tau - 2] : 0.0;
+  Residual f;
+  f.A = q == 0.0 ? 0.0 : exp(res) / q;
+  f.B = !r.p || p == 0.0 ? 0.0 : 1.0 / p;
+  f.mq = laws[(int64_t)b * (2 * K + 1) + r.iq].m;
+  f.mp = r.p ? laws[(int64_t)b * (2 * K + 1) + r.ip].m : 0.f;
+  if (f.mq == -INFINITY) f.mq = 0.f;
+  if (f.mp == -INFINITY) f.mp = 0.f;
+  return f;
+}
+__device__ __forceinline__ double residual_weight(const Residual& f, float x, float y, double inv_t) {
+  const double w = fma(f.A, weight(x, f.mq, inv_t), -(f.B * weight(y, f.mp, inv_t)));
+  return w > 0.0 ? w : 0.0;
+}
+
+// Slices of the residual's mass.
+template <class T, int E>
+__global__ __launch_bounds__(kThreads) void draw_mass_kernel(Rows rows, int K, int V, int S, int mode, double inv_t,
+                                                             const int32_t* __restrict__ kb,
+                                                             const int32_t* __restrict__ tau,
+                                                             const Law* __restrict__ laws,
+                                                             const double* __restrict__ la,
+                                                             const Mass* __restrict__ sums,
+                                                             double* __restrict__ mass) {
+  __shared__ double red[4];
+  const int slice = blockIdx.x % S, b = blockIdx.x / S;
+  const Pair<T> r = drawn_rows<T>(rows, b, K, drafts(kb, b, K), tau[b]);
+  if (!r.any) return;
+  const Residual f = residual_of<T>(r, b, K, S, mode, tau[b], laws, la, sums, red);
+  const int a = lead<T>(r.q);
+  float x[E], y[E];
+  load_slice<T, E>(r.q, a, V, slice, x);
+  if (r.p) {
+    load_slice<T, E>(r.p, a, V, slice, y);
+  } else {
+#pragma unroll
+    for (int i = 0; i < E; ++i) y[i] = -INFINITY;
+  }
+  double s = 0.0;
+#pragma unroll
+  for (int i = 0; i < E; ++i) s += residual_weight(f, x[i], y[i], inv_t);
+  s = block_sum(s, red);
+  if (threadIdx.x == 0) mass[blockIdx.x] = s;
+}
+
+// One workgroup a chain: the slice that the uniform falls into, and the token in
+// it.  Here a thread takes E elements that follow one another.
+template <class T, int E>
+__global__ __launch_bounds__(kThreads) void draw_pick_kernel(Rows rows, int K, int V, int S, int mode, double inv_t,
+                                                             const int32_t* __restrict__ kb,
+                                                             const int32_t* __restrict__ tau,
+                                                             const double* __restrict__ uniforms,
+                                                             const uint32_t* __restrict__ round, uint64_t seed,
+                                                             const Law* __restrict__ laws,
+                                                             const double* __restrict__ la,
+                                                             const Mass* __restrict__ sums,
+                                                             const double* __restrict__ mass,
+                                                             int32_t* __restrict__ token) {
+  __shared__ double red[4];
+  __shared__ int ired[4];
+  __shared__ double before_s;
+  __shared__ int slice_s, tok_s;
+  const int b = blockIdx.x, t = threadIdx.x;
+  const Pair<T> r = drawn_rows<T>(rows, b, K, drafts(kb, b, K), tau[b]);
+  if (!r.any) {
+    if (t == 0) token[b] = -1;
+    return;
+  }
+  Residual f = residual_of<T>(r, b, K, S, mode, tau[b], laws, la, sums, red);
+  double u;
+  if (uniforms) {
+    u = uniforms[(int64_t)b * (K + 1) + K];
+  } else {
+    const uint4 w = philox(0u, (uint32_t)b, round[b], TAG_USAMPLE << 24, seed);
+    u = ((double)(((uint64_t)(w.x >> 6) << 26) | (w.y >> 6)) + 0.5) * 0x1p-52;
+  }
+  // Laws without mass or with a NaN: the residual's sums come out 0 (a NaN weight
+  // counts 0), the target's are then taken, and those decide.
+  const int per = (S + kThreads - 1) / kThreads, s0 = min(t * per, S), s1 = min(s0 + per, S);
+  double v = 0.0;
+  for (int s = s0; s < s1; ++s) v += mass[(int64_t)b * S + s];
+  double cum = block_scan(v, red);
+  __syncthreads();
+  if (t == kThreads - 1) before_s = cum;
+  if (t == 0) {
+    slice_s = -1;
+    tok_s = -1;
+  }
+  __syncthreads();
+  double all = before_s;
+  const double qsum = f.A;  // 0 or NaN where the target has no law
+  const bool use_q = !(all > 0.0);
+  const bool nan = !(qsum > 0.0) || !isfinite(qsum) || (r.p && !isfinite(f.B));
+  if (nan) {
+    if (t == 0) token[b] = -1;
+    return;
+  }
+  if (use_q) {
+    f.B = 0.0;
+    v = 0.0;
+    for (int s = s0; s < s1; ++s) v += sums[(int64_t)b * S + s].q * f.A;
+    cum = block_scan(v, red);
+    __syncthreads();
+    if (t == kThreads - 1) before_s = cum;
+    __syncthreads();
+    all = before_s;
+  }
+  const double goal = u * all;
+  int owner = block_first(cum > goal, ired);
+  if (owner == kThreads) owner = block_last(v > 0.0, ired);  // u next to 1
+  if (owner < 0) {
+    if (t == 0) token[b] = -1;
+    return;
+  }
+  __syncthreads();
+  if (t == owner) {
+    double c = cum - v;
+    int last = s0;
+    for (int s = s0; s < s1; ++s) {
+      const double g = use_q ? sums[(int64_t)b * S + s].q * f.A : mass[(int64_t)b * S + s];
+      if (g > 0.0) {
+        last = s;
+        before_s = c;
+        if (c + g > goal) break;
+      }
+      c += g;
+    }
+    slice_s = last;
+  }
+  __syncthreads();
+  const int slice = slice_s;
+  const double before = before_s;
+  const int a = lead<T>(r.q), e0 = slice * kThreads * E + t * E - a;
+  double w[E], mine = 0.0;
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    const int e = e0 + i;
+    const bool in = e >= 0 && e < V;
+    w[i] = in ? residual_weight(f, T::value(r.q[e]), r.p && !use_q ? T::value(r.p[e]) : -INFINITY, inv_t) : 0.0;
+    mine += w[i];
+  }
+  const double upto = before + block_scan(mine, red);
+  int who = block_first(upto > goal, ired);
+  if (who == kThreads) who = block_last(mine > 0.0, ired);
+  if (t == who) {
+    double c = upto - mine;
+    int at = -1;
+    bool found = false;
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      c += w[i];
+      if (!found && w[i] > 0.0) {
+        at = e0 + i;
+        found = c > goal;
+      }
+    }
+    tok_s = at;
+  }
+  __syncthreads();
+  if (t == 0) token[b] = tok_s;
+}
+
+// The workspace's parts, each at a multiple of 256 bytes.
+inline size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
+
+template <class T, int E>
+hipError_t logprobs_run(int rows, int V, const void* x, int64_t ld, double inv_t, int n_tok, const int32_t* tokens,
+                        float* logprob, float* entropy, float* lse, int n, int32_t* ids, float* tops, void* ws,
+                        hipStream_t s) {
+  typedef typename T::raw raw;
+  const int S = slices(V, E);
+  Part* parts = static_cast<Part*>(ws);
+  uint64_t* keys = reinterpret_cast<uint64_t*>(static_cast<char*>(ws) + up256(sizeof(Part) * (size_t)rows * S));
+  hipError_t e = launch_timed("logprobs_slice", logprobs_slice_kernel<T, E>, dim3((unsigned)((int64_t)rows * S)),
+                              dim3(kThreads), s, static_cast<const raw*>(x), ld, V, S, (float)(inv_t * kLog2e), n,
+                              parts, keys);
+  if (e != hipSuccess) return e;
+  return launch_timed("logprobs_join", logprobs_join_kernel<T>, dim3(rows), dim3(kThreads), s,
+                      static_cast<const raw*>(x), ld, V, S, inv_t, n_tok, tokens, logprob, entropy, lse, n, ids, tops,
+                      (const Part*)parts, (const uint64_t*)keys);
+}
+
+struct VerifyWs {
+  size_t parts, laws, la, excess, sums, mass, bytes;
+};
+VerifyWs verify_layout(int B, int K, int V) {
+  const int64_t rows = (int64_t)B * (2 * K + 1);
+  const size_t S = (size_t)slices(V, per_thread(rows, V)), Sd = (size_t)slices(V, per_thread(B, V));
+  VerifyWs w;
+  w.parts = 0;
+  w.laws = w.parts + up256(sizeof(Part) * (size_t)rows * S);
+  w.la = w.laws + up256(sizeof(Law) * (size_t)rows);
+  w.excess = w.la + up256(sizeof(double) * (size_t)B * K);
+  w.sums = w.excess + up256(sizeof(double) * (size_t)B * K * S);
+  w.mass = w.sums + up256(sizeof(Mass) * (size_t)B * Sd);
+  w.bytes = w.mass + up256(sizeof(double) * (size_t)B * Sd);
+  return w;
+}
+
+template <class T, int E>
+hipError_t verify_run(const Rows& rows, int B, int K, int V, int mode, double inv_t, const int32_t* tokens,
+                      const int32_t* kb, const double* uniforms, const uint32_t* round, uint64_t seed, int32_t* tau,
+                      float* lar, float* ratio, uint64_t* coins, char* ws, const VerifyWs& w, hipStream_t s) {
+  const int S = slices(V, E);
+  const float c = (float)(inv_t * kLog2e);
+  Part* parts = reinterpret_cast<Part*>(ws + w.parts);
+  Law* laws = reinterpret_cast<Law*>(ws + w.laws);
+  double *la = reinterpret_cast<double*>(ws + w.la), *excess = reinterpret_cast<double*>(ws + w.excess);
+  hipError_t e = launch_timed("verify_sums", verify_sums_kernel<T, E>, dim3((unsigned)((int64_t)B * (2 * K + 1) * S)),
+                              dim3(kThreads), s, rows, K, V, S, c, kb, parts);
+  if (e != hipSuccess) return e;
+  e = launch_timed("verify_join", verify_join_kernel<T>, dim3(B), dim3(64), s, rows, K, V, S, mode, inv_t, tokens, kb,
+                   uniforms, round, seed, (const Part*)parts, laws, la, tau, lar, ratio, coins);
+  if (e != hipSuccess || mode != SD_BLOCK) return e;
+  if (K > 1) {
+    e = launch_timed("verify_excess", verify_excess_kernel<T, E>, dim3((unsigned)((int64_t)B * (K - 1) * S)),
+                     dim3(kThreads), s, rows, K, V, S, c, kb, (const Law*)laws, (const double*)la, excess);
+    if (e != hipSuccess) return e;
+  }
+  return launch_timed("verify_decide", verify_decide_kernel, dim3(B), dim3(64), s, K, S, kb, uniforms, round, seed,
+                      (const double*)la, (const double*)excess, tau, lar, coins);
+}
+
+template <class T, int E>
+hipError_t draw_run(const Rows& rows, int B, int K, int V, int mode, double inv_t, const int32_t* kb,
+                    const double* uniforms, const uint32_t* round, uint64_t seed, const int32_t* tau, int32_t* token,
+                    char* ws, const VerifyWs& w, hipStream_t s) {
+  const int S = slices(V, E);
+  const Law* laws = reinterpret_cast<const Law*>(ws + w.laws);
+  const double* la = reinterpret_cast<const double*>(ws + w.la);
+  Mass* sums = reinterpret_cast<Mass*>(ws + w.sums);
+  double* mass = reinterpret_cast<double*>(ws + w.mass);
+  const dim3 grid((unsigned)((int64_t)B * S));
+  hipError_t e = launch_timed("draw_sums", draw_sums_kernel<T, E>, grid, dim3(kThreads), s, rows, K, V, S, inv_t, kb,
+                              tau, laws, sums);
+  if (e != hipSuccess) return e;
+  e = launch_timed("draw_mass", draw_mass_kernel<T, E>, grid, dim3(kThreads), s, rows, K, V, S, mode, inv_t, kb, tau,
+                   laws, la, (const Mass*)sums, mass);
+  if (e != hipSuccess) return e;
+  return launch_timed("draw_pick", draw_pick_kernel<T, E>, dim3(B), dim3(kThreads), s, rows, K, V, S, mode, inv_t, kb,
+                      tau, uniforms, round, seed, laws, la, (const Mass*)sums, (const double*)mass, token);
+}
+
+// f with the element type's tag.
+template <class F>
+hipError_t by_type(sd_type type, F&& f) {
+  return type == SD_TYPE_F32 ? f(F32{}) : type == SD_TYPE_BF16 ? f(BF16{}) : f(F16{});
+}
+
+}  // namespace
+
+size_t logprobs_ws_bytes(int rows, int V, int n) {
+  const size_t S = (size_t)slices(V, per_thread(rows, V));
+  return up256(sizeof(Part) * (size_t)rows * S) + up256(sizeof(uint64_t) * (size_t)rows * S * (size_t)n);
+}
+int64_t logprobs_groups(int rows, int V) { return (int64_t)rows * slices(V, per_thread(rows, V)); }
+
+hipError_t logprobs_launch(int rows, int V, sd_type type, const void* x, int64_t ld, double temperature, int n_tok,
+                           const int32_t* tokens, float* logprob, float* entropy, float* lse, int n, int32_t* ids,
+                           float* tops, void* ws, hipStream_t s) {
+  const double inv_t = 1.0 / temperature;
+  return by_type(type, [&](auto tag) {
+    typedef decltype(tag) T;
+    return per_thread(rows, V) == 32
+               ? logprobs_run<T, 32>(rows, V, x, ld, inv_t, n_tok, tokens, logprob, entropy, lse, n, ids, tops, ws, s)
+               : logprobs_run<T, 8>(rows, V, x, ld, inv_t, n_tok, tokens, logprob, entropy, lse, n, ids, tops, ws, s);
+  });
+}
+
+size_t verify_tokens_ws_bytes(int B, int K, int V) { return verify_layout(B, K, V).bytes; }
+int64_t verify_tokens_groups(int B, int K, int V) {
+  const int64_t rows = (int64_t)B * (2 * K + 1);
+  return rows * slices(V, per_thread(rows, V));
+}
+
+hipError_t verify_tokens_launch(int B, int K, int V, int mode, sd_type type, double temperature, const void* draft,
+                                sd_stride ds, const void* target, sd_stride ts, const int32_t* tokens,
+                                const int32_t* kb, const double* uniforms, const uint32_t* round, uint64_t seed,
+                                int32_t* tau, int32_t* token, float* lar, float* ratio, uint64_t* coins, void* ws,
+                                hipStream_t s) {
+  const double inv_t = 1.0 / temperature;
+  const Rows rows{draft, target, ds, ts};
+  const VerifyWs w = verify_layout(B, K, V);
+  char* base = static_cast<char*>(ws);
+  return by_type(type, [&](auto tag) {
+    typedef decltype(tag) T;
+    hipError_t e = per_thread((int64_t)B * (2 * K + 1), V) == 32
+                       ? verify_run<T, 32>(rows, B, K, V, mode, inv_t, tokens, kb, uniforms, round, seed, tau, lar,
+                                           ratio, coins, base, w, s)
+                       : verify_run<T, 8>(rows, B, K, V, mode, inv_t, tokens, kb, uniforms, round, seed, tau, lar,
+                                          ratio, coins, base, w, s);
+    if (e != hipSuccess) return e;
+    return per_thread(B, V) == 32 ? draw_run<T, 32>(rows, B, K, V, mode, inv_t, kb, uniforms, round, seed, tau, token,
+                                                    base, w, s)
+                                  : draw_run<T, 8>(rows, B, K, V, mode, inv_t, kb, uniforms, round, seed, tau, token,
+                                                   base, w, s);
+  });
+}
+
+}  // namespace sd

@@ -1,0 +1,86 @@
+"""Refusals of the language-model calls, none of which reaches a HIP call."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2606_13426_amd import _lib
+
+P = ctypes.c_void_p(256)  # never dereferenced: validation fails first
+ODD = ctypes.c_void_p(257)
+
+
+@pytest.fixture(scope="module")
+def lib():
+    import os
+    if not os.path.exists(_lib.LIB_PATH):
+        from paper_2606_13426_amd import build
+        build.build()
+    return _lib.load()
+
+
+def _refused(status, needle):
+    assert status == _lib.SD_EINVAL
+    assert needle in _lib.last_error(), _lib.last_error()
+
+
+def _logprobs(lib, **kw):
+    a = dict(rows=2, V=10, type=0, logits=P, ld=10, T=1.0, n_tok=1, tokens=P, logprob=P, entropy=None, lse=None,
+             n_top=2, ids=P, tops=P, ws=P, ws_bytes=1 << 30)
+    a.update(kw)
+    return lib.sd_token_logprobs(*a.values(), None)
+
+
+@pytest.mark.parametrize("kw,needle", [
+    (dict(rows=0), "rows = 0"), (dict(V=0), "V = 0"), (dict(V=(1 << 24) + 1, ld=1 << 30), "V = 16777217"),
+    (dict(type=3), "type"), (dict(n_tok=-1), "n_tok"), (dict(n_top=33), "n_top = 33"), (dict(n_top=-1), "n_top"),
+    (dict(T=0.0), "temperature"), (dict(T=float("nan")), "temperature"), (dict(T=float("inf")), "temperature"),
+    (dict(T=-1.0), "temperature"), (dict(logits=None), "non-NULL"), (dict(ws=None), "non-NULL"),
+    (dict(tokens=None), "tokens"), (dict(logprob=None), "tokens"), (dict(ids=None), "top_ids"),
+    (dict(ld=9), "row stride"), (dict(logits=ODD), "aligned"), (dict(logits=ODD, type=1), "aligned"),
+    (dict(ws_bytes=8), "workspace 8 <"), (dict(ws=ctypes.c_void_p(128)), "256-byte"),
+    (dict(rows=2 ** 31 - 1, V=1 << 20, ld=1 << 20, n_top=0, ids=None, ws_bytes=2 ** 62), "too many rows")])
+def test_token_logprobs_refuses(lib, kw, needle):
+    _refused(_logprobs(lib, **kw), needle)
+
+
+def _verify(lib, **kw):
+    s = _lib.sd_stride
+    a = dict(B=2, K=3, V=10, mode=0, type=0, T=1.0, draft=P, ds=s(30, 10), target=P, ts=s(40, 10), tokens=P, kb=P,
+             uniforms=P, round=None, seed=0, tau=P, token=P, lar=P, ratio=P, coins=None, ws=P, ws_bytes=1 << 30)
+    a.update(kw)
+    return lib.sd_verify_tokens(*a.values(), None)
+
+
+@pytest.mark.parametrize("kw,needle", [
+    (dict(B=0), "B = 0"), (dict(K=0), "K = 0"), (dict(K=65), "K = 65"), (dict(V=0), "V = 0"), (dict(mode=2), "mode"),
+    (dict(type=-1), "type"), (dict(T=0.0), "temperature"), (dict(draft=None), "NULL"), (dict(tau=None), "NULL"),
+    (dict(uniforms=None), "uniforms and round"), (dict(ds=_lib.sd_stride(30, 9)), "draft stride"),
+    (dict(ts=_lib.sd_stride(39, 10)), "target stride"), (dict(draft=ODD), "aligned"),
+    (dict(target=ODD, type=2), "aligned"), (dict(ws_bytes=100), "workspace 100 <"),
+    (dict(ws=ctypes.c_void_p(64)), "256-byte"),
+    (dict(B=2 ** 31 - 1, ws_bytes=2 ** 63 - 1, V=1 << 15, ds=_lib.sd_stride(1 << 20, 1 << 15),
+          ts=_lib.sd_stride(1 << 20, 1 << 15)), "too many rows")])
+def test_verify_tokens_refuses(lib, kw, needle):
+    _refused(_verify(lib, **kw), needle)
+
+
+def test_workspace_queries_of_refused_sizes_are_zero(lib):
+    assert lib.sd_token_logprobs_workspace(0, 10, 0) == 0
+    assert lib.sd_token_logprobs_workspace(1, 0, 0) == 0
+    assert lib.sd_token_logprobs_workspace(1, 10, 33) == 0
+    assert lib.sd_verify_tokens_workspace(1, 65, 10) == 0
+    assert lib.sd_verify_tokens_workspace(1, 1, (1 << 24) + 1) == 0
+    assert lib.sd_token_logprobs_workspace(1, 10, 4) > 0 and lib.sd_verify_tokens_workspace(1, 1, 10) > 0
+
+
+def test_the_binding_refuses_operands_off_the_gpu_or_of_another_shape():
+    x = torch.zeros(2, 10)
+    with pytest.raises(_lib.SpecDiffError, match="not on the current GPU"):
+        _lib.sd_token_logprobs(x)
+    with pytest.raises(_lib.SpecDiffError, match="contiguous rows"):
+        _lib.sd_token_logprobs(torch.zeros(10, 2).T)
+    with pytest.raises(_lib.SpecDiffError, match="target must be"):
+        _lib.sd_verify_tokens(torch.zeros(2, 3, 10), torch.zeros(2, 3, 10), None, None)
+    with pytest.raises(_lib.SpecDiffError, match="one type"):
+        _lib.sd_verify_tokens(torch.zeros(2, 3, 10), torch.zeros(2, 4, 10).half(), None, None)

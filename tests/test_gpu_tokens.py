@@ -1,0 +1,333 @@
+"""sd_token_logprobs and sd_verify_tokens against the float64 oracle.
+
+Tolerances, with d = (x - m) / T of a row, E the mean under its law, u = 2^-24:
+an exponential is off by 2u (the instruction) and 2u |d| (the rounded argument),
+a thread's sum of up to 8 terms by 8u, so the row's sum S by (10 + 2 E|d|) u
+relative, which is what lse is off by; the entropy's second sum is off by (12 E|d|
++ 2 E d^2) u and by S's error times E|d|.  A float32 output adds u relative.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import tokens as otok
+from paper_2606_13426_amd import _lib
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+U = 2.0 ** -24
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+def _spread(z, T=1.0):
+    """E|d| and E d^2 of a row."""
+    lp = otok.row_law(z, T)
+    if lp is None or lp.max() == -np.inf:
+        return 0.0, 0.0
+    p = np.exp(lp)
+    d = np.where(p > 0, (np.where(np.isfinite(z), z, 0.0) - np.max(z)) / T, 0.0)
+    return float((p * np.abs(d)).sum()), float((p * d * d).sum())
+
+
+def _close(got, want, tol, what):
+    got, want = np.float64(got), np.float64(want)
+    if np.isnan(want):
+        assert np.isnan(got), (what, got, want)
+    elif np.isinf(want):
+        assert got == want, (what, got, want)
+    else:
+        assert abs(got - want) <= tol + U * abs(want), (what, got, want, tol)
+
+
+def _check_logprobs(x, tokens, n_top, T, r, rows):
+    z = x.double().cpu().numpy()
+    got = {k: v.cpu().numpy() for k, v in r.items()}
+    tok = None if tokens is None else tokens.cpu().numpy().reshape(len(z), -1)
+    for i in rows:
+        w = otok.logprobs(z[i], None if tok is None else tok[i], n_top, T)
+        e1, e2 = _spread(z[i], T)
+        ds = (10 + 2 * e1) * U
+        _close(got["lse"][i], w["lse"], ds, ("lse", i))
+        _close(got["entropy"][i], w["entropy"], ds * (1 + e1) + (12 * e1 + 2 * e2) * U, ("entropy", i))
+        if tok is not None:
+            for a, b in zip(got["logprob"].reshape(len(z), -1)[i], w["logprob"]):
+                _close(a, b, ds, ("logprob", i))
+        if n_top:
+            assert list(got["top_ids"][i]) == list(w["top_ids"]), (i, got["top_ids"][i], w["top_ids"])
+            for a, b in zip(got["top_logprobs"][i], w["top_logprobs"]):
+                _close(a, b, ds, ("top", i))
+
+
+def _rows(rows, V, t, seed, scale=3.0, pad=0, off=0):
+    """Logits as a view whose rows start off elements into rows of V + pad."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    base = torch.randn(rows, V + pad + off, generator=g, device=DEV) * scale
+    return base.to(TYPES[t])[:, off:off + V]
+
+
+@pytest.mark.parametrize("t", list(TYPES))
+@pytest.mark.parametrize("V,rows,n_top,n_tok,pad,off", [
+    (1, 3, 2, 1, 0, 0), (2, 1, 2, 1, 0, 1), (7, 5, 32, 3, 2, 3), (8, 2, 8, 1, 0, 0), (63, 4, 5, 1, 1, 0),
+    (1000, 3, 20, 2, 0, 0), (2041, 2, 32, 1, 0, 7), (2048, 2, 1, 1, 8, 0), (8192, 2, 32, 1, 0, 0),
+    (8193, 3, 20, 1, 0, 5), (50001, 2, 32, 3, 0, 0), (131072, 1, 20, 1, 0, 0)])
+def test_logprobs(V, rows, n_top, n_tok, pad, off, t):
+    x = _rows(rows, V, t, 11 * V + rows, pad=pad, off=off)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(3)
+    tokens = torch.randint(-1, V + 1, (rows, n_tok), generator=g, device=DEV).to(torch.int32)
+    r = _lib.sd_token_logprobs(x, tokens, n_top=n_top)
+    _check_logprobs(x, tokens, n_top, 1.0, r, range(rows))
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,V,n_top", [(1100, 300, 4), (600, 9001, 32), (1030, 8191, 0)])
+def test_logprobs_of_many_rows(rows, V, n_top, t):
+    # enough rows for 32 elements a thread, with one and two slices a row
+    x = _rows(rows, V, t, 5)
+    tokens = (torch.arange(rows, device=DEV) * 7 % V).to(torch.int32)
+    r = _lib.sd_token_logprobs(x, tokens, n_top=n_top)
+    assert r["logprob"].shape == (rows,)
+    _check_logprobs(x, tokens, n_top, 1.0, r, list(range(0, rows, 97)) + [rows - 1])
+
+
+@pytest.mark.parametrize("T", [0.25, 0.7, 3.0, 2.0 ** -40, 2.0 ** 40])
+def test_logprobs_with_temperature(T):
+    x = _rows(3, 5000, "f32", 2)
+    tokens = torch.tensor([0, 17, 4999], dtype=torch.int32, device=DEV)
+    r = _lib.sd_token_logprobs(x, tokens, n_top=6, temperature=T)
+    _check_logprobs(x, tokens, 6, T, r, range(3))
+
+
+@pytest.mark.parametrize("t", list(TYPES))
+@pytest.mark.parametrize("V", [5, 700, 9000])
+def test_logprobs_of_masked_and_lawless_rows(V, t):
+    inf = float("inf")
+    low = torch.finfo(TYPES[t]).min
+    x = _rows(10, V, t, 4).contiguous()
+    x[0] = -inf
+    x[1] = low
+    x[2] = -inf
+    x[2, V // 2] = 1.5
+    x[3] = low
+    x[3, V - 1] = 2.0
+    x[4, V // 3] = inf
+    x[5, V - 1] = float("nan")
+    x[6] = 0.25
+    x[7] = -inf
+    x[7, 1::3] = 0.5
+    x[8] = torch.finfo(TYPES[t]).max
+    x[9] = inf
+    tokens = torch.full((10, 3), V // 2, dtype=torch.int32, device=DEV)
+    tokens[:, 1], tokens[:, 2] = 1, 2 ** 31 - 1
+    r = _lib.sd_token_logprobs(x, tokens, n_top=4)
+    _check_logprobs(x, tokens, 4, 1.0, r, range(10))
+
+
+@pytest.mark.parametrize("order", ["rising", "falling", "blocks", "equal"])
+@pytest.mark.parametrize("V,rows", [(9000, 2), (20000, 1030)])
+def test_alternatives_of_rows_in_an_order(V, rows, order):
+    """Orders that put many of the largest elements into few threads (the pool overflows), and equal values."""
+    i = torch.arange(V, device=DEV, dtype=torch.float32)
+    if order == "rising":
+        x = i / 512
+    elif order == "falling":
+        x = -i / 512
+    elif order == "equal":
+        x = torch.zeros(V, device=DEV)
+    else:
+        # large values in the elements of a few threads of every slice: vectors of 4 repeat every 1024 elements
+        x = torch.where((i.long() % 1024) < 31 * 4 * 4, 8.0 + (i.long() * 7919 % 4093).float() / 4096, i * 0)
+    x = x[None].expand(rows, V).contiguous()
+    r = _lib.sd_token_logprobs(x, None, n_top=32)
+    _check_logprobs(x, None, 32, 1.0, r, [0, rows - 1])
+
+
+# ------------------------------------------------------------ verification --
+def _blocks(B, K, V, t, seed, near=0.6, pad=0, off=0):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    full = torch.randn(B, K + 1, V + pad + off, generator=g, device=DEV) * 2.5
+    target = full.to(TYPES[t])[:, :, off:off + V]
+    dfull = full[:, :K] + near * torch.randn(B, K, V + pad + off, generator=g, device=DEV)
+    draft = dfull.to(TYPES[t])[:, :, off:off + V]
+    e = torch.rand(B, K, V, generator=g, device=DEV).clamp_(1e-6, 1 - 1e-6)
+    tokens = (draft.float() - torch.log(-torch.log(e))).argmax(-1).to(torch.int32)
+    kb = (torch.arange(B, device=DEV) % (K + 2) - 1).to(torch.int32)  # -1, 0 (inactive) .. K
+    kb[-1] = K + 3  # clamped
+    un = torch.rand(B, K + 1, generator=g, device=DEV, dtype=torch.float64)
+    return draft, target, tokens, kb, un
+
+
+def _check_verify(draft, target, tokens, kb, un, mode, T, r, chains=None):
+    B, K, V = draft.shape
+    d, q = draft.double().cpu().numpy(), target.double().cpu().numpy()
+    x, n, u = tokens.cpu().numpy(), kb.cpu().numpy(), un.cpu().numpy()
+    g = {k: v.cpu().numpy() for k, v in r.items()}
+    decided = drawn = 0
+    for b in range(B) if chains is None else chains:
+        k = min(max(int(n[b]), 0), K)
+        w = otok.verify_chain(d[b], q[b], x[b], k, u[b, :K], u[b, K], "block" if mode == _lib.SD_BLOCK else "token", T)
+        tol = 0.0
+        for j in range(k):
+            tol_j = (20 + 2 * _spread(q[b, j], T)[0] + 2 * _spread(d[b, j], T)[0]) * U
+            tol += tol_j
+            _close(g["log_ratio"][b, j], w["ell"][j], tol_j, ("log_ratio", b, j))
+        assert (g["log_ratio"][b, k:] == 0).all()
+        # a coin as near to its threshold as the log-ratios' errors reach (h moves by less than
+        # twice what log alpha does, and its own sums' errors are of that size) may fall either way
+        if any(abs(u[b, j] - w["h"][j]) <= 4 * tol + 1e-9 for j in range(k)):
+            continue
+        decided += 1
+        assert g["tau"][b] == w["tau"], (b, g["tau"][b], w)
+        assert int(g["coins"][b]) & (2 ** 64 - 1) == w["coins"], b
+        _close(g["log_alpha_res"][b], w["log_alpha_res"], tol, ("log_alpha_res", b))
+        if w["w"] is not None:
+            c = np.cumsum(w["w"]) / w["w"].sum()
+            if np.abs(c - u[b, K]).min() <= 1e-11:
+                continue
+        drawn += 1
+        assert g["token"][b] == w["token"], (b, g["token"][b], w["token"], w["tau"])
+    return decided, drawn
+
+
+@pytest.mark.parametrize("mode", [_lib.SD_BLOCK, _lib.SD_TOKEN])
+@pytest.mark.parametrize("t", list(TYPES))
+@pytest.mark.parametrize("B,K,V,pad,off", [(1, 1, 1, 0, 0), (7, 1, 2, 0, 0), (9, 3, 5, 3, 1), (12, 4, 1000, 0, 0),
+                                            (11, 5, 2049, 0, 3), (10, 8, 8193, 2, 1), (3, 64, 40, 0, 0),
+                                            (6, 2, 50001, 0, 0)])
+def test_verify_tokens(B, K, V, pad, off, t, mode):
+    draft, target, tokens, kb, un = _blocks(B, K, V, t, B * 100 + K, pad=pad, off=off)
+    r = _lib.sd_verify_tokens(draft, target, tokens, kb, uniforms=un, mode=mode)
+    decided, drawn = _check_verify(draft, target, tokens, kb, un, mode, 1.0, r)
+    assert decided >= B - 1 and drawn >= decided - 1
+
+
+@pytest.mark.parametrize("mode", [_lib.SD_BLOCK, _lib.SD_TOKEN])
+def test_verify_tokens_of_many_chains(mode):
+    # enough rows for 32 elements a thread in the sums, and enough chains for it in the draw
+    draft, target, tokens, kb, un = _blocks(1050, 2, 300, "bf16", 8)
+    r = _lib.sd_verify_tokens(draft, target, tokens, kb, uniforms=un, mode=mode)
+    decided, drawn = _check_verify(draft, target, tokens, kb, un, mode, 1.0, r)
+    assert decided >= 1040 and drawn >= decided - 2
+
+
+@pytest.mark.parametrize("T", [0.5, 1.7])
+def test_verify_tokens_with_temperature_and_drawn_uniforms(T):
+    B, K, V, seed = 16, 4, 3001, 77
+    draft, target, tokens, kb, _ = _blocks(B, K, V, "f16", 9)
+    rnd = torch.arange(B, device=DEV, dtype=torch.int32) * 3
+    r = _lib.sd_verify_tokens(draft, target, tokens, kb, rnd=rnd, seed=seed, temperature=T)
+    un = torch.tensor(np.array([np.append(otok.coin_uniforms(seed, b, 3 * b, K), otok.draw_uniform(seed, b, 3 * b))
+                                for b in range(B)]))
+    decided, drawn = _check_verify(draft, target, tokens, kb, un, _lib.SD_BLOCK, T, r)
+    assert decided >= B - 1 and drawn >= decided - 1
+
+
+@pytest.mark.parametrize("mode", [_lib.SD_BLOCK, _lib.SD_TOKEN])
+def test_verify_tokens_of_equal_laws_accepts_everything(mode):
+    draft, target, tokens, kb, un = _blocks(8, 3, 777, "f32", 3)
+    draft = target[:, :3].contiguous()
+    kb.fill_(3)
+    r = _lib.sd_verify_tokens(draft, target, tokens, kb, uniforms=un, mode=mode)
+    assert (r["tau"] == 4).all() and (r["log_ratio"] == 0).all()
+    assert _check_verify(draft, target, tokens, kb, un, mode, 1.0, r) == (8, 8)
+
+
+@pytest.mark.parametrize("mode", [_lib.SD_BLOCK, _lib.SD_TOKEN])
+def test_verify_tokens_of_masked_and_lawless_rows(mode):
+    inf, nan = float("inf"), float("nan")
+    B, K, V = 12, 3, 600
+    draft, target, tokens, kb, un = _blocks(B, K, V, "f32", 21)
+    draft, target = draft.contiguous(), target.contiguous()
+    kb.fill_(K)
+    un.fill_(0.37)
+    target[0, 1] = -inf             # nothing allowed after the first draft
+    target[1, 0, 5] = nan           # no law at the first row
+    target[2, 3, 7] = inf           # no law behind the last draft
+    draft[3, 1, 9] = nan
+    draft[4, 0] = -inf              # the draft's law is empty: its token is accepted
+    target[5, 0] = -inf
+    target[5, 0, 3] = 0.0           # one token allowed, another drafted
+    tokens[5, 0] = 4
+    tokens[6, 1] = V                # outside the vocabulary
+    tokens[7, 0] = -1
+    target[8, 0, tokens[8, 0].long()] = -inf
+    draft[9, 0, tokens[9, 0].long()] = -inf
+    draft[10, 2] = -inf
+    draft[11, 0] = inf
+    r = _lib.sd_verify_tokens(draft, target, tokens, kb, uniforms=un, mode=mode)
+    decided, drawn = _check_verify(draft, target, tokens, kb, un, mode, 1.0, r)
+    assert decided >= 11 and drawn >= 11
+    assert r["tau"][1] == 1 and r["token"][1] == -1
+
+
+def test_uniforms_at_the_ends_draw_the_first_and_the_last_token():
+    B, V = 2, 4000
+    draft, target, tokens, kb, un = _blocks(B, 1, V, "f32", 2)
+    draft, target = draft.contiguous(), target.contiguous()
+    target[:, 0, tokens[:, 0].long()] = -float("inf")  # rejected
+    target[:, 0, :3] = -float("inf")
+    target[:, 0, V - 2:] = -float("inf")
+    draft[:, 0, :] = -float("inf")
+    draft[:, 0, 100] = 0.0
+    tokens.fill_(100)
+    target[:, 0, 100] = -float("inf")
+    kb.fill_(1)
+    un[0, 1], un[1, 1] = 1e-300, 1.0 - 2.0 ** -53
+    r = _lib.sd_verify_tokens(draft, target, tokens, kb, uniforms=un)
+    assert r["token"].tolist() == [3, V - 3] and r["tau"].tolist() == [1, 1]
+
+
+def test_calls_repeat_to_the_bit_and_replay_in_a_graph():
+    B, K, V = 5, 4, 12000
+    draft, target, tokens, kb, un = _blocks(B, K, V, "bf16", 6)
+    rows = target.reshape(-1, V)
+    given = torch.zeros(rows.shape[0], dtype=torch.int32, device=DEV)
+    ws1 = torch.empty(_lib.sd_verify_tokens_workspace(B, K, V), dtype=torch.uint8, device=DEV)
+    ws2 = torch.empty(_lib.sd_token_logprobs_workspace(rows.shape[0], V, 7), dtype=torch.uint8, device=DEV)
+
+    def call():
+        a = _lib.sd_verify_tokens(draft, target, tokens, kb, uniforms=un, ws=ws1)
+        return {**a, **_lib.sd_token_logprobs(rows, given, n_top=7, ws=ws2)}
+
+    want = {k: v.clone() for k, v in call().items()}
+    again = call()
+    assert all(torch.equal(want[k], again[k]) for k in want)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        other = call()
+    torch.cuda.synchronize()
+    assert all(torch.equal(want[k], other[k]) for k in want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = call()
+    for i in range(3):
+        ws1.fill_(0xFF if i else 0)  # nothing is kept in the workspace from one call for the next
+        ws2.fill_(0xFF if i else 0)
+        for v in held.values():
+            v.fill_(-5)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(want[k], held[k]) for k in want), i
+    target.copy_(target.flip(0))
+    fresh = {k: v.clone() for k, v in call().items()}
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(fresh[k], held[k]) for k in fresh)
+
+
+def test_rows_of_a_view_are_read_where_they_lie():
+    # target and draft rows interleaved in one buffer, outputs of the packed copies
+    B, K, V = 3, 2, 501
+    g = torch.Generator(device=DEV)
+    g.manual_seed(1)
+    buf = torch.randn(B, 2 * K + 1, V, generator=g, device=DEV).to(torch.bfloat16)
+    tokens = torch.randint(0, V, (B, K), generator=g, device=DEV).to(torch.int32)
+    kb = torch.full((B,), K, dtype=torch.int32, device=DEV)
+    un = torch.rand(B, K + 1, generator=g, device=DEV, dtype=torch.float64)
+    a = _lib.sd_verify_tokens(buf[:, K + 1:], buf[:, :K + 1], tokens, kb, uniforms=un)
+    b = _lib.sd_verify_tokens(buf[:, K + 1:].contiguous(), buf[:, :K + 1].contiguous(), tokens, kb, uniforms=un)
+    assert all(torch.equal(a[k], b[k]) for k in ("tau", "token", "coins"))
+    assert torch.allclose(a["log_ratio"], b["log_ratio"], rtol=0, atol=1e-5)
