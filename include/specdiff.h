@@ -419,6 +419,42 @@ sd_status sd_run_plain_em(sd_target target, int32_t B, uint64_t seed, float* y_o
  * float32 or float64 whatever the type. */
 typedef enum { SD_TYPE_F32 = 0, SD_TYPE_BF16 = 1, SD_TYPE_F16 = 2 } sd_type;
 
+/* Strides in elements of a [sequence][row][head][d] (or [token][head][d], seq
+ * unused) view; the d elements are contiguous. */
+typedef struct {
+  int64_t seq, row, head;
+} sd_stride_h;
+
+/* Attention of Q query rows a sequence over a paged cache of one latent vector a
+ * token (the absorbed form: the keys' and values' up-projections are folded into
+ * q and the output projection): the key of a cached vector c is all of it, its
+ * value the first d_latent elements.  With n_b = rows[b] (NULL: Q) rows of sequence b
+ * and len_b = lens[b] cached tokens, the last n_b of them the rows' own, row i < n_b
+ * of every head sees tokens j < len_b - n_b + i + 1:
+ *   s_j = scale q . c_j,  lse = log sum_j e^{s_j},  out = sum_j e^{s_j - lse} c_j[0..d_latent).
+ * A row that sees no token has out 0 and lse -inf.  Rows i >= n_b are not read
+ * or written.  Tokens that a row does not see have no part in it, whatever they
+ * hold.
+ * Token j of sequence b lies in page pages[b][j / page_size], at place j % page_size;
+ * with pages NULL in page b (n_pages >= B): a plain [B][page_size] cache.  A token
+ * whose page is outside [0, n_pages) counts as unseen by every row.  lens is
+ * clamped to the table's (the page's) tokens, rows to [0, Q].
+ * q [B][Q][H][d_latent + d_rope], cache [n_pages][page_size][d_latent + d_rope], out
+ * [B][Q][H][d_latent] of `type` (SD_TYPE_BF16 or SD_TYPE_F16); lse [B][Q][H],
+ * nullable.  d_latent a multiple of 8 in [8, 512], d_rope a multiple of 8 in
+ * [0, 64]; q, cache and out at 16-byte addresses, their strides multiples of 8
+ * elements and at least what they step over.  The products take q and cache as they
+ * are and the softmax's weights rounded to `type`, and add in float32.
+ * ws: >= sd_latent_attention_workspace bytes, 256-byte aligned. */
+size_t sd_latent_attention_workspace(int32_t B, int32_t Q, int32_t H, int32_t d_latent, int32_t d_rope);
+sd_status sd_latent_attention(int32_t B, int32_t Q, int32_t H, int32_t d_latent, int32_t d_rope,
+                              sd_type type, double scale, const void* q, sd_stride_h qs,
+                              const void* cache, int64_t page_stride, int64_t token_stride,
+                              int32_t n_pages, int32_t page_size, const int32_t* pages,
+                              int64_t pages_stride, int32_t max_pages, const int32_t* lens,
+                              const int32_t* rows, void* out, sd_stride_h os, float* lse, void* ws,
+                              size_t ws_bytes, sd_stream stream);
+
 #define SD_MAX_TOP 32
 #define SD_MAX_VOCAB (1 << 24)
 

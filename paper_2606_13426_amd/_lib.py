@@ -35,6 +35,10 @@ class sd_stride(ctypes.Structure):
     _fields_ = [("chain", c_int64), ("row", c_int64)]
 
 
+class sd_stride_h(ctypes.Structure):
+    _fields_ = [("seq", c_int64), ("row", c_int64), ("head", c_int64)]
+
+
 class sd_stats(ctypes.Structure):
     _fields_ = [("rounds", c_int64), ("chain_rounds", c_int64), ("steps", c_int64),
                 ("ties", c_int64), ("mean_tau", c_double), ("finished", c_int32),
@@ -66,6 +70,7 @@ class SpecDiffError(RuntimeError):
 
 P = c_void_p
 S = sd_stride
+SH = sd_stride_h
 # (name, restype, argtypes) of every exported function, in header order
 SIGNATURES = [
     ("sd_abi_version", c_int32, []),
@@ -98,6 +103,9 @@ SIGNATURES = [
                                    ctypes.POINTER(sd_sampler_view)]),
     ("sd_plain_em_workspace", c_size_t, [P, c_int32]),
     ("sd_run_plain_em", c_int32, [P, c_int32, c_uint64, P, P, c_size_t, P]),
+    ("sd_latent_attention_workspace", c_size_t, [c_int32] * 5),
+    ("sd_latent_attention", c_int32, [c_int32, c_int32, c_int32, c_int32, c_int32, c_int32, c_double, P, SH, P, c_int64,
+                                      c_int64, c_int32, c_int32, P, c_int64, c_int32, P, P, P, SH, P, P, c_size_t, P]),
     ("sd_token_logprobs_workspace", c_size_t, [c_int32, c_int32, c_int32]),
     ("sd_token_logprobs", c_int32, [c_int32, c_int32, c_int32, P, c_int64, c_double, c_int32, P, P, P, P, c_int32,
                                     P, P, P, c_size_t, P]),
@@ -428,6 +436,46 @@ def _operands(name, dtypes, tensors):
 def _workspace(ws, need, device):
     import torch
     return torch.empty(need, dtype=torch.uint8, device=device) if ws is None else ws
+
+
+def sd_latent_attention_workspace(B, Q, H, d_latent, d_rope):
+    return load().sd_latent_attention_workspace(B, Q, H, d_latent, d_rope)
+
+
+def sd_latent_attention(q, cache, lens, d_latent, pages=None, rows=None, scale=None, out=None, lse=None, ws=None):
+    """q [B][Q][H][d_latent + d_rope] and cache [n_pages][page_size][d_latent + d_rope] of one
+    16-bit type (last dimension contiguous); lens [B], pages [B][max_pages] (None: page b is
+    sequence b), rows [B] (None: Q rows each) int32; scale defaults to (d_latent + d_rope)^-1/2.
+
+    Returns (out [B][Q][H][d_latent], lse [B][Q][H] float32).
+    """
+    import torch
+    name, i32 = "sd_latent_attention", torch.int32
+    _need(q.dim() == 4 and cache.dim() == 3 and q.stride(3) == 1 and cache.stride(2) == 1, name,
+          "q must be [B][Q][H][d] and cache [n_pages][page_size][d] with contiguous d")
+    B, Q, H, d = q.shape
+    _need(cache.shape[2] == d and cache.dtype == q.dtype, name, "q and cache must agree in d and type")
+    if out is None:
+        out = torch.empty(B, Q, H, d_latent, dtype=q.dtype, device=q.device)
+    if lse is None:
+        lse = torch.empty(B, Q, H, dtype=torch.float32, device=q.device)
+    _operands(name, dict(lens=i32, pages=i32, rows=i32, out=q.dtype, lse=torch.float32, ws=torch.uint8),
+              dict(q=q, cache=cache, lens=lens, pages=pages, rows=rows, out=out, lse=lse, ws=ws))
+    _need(tuple(lens.shape) == (B,) and lens.is_contiguous(), name, "lens must be contiguous [B]")
+    _need(rows is None or (tuple(rows.shape) == (B,) and rows.is_contiguous()), name, "rows must be contiguous [B]")
+    _need(pages is None or (pages.dim() == 2 and pages.shape[0] == B and pages.stride(1) == 1), name,
+          "pages must be [B][max_pages] with contiguous rows")
+    _need(tuple(out.shape) == (B, Q, H, d_latent) and out.stride(3) == 1, name, "out must be [B][Q][H][d_latent]")
+    _need(tuple(lse.shape) == (B, Q, H) and lse.is_contiguous(), name, "lse must be contiguous [B][Q][H]")
+    ws = _workspace(ws, sd_latent_attention_workspace(B, Q, H, d_latent, d - d_latent), q.device)
+    _check(load().sd_latent_attention(B, Q, H, d_latent, d - d_latent, _type(q),
+                                      d ** -0.5 if scale is None else float(scale), _p(q),
+                                      sd_stride_h(*q.stride()[:3]), _p(cache), cache.stride(0), cache.stride(1),
+                                      cache.shape[0], cache.shape[1], _p(pages),
+                                      0 if pages is None else pages.stride(0),
+                                      0 if pages is None else pages.shape[1], _p(lens), _p(rows), _p(out),
+                                      sd_stride_h(*out.stride()[:3]), _p(lse), _p(ws), ws.numel(), _stream()), name)
+    return out, lse
 
 
 def sd_token_logprobs_workspace(rows, V, n_top=0):

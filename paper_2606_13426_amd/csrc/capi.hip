@@ -1107,6 +1107,58 @@ static bool aligned(const void* p, size_t n) { return ((uintptr_t)p & (n - 1)) =
 static bool temperature_ok(double t) { return t >= 0x1p-60 && t <= 0x1p60; }
 constexpr int64_t kMaxGroups = ((int64_t)1 << 31) - 1;  // workgroups of a launch
 
+static bool latent_shape_ok(int32_t B, int32_t Q, int32_t H, int32_t dc, int32_t dr) {
+  return B >= 1 && Q >= 1 && H >= 1 && (int64_t)Q * H <= ((int64_t)1 << 30) / B && dc >= 8 && dc <= 512 && dc % 8 == 0 &&
+         dr >= 0 && dr <= 64 && dr % 8 == 0;
+}
+// Strides of a [seq][rows][heads][d] view: multiples of 8 elements, a head's d apart at least, and
+// no two rows in one place (rows over heads or heads over rows).
+static bool stride_h_ok(sd_stride_h s, int seqs, int rows, int heads, int d) {
+  const int64_t row = rows == 1 ? 0 : s.row, head = heads == 1 ? 0 : s.head, seq = seqs == 1 ? 0 : s.seq;
+  return row % 8 == 0 && head % 8 == 0 && seq % 8 == 0 && (heads == 1 || head >= d) && (rows == 1 || row >= d) &&
+         (seqs == 1 || seq >= d) &&
+         (heads == 1 || rows == 1 || row >= heads * head || head >= rows * row);
+}
+
+size_t sd_latent_attention_workspace(int32_t B, int32_t Q, int32_t H, int32_t d_latent, int32_t d_rope) {
+  return latent_shape_ok(B, Q, H, d_latent, d_rope) ? latent_ws_bytes(B, Q, H, d_latent) : 0;
+}
+
+sd_status sd_latent_attention(int32_t B, int32_t Q, int32_t H, int32_t d_latent, int32_t d_rope, sd_type type,
+                              double scale, const void* q, sd_stride_h qs, const void* cache, int64_t page_stride,
+                              int64_t token_stride, int32_t n_pages, int32_t page_size, const int32_t* pages,
+                              int64_t pages_stride, int32_t max_pages, const int32_t* lens, const int32_t* rows,
+                              void* out, sd_stride_h os, float* lse, void* ws, size_t ws_bytes, sd_stream stream) {
+  SD_CHECK_ARG(B >= 1 && Q >= 1 && H >= 1, "sd_latent_attention: need B >= 1, Q >= 1 and H >= 1");
+  SD_CHECK_ARG(d_latent >= 8 && d_latent <= 512 && d_latent % 8 == 0, "sd_latent_attention: d_latent = %d is no multiple of 8 in [8, 512]", d_latent);
+  SD_CHECK_ARG(d_rope >= 0 && d_rope <= 64 && d_rope % 8 == 0, "sd_latent_attention: d_rope = %d is no multiple of 8 in [0, 64]", d_rope);
+  SD_CHECK_ARG(latent_shape_ok(B, Q, H, d_latent, d_rope), "sd_latent_attention: more than 2^30 rows");
+  SD_CHECK_ARG(type == SD_TYPE_BF16 || type == SD_TYPE_F16, "sd_latent_attention: type must be SD_TYPE_BF16 or SD_TYPE_F16");
+  SD_CHECK_ARG(isfinite(scale) && fabs(scale) <= 0x1p60, "sd_latent_attention: scale must be finite");
+  SD_CHECK_ARG(q && cache && lens && out && ws, "sd_latent_attention: NULL pointer argument");
+  SD_CHECK_ARG(n_pages >= 1 && page_size >= 1, "sd_latent_attention: need n_pages >= 1 and page_size >= 1");
+  if (pages) {
+    SD_CHECK_ARG(max_pages >= 1 && pages_stride >= max_pages, "sd_latent_attention: need max_pages >= 1 and pages_stride >= max_pages");
+    SD_CHECK_ARG((int64_t)max_pages * page_size < ((int64_t)1 << 30), "sd_latent_attention: a sequence's pages hold 2^30 tokens or more");
+  } else {
+    SD_CHECK_ARG(n_pages >= B, "sd_latent_attention: without a table n_pages = %d must be >= B = %d", n_pages, B);
+    SD_CHECK_ARG(page_size < (1 << 30), "sd_latent_attention: a page holds 2^30 tokens or more");
+  }
+  const int d = d_latent + d_rope;
+  SD_CHECK_ARG(token_stride >= d && token_stride % 8 == 0 && page_stride % 8 == 0 &&
+                   (n_pages == 1 || page_stride >= (int64_t)page_size * token_stride),
+               "sd_latent_attention: cache strides must be multiples of 8 elements that step over a token and a page");
+  SD_CHECK_ARG(stride_h_ok(qs, B, Q, H, d), "sd_latent_attention: q strides must be multiples of 8 elements that step over a row");
+  SD_CHECK_ARG(stride_h_ok(os, B, Q, H, d_latent), "sd_latent_attention: out strides must be multiples of 8 elements that step over a row");
+  SD_CHECK_ARG(aligned(q, 16) && aligned(cache, 16) && aligned(out, 16), "sd_latent_attention: q, cache and out must be 16-byte aligned");
+  const size_t need = latent_ws_bytes(B, Q, H, d_latent);
+  SD_CHECK_ARG(ws_bytes >= need, "sd_latent_attention: workspace %zu < %zu bytes", ws_bytes, need);
+  SD_CHECK_ARG(aligned(ws, 256), "sd_latent_attention: workspace must be 256-byte aligned");
+  SD_HIP(latent_launch(B, Q, H, d_latent, d_rope, type, scale, q, qs, cache, page_stride, token_stride, n_pages,
+                       page_size, pages, pages_stride, max_pages, lens, rows, out, os, lse, ws, (hipStream_t)stream));
+  return SD_OK;
+}
+
 size_t sd_token_logprobs_workspace(int32_t rows, int32_t V, int32_t n_top) {
   if (rows < 1 || V < 1 || V > SD_MAX_VOCAB || n_top < 0 || n_top > SD_MAX_TOP) return 0;
   return logprobs_ws_bytes(rows, V, n_top);

@@ -284,6 +284,11 @@ hipError_t philox_normals_launch(uint64_t seed, uint32_t chain, uint32_t rnd, ui
 hipError_t mfma_loop_launch(int blocks, int iters, float* out, hipStream_t s);
 
 // ----------------------------------------------- language-model verification --
+size_t latent_ws_bytes(int B, int Q, int H, int dc);
+hipError_t latent_launch(int B, int Q, int H, int dc, int dr, sd_type type, double scale, const void* q, sd_stride_h qs,
+                         const void* cache, int64_t page_stride, int64_t token_stride, int n_pages, int page_size,
+                         const int32_t* pages, int64_t pages_stride, int max_pages, const int32_t* lens,
+                         const int32_t* rows, void* out, sd_stride_h os, float* lse, void* ws, hipStream_t s);
 // Workgroups of the widest launch, workspace and launches of sd_token_logprobs
 // and sd_verify_tokens.
 int64_t logprobs_groups(int rows, int V);

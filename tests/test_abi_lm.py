@@ -84,3 +84,39 @@ def test_the_binding_refuses_operands_off_the_gpu_or_of_another_shape():
         _lib.sd_verify_tokens(torch.zeros(2, 3, 10), torch.zeros(2, 3, 10), None, None)
     with pytest.raises(_lib.SpecDiffError, match="one type"):
         _lib.sd_verify_tokens(torch.zeros(2, 3, 10), torch.zeros(2, 4, 10).half(), None, None)
+
+
+def _latent(lib, **kw):
+    s = _lib.sd_stride_h
+    a = dict(B=2, Q=2, H=4, dc=128, dr=64, type=1, scale=0.1, q=P, qs=s(1536, 768, 192), cache=P, ps=16 * 192, ts=192,
+             n_pages=9, size=16, pages=P, pstride=4, max_pages=4, lens=P, rows=None, out=P, os=s(1024, 512, 128), lse=None,
+             ws=P, ws_bytes=1 << 40)
+    a.update(kw)
+    return lib.sd_latent_attention(*a.values(), None)
+
+
+@pytest.mark.parametrize("kw,needle", [
+    (dict(B=0), "B >= 1"), (dict(Q=0), "B >= 1"), (dict(H=0), "B >= 1"), (dict(dc=0), "d_latent = 0"),
+    (dict(dc=520), "d_latent = 520"), (dict(dc=132), "d_latent = 132"), (dict(dr=72), "d_rope = 72"),
+    (dict(dr=-8), "d_rope"), (dict(dr=4), "d_rope = 4"), (dict(type=0), "type"), (dict(scale=float("nan")), "scale"),
+    (dict(scale=float("inf")), "scale"), (dict(q=None), "NULL"), (dict(lens=None), "NULL"), (dict(ws=None), "NULL"),
+    (dict(n_pages=0), "n_pages"), (dict(size=0), "page_size"), (dict(max_pages=5), "pages_stride"),
+    (dict(size=1 << 28, ps=1 << 40), "2^30 tokens"), (dict(pages=None, n_pages=1), "n_pages = 1"),
+    (dict(ts=184), "cache strides"), (dict(ts=196), "cache strides"), (dict(ps=100), "cache strides"),
+    (dict(qs=_lib.sd_stride_h(1536, 768, 190)), "q strides"), (dict(qs=_lib.sd_stride_h(1536, 192, 192)), "q strides"),
+    (dict(os=_lib.sd_stride_h(1024, 512, 120)), "out strides"), (dict(q=ctypes.c_void_p(264)), "16-byte"),
+    (dict(cache=ctypes.c_void_p(258)), "16-byte"), (dict(ws_bytes=64), "workspace 64 <"),
+    (dict(ws=ctypes.c_void_p(128)), "256-byte"), (dict(B=1 << 20, Q=1 << 10), "2^30 rows")])
+def test_latent_attention_refuses(lib, kw, needle):
+    _refused(_latent(lib, **kw), needle)
+
+
+def test_latent_binding_refuses():
+    assert _lib.sd_latent_attention_workspace(1, 1, 1, 12, 0) == 0
+    q, c, n = torch.zeros(1, 1, 2, 192).half(), torch.zeros(3, 16, 192).half(), torch.ones(1, dtype=torch.int32)
+    with pytest.raises(_lib.SpecDiffError, match="agree in d"):
+        _lib.sd_latent_attention(q, c[..., :184], n, 128)
+    with pytest.raises(_lib.SpecDiffError, match="agree in d and type"):
+        _lib.sd_latent_attention(q, c.bfloat16(), n, 128)
+    with pytest.raises(_lib.SpecDiffError, match="not on the current GPU"):
+        _lib.sd_latent_attention(q, c, n, 128)
