@@ -455,6 +455,33 @@ sd_status sd_latent_attention(int32_t B, int32_t Q, int32_t H, int32_t d_latent,
                               const int32_t* rows, void* out, sd_stride_h os, float* lse, void* ws,
                               size_t ws_bytes, sd_stream stream);
 
+/* The expanded form, for prompts: n sequences of query rows [cu_q[b], cu_q[b+1]) of
+ * q [Tq][H][d_nope + d_rope] and keys [cu_k[b], cu_k[b+1]) of k [Tk][H][d_nope] (the
+ * heads' own part), k_rope [Tk][d_rope] (the rotary part, one for all heads) and v
+ * [Tk][H][d_v].  Row i of a sequence's n_q sees its keys j < n_k - n_q + i + 1 (a chunk
+ * of queries at the end of its keys):
+ *   s_j = scale (q_nope . k_j + q_rope . k_rope_j),  lse = log sum_j e^{s_j},
+ *   out = sum_j e^{s_j - lse} v_j.
+ * A row that sees no key has out 0 and lse -inf; keys that a row does not see have no
+ * part in it, whatever they hold.  Rows of no sequence are not read or written.
+ * cu_q, cu_k [n+1] rise from >= 0 to <= Tq, <= Tk (values outside are clamped).
+ * All of one 16-bit `type` with float32 sums as in sd_latent_attention; d_nope and d_v
+ * multiples of 8 in [8, 128], d_rope of 8 in [0, 64]; pointers at 16-byte addresses
+ * (k_rope too, not read where d_rope = 0: NULL then), strides (row: a token's,
+ * head; seq is not read) multiples of 8 elements below 2^24 that step over a head's
+ * elements; out [Tq][H][d_v]; lse [Tq][H], nullable.
+ * ws: >= sd_latent_attention_expanded_workspace bytes (0 where no keys are split:
+ * NULL then), 256-byte aligned. */
+size_t sd_latent_attention_expanded_workspace(int32_t n, int32_t H, int32_t d_nope, int32_t d_rope,
+                                              int32_t d_v, int32_t Tq, int32_t Tk);
+sd_status sd_latent_attention_expanded(int32_t n, int32_t H, int32_t d_nope, int32_t d_rope,
+                                       int32_t d_v, sd_type type, double scale, int32_t Tq,
+                                       const void* q, sd_stride_h qs, int32_t Tk, const void* k,
+                                       sd_stride_h ks, const void* k_rope, int64_t k_rope_stride,
+                                       const void* v, sd_stride_h vs, const int32_t* cu_q,
+                                       const int32_t* cu_k, void* out, sd_stride_h os, float* lse,
+                                       void* ws, size_t ws_bytes, sd_stream stream);
+
 #define SD_MAX_TOP 32
 #define SD_MAX_VOCAB (1 << 24)
 

@@ -106,6 +106,9 @@ SIGNATURES = [
     ("sd_latent_attention_workspace", c_size_t, [c_int32] * 5),
     ("sd_latent_attention", c_int32, [c_int32, c_int32, c_int32, c_int32, c_int32, c_int32, c_double, P, SH, P, c_int64,
                                       c_int64, c_int32, c_int32, P, c_int64, c_int32, P, P, P, SH, P, P, c_size_t, P]),
+    ("sd_latent_attention_expanded_workspace", c_size_t, [c_int32] * 7),
+    ("sd_latent_attention_expanded", c_int32, [c_int32, c_int32, c_int32, c_int32, c_int32, c_int32, c_double, c_int32, P,
+                                               SH, c_int32, P, SH, P, c_int64, P, SH, P, P, P, SH, P, P, c_size_t, P]),
     ("sd_token_logprobs_workspace", c_size_t, [c_int32, c_int32, c_int32]),
     ("sd_token_logprobs", c_int32, [c_int32, c_int32, c_int32, P, c_int64, c_double, c_int32, P, P, P, P, c_int32,
                                     P, P, P, c_size_t, P]),
@@ -475,6 +478,52 @@ def sd_latent_attention(q, cache, lens, d_latent, pages=None, rows=None, scale=N
                                       0 if pages is None else pages.stride(0),
                                       0 if pages is None else pages.shape[1], _p(lens), _p(rows), _p(out),
                                       sd_stride_h(*out.stride()[:3]), _p(lse), _p(ws), ws.numel(), _stream()), name)
+    return out, lse
+
+
+def sd_latent_attention_expanded_workspace(n, H, d_nope, d_rope, d_v, Tq, Tk):
+    return load().sd_latent_attention_expanded_workspace(n, H, d_nope, d_rope, d_v, Tq, Tk)
+
+
+def sd_latent_attention_expanded(q, k, k_rope, v, cu_q, cu_k, scale=None, out=None, lse=None, ws=None):
+    """q [Tq][H][d_nope + d_rope], k [Tk][H][d_nope], k_rope [Tk][d_rope] (None: d_rope = 0), v [Tk][H][d_v]
+    of one 16-bit type (last dimension contiguous); cu_q, cu_k [n+1] int32 offsets of the sequences;
+    scale defaults to (d_nope + d_rope)^-1/2.
+
+    Returns (out [Tq][H][d_v], lse [Tq][H] float32).
+    """
+    import torch
+    name, i32 = "sd_latent_attention_expanded", torch.int32
+    _need(q.dim() == 3 and k.dim() == 3 and v.dim() == 3 and q.stride(2) == k.stride(2) == v.stride(2) == 1, name,
+          "q, k and v must be [tokens][H][d] with contiguous d")
+    Tq, H, d = q.shape
+    Tk, _, dn = k.shape
+    dr, dv = d - dn, v.shape[2]
+    _need(k.shape[1] == H and tuple(v.shape[:2]) == (Tk, H) and k.dtype == v.dtype == q.dtype, name,
+          "q, k and v must agree in heads, tokens and type")
+    _need((k_rope is None and dr == 0) or (k_rope is not None and tuple(k_rope.shape) == (Tk, dr) and
+                                           k_rope.dtype == q.dtype and k_rope.stride(1) == 1), name,
+          "k_rope must be [Tk][d_rope] of q's type with contiguous rows")
+    if out is None:
+        out = torch.empty(Tq, H, dv, dtype=q.dtype, device=q.device)
+    if lse is None:
+        lse = torch.empty(Tq, H, dtype=torch.float32, device=q.device)
+    _operands(name, dict(cu_q=i32, cu_k=i32, out=q.dtype, lse=torch.float32, ws=torch.uint8),
+              dict(q=q, k=k, k_rope=k_rope, v=v, cu_q=cu_q, cu_k=cu_k, out=out, lse=lse, ws=ws))
+    n = cu_q.numel() - 1
+    _need(cu_q.dim() == 1 and tuple(cu_k.shape) == (n + 1,) and cu_q.is_contiguous() and cu_k.is_contiguous(), name,
+          "cu_q and cu_k must be contiguous [n + 1]")
+    _need(tuple(out.shape) == (Tq, H, dv) and out.stride(2) == 1, name, "out must be [Tq][H][d_v]")
+    _need(tuple(lse.shape) == (Tq, H) and lse.is_contiguous(), name, "lse must be contiguous [Tq][H]")
+    need = sd_latent_attention_expanded_workspace(n, H, dn, dr, dv, Tq, Tk)
+    if need > 0:
+        ws = _workspace(ws, need, q.device)
+    strides = [sd_stride_h(0, x.stride(0), x.stride(1)) for x in (q, k, v, out)]
+    _check(load().sd_latent_attention_expanded(n, H, dn, dr, dv, _type(q), d ** -0.5 if scale is None else float(scale),
+                                               Tq, _p(q), strides[0], Tk, _p(k), strides[1], _p(k_rope),
+                                               k_rope.stride(0) if k_rope is not None else 0, _p(v), strides[2],
+                                               _p(cu_q), _p(cu_k), _p(out), strides[3], _p(lse), _p(ws),
+                                               ws.numel() if ws is not None else 0, _stream()), name)
     return out, lse
 
 

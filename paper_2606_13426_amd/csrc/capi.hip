@@ -1159,6 +1159,53 @@ sd_status sd_latent_attention(int32_t B, int32_t Q, int32_t H, int32_t d_latent,
   return SD_OK;
 }
 
+static bool expanded_shape_ok(int32_t n, int32_t H, int32_t dn, int32_t dr, int32_t dv, int32_t Tq, int32_t Tk) {
+  return n >= 1 && H >= 1 && Tq >= 1 && Tk >= 1 && dn >= 8 && dn <= 128 && dn % 8 == 0 && dv >= 8 && dv <= 128 &&
+         dv % 8 == 0 && dr >= 0 && dr <= 64 && dr % 8 == 0 && Tk < (1 << 30) && n < (1 << 24) &&
+         (int64_t)Tq * H <= ((int64_t)1 << 30) && expanded_groups(n, H, Tq, Tk) <= kMaxGroups;
+}
+static bool token_stride_ok(sd_stride_h s, int tokens, int heads, int d) {
+  return stride_h_ok(sd_stride_h{0, s.row, s.head}, 1, tokens, heads, d) && (tokens == 1 || s.row < (1 << 24)) &&
+         (heads == 1 || s.head < ((int64_t)1 << 40));
+}
+
+size_t sd_latent_attention_expanded_workspace(int32_t n, int32_t H, int32_t d_nope, int32_t d_rope, int32_t d_v,
+                                              int32_t Tq, int32_t Tk) {
+  return expanded_shape_ok(n, H, d_nope, d_rope, d_v, Tq, Tk) ? expanded_ws_bytes(n, H, d_nope, d_v, Tq, Tk) : 0;
+}
+
+sd_status sd_latent_attention_expanded(int32_t n, int32_t H, int32_t d_nope, int32_t d_rope, int32_t d_v, sd_type type,
+                                       double scale, int32_t Tq, const void* q, sd_stride_h qs, int32_t Tk,
+                                       const void* k, sd_stride_h ks, const void* k_rope, int64_t k_rope_stride,
+                                       const void* v, sd_stride_h vs, const int32_t* cu_q, const int32_t* cu_k,
+                                       void* out, sd_stride_h os, float* lse, void* ws, size_t ws_bytes,
+                                       sd_stream stream) {
+  SD_CHECK_ARG(n >= 1 && H >= 1 && Tq >= 1 && Tk >= 1, "sd_latent_attention_expanded: need n, H, Tq and Tk >= 1");
+  SD_CHECK_ARG(d_nope >= 8 && d_nope <= 128 && d_nope % 8 == 0, "sd_latent_attention_expanded: d_nope = %d is no multiple of 8 in [8, 128]", d_nope);
+  SD_CHECK_ARG(d_v >= 8 && d_v <= 128 && d_v % 8 == 0, "sd_latent_attention_expanded: d_v = %d is no multiple of 8 in [8, 128]", d_v);
+  SD_CHECK_ARG(d_rope >= 0 && d_rope <= 64 && d_rope % 8 == 0, "sd_latent_attention_expanded: d_rope = %d is no multiple of 8 in [0, 64]", d_rope);
+  SD_CHECK_ARG(expanded_shape_ok(n, H, d_nope, d_rope, d_v, Tq, Tk), "sd_latent_attention_expanded: too many rows for one call");
+  SD_CHECK_ARG(type == SD_TYPE_BF16 || type == SD_TYPE_F16, "sd_latent_attention_expanded: type must be SD_TYPE_BF16 or SD_TYPE_F16");
+  SD_CHECK_ARG(isfinite(scale) && fabs(scale) <= 0x1p60, "sd_latent_attention_expanded: scale must be finite");
+  SD_CHECK_ARG(q && k && (k_rope || d_rope == 0) && v && cu_q && cu_k && out, "sd_latent_attention_expanded: NULL pointer argument");
+  SD_CHECK_ARG(token_stride_ok(qs, Tq, H, d_nope + d_rope), "sd_latent_attention_expanded: q strides must be multiples of 8 elements that step over a head");
+  SD_CHECK_ARG(token_stride_ok(ks, Tk, H, d_nope), "sd_latent_attention_expanded: k strides must be multiples of 8 elements that step over a head");
+  SD_CHECK_ARG(token_stride_ok(vs, Tk, H, d_v), "sd_latent_attention_expanded: v strides must be multiples of 8 elements that step over a head");
+  SD_CHECK_ARG(token_stride_ok(os, Tq, H, d_v), "sd_latent_attention_expanded: out strides must be multiples of 8 elements that step over a head");
+  SD_CHECK_ARG(d_rope == 0 || Tk == 1 || (k_rope_stride >= d_rope && k_rope_stride % 8 == 0 && k_rope_stride < (1 << 24)),
+               "sd_latent_attention_expanded: k_rope stride must be a multiple of 8 elements that steps over a token");
+  SD_CHECK_ARG(aligned(q, 16) && aligned(k, 16) && aligned(k_rope, 16) && aligned(v, 16) && aligned(out, 16),
+               "sd_latent_attention_expanded: q, k, k_rope, v and out must be 16-byte aligned");
+  const size_t need = expanded_ws_bytes(n, H, d_nope, d_v, Tq, Tk);
+  SD_CHECK_ARG(need == 0 || ws, "sd_latent_attention_expanded: NULL workspace");
+  SD_CHECK_ARG(ws_bytes >= need, "sd_latent_attention_expanded: workspace %zu < %zu bytes", ws_bytes, need);
+  SD_CHECK_ARG(aligned(ws, 256), "sd_latent_attention_expanded: workspace must be 256-byte aligned");
+  SD_HIP(expanded_launch(n, H, d_nope, d_rope, d_v, type, scale, Tq, q, qs, Tk, k, ks, k_rope,
+                         d_rope == 0 || Tk == 1 ? 0 : k_rope_stride, v, vs, cu_q, cu_k, out, os, lse, ws,
+                         (hipStream_t)stream));
+  return SD_OK;
+}
+
 size_t sd_token_logprobs_workspace(int32_t rows, int32_t V, int32_t n_top) {
   if (rows < 1 || V < 1 || V > SD_MAX_VOCAB || n_top < 0 || n_top > SD_MAX_TOP) return 0;
   return logprobs_ws_bytes(rows, V, n_top);

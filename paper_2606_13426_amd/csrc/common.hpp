@@ -289,6 +289,12 @@ hipError_t latent_launch(int B, int Q, int H, int dc, int dr, sd_type type, doub
                          const void* cache, int64_t page_stride, int64_t token_stride, int n_pages, int page_size,
                          const int32_t* pages, int64_t pages_stride, int max_pages, const int32_t* lens,
                          const int32_t* rows, void* out, sd_stride_h os, float* lse, void* ws, hipStream_t s);
+int64_t expanded_groups(int n, int H, int Tq, int Tk);
+size_t expanded_ws_bytes(int n, int H, int dn, int dv, int Tq, int Tk);
+hipError_t expanded_launch(int n, int H, int dn, int dr, int dv, sd_type type, double scale, int Tq, const void* q,
+                           sd_stride_h qs, int Tk, const void* k, sd_stride_h ks, const void* kr, int64_t kr_stride,
+                           const void* v, sd_stride_h vs, const int32_t* cu_q, const int32_t* cu_k, void* out,
+                           sd_stride_h os, float* lse, void* ws, hipStream_t s);
 // Workgroups of the widest launch, workspace and launches of sd_token_logprobs
 // and sd_verify_tokens.
 int64_t logprobs_groups(int rows, int V);

@@ -33,47 +33,12 @@
 #include <math.h>
 #include <stdint.h>
 
-#include "common.hpp"
+#include "latent_common.hpp"
 
 namespace sd {
 namespace latent {
 
-constexpr int kThreads = 256, kTile = 64;
 constexpr int kGroups = 256;  // workgroups: one a compute unit (the tiles fill its LDS)
-constexpr float kLn2 = 0.69314718f;
-constexpr int kRope = 64;     // columns of the rotary part, zero past d_rope
-
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
-typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-
-struct Bf16 {
-  typedef __bf16 x8 __attribute__((ext_vector_type(8)));
-  __device__ static f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
-  }
-  __device__ static uint32_t pack(float lo, float hi) {
-    typedef __bf16 x2 __attribute__((ext_vector_type(2)));
-    const x2 r = {(__bf16)lo, (__bf16)hi};
-    return __builtin_bit_cast(uint32_t, r);
-  }
-  __device__ static float value(uint16_t v) { return __builtin_bit_cast(float, (uint32_t)v << 16); }
-  static constexpr uint32_t kExponent = 0x7f80;  // all set: an infinity or NaN
-};
-struct F16 {
-  typedef _Float16 x8 __attribute__((ext_vector_type(8)));
-  __device__ static f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
-  }
-  __device__ static uint32_t pack(float lo, float hi) {
-    typedef _Float16 x2 __attribute__((ext_vector_type(2)));
-    const x2 r = {(_Float16)lo, (_Float16)hi};
-    return __builtin_bit_cast(uint32_t, r);
-  }
-  __device__ static float value(uint16_t v) { return (float)__builtin_bit_cast(_Float16, v); }
-  static constexpr uint32_t kExponent = 0x7c00;
-};
 
 // How the rows of a sequence are dealt to workgroups: blocks of 16 R rows, teams
 // of `team` blocks that walk the same tokens, `supers` teams' worth a sequence.
@@ -122,27 +87,6 @@ __device__ __forceinline__ int rows_of(const Args& a, int b) {
 // The first tile of a team's run of a list of `total`.
 __device__ __forceinline__ int64_t run_begin(int64_t total, int team, int teams) { return total * team / teams; }
 __device__ __forceinline__ int tiles_of(int len) { return (len + kTile - 1) / kTile; }
-
-// The permutation of a token's 16-byte pieces (on the low three bits of their
-// number): eight tokens in a row have eight different ones, and so have the
-// piece pairs of four tokens in a row.
-__device__ __forceinline__ int perm(int token) { return ((token & 3) << 1) | ((token >> 2) & 1); }
-
-// LDS by byte offsets: one base and immediate offsets for a lane's reads.
-typedef __attribute__((address_space(3))) char* Lds;
-__device__ __forceinline__ Lds lds_of(void* p) { return (Lds)p; }
-template <class V>
-__device__ __forceinline__ V lds_read(Lds p) {
-  return *(__attribute__((address_space(3))) V*)p;
-}
-__device__ __forceinline__ u32x2 lds_read_tr(Lds p) {
-  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p));
-}
-// 16 bytes a lane from global memory to LDS at dst + 16 lane (dst uniform).
-typedef const __attribute__((address_space(1))) char* Global;
-__device__ __forceinline__ void load_lds(Global src, Lds dst) {
-  __builtin_amdgcn_global_load_lds(src, dst, 16, 0, 0);
-}
 
 template <class T, int R, int DC>
 __global__ __launch_bounds__(kThreads, 1) void latent_kernel(Args a) {
@@ -400,7 +344,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_kernel(Args a) {
         const int from = max(lim_lo - tl * kTile, 0), to = min(lim_hi - tl * kTile, kTile);
         for (int i = t; i < (to - from) * DC / 2; i += kThreads) {
           const uint32_t v = reinterpret_cast<const uint32_t*>(cur + (from + i / (DC / 2)) * C * 8)[i % (DC / 2)];
-          bad |= (v & T::kExponent) == T::kExponent || (v >> 16 & T::kExponent) == T::kExponent;
+          bad |= (lawless<T>(v) & 0x80008000u) != 0;
         }
         odd = __syncthreads_or(bad);
       } else {

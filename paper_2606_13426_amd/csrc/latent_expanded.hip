@@ -1,0 +1,436 @@
+// Causal attention of ragged sequences with per-head keys and values and one
+// rotary key a token that all heads share (the expanded form of latent
+// attention), for prompts (gfx950).
+//
+// A workgroup of four wavefronts takes 128 query rows of one head of one
+// sequence, a wavefront 32 of them, and walks the keys 64 at a time:
+//   S^T [keys][rows] = K Q^T      on v_mfma_f32_32x32x16, Q in registers
+//   P = 2^{S c - m}, c = scale log2(e)
+//   O^T [values][rows] += V^T P^T
+// In both results a lane holds one row (of the two halves of a wavefront, the same
+// row twice with other keys), so the softmax takes one exchange between the
+// halves, and S^T's registers are P^T's operand as they are: the instruction's
+// places along k are free to mean any keys as long as V^T, read by transposing LDS
+// loads, has the same order.  No value of S or P passes through LDS.
+//
+// m is a reference and not the maximum: it moves when a score exceeds it by
+// kSlack (weights then reach 2^kSlack, harmless in float32 and in fp16), so the
+// rescaling of O is left out of almost every tile.
+//
+// Tiles (K rotary and not, V) come by loads that write LDS directly, into the other
+// of two buffers while this one is multiplied; one barrier a tile.  80 KB of LDS
+// and at most 256 registers: two workgroups a compute unit, so one's products
+// cover the other's softmax.
+//
+// Where the rows' tiles do not fill the compute units the keys are split too, and
+// expanded_join_kernel joins the parts.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "common.hpp"
+#include "latent_common.hpp"
+
+namespace sd {
+namespace {
+
+using namespace latent;
+
+constexpr int kRows = 128;
+constexpr float kSlack = 8.f;
+
+struct Expanded {
+  int n, H, dn, dr, dv, Tq, Tk;
+  float c;     // |scale| log2(e)
+  uint32_t flip;  // sign bits of a pair, to negate q where scale is negative
+  const uint16_t *q, *k, *kr, *v;
+  int64_t qt, qh, kt, kh, krt, vt, vh;
+  const int32_t *cu_q, *cu_k;
+  uint16_t* out;
+  int64_t ot, oh;
+  float* lse;
+  int tiles, split;
+  float* part;   // [split][Tq][H][DV] unnormalised O
+  float2* stat;  // [split][Tq][H] (reference, sum)
+};
+
+__device__ __forceinline__ int offset_of(const int32_t* cu, int i, int total) { return min(max(cu[i], 0), total); }
+
+template <class T, int DN, int DV>
+__global__ __launch_bounds__(kThreads, 2) void expanded_kernel(Expanded a) {
+  constexpr int DK = DN + kRope, KS = DK / 16, NV = DV / 32;
+  constexpr int CN = DN / 8, CR = kRope / 8, CV = DV / 8;  // 16-byte pieces a token in the three parts
+  constexpr int kKr = kTile * DN * 2, kV = kKr + kTile * kRope * 2, kStage = kV + kTile * DV * 2;
+  __shared__ __align__(16) char buf[2 * kStage];
+  const int t = threadIdx.x, w = t >> 6, lane = t & 63, n = lane & 31, h = lane >> 5;
+
+  // the tiles of a head from the last to the first, a head's tiles on one XCD
+  const int id = xcd_tile((int)(gridDim.x * gridDim.y * gridDim.z));
+  const int part = id % a.split, tile = a.tiles - 1 - id / a.split % a.tiles, head = id / a.split / a.tiles;
+  // sequence b's tiles are numbered from cu_q[b] / 128 + b
+  int before = 0;
+  for (int b0 = 0; b0 < a.n; b0 += 64) {
+    const int b = b0 + lane;
+    before += __popcll(__ballot(b < a.n && offset_of(a.cu_q, b < a.n ? b : 0, a.Tq) / kRows + b <= tile));
+  }
+  const int b = __builtin_amdgcn_readfirstlane(max(before - 1, 0));
+  const int qb = offset_of(a.cu_q, b, a.Tq), kb = offset_of(a.cu_k, b, a.Tk);
+  const int nq = max(offset_of(a.cu_q, b + 1, a.Tq) - qb, 0), nk = max(offset_of(a.cu_k, b + 1, a.Tk) - kb, 0);
+  const int q0 = (tile - (qb / kRows + b)) * kRows;
+  if (q0 < 0 || q0 >= nq) return;
+  const int shift = nk - nq + 1;  // row i sees keys below i + shift
+  const int end = min(max(min(q0 + kRows, nq) - 1 + shift, 0), nk);
+  const int all = (end + kTile - 1) / kTile;
+  const int t0 = (int)((int64_t)all * part / a.split), t1 = (int)((int64_t)all * (part + 1) / a.split);
+
+  const int row = q0 + 32 * w + n;
+  const bool real = row < nq;
+  const int lim = real ? min(max(row + shift, 0), nk) : 0;
+  // the least and the largest limit of this wavefront's real rows
+  const int w_lo = min(max(q0 + 32 * w + shift, 0), nk);
+  const int w_hi = q0 + 32 * w < nq ? min(max(min(q0 + 32 * w + 31, nq - 1) + shift, 0), nk) : 0;
+
+  u32x4 qf[KS];
+  {
+    const uint16_t* src = a.q + (int64_t)(qb + min(row, nq - 1)) * a.qt + (int64_t)head * a.qh;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      const int col = 16 * k + 8 * h;
+      const int at = col < DN ? (col < a.dn ? col : -1) : (col - DN < a.dr ? a.dn + col - DN : -1);
+      qf[k] = u32x4{0u, 0u, 0u, 0u};
+      if (at >= 0) qf[k] = *reinterpret_cast<const u32x4*>(src + at);
+      qf[k] ^= a.flip;
+    }
+  }
+  f32x16 o[NV];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) o[k] = f32x16{};
+  float m = -INFINITY, l = 0.f;
+
+  // Piece 64 (w + 4 i) + lane of each part of a tile: its token, and the column (permuted among
+  // eight; -1 past the part's own).
+  const Global gk = (Global)(a.k + (int64_t)kb * a.kt + (int64_t)head * a.kh);
+  const Global gr = (Global)(a.kr + (int64_t)kb * a.krt);
+  const Global gv = (Global)(a.v + (int64_t)kb * a.vt + (int64_t)head * a.vh);
+  const Lds lds = lds_of(buf);
+  const bool padded = a.dn != DN || a.dr != kRope || a.dv != DV;
+  uint32_t off[(CN + CR + CV) / 4];
+  auto place = [&](int P, int i, int* tok) {
+    const int s = 64 * (w + 4 * i) + lane, pc = s % P;
+    *tok = s / P;
+    return ((pc & ~7) | ((pc ^ perm(*tok)) & 7)) * 8;
+  };
+  auto set_offsets = [&](int P, int64_t stride, uint32_t* to) {
+    for (int i = 0; i < P / 4; ++i) {
+      int tok;
+      const int col = place(P, i, &tok);
+      to[i] = 2u * (uint32_t)(tok * (int)stride + col);
+    }
+  };
+  set_offsets(CN, a.kt, off);
+  set_offsets(CR, a.krt, off + CN / 4);
+  set_offsets(CV, a.vt, off + (CN + CR) / 4);
+  auto load_part = [&](int P, const uint32_t* offs, Global base, int64_t stride, int d, int tl, Lds dst) {
+    const Global src = base + (int64_t)tl * kTile * stride * 2;
+    const int last = nk - 1 - tl * kTile;  // places behind the last key repeat it; their weights are 0
+    if (last >= kTile - 1 && !padded) {
+#pragma unroll
+      for (int i = 0; i < P / 4; ++i) load_lds(src + offs[i], dst + 1024 * (w + 4 * i));
+    } else {
+#pragma unroll
+      for (int i = 0; i < P / 4; ++i) {
+        int tok;
+        const int col = place(P, i, &tok);
+        if (col < d) load_lds(src + 2u * (uint32_t)(min(tok, last) * (int)stride + col), dst + 1024 * (w + 4 * i));
+      }
+    }
+  };
+  auto load_tile = [&](int tl, Lds dst) {
+    load_part(CN, off, gk, a.kt, a.dn, tl, dst);
+    load_part(CR, off + CN / 4, gr, a.krt, a.dr, tl, dst + kKr);
+    load_part(CV, off + (CN + CR) / 4, gv, a.vt, a.dv, tl, dst + kV);
+  };
+  if (padded) {
+    // pieces that no load writes are zero in both buffers
+    for (int i = t; i < 2 * kStage / 16; i += kThreads) reinterpret_cast<u32x4*>(buf)[i] = u32x4{0u, 0u, 0u, 0u};
+    __syncthreads();
+  }
+  if (t0 < t1) load_tile(t0, lds);
+
+  // what a lane reads of a tile, in bytes: of key n (and n + 32) piece 2 k + h; of values four tokens by
+  // sixteen columns, of which the lanes from 16 and 48 on take the upper sixteen of a block of 32
+  const int kx = h ^ perm(n);
+  const int vtok = 4 * h + ((lane & 15) >> 2), vch = 2 * (lane >> 4 & 1) + ((lane & 3) >> 1);
+  const int vrow[2] = {vtok * DV * 2 + (vch ^ perm(vtok)) * 16 + 8 * (lane & 1),
+                       vtok * DV * 2 + ((vch + 4) ^ perm(vtok)) * 16 + 8 * (lane & 1)};
+
+  for (int tl = t0; tl < t1; ++tl) {
+    const Lds here = lds + (tl - t0 & 1) * kStage;
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    if (tl + 1 < t1) load_tile(tl + 1, lds + (tl - t0 + 1 & 1) * kStage);
+    if (tl * kTile >= w_hi) continue;  // none of this wavefront's rows sees the tile
+
+    f32x16 s[2];
+#pragma unroll
+    for (int b2 = 0; b2 < 2; ++b2) {
+      s[b2] = f32x16{};
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        const int base = k < DN / 16 ? (32 * b2 + n) * DN * 2 : kKr + (32 * b2 + n) * kRope * 2;
+        const int kk = k < DN / 16 ? k : k - DN / 16;
+        const u32x4 kf = lds_read<u32x4>(here + base + (kk >> 2) * 128 + ((2 * (kk & 3)) ^ kx) * 16);
+        s[b2] = T::mfma32(kf, qf[k], s[b2]);
+      }
+    }
+#pragma unroll
+    for (int b2 = 0; b2 < 2; ++b2) asm volatile("" : "+v"(s[b2]));  // taken up before any branch
+    const bool edge = (tl + 1) * kTile > w_lo;
+    if (edge) {
+#pragma unroll
+      for (int b2 = 0; b2 < 2; ++b2)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          s[b2][i] = tl * kTile + 32 * b2 + 8 * (i >> 2) + 4 * h + (i & 3) < lim ? s[b2][i] : -INFINITY;
+    }
+    float mx = s[0][0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[0][i]);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[1][i]);
+    mx = fmaxf(mx, __shfl_xor(mx, 32)) * a.c;
+    // (a NaN score passes the maximum over and makes its row NaN by its weight)
+    const bool up = mx > m + kSlack || (m == -INFINITY && mx > -INFINITY);
+    if (__any(up)) {
+      const float to = up ? mx : m, f = up ? __builtin_amdgcn_exp2f(m - to) : 1.f;
+#pragma unroll
+      for (int k = 0; k < NV; ++k) o[k] *= f;
+      l *= f;
+      m = to;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;
+    u32x4 pf[4];
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int b2 = 0; b2 < 2; ++b2)
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) {
+        const float p0 = __builtin_amdgcn_exp2f(__fmaf_rn(s[b2][i], a.c, -ref));
+        const float p1 = __builtin_amdgcn_exp2f(__fmaf_rn(s[b2][i + 1], a.c, -ref));
+        sum[i & 2] += p0;
+        sum[(i & 2) + 1] += p1;
+        pf[2 * b2 + (i >> 3)][(i & 7) >> 1] = T::pack(p0, p1);
+      }
+    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+
+    auto values = [&](int st, int k) {
+      const Lds src = here + kV + st * 16 * DV * 2 + vrow[k & 1] + (k >> 1) * 128;
+      const u32x2 lo = lds_read_tr(src), hi = lds_read_tr(src + 8 * DV * 2);
+      return u32x4{lo[0], lo[1], hi[0], hi[1]};
+    };
+    // A key that some rows see and others do not: its weight for those is 0, and 0 times
+    // an infinity or NaN in its value is not.
+    if (edge) {
+      const int from = max(w_lo - tl * kTile, 0);
+      uint32_t bad = 0;
+      for (int i = lane; i < (kTile - from) * CV; i += 64) {
+        const u32x4 v = lds_read<u32x4>(here + kV + from * DV * 2 + 16 * i);
+        bad |= (lawless<T>(v[0]) | lawless<T>(v[1])) | (lawless<T>(v[2]) | lawless<T>(v[3]));
+      }
+      if (__any((bad & 0x80008000u) != 0)) {
+        // finite values as they are, and whether a row sees an infinity of either sign (a NaN counts as both)
+        u32x4 seen[4];
+#pragma unroll
+        for (int st = 0; st < 4; ++st)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int key = tl * kTile + 16 * st + 8 * (j >> 1) + 4 * h + 2 * (j & 1);
+            seen[st][j] = (key < lim ? T::kOne : 0u) | (key + 1 < lim ? T::kOne << 16 : 0u);
+          }
+        auto sign = [&](uint32_t v, bool minus) {
+          uint32_t r = 0;
+#pragma unroll
+          for (int u = 0; u < 32; u += 16) {
+            const uint32_t x = v >> u & 0xffffu;
+            const bool inf = (x & 0x7fffu) == T::kExponent, nan = (x & 0x7fffu) > T::kExponent;
+            if (nan || (inf && (x >> 15 != 0) == minus)) r |= T::kOne << u;
+          }
+          return r;
+        };
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+          uint32_t mark = 0;  // bits i: an infinity, 16 + i: minus one
+#pragma unroll 1
+          for (int minus = 0; minus < 2; ++minus) {
+            f32x16 c = f32x16{};
+#pragma unroll
+            for (int st = 0; st < 4; ++st) {
+              const u32x4 v = values(st, k);
+              c = T::mfma32(u32x4{sign(v[0], minus), sign(v[1], minus), sign(v[2], minus), sign(v[3], minus)}, seen[st], c);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) mark |= c[i] > 0.f ? 1u << (16 * minus + i) : 0u;
+          }
+#pragma unroll
+          for (int st = 0; st < 4; ++st) {
+            u32x4 v = values(st, k);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const uint32_t x = lawless<T>(v[j]);
+              v[j] &= ((x & 0x8000u) ? 0u : 0xffffu) | ((x & 0x80000000u) ? 0u : 0xffff0000u);
+            }
+            o[k] = T::mfma32(v, pf[st], o[k]);
+          }
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            if (mark >> i & 1u) o[k][i] += INFINITY;
+            if (mark >> (16 + i) & 1u) o[k][i] -= INFINITY;
+          }
+        }
+        continue;
+      }
+    }
+#pragma unroll
+    for (int st = 0; st < 4; ++st)
+#pragma unroll
+      for (int k = 0; k < NV; ++k) o[k] = T::mfma32(values(st, k), pf[st], o[k]);
+    // wait states for a read of the last results behind the loop's branch
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_nop 15\n\ts_nop 15");
+    __builtin_amdgcn_sched_barrier(0);
+  }
+
+  l += __shfl_xor(l, 32);
+  if (!real) return;
+  const int64_t at = (int64_t)(qb + row) * a.H + head;
+  if (a.split > 1) {
+    float* dst = a.part + ((int64_t)part * a.Tq * a.H + at) * DV;
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4)
+        *reinterpret_cast<f32x4*>(dst + 32 * k + 2 * i + 4 * h) = f32x4{o[k][i], o[k][i + 1], o[k][i + 2], o[k][i + 3]};
+    if (h == 0) a.stat[(int64_t)part * a.Tq * a.H + at] = make_float2(m, l);
+    return;
+  }
+  const float f = l > 0.f ? 1.f / l : l != l ? NAN : 0.f;
+  uint16_t* dst = a.out + (int64_t)(qb + row) * a.ot + (int64_t)head * a.oh;
+#pragma unroll
+  for (int k = 0; k < NV; ++k)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      const int col = 32 * k + 2 * i + 4 * h;
+      if (col < a.dv)
+        *reinterpret_cast<u32x2*>(dst + col) = u32x2{T::pack(o[k][i] * f, o[k][i + 1] * f), T::pack(o[k][i + 2] * f, o[k][i + 3] * f)};
+    }
+  if (a.lse && h == 0) a.lse[at] = (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// The parts of rows whose keys were split, joined: DV / 4 threads a row.
+template <class T, int DV>
+__global__ __launch_bounds__(kThreads) void expanded_join_kernel(Expanded a) {
+  constexpr int kWays = DV / 4;
+  const int64_t at = (int64_t)blockIdx.x * (kThreads / kWays) + threadIdx.x / kWays, rows = (int64_t)a.Tq * a.H;
+  if (at >= rows) return;
+  const int tok = (int)(at / a.H), head = (int)(at % a.H), c = threadIdx.x % kWays * 4;
+  // rows before the first sequence and behind the last are nobody's
+  if (tok < offset_of(a.cu_q, 0, a.Tq) || tok >= offset_of(a.cu_q, a.n, a.Tq)) return;
+  float m = -INFINITY;
+  for (int s = 0; s < a.split; ++s) m = fmaxf(m, a.stat[s * rows + at].x);
+  const float ref = m == -INFINITY ? 0.f : m;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  float l = 0.f;
+  for (int s = 0; s < a.split; ++s) {
+    const float2 st = a.stat[s * rows + at];
+    const float f = __builtin_amdgcn_exp2f(st.x - ref);
+    l += st.y * f;
+    o += *reinterpret_cast<const f32x4*>(a.part + (s * rows + at) * DV + c) * f;
+  }
+  const float f = l > 0.f ? 1.f / l : l != l ? NAN : 0.f;
+  if (c < a.dv)
+    *reinterpret_cast<u32x2*>(a.out + (int64_t)tok * a.ot + (int64_t)head * a.oh + c) =
+        u32x2{T::pack(o[0] * f, o[1] * f), T::pack(o[2] * f, o[3] * f)};
+  if (a.lse && c == 0) a.lse[at] = (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+inline size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
+inline int tiles_of(int Tq, int n) { return Tq / kRows + n; }
+// The parts that a row's keys are split into: as many as fill 256 compute units
+// with two workgroups, at most 8, and none of fewer than 256 keys where all have
+// the same number.
+inline int split_of(int n, int H, int Tq, int Tk) {
+  const int64_t groups = (int64_t)tiles_of(Tq, n) * H;
+  int s = 1;
+  while (s < 8 && groups * 2 * s <= 512 && Tk / n >= 512 * s) s *= 2;
+  return s;
+}
+inline int padded_dv(int dn, int dv) { return dn <= 64 && dv <= 64 ? 64 : 128; }
+
+template <class T>
+hipError_t run(const Expanded& a, hipStream_t s) {
+  const dim3 grid((unsigned)(a.tiles * a.split), (unsigned)a.H), block(kThreads);
+  const bool small = padded_dv(a.dn, a.dv) == 64;
+  hipError_t e = small ? launch_timed("latent_expanded", expanded_kernel<T, 64, 64>, grid, block, s, a)
+                       : launch_timed("latent_expanded", expanded_kernel<T, 128, 128>, grid, block, s, a);
+  if (e != hipSuccess || a.split == 1) return e;
+  const int per = kThreads / (small ? 16 : 32);
+  const dim3 jgrid((unsigned)(((int64_t)a.Tq * a.H + per - 1) / per));
+  return small ? launch_timed("latent_expanded_join", expanded_join_kernel<T, 64>, jgrid, block, s, a)
+               : launch_timed("latent_expanded_join", expanded_join_kernel<T, 128>, jgrid, block, s, a);
+}
+
+}  // namespace
+
+size_t expanded_ws_bytes(int n, int H, int dn, int dv, int Tq, int Tk) {
+  const int split = split_of(n, H, Tq, Tk);
+  if (split == 1) return 0;
+  const size_t rows = (size_t)split * Tq * H;
+  return up256(rows * padded_dv(dn, dv) * sizeof(float)) + up256(rows * sizeof(float2));
+}
+int64_t expanded_groups(int n, int H, int Tq, int Tk) {
+  return (int64_t)tiles_of(Tq, n) * H * split_of(n, H, Tq, Tk);
+}
+
+hipError_t expanded_launch(int n, int H, int dn, int dr, int dv, sd_type type, double scale, int Tq, const void* q,
+                           sd_stride_h qs, int Tk, const void* k, sd_stride_h ks, const void* kr, int64_t kr_stride,
+                           const void* v, sd_stride_h vs, const int32_t* cu_q, const int32_t* cu_k, void* out,
+                           sd_stride_h os, float* lse, void* ws, hipStream_t s) {
+  Expanded a;
+  a.n = n;
+  a.H = H;
+  a.dn = dn;
+  a.dr = dr;
+  a.dv = dv;
+  a.Tq = Tq;
+  a.Tk = Tk;
+  // |scale| at least 1e-30, so that a masked score stays -inf where scale is 0
+  a.c = (float)fmax(fabs(scale) * 1.44269504088896340736, 1e-30);
+  a.flip = scale < 0.0 ? 0x80008000u : 0u;
+  a.q = static_cast<const uint16_t*>(q);
+  a.k = static_cast<const uint16_t*>(k);
+  a.kr = static_cast<const uint16_t*>(kr);
+  a.v = static_cast<const uint16_t*>(v);
+  a.qt = qs.row;
+  a.qh = qs.head;
+  a.kt = ks.row;
+  a.kh = ks.head;
+  a.krt = kr_stride;
+  a.vt = vs.row;
+  a.vh = vs.head;
+  a.cu_q = cu_q;
+  a.cu_k = cu_k;
+  a.out = static_cast<uint16_t*>(out);
+  a.ot = os.row;
+  a.oh = os.head;
+  a.lse = lse;
+  a.tiles = tiles_of(Tq, n);
+  a.split = split_of(n, H, Tq, Tk);
+  a.part = static_cast<float*>(ws);
+  a.stat = reinterpret_cast<float2*>(static_cast<char*>(ws) +
+                                     up256((size_t)a.split * Tq * H * padded_dv(dn, dv) * sizeof(float)));
+  return type == SD_TYPE_BF16 ? run<Bf16>(a, s) : run<F16>(a, s);
+}
+
+}  // namespace sd

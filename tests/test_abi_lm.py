@@ -120,3 +120,39 @@ def test_latent_binding_refuses():
         _lib.sd_latent_attention(q, c.bfloat16(), n, 128)
     with pytest.raises(_lib.SpecDiffError, match="not on the current GPU"):
         _lib.sd_latent_attention(q, c, n, 128)
+
+
+def _expanded(lib, **kw):
+    s = _lib.sd_stride_h
+    a = dict(n=2, H=4, dn=128, dr=64, dv=128, type=1, scale=0.1, Tq=50, q=P, qs=s(0, 768, 192), Tk=90, k=P,
+             ks=s(0, 1024, 256), kr=P, krs=64, v=P, vs=s(0, 1024, 256), cu_q=P, cu_k=P, out=P, os=s(0, 512, 128), lse=None,
+             ws=P, ws_bytes=1 << 40)
+    a.update(kw)
+    return lib.sd_latent_attention_expanded(*a.values(), None)
+
+
+@pytest.mark.parametrize("kw,needle", [
+    (dict(n=0), ">= 1"), (dict(H=0), ">= 1"), (dict(Tq=0), ">= 1"), (dict(Tk=0), ">= 1"), (dict(dn=136), "d_nope = 136"),
+    (dict(dn=0), "d_nope = 0"), (dict(dv=20), "d_v = 20"), (dict(dr=72), "d_rope = 72"), (dict(dr=60), "d_rope = 60"),
+    (dict(type=0), "type"), (dict(scale=float("nan")), "scale"), (dict(q=None), "NULL"), (dict(kr=None), "NULL"),
+    (dict(cu_k=None), "NULL"), (dict(qs=_lib.sd_stride_h(0, 768, 190)), "q strides"),
+    (dict(qs=_lib.sd_stride_h(0, 700, 192)), "q strides"), (dict(ks=_lib.sd_stride_h(0, 1024, 120)), "k strides"),
+    (dict(ks=_lib.sd_stride_h(0, 1 << 24, 256)), "k strides"), (dict(vs=_lib.sd_stride_h(0, 128, 128)), "v strides"),
+    (dict(os=_lib.sd_stride_h(0, 512, 64)), "out strides"), (dict(krs=56), "k_rope stride"),
+    (dict(krs=68), "k_rope stride"), (dict(v=ctypes.c_void_p(264)), "16-byte"), (dict(Tk=1 << 30), "too many rows"),
+    (dict(Tq=1 << 29, H=8, qs=_lib.sd_stride_h(0, 1536, 192)), "too many rows"),
+    (dict(n=1, Tk=8000, ws=None), "NULL workspace"), (dict(n=1, Tk=8000, ws_bytes=10), "workspace 10 <"),
+    (dict(n=1, Tk=8000, ws=ctypes.c_void_p(128)), "256-byte")])
+def test_expanded_refuses(lib, kw, needle):
+    _refused(_expanded(lib, **kw), needle)
+
+
+def test_expanded_binding_refuses():
+    h, i = (lambda *s: torch.zeros(*s).half()), torch.zeros(3, dtype=torch.int32)
+    with pytest.raises(_lib.SpecDiffError, match="agree in heads"):
+        _lib.sd_latent_attention_expanded(h(5, 2, 192), h(9, 3, 128), h(9, 64), h(9, 3, 128), i, i)
+    with pytest.raises(_lib.SpecDiffError, match="k_rope must be"):
+        _lib.sd_latent_attention_expanded(h(5, 2, 192), h(9, 2, 128), None, h(9, 2, 128), i, i)
+    with pytest.raises(_lib.SpecDiffError, match="not on the current GPU"):
+        _lib.sd_latent_attention_expanded(h(5, 2, 192), h(9, 2, 128), h(9, 64), h(9, 2, 128), i, i)
+    assert _lib.sd_latent_attention_expanded_workspace(1, 2, 130, 64, 128, 5, 9) == 0
