@@ -1144,6 +1144,9 @@ sd_status sd_latent_attention(int32_t B, int32_t Q, int32_t H, int32_t d_latent,
     SD_CHECK_ARG(n_pages >= B, "sd_latent_attention: without a table n_pages = %d must be >= B = %d", n_pages, B);
     SD_CHECK_ARG(page_size < (1 << 30), "sd_latent_attention: a page holds 2^30 tokens or more");
   }
+  // (a sequence's rows are walked by at most one workgroup for every 64 of them)
+  SD_CHECK_ARG(((int64_t)(pages ? max_pages : 1) * page_size / 64 + 1) * B * ((int64_t)Q * H / 64 + 1) < ((int64_t)1 << 31),
+               "sd_latent_attention: too many rows and tokens for one call");
   const int d = d_latent + d_rope;
   SD_CHECK_ARG(token_stride >= d && token_stride % 8 == 0 && page_stride % 8 == 0 &&
                    (n_pages == 1 || page_stride >= (int64_t)page_size * token_stride),

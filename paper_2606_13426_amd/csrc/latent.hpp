@@ -2,28 +2,30 @@
 // vector a token (gfx950): keys are the whole vector (latent and rotary part),
 // values its latent part.
 //
-// A workgroup of four wavefronts takes 16 R rows (row, head pairs) of one
-// sequence and a run of its tokens, 64 at a time.  A tile of the cache enters LDS
-// once and serves both products, so a token's bytes come from HBM once for all
-// the rows of a workgroup:
-//   S^T [tokens][rows] = C Q^T   wavefront w: tokens 16 w .. 16 w + 15, all rows;
-//                                its part of Q stays in registers
-//   P = e^{S - m}                running maxima over the four wavefronts by LDS
-//   O^T [latent][rows] = C^T P^T wavefront w: a quarter of the latent columns,
-//                                all rows, accumulators in registers
+// A workgroup takes 16 R rows (row, head pairs) of one sequence and a run of its
+// tokens, 64 at a time.  A tile of the cache enters LDS once and serves both
+// products, so a token's bytes come from HBM once for all the rows of a workgroup:
+//   S^T [tokens][rows] = C Q^T   a wavefront: 16 tokens, the rows of one of WR
+//                                groups; its part of Q stays in registers
+//   P = 2^{S c - m}, c = scale log2(e); maxima over the tokens' wavefronts by LDS
+//   O^T [latent][rows] = C^T P^T a wavefront: DC / (4 WR) latent columns, all
+//                                rows, accumulators in registers
 // on v_mfma_f32_16x16x32.  In both results a lane holds one row of each block of
 // 16, so its maximum, sum and rescaling need no exchange inside the products.
 // C^T is read by transposing LDS loads; the order in which the 32 tokens of a
 // step meet the instruction's k places is the one those loads give, and P is
 // stored to match.
 //
+// m is a reference and not the maximum: it moves when a score exceeds it by kSlack,
+// so the rescaling of O is left out of almost every tile.
+//
 // Tiles come by loads that write LDS directly, the next one while this one is
 // multiplied.  A token's 16-byte pieces are permuted inside each 128 bytes by
 // perm(token), which the lanes' global addresses do, so that both products'
 // reads meet every bank once.
 //
-// The tokens of all sequences form one list that is cut into equal runs, one a
-// workgroup (a team of workgroups where one sequence's rows take several: they
+// The tokens of all sequences form one list of tiles that is cut into equal runs,
+// one a workgroup (a team of workgroups where one sequence's rows take several: they
 // run on one XCD, whose L2 then holds the tile for all of them).  A run may end
 // inside a sequence: its part is left in the workspace and joined by
 // latent_join_kernel.
@@ -32,6 +34,8 @@
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
+
+#include <type_traits>
 
 #include "latent_common.hpp"
 
@@ -58,7 +62,8 @@ inline Plan plan(int Q, int H) {
 
 struct Args {
   int B, Q, H, dc, dr;
-  float c;  // scale log2(e)
+  float c;        // |scale| log2(e)
+  uint32_t flip;  // sign bits of a pair, to negate q where scale is negative
   const uint16_t* q;
   int64_t qs, qr, qh;
   const uint16_t* cache;
@@ -74,116 +79,120 @@ struct Args {
   float* lse;  // null, or [B][Q][H]
   Plan p;
   float* part;     // [kGroups][2][16 R][DC] unnormalised O
-  float2* stat;    // [kGroups][2][16 R] (maximum in log2 units, sum)
+  float2* stat;    // [kGroups][2][16 R] (reference in log2 units, sum)
   int32_t* first;  // [B][supers] 2 team + slot of the run that starts the sequence; -1: one run did it all
   int32_t* last;   // [B][supers] the team that ends it
-  int64_t* total;  // the list's tiles
 };
 
 __device__ __forceinline__ int length_of(const Args& a, int b) { return min(max(a.lens[b], 0), a.capacity); }
 __device__ __forceinline__ int rows_of(const Args& a, int b) {
   return a.rows ? min(max(a.rows[b], 0), a.Q) : a.Q;
 }
-// The first tile of a team's run of a list of `total`.
-__device__ __forceinline__ int64_t run_begin(int64_t total, int team, int teams) { return total * team / teams; }
 __device__ __forceinline__ int tiles_of(int len) { return (len + kTile - 1) / kTile; }
+// Team `team` of `teams` (a multiple of 8 that go round the XCDs) runs as workgroups group_of(.., 0..).
+__device__ __forceinline__ int group_of(int team, int member, int size) {
+  return (team / 8 * size + member) * 8 + team % 8;
+}
 
 template <class T, int R, int DC>
-__global__ __launch_bounds__(kThreads, 1) void latent_kernel(Args a) {
-  constexpr int C = (DC + kRope) / 8;      // 16-byte pieces of a token
-  constexpr int KS = (DC + kRope) / 32;    // steps of 32 columns of Q
-  constexpr int NB = DC / 64;              // blocks of 16 latent columns of a wavefront
-  constexpr int NL = C / 4;                // loads of 64 pieces for a wavefront's 16 tokens
-  static_assert(C % 8 == 0 && DC % 128 == 0, "whole 128-byte segments, and whole blocks a wavefront");
+__global__ __launch_bounds__(R == 1 ? 256 : 512) void latent_kernel(Args a) {
+  constexpr int WR = R == 1 ? 1 : 2, kWaves = 4 * WR, kLanes = 64 * kWaves, RB = R / WR;
+  constexpr int C = (DC + kRope) / 8;     // 16-byte pieces of a token
+  constexpr int KS = (DC + kRope) / 32;   // steps of 32 columns of Q
+  constexpr int NB = DC / (16 * kWaves);  // blocks of 16 latent columns of a wavefront
+  constexpr int TW = kTile / kWaves;      // tokens that a wavefront loads
+  constexpr int NL = TW * C / 64;         // its loads, of 64 pieces
+  constexpr int NV = NB < 4 ? NB : 4;
+  static_assert(C % 8 == 0 && DC % 128 == 0 && NL * 64 == TW * C, "whole 128-byte segments, blocks and loads");
   __shared__ __align__(16) uint16_t tile[2][kTile * C * 8];
   __shared__ __align__(16) uint16_t pl[16 * R * kTile];
   __shared__ float red[4][16 * R];
-  __shared__ int64_t scan[4];
-  __shared__ int64_t found[2];
+  __shared__ float fac[16 * R];
+  __shared__ int limits[16 * R];
+  __shared__ int moved[2][WR];
+  __shared__ uint32_t present[kWaves];
 
-  const int t = threadIdx.x, w = t >> 6, lane = t & 63, n = lane & 15, g = lane >> 4;
-  const int L = blockIdx.x, per = kGroups / 8 / a.p.team;
-  const int i8 = L / 8, team = (L % 8) * per + i8 / a.p.team, member = i8 % a.p.team;
-  if (i8 >= per * a.p.team) return;
+  const int t = threadIdx.x, lane = t & 63, n = lane & 15, g = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(t >> 6), wt = w & 3, wr = w >> 2;
+  const int L = blockIdx.x, i8 = L / 8, team = i8 / a.p.team * 8 + L % 8, member = i8 % a.p.team;
 
-  // this team's run of the list of all sequences' tiles
-  int64_t mine = 0;
-  const int bper = (a.B + kThreads - 1) / kThreads, b0 = min(t * bper, a.B), b1 = min(b0 + bper, a.B);
-  for (int b = b0; b < b1; ++b) mine += (int64_t)tiles_of(length_of(a, b)) * a.p.supers;
-  int64_t upto = mine;
+  // this team's run of the list of all sequences' tiles: found by each wavefront for itself
+  int total = 0;
+  for (int b0 = 0; b0 < a.B; b0 += 64) {
+    const int b = b0 + lane;
+    total += b < a.B ? tiles_of(length_of(a, b)) * a.p.supers : 0;
+  }
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int64_t o = __shfl_up((long long)upto, d);
-    if (lane >= d) upto += o;
-  }
-  if (lane == 63) scan[w] = upto;
-  __syncthreads();
-  for (int i = 0; i < w; ++i) upto += scan[i];
-  const int64_t total = scan[0] + scan[1] + scan[2] + scan[3];
-  const int64_t begin = run_begin(total, team, a.p.teams), end = run_begin(total, team + 1, a.p.teams);
-  if (L == 0 && t == 0) *a.total = total;
-  if (begin >= end) return;
-  if (begin < upto && begin >= upto - mine) {
-    int64_t at = upto - mine;
-    for (int b = b0; b < b1; ++b) {
-      const int64_t nb = (int64_t)tiles_of(length_of(a, b)) * a.p.supers;
-      if (begin < at + nb) {
-        found[0] = b;
-        found[1] = begin - at;
-        break;
-      }
-      at += nb;
+  for (int d = 1; d < 64; d <<= 1) total += __shfl_xor(total, d);
+  total = __builtin_amdgcn_readfirstlane(total);
+  const int teams = min(a.p.teams, total);
+  if (team >= teams) return;
+  const int share = total / teams, more = total - share * teams;
+  const int begin = team * share + min(team, more);
+  int left = share + (team < more ? 1 : 0);
+  int b = 0, within = 0;
+  for (int b0 = 0, at = 0;; b0 += 64) {
+    const int bb = b0 + lane, mine = bb < a.B ? tiles_of(length_of(a, bb)) * a.p.supers : 0;
+    int upto = mine;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int o = __shfl_up(upto, d);
+      if (lane >= d) upto += o;
     }
+    const uint64_t hit = __ballot(at + upto > begin);
+    if (hit) {
+      const int i = __ffsll((unsigned long long)hit) - 1;
+      b = b0 + i;
+      within = begin - at - __builtin_amdgcn_readlane(upto - mine, i);
+      break;
+    }
+    at += __builtin_amdgcn_readlane(upto, 63);
+    if (b0 + 64 >= a.B) return;  // (not reached: begin is below the total)
   }
-  __syncthreads();
-  int b = __builtin_amdgcn_readfirstlane((int)found[0]);
-  int64_t within = found[1];
-  int64_t left = end - begin;
 
-  // The pieces that this lane loads: piece 64 i + lane of the wavefront's sixteen
-  // tokens, in bytes from the first one's address where they lie one after another.
+  // The pieces that this lane loads: piece 64 i + lane of the wavefront's TW tokens.
   auto piece_token = [&](int i) { return (8 * i + (lane >> 3)) / (C / 8); };
   auto piece_col = [&](int i) {  // its column in a token, -1 past d_latent or d_rope
     const int tok = piece_token(i), pc = 64 * i + lane - tok * C, col = ((pc & ~7) | ((pc ^ perm(tok)) & 7)) * 8;
     return col < DC ? (col < a.dc ? col : -1) : (col - DC < a.dr ? a.dc + col - DC : -1);
   };
   const bool padded = a.dc != DC || a.dr != kRope;
-  const bool rowed = (a.pages == nullptr || a.page_size % 16 == 0) && a.token_stride < (1 << 24);
+  // Where a wavefront's tokens lie one after another in one page, a tile's loads have one scalar
+  // address and a lane's fixed offsets.
+  const bool rowed = (a.pages == nullptr || a.page_size % TW == 0) && a.token_stride < (1 << 24) && !padded;
   uint32_t off[NL];
 #pragma unroll
   for (int i = 0; i < NL; ++i) off[i] = 2u * (uint32_t)(piece_token(i) * (int)a.token_stride + piece_col(i));
   // what a lane reads of a tile and of P, in bytes
   const int kx = g ^ perm(n);
-  const int krow[2] = {((16 * w + n) * C + kx) * 16, ((16 * w + n) * C + (kx ^ 4)) * 16};
-  int vrow[NB < 4 ? NB : 4];
+  const int krow[2] = {((16 * wt + n) * C + kx) * 16, ((16 * wt + n) * C + (kx ^ 4)) * 16};
+  int vrow[NV];
 #pragma unroll
-  for (int k = 0; k < (NB < 4 ? NB : 4); ++k) {
+  for (int k = 0; k < NV; ++k) {
     // lanes 4 r' .. 4 r' + 3 of a group of 16 read token 4 g + r' (and 16 later), 16 columns together
     const int tok = 4 * g + (n >> 2), ch = (w * NB + k) * 2 + ((lane & 3) >> 1);
     vrow[k] = (tok * C + ((ch & ~7) | ((ch ^ perm(tok)) & 7))) * 16 + 8 * (lane & 1);
   }
   const int px = g ^ (n & 7), prow[2] = {n * 128 + px * 16, n * 128 + (px ^ 4) * 16};
-  // block 4 w + g of four tokens: step w / 2, place g, half w % 2
-  const int pdst = n * 128 + ((4 * (w >> 1) + g) ^ (n & 7)) * 16 + 8 * (w & 1);
+  // block 4 wt + g of four tokens: step wt / 2, place g, half wt % 2
+  const int pdst = n * 128 + ((4 * (wt >> 1) + g) ^ (n & 7)) * 16 + 8 * (wt & 1) + 2048 * RB * wr;
   const Lds tiles = lds_of(tile), weights = lds_of(pl);
-  // pieces that no load writes are zero in both buffers
-  for (int i = t; i < kTile * C; i += kThreads) {
-    const u32x4 z = {0u, 0u, 0u, 0u};
-    reinterpret_cast<u32x4*>(tile[0])[i] = z;
-    reinterpret_cast<u32x4*>(tile[1])[i] = z;
+
+  if (padded) {
+    // pieces that no load writes are zero in both buffers
+    for (int i = t; i < 2 * kTile * C; i += kLanes) reinterpret_cast<u32x4*>(tile)[i] = u32x4{0u, 0u, 0u, 0u};
   }
   __syncthreads();
 
   for (int seg = 0; left > 0; ++seg) {
-    const int len = __builtin_amdgcn_readfirstlane(length_of(a, b)), nt = tiles_of(len);
-    const int64_t units = (int64_t)nt * a.p.supers;
+    const int len = __builtin_amdgcn_readfirstlane(length_of(a, b)), nt = tiles_of(len), units = nt * a.p.supers;
     if (within >= units) {
       within -= units;
       ++b;
+      --seg;
       continue;
     }
-    const int super = __builtin_amdgcn_readfirstlane((int)(within / nt)), t0 = __builtin_amdgcn_readfirstlane((int)(within % nt));
-    const int t1 = __builtin_amdgcn_readfirstlane((int)(left < nt - t0 ? t0 + left : nt));
+    const int super = within / nt, t0 = within - super * nt, t1 = min(t0 + left, nt);
     within += t1 - t0;
     left -= t1 - t0;
     const int slot = seg == 0 ? 0 : 1;
@@ -197,183 +206,192 @@ __global__ __launch_bounds__(kThreads, 1) void latent_kernel(Args a) {
     // query rows' limits: row i of n sees len - n + i + 1 tokens
     const int rlast = min(r0 + 16 * R, nrow * a.H) - 1;
     const int lim_lo = max(len - nrow + r0 / a.H + 1, 0), lim_hi = max(len - nrow + rlast / a.H + 1, 0);
-    int lim[R];
-    u32x4 qf[R][KS];
+
+    // Tile tl's part of this wavefront: tokens tl * 64 + TW w .. + TW - 1.  Returns which of them some
+    // row sees and whose page exists; the others are not loaded.
+    const int32_t* table = a.pages ? a.pages + (int64_t)b * a.pages_stride : nullptr;
+    auto load_tile = [&](int tl, Lds dst) -> uint32_t {
+      const int j0 = tl * kTile + TW * w, count = min(max(lim_hi - j0, 0), TW);
+      dst += TW * w * C * 16;
+      if (rowed && count == TW) {
+        const int pg = table ? j0 / a.page_size : 0, page = table ? table[pg] : b;
+        if (page < 0 || page >= a.n_pages) return 0u;
+        const Global base = (Global)(a.cache + (int64_t)page * a.page_stride +
+                                     (int64_t)(j0 - pg * a.page_size) * a.token_stride);
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const int row = r0 + 16 * r + n, i = row / a.H, h = row - i * a.H;
-      const bool in = row <= rlast;
-      lim[r] = in ? max(len - nrow + i + 1, 0) : 0;
+        for (int i = 0; i < NL; ++i) load_lds(base + off[i], dst + 1024 * i);
+        return (1u << TW) - 1u;
+      }
+      const int j = j0 + lane % TW, pg = j / a.page_size;
+      const int page = lane % TW < count ? (table ? table[pg] : b) : -1;
+      const bool ok = page >= 0 && page < a.n_pages;
+      const uint32_t valid = (uint32_t)__ballot(ok) & ((1u << TW) - 1u);
+      const uint64_t adr = reinterpret_cast<uint64_t>(
+          a.cache + (ok ? (int64_t)page * a.page_stride + (int64_t)(table ? j - pg * a.page_size : j) * a.token_stride : 0));
+#pragma unroll 1
+      for (int i = 0; i < NL; ++i) {
+        const int tok = piece_token(i), col = piece_col(i);
+        const uint32_t lo = __shfl((int)(uint32_t)adr, tok), hi = __shfl((int)(uint32_t)(adr >> 32), tok);
+        if (col >= 0 && (valid >> tok & 1u)) load_lds((Global)(((uint64_t)hi << 32) | lo) + 2 * col, dst + 1024 * i);
+      }
+      return valid;
+    };
+    // tokens that no row sees, or of no page, become zero vectors
+    auto clear_rest = [&](uint32_t valid, Lds dst) {
+      dst += TW * w * C * 16;
+      for (int i = lane; i < TW * C; i += 64)
+        if (!(valid >> (i / C) & 1u)) *(__attribute__((address_space(3))) u32x4*)(dst + 16 * i) = u32x4{0u, 0u, 0u, 0u};
+    };
+    uint32_t valid = load_tile(t0, tiles);
+    if (t < 2 * WR) moved[t / WR][t % WR] = 0;
+    if (t < 16 * R) limits[t] = r0 + t <= rlast ? len - nrow + (r0 + t) / a.H + 1 : 0;
+
+    int lim[RB];
+    u32x4 qf[RB][KS];
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+      const int row = r0 + 16 * (RB * wr + r) + n, i = min(row, rlast) / a.H, h = min(row, rlast) - i * a.H;
+      lim[r] = row <= rlast ? max(len - nrow + i + 1, 0) : 0;
       const uint16_t* src = a.q + (int64_t)b * a.qs + (int64_t)i * a.qr + (int64_t)h * a.qh;
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
         const int col = 32 * k + 8 * g;
         const int at = col < DC ? (col < a.dc ? col : -1) : (col - DC < a.dr ? a.dc + col - DC : -1);
         qf[r][k] = u32x4{0u, 0u, 0u, 0u};
-        if (in && at >= 0) qf[r][k] = *reinterpret_cast<const u32x4*>(src + at);
+        if (!padded || at >= 0) qf[r][k] = *reinterpret_cast<const u32x4*>(src + at);
+        qf[r][k] ^= a.flip;
       }
     }
     f32x4 o[R][NB];
-    float m[R], l[R];
+    float m[RB], l[RB];
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      m[r] = -INFINITY;
-      l[r] = 0.f;
+    for (int r = 0; r < R; ++r)
 #pragma unroll
       for (int k = 0; k < NB; ++k) o[r][k] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
-
-    // The address of token `tile * 64 + 16 w + n` of this wavefront's sixteen, and
-    // whether any row of the workgroup sees it and its page exists.
-    const int32_t* table = a.pages ? a.pages + (int64_t)b * a.pages_stride : nullptr;
-    auto page_of = [&](int tl) {
-      const int j = tl * kTile + 16 * w + n;
-      return j < lim_hi ? (table ? table[j / a.page_size] : b) : -1;
-    };
-    auto load_tile = [&](int tl, int page, Lds dst) {
-      const int j0 = tl * kTile + 16 * w, j = j0 + n;
-      const bool ok = page >= 0 && page < a.n_pages;
-      const uint32_t valid = (uint32_t)__ballot(ok) & 0xffffu;
-      const uint64_t adr = reinterpret_cast<uint64_t>(
-          a.cache + (ok ? (int64_t)page * a.page_stride + (int64_t)(j % a.page_size) * a.token_stride : 0));
-      const uint32_t alo = (uint32_t)adr, ahi = (uint32_t)(adr >> 32);
-      dst += 16 * w * C * 16;
-      if (rowed && valid == 0xffffu && !padded) {
-        const Global base = (Global)(((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)ahi) << 32) |
-                                     (uint32_t)__builtin_amdgcn_readfirstlane((int)alo));
 #pragma unroll
-        for (int i = 0; i < NL; ++i) load_lds(base + off[i], dst + 1024 * i);
-      } else {
-#pragma unroll 1
-        for (int i = 0; i < NL; ++i) {
-          const int tok = piece_token(i), col = piece_col(i);
-          const uint32_t lo = __shfl((int)alo, tok), hi = __shfl((int)ahi, tok);
-          if (col >= 0 && (valid >> tok & 1u)) load_lds((Global)(((uint64_t)hi << 32) | lo) + 2 * col, dst + 1024 * i);
-        }
-      }
-      return valid;
-    };
-    int page = page_of(t0);
-    uint32_t valid = load_tile(t0, page, tiles);
-    page = t0 + 1 < t1 ? page_of(t0 + 1) : -1;
+    for (int r = 0; r < RB; ++r) {
+      m[r] = -INFINITY;
+      l[r] = 0.f;
+    }
 
     for (int tl = t0; tl < t1; ++tl) {
       uint16_t* cur = tile[(tl - t0) & 1];
       const Lds here = tiles + ((tl - t0) & 1) * (kTile * C * 16);
       __builtin_amdgcn_s_waitcnt(0);
-      if (valid != 0xffffu) {
-        // tokens that no row sees, or of no page, are zero vectors
-        for (int i = lane; i < 16 * C; i += 64)
-          if (!(valid >> (i / C) & 1u)) reinterpret_cast<u32x4*>(cur)[16 * w * C + i] = u32x4{0u, 0u, 0u, 0u};
-      }
+      if (valid != (1u << TW) - 1u) clear_rest(valid, here);
+      if (lane == 0) present[w] = valid;
       __syncthreads();
-      const uint32_t seen = valid;
-      if (tl + 1 < t1) {
-        valid = load_tile(tl + 1, page, tiles + ((tl - t0 + 1) & 1) * (kTile * C * 16));
-        page = tl + 2 < t1 ? page_of(tl + 2) : -1;
-      }
+      if (t < WR) moved[(tl - t0 + 1) & 1][t] = 0;
+      if (tl + 1 < t1) valid = load_tile(tl + 1, tiles + ((tl - t0 + 1) & 1) * (kTile * C * 16));
 
-      // S^T of this wavefront's sixteen tokens
-      f32x4 s[R];
+      f32x4 s[RB];
 #pragma unroll
-      for (int r = 0; r < R; ++r) s[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int r = 0; r < RB; ++r) s[r] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
         const u32x4 kf = lds_read<u32x4>(here + krow[k & 1] + (k >> 1) * 128);
 #pragma unroll
-        for (int r = 0; r < R; ++r) s[r] = T::mfma(kf, qf[r][k], s[r]);
+        for (int r = 0; r < RB; ++r) s[r] = T::mfma(kf, qf[r][k], s[r]);
       }
       // The products' results are taken up here, in the block that made them: the
       // compiler leaves too few wait states before a read behind a branch.
 #pragma unroll
-      for (int r = 0; r < R; ++r) {
-        s[r] *= a.c;
-        asm volatile("" : "+v"(s[r]));
-      }
-      if ((tl + 1) * kTile > lim_lo || seen != 0xffffu) {
-        const int j0 = tl * kTile + 16 * w + 4 * g;
+      for (int r = 0; r < RB; ++r) asm volatile("" : "+v"(s[r]));
+      const uint32_t seen = __builtin_amdgcn_readfirstlane(
+          WR == 1 ? (int)present[wt] : (int)(present[2 * wt % kWaves] | present[(2 * wt + 1) % kWaves] << 8));
+      const bool edge = (tl + 1) * kTile > lim_lo;
+      if (edge || seen != 0xffffu) {
+        const int j0 = tl * kTile + 16 * wt + 4 * g;
 #pragma unroll
-        for (int r = 0; r < R; ++r)
+        for (int r = 0; r < RB; ++r)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
             s[r][i] = j0 + i < lim[r] && (seen >> (4 * g + i) & 1u) ? s[r][i] : -INFINITY;
       }
-      const bool edge = (tl + 1) * kTile > lim_lo;
 #pragma unroll
-      for (int r = 0; r < R; ++r) {
+      for (int r = 0; r < RB; ++r) {
         // a NaN score makes the row's result NaN through its exponential; the maximum passes over it
         float mx = fmaxf(fmaxf(s[r][0], s[r][1]), fmaxf(s[r][2], s[r][3]));
         mx = fmaxf(mx, __shfl_xor(mx, 16));
         mx = fmaxf(mx, __shfl_xor(mx, 32));
-        if (g == 0) red[w][16 * r + n] = mx;
+        if (g == 0) red[wt][16 * (RB * wr + r) + n] = mx;
       }
       __syncthreads();
-      float f[R];
-      bool moved = false;
+      float to[RB];
+      bool up = false;
 #pragma unroll
-      for (int r = 0; r < R; ++r) {
-        float mx = m[r];
+      for (int r = 0; r < RB; ++r) {
+        const int row = 16 * (RB * wr + r) + n;
+        const float mx = fmaxf(fmaxf(red[0][row], red[1][row]), fmaxf(red[2][row], red[3][row])) * a.c;
+        const bool u = mx > m[r] + kSlack;
+        to[r] = u ? mx : m[r];
+        up |= u;
+      }
+      if (__any(up)) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) mx = fmaxf(mx, red[i][16 * r + n]);
-        const float ref = mx == -INFINITY ? 0.f : mx;
-        f[r] = __builtin_amdgcn_exp2f(m[r] - ref);
-        moved |= mx != m[r];
-        m[r] = mx;
-        float p[4], sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          p[i] = __builtin_amdgcn_exp2f(s[r][i] - ref);
-          sum += p[i];
+        for (int r = 0; r < RB; ++r) {
+          const float f = to[r] == m[r] ? 1.f : __builtin_amdgcn_exp2f(m[r] - to[r]);
+          m[r] = to[r];
+          l[r] *= f;
+          if (wt == 0 && g == 0) fac[16 * (RB * wr + r) + n] = f;
         }
-        l[r] = mx == -INFINITY ? 0.f : l[r] * f[r] + sum;
+        if (wt == 0) moved[(tl - t0) & 1][wr] = 1;
+      }
+#pragma unroll
+      for (int r = 0; r < RB; ++r) {
+        const float ref = m[r] == -INFINITY ? 0.f : m[r];
+        float p[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(__fmaf_rn(s[r][i], a.c, -ref));
+        l[r] += (p[0] + p[1]) + (p[2] + p[3]);
         *(__attribute__((address_space(3))) u32x2*)(weights + pdst + 2048 * r) =
             u32x2{T::pack(p[0], p[1]), T::pack(p[2], p[3])};
-      }
-      // a maximum that moved (seldom, after the first tiles) rescales the rows' sums
-      if (__any(moved)) {
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-#pragma unroll
-          for (int k = 0; k < NB; ++k) o[r][k] *= f[r];
       }
       // A token that some rows see and others do not: their weight for it is 0, and 0
       // times an infinity or NaN is not.
       bool odd = false;
       if (edge && lim_lo < lim_hi) {
-        bool bad = false;
-        const int from = max(lim_lo - tl * kTile, 0), to = min(lim_hi - tl * kTile, kTile);
-        for (int i = t; i < (to - from) * DC / 2; i += kThreads) {
-          const uint32_t v = reinterpret_cast<const uint32_t*>(cur + (from + i / (DC / 2)) * C * 8)[i % (DC / 2)];
-          bad |= (lawless<T>(v) & 0x80008000u) != 0;
-        }
-        odd = __syncthreads_or(bad);
+        uint32_t bad = 0;
+        const int from = max(lim_lo - tl * kTile, 0), to_j = min(lim_hi - tl * kTile, kTile);
+        for (int i = t; i < (to_j - from) * DC / 2; i += kLanes)
+          bad |= lawless<T>(reinterpret_cast<const uint32_t*>(cur + (from + i / (DC / 2)) * C * 8)[i % (DC / 2)]);
+        odd = __syncthreads_or((bad & 0x80008000u) != 0);
       } else {
         __syncthreads();
       }
+#pragma unroll
+      for (int q = 0; q < WR; ++q)
+        if (__builtin_amdgcn_readfirstlane(moved[(tl - t0) & 1][q])) {
+#pragma unroll
+          for (int r = RB * q; r < RB * (q + 1); ++r) {
+            const float f = fac[16 * r + n];
+#pragma unroll
+            for (int k = 0; k < NB; ++k) o[r][k] *= f;
+          }
+        }
       if (odd) {
         // what the infinities and NaN give to the rows that see them, and zeros in their place
-        const int first = tl * kTile, to = min(lim_hi - first, kTile);
+        const int first = tl * kTile, to_j = min(lim_hi - first, kTile);
 #pragma clang loop unroll(disable)
-        for (int j = max(lim_lo - first, 0); j < to; ++j) {
+        for (int j = max(lim_lo - first, 0); j < to_j; ++j) {
           const int blk = j >> 2, at = 4 * (blk >> 3) + (blk & 3), part = 4 * (blk >> 2 & 1) + (j & 3);
 #pragma unroll
           for (int k = 0; k < NB; ++k)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const int ch = (w * NB + k) * 2 + (g >> 1), pc = (ch & ~7) | ((ch ^ perm(j)) & 7);
-              uint16_t* at_v = cur + (j * C + pc) * 8 + 4 * (g & 1) + i;
-              const uint16_t v = *at_v;
+              const uint16_t v = cur[(j * C + pc) * 8 + 4 * (g & 1) + i];
               if ((v & T::kExponent) == T::kExponent) {
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
                   const float p = T::value(pl[(16 * r + n) * kTile + (at ^ (n & 7)) * 8 + part]);
-                  if (first + j < lim[r]) o[r][k][i] += p * T::value(v);
+                  if (first + j < limits[16 * r + n]) o[r][k][i] += p * T::value(v);
                 }
               }
             }
         }
         __syncthreads();
-        for (int i = t; i < to * DC; i += kThreads) {
+        for (int i = t; i < to_j * DC; i += kLanes) {
           uint16_t* v = cur + (i / DC) * C * 8 + i % DC;
           if (first + i / DC >= lim_lo && (*v & T::kExponent) == T::kExponent) *v = 0;
         }
@@ -403,16 +421,19 @@ __global__ __launch_bounds__(kThreads, 1) void latent_kernel(Args a) {
     // the rows' sums over the lanes and wavefronts that hold their tokens
     __syncthreads();
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
+    for (int r = 0; r < RB; ++r) {
+      const int row = 16 * (RB * wr + r) + n;
       l[r] += __shfl_xor(l[r], 16);
       l[r] += __shfl_xor(l[r], 32);
-      if (g == 0) red[w][16 * r + n] = l[r];
+      if (g == 0) red[wt][row] = l[r];
+      if (g == 0 && wt == 0) fac[row] = m[r];
     }
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       const int row = r0 + 16 * r + n;
       const float sum = red[0][16 * r + n] + red[1][16 * r + n] + (red[2][16 * r + n] + red[3][16 * r + n]);
+      const float ref = fac[16 * r + n];
       if (whole) {
         if (row > rlast) continue;
         const int i = row / a.H, h = row - i * a.H;
@@ -426,96 +447,113 @@ __global__ __launch_bounds__(kThreads, 1) void latent_kernel(Args a) {
                                                          T::pack(o[r][k][2] * f, o[r][k][3] * f)};
         }
         if (a.lse && w == 0 && g == 0)
-          a.lse[((int64_t)b * a.Q + i) * a.H + h] = (m[r] + __builtin_amdgcn_logf(sum)) * kLn2;
+          a.lse[((int64_t)b * a.Q + i) * a.H + h] = (ref + __builtin_amdgcn_logf(sum)) * kLn2;
       } else {
         const int64_t at = ((int64_t)L * 2 + slot) * 16 * R + 16 * r + n;
 #pragma unroll
         for (int k = 0; k < NB; ++k)
           *reinterpret_cast<f32x4*>(a.part + at * DC + (w * NB + k) * 16 + 4 * g) = o[r][k];
-        if (w == 0 && g == 0) a.stat[at] = make_float2(m[r], sum);
+        if (w == 0 && g == 0) a.stat[at] = make_float2(ref, sum);
       }
     }
     __syncthreads();
   }
 }
 
-// The rows of sequences that no run did whole: parts joined against the common
-// maximum; rows without a token.  One workgroup a row at a time.
-template <class T>
-__global__ __launch_bounds__(kThreads) void latent_join_kernel(Args a, int DC) {
-  const int t = threadIdx.x, R = a.p.R;
-  __shared__ float4 acc[kThreads];
-  const int64_t rows = (int64_t)a.B * a.Q * a.H;
-  for (int64_t id = blockIdx.x; id < rows; id += gridDim.x) {
-    const int b = (int)(id / ((int64_t)a.Q * a.H)), row = (int)(id % ((int64_t)a.Q * a.H)), i = row / a.H, h = row - i * a.H;
+// The rows of sequences that no run did whole: parts joined against the largest
+// reference; rows without a token.  WAYS wavefronts take a row's parts in turn.
+template <class T, int DC, int WAYS>
+__global__ __launch_bounds__(kThreads) void latent_join_kernel(Args a) {
+  constexpr int NC = DC / 128;  // pairs of columns of a lane
+  __shared__ float acc[WAYS == 1 ? 1 : 4][DC];
+  __shared__ float sums[4];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int way = WAYS == 1 ? 0 : w, per_group = 4 / WAYS;
+  const int rows = a.B * a.Q * a.H, R = a.p.R;
+  for (int base = blockIdx.x * per_group; base < rows; base += gridDim.x * per_group) {
+    const int id = base + (WAYS == 1 ? w : 0);
+    if (id >= rows) break;
+    const int b = id / (a.Q * a.H), row = id - b * a.Q * a.H, i = row / a.H, h = row - i * a.H;
     if (i >= rows_of(a, b)) continue;
     uint16_t* dst = a.out + (int64_t)b * a.os + (int64_t)i * a.orow + (int64_t)h * a.oh;
     if (length_of(a, b) == 0) {
-      for (int c = t; c < a.dc / 2; c += kThreads) reinterpret_cast<uint32_t*>(dst)[c] = 0u;
-      if (a.lse && t == 0) a.lse[id] = -INFINITY;
+      for (int c = lane; way == 0 && c < a.dc / 2; c += 64) reinterpret_cast<uint32_t*>(dst)[c] = 0u;
+      if (a.lse && way == 0 && lane == 0) a.lse[id] = -INFINITY;
       continue;
     }
-    const int block = row / (16 * R), super = block / a.p.team, member = block % a.p.team;
+    const int block = row / (16 * R), super = block / a.p.team, member = block - super * a.p.team;
     const int first = a.first[(int64_t)b * a.p.supers + super];
     if (first < 0) continue;
-    const int64_t total = *a.total;
-    auto idle = [&](int team) { return run_begin(total, team, a.p.teams) == run_begin(total, team + 1, a.p.teams); };
-    const int ta = first >> 1, tb = a.last[(int64_t)b * a.p.supers + super], per = kGroups / 8 / a.p.team;
+    const int ta = first >> 1, tb = a.last[(int64_t)b * a.p.supers + super];
     auto part_of = [&](int team) {
-      const int L = ((team % per) * a.p.team + member) * 8 + team / per;
-      return ((int64_t)L * 2 + (team == ta ? first & 1 : 0)) * 16 * R + row % (16 * R);
+      return (group_of(team, member, a.p.team) * 2 + (team == ta ? first & 1 : 0)) * 16 * R + row % (16 * R);
     };
     float m = -INFINITY;
-    for (int k = ta + (t & 63); k <= tb; k += 64)
-      if (!idle(k)) m = fmaxf(m, a.stat[part_of(k)].x);
+    for (int k = ta + lane; k <= tb; k += 64) m = fmaxf(m, a.stat[part_of(k)].x);
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
     const float ref = m == -INFINITY ? 0.f : m;
-    // a quarter or more of the parts to each group of DC / 4 threads
-    const int cols = DC / 4, ways = kThreads / cols, way = t / cols, c = t % cols;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    float2 o[NC];
+#pragma unroll
+    for (int k = 0; k < NC; ++k) o[k] = make_float2(0.f, 0.f);
     float sum = 0.f;
-    for (int k = ta + way; k <= tb; k += ways) {
-      if (idle(k)) continue;
-      const int64_t at = part_of(k);
-      const float2 st = a.stat[at];
+    for (int k0 = ta + way; k0 <= tb; k0 += 64 * WAYS) {
+      // lane j: the weight and place of part k0 + WAYS j
+      const int mine = k0 + WAYS * lane, at = mine <= tb ? part_of(mine) : 0;
+      const float2 st = mine <= tb ? a.stat[at] : make_float2(-INFINITY, 0.f);
       const float f = __builtin_amdgcn_exp2f(st.x - ref);
-      const float4 v = *reinterpret_cast<const float4*>(a.part + at * DC + 4 * c);
-      sum += st.y * f;
-      o.x += v.x * f;
-      o.y += v.y * f;
-      o.z += v.z * f;
-      o.w += v.w * f;
-    }
-    __shared__ float sums[8];
-    __syncthreads();
-    acc[t] = o;
-    if (c == 0) sums[way] = sum;
-    __syncthreads();
-    if (way == 0) {
-      for (int k = 1; k < ways; ++k) {
-        const float4 v = acc[k * cols + c];
-        o.x += v.x;
-        o.y += v.y;
-        o.z += v.z;
-        o.w += v.w;
-        sum += sums[k];
+      sum += mine <= tb ? st.y * f : 0.f;
+      const int count = min((tb - k0) / WAYS + 1, 64);
+#pragma unroll 4
+      for (int j = 0; j < count; ++j) {
+        const float fj = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), j));
+        const float2* src = reinterpret_cast<const float2*>(a.part + (int64_t)__builtin_amdgcn_readlane(at, j) * DC) + lane;
+#pragma unroll
+        for (int k = 0; k < NC; ++k) {
+          const float2 v = src[64 * k];
+          o[k].x = __fmaf_rn(v.x, fj, o[k].x);
+          o[k].y = __fmaf_rn(v.y, fj, o[k].y);
+        }
       }
-      const float f = sum > 0.f ? 1.f / sum : sum != sum ? NAN : 0.f;
-      if (4 * c < a.dc)
-        *reinterpret_cast<u32x2*>(dst + 4 * c) = u32x2{T::pack(o.x * f, o.y * f), T::pack(o.z * f, o.w * f)};
-      if (a.lse && c == 0) a.lse[id] = (m + __builtin_amdgcn_logf(sum)) * kLn2;
     }
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
+    if (WAYS > 1) {
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < NC; ++k) *reinterpret_cast<float2*>(&acc[way][2 * lane + 128 * k]) = o[k];
+      if (lane == 0) sums[way] = sum;
+      __syncthreads();
+      if (way > 0) continue;
+      sum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+#pragma unroll
+      for (int k = 0; k < NC; ++k)
+        for (int q = 1; q < WAYS; ++q) {
+          const float2 v = *reinterpret_cast<const float2*>(&acc[q][2 * lane + 128 * k]);
+          o[k].x += v.x;
+          o[k].y += v.y;
+        }
+    }
+    const float f = sum > 0.f ? 1.f / sum : sum != sum ? NAN : 0.f;
+#pragma unroll
+    for (int k = 0; k < NC; ++k) {
+      const int c = 2 * lane + 128 * k;
+      if (c < a.dc) *reinterpret_cast<uint32_t*>(dst + c) = T::pack(o[k].x * f, o[k].y * f);
+    }
+    if (a.lse && lane == 0) a.lse[id] = (m + __builtin_amdgcn_logf(sum)) * kLn2;
   }
 }
 
 template <class T, int R, int DC>
 hipError_t run(const Args& a, hipStream_t s) {
-  hipError_t e = launch_timed("latent_attention", latent_kernel<T, R, DC>, dim3(kGroups), dim3(kThreads), s, a);
+  hipError_t e = launch_timed("latent_attention", latent_kernel<T, R, DC>, dim3(kGroups), dim3(R == 1 ? 256 : 512), s, a);
   if (e != hipSuccess) return e;
-  const int64_t rows = (int64_t)a.B * a.Q * a.H;
-  return launch_timed("latent_join", latent_join_kernel<T>, dim3((unsigned)(rows < 2048 ? rows : 2048)), dim3(kThreads),
-                      s, a, DC);
+  // four wavefronts a row where a sequence may have eight parts or more, else one
+  const int rows = a.B * a.Q * a.H;
+  return a.p.teams >= 8 * (int64_t)a.B * a.p.supers
+             ? launch_timed("latent_join", latent_join_kernel<T, DC, 4>, dim3(rows < 4096 ? rows : 4096), dim3(kThreads), s, a)
+             : launch_timed("latent_join", latent_join_kernel<T, DC, 1>,
+                            dim3((rows + 3) / 4 < 4096 ? (rows + 3) / 4 : 4096), dim3(kThreads), s, a);
 }
 
 template <class T>

@@ -14,7 +14,10 @@ namespace latent {
 
 constexpr int kThreads = 256, kTile = 64;
 constexpr float kLn2 = 0.69314718f;
-constexpr int kRope = 64;     // columns of the rotary part, zero past d_rope
+// How far (in powers of 2) a score may exceed its row's reference: weights then reach 2^kSlack,
+// harmless in float32 sums and in fp16.
+constexpr float kSlack = 8.f;
+constexpr int kRope = 64;  // columns of the rotary part, zero past d_rope
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));

@@ -14,8 +14,7 @@
 // loads, has the same order.  No value of S or P passes through LDS.
 //
 // m is a reference and not the maximum: it moves when a score exceeds it by
-// kSlack (weights then reach 2^kSlack, harmless in float32 and in fp16), so the
-// rescaling of O is left out of almost every tile.
+// kSlack, so the rescaling of O is left out of almost every tile.
 //
 // Tiles (K rotary and not, V) come by loads that write LDS directly, into the other
 // of two buffers while this one is multiplied; one barrier a tile.  80 KB of LDS
@@ -39,7 +38,6 @@ namespace {
 using namespace latent;
 
 constexpr int kRows = 128;
-constexpr float kSlack = 8.f;
 
 struct Expanded {
   int n, H, dn, dr, dv, Tq, Tk;

@@ -9,7 +9,7 @@ namespace {
 inline size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
 inline int padded(int dc) { return (dc + 127) / 128 * 128; }
 struct Layout {
-  size_t part, stat, first, last, total, bytes;
+  size_t part, stat, first, last, bytes;
 };
 Layout layout(int B, int dc, const latent::Plan& p) {
   const size_t rows = (size_t)latent::kGroups * 2 * 16 * p.R;
@@ -18,8 +18,7 @@ Layout layout(int B, int dc, const latent::Plan& p) {
   l.stat = up256(rows * padded(dc) * sizeof(float));
   l.first = l.stat + up256(rows * sizeof(float2));
   l.last = l.first + up256((size_t)B * p.supers * sizeof(int32_t));
-  l.total = l.last + up256((size_t)B * p.supers * sizeof(int32_t));
-  l.bytes = l.total + 256;
+  l.bytes = l.last + up256((size_t)B * p.supers * sizeof(int32_t));
   return l;
 }
 }  // namespace
@@ -36,7 +35,9 @@ hipError_t latent_launch(int B, int Q, int H, int dc, int dr, sd_type type, doub
   a.H = H;
   a.dc = dc;
   a.dr = dr;
-  a.c = (float)(scale * 1.44269504088896340736);
+  // |scale| at least 1e-30, so that a masked score stays -inf where scale is 0
+  a.c = (float)fmax(fabs(scale) * 1.44269504088896340736, 1e-30);
+  a.flip = scale < 0.0 ? 0x80008000u : 0u;
   a.q = static_cast<const uint16_t*>(q);
   a.qs = qs.seq;
   a.qr = qs.row;
@@ -63,7 +64,6 @@ hipError_t latent_launch(int B, int Q, int H, int dc, int dr, sd_type type, doub
   a.stat = reinterpret_cast<float2*>(base + l.stat);
   a.first = reinterpret_cast<int32_t*>(base + l.first);
   a.last = reinterpret_cast<int32_t*>(base + l.last);
-  a.total = reinterpret_cast<int64_t*>(base + l.total);
   return type == SD_TYPE_BF16 ? latent_bf16_launch(a, s) : latent::run_type<latent::F16>(a, s);
 }
 

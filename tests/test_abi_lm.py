@@ -106,7 +106,8 @@ def _latent(lib, **kw):
     (dict(qs=_lib.sd_stride_h(1536, 768, 190)), "q strides"), (dict(qs=_lib.sd_stride_h(1536, 192, 192)), "q strides"),
     (dict(os=_lib.sd_stride_h(1024, 512, 120)), "out strides"), (dict(q=ctypes.c_void_p(264)), "16-byte"),
     (dict(cache=ctypes.c_void_p(258)), "16-byte"), (dict(ws_bytes=64), "workspace 64 <"),
-    (dict(ws=ctypes.c_void_p(128)), "256-byte"), (dict(B=1 << 20, Q=1 << 10), "2^30 rows")])
+    (dict(ws=ctypes.c_void_p(128)), "256-byte"), (dict(B=1 << 20, Q=1 << 10), "2^30 rows"),
+    (dict(B=1 << 20, size=1 << 24, max_pages=4, ps=1 << 40), "too many rows and tokens")])
 def test_latent_attention_refuses(lib, kw, needle):
     _refused(_latent(lib, **kw), needle)
 
