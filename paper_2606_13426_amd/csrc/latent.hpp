@@ -5,11 +5,11 @@
 // A workgroup takes 16 R rows (row, head pairs) of one sequence and a run of its
 // tokens, 64 at a time.  A tile of the cache enters LDS once and serves both
 // products, so a token's bytes come from HBM once for all the rows of a workgroup:
-//   S^T [tokens][rows] = C Q^T   a wavefront: 16 tokens, the rows of one of WR
-//                                groups; its part of Q stays in registers
+//   S^T [tokens][rows] = C Q^T   a wavefront: 16 or 32 tokens, 16 rows, whose Q stays
+//                                in its registers
 //   P = 2^{S c - m}, c = scale log2(e); maxima over the tokens' wavefronts by LDS
-//   O^T [latent][rows] = C^T P^T a wavefront: DC / (4 WR) latent columns, all
-//                                rows, accumulators in registers
+//   O^T [latent][rows] = C^T P^T a wavefront: a quarter or an eighth of the latent
+//                                columns, all rows, accumulators in registers
 // on v_mfma_f32_16x16x32.  In both results a lane holds one row of each block of
 // 16, so its maximum, sum and rescaling need no exchange inside the products.
 // C^T is read by transposing LDS loads; the order in which the 32 tokens of a
@@ -96,7 +96,8 @@ __device__ __forceinline__ int group_of(int team, int member, int size) {
 
 template <class T, int R, int DC>
 __global__ __launch_bounds__(R == 1 ? 256 : 512) void latent_kernel(Args a) {
-  constexpr int WR = R == 1 ? 1 : 2, kWaves = 4 * WR, kLanes = 64 * kWaves, RB = R / WR;
+  constexpr int kWaves = R == 1 ? 4 : 8, kLanes = 64 * kWaves;
+  constexpr int WR = R, WT = kWaves / WR, TB = kTile / 16 / WT;  // row groups of 16, token groups of 16 TB
   constexpr int C = (DC + kRope) / 8;     // 16-byte pieces of a token
   constexpr int KS = (DC + kRope) / 32;   // steps of 32 columns of Q
   constexpr int NB = DC / (16 * kWaves);  // blocks of 16 latent columns of a wavefront
@@ -106,14 +107,14 @@ __global__ __launch_bounds__(R == 1 ? 256 : 512) void latent_kernel(Args a) {
   static_assert(C % 8 == 0 && DC % 128 == 0 && NL * 64 == TW * C, "whole 128-byte segments, blocks and loads");
   __shared__ __align__(16) uint16_t tile[2][kTile * C * 8];
   __shared__ __align__(16) uint16_t pl[16 * R * kTile];
-  __shared__ float red[4][16 * R];
+  __shared__ float red[WT][16 * R];
   __shared__ float fac[16 * R];
   __shared__ int limits[16 * R];
   __shared__ int moved[2][WR];
   __shared__ uint32_t present[kWaves];
 
   const int t = threadIdx.x, lane = t & 63, n = lane & 15, g = lane >> 4;
-  const int w = __builtin_amdgcn_readfirstlane(t >> 6), wt = w & 3, wr = w >> 2;
+  const int w = __builtin_amdgcn_readfirstlane(t >> 6), wt = w % WT, wr = w / WT;
   const int L = blockIdx.x, i8 = L / 8, team = i8 / a.p.team * 8 + L % 8, member = i8 % a.p.team;
 
   // this team's run of the list of all sequences' tiles: found by each wavefront for itself
@@ -165,7 +166,7 @@ __global__ __launch_bounds__(R == 1 ? 256 : 512) void latent_kernel(Args a) {
   for (int i = 0; i < NL; ++i) off[i] = 2u * (uint32_t)(piece_token(i) * (int)a.token_stride + piece_col(i));
   // what a lane reads of a tile and of P, in bytes
   const int kx = g ^ perm(n);
-  const int krow[2] = {((16 * wt + n) * C + kx) * 16, ((16 * wt + n) * C + (kx ^ 4)) * 16};
+  const int krow[2] = {((16 * TB * wt + n) * C + kx) * 16, ((16 * TB * wt + n) * C + (kx ^ 4)) * 16};
   int vrow[NV];
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
@@ -174,8 +175,13 @@ __global__ __launch_bounds__(R == 1 ? 256 : 512) void latent_kernel(Args a) {
     vrow[k] = (tok * C + ((ch & ~7) | ((ch ^ perm(tok)) & 7))) * 16 + 8 * (lane & 1);
   }
   const int px = g ^ (n & 7), prow[2] = {n * 128 + px * 16, n * 128 + (px ^ 4) * 16};
-  // block 4 wt + g of four tokens: step wt / 2, place g, half wt % 2
-  const int pdst = n * 128 + ((4 * (wt >> 1) + g) ^ (n & 7)) * 16 + 8 * (wt & 1) + 2048 * RB * wr;
+  // four tokens 4 g of 16-token block v = TB wt + j: step v / 2, place g, half v % 2
+  int pdst[TB];
+#pragma unroll
+  for (int j = 0; j < TB; ++j) {
+    const int v = TB * wt + j;
+    pdst[j] = n * 128 + ((4 * (v >> 1) + g) ^ (n & 7)) * 16 + 8 * (v & 1) + 2048 * wr;
+  }
   const Lds tiles = lds_of(tile), weights = lds_of(pl);
 
   if (padded) {
@@ -214,12 +220,13 @@ __global__ __launch_bounds__(R == 1 ? 256 : 512) void latent_kernel(Args a) {
       const int j0 = tl * kTile + TW * w, count = min(max(lim_hi - j0, 0), TW);
       dst += TW * w * C * 16;
       if (rowed && count == TW) {
-        const int pg = table ? j0 / a.page_size : 0, page = table ? table[pg] : b;
+        const int pg = table ? j0 / a.page_size : 0, page = __builtin_amdgcn_readfirstlane(table ? table[pg] : b);
         if (page < 0 || page >= a.n_pages) return 0u;
-        const Global base = (Global)(a.cache + (int64_t)page * a.page_stride +
-                                     (int64_t)(j0 - pg * a.page_size) * a.token_stride);
+        const auto view = buf_view(
+            a.cache + (int64_t)page * a.page_stride + (int64_t)(j0 - pg * a.page_size) * a.token_stride,
+            2 * ((TW - 1) * a.token_stride + a.dc + a.dr));
 #pragma unroll
-        for (int i = 0; i < NL; ++i) load_lds(base + off[i], dst + 1024 * i);
+        for (int i = 0; i < NL; ++i) load_lds(view, off[i], dst + 1024 * i);
         return (1u << TW) - 1u;
       }
       const int j = j0 + lane % TW, pg = j / a.page_size;
@@ -246,33 +253,27 @@ __global__ __launch_bounds__(R == 1 ? 256 : 512) void latent_kernel(Args a) {
     if (t < 2 * WR) moved[t / WR][t % WR] = 0;
     if (t < 16 * R) limits[t] = r0 + t <= rlast ? len - nrow + (r0 + t) / a.H + 1 : 0;
 
-    int lim[RB];
-    u32x4 qf[RB][KS];
-#pragma unroll
-    for (int r = 0; r < RB; ++r) {
-      const int row = r0 + 16 * (RB * wr + r) + n, i = min(row, rlast) / a.H, h = min(row, rlast) - i * a.H;
-      lim[r] = row <= rlast ? max(len - nrow + i + 1, 0) : 0;
+    int lim;
+    u32x4 qf[KS];
+    {
+      const int row = r0 + 16 * wr + n, i = min(row, rlast) / a.H, h = min(row, rlast) - i * a.H;
+      lim = row <= rlast ? max(len - nrow + i + 1, 0) : 0;
       const uint16_t* src = a.q + (int64_t)b * a.qs + (int64_t)i * a.qr + (int64_t)h * a.qh;
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
         const int col = 32 * k + 8 * g;
         const int at = col < DC ? (col < a.dc ? col : -1) : (col - DC < a.dr ? a.dc + col - DC : -1);
-        qf[r][k] = u32x4{0u, 0u, 0u, 0u};
-        if (!padded || at >= 0) qf[r][k] = *reinterpret_cast<const u32x4*>(src + at);
-        qf[r][k] ^= a.flip;
+        qf[k] = u32x4{0u, 0u, 0u, 0u};
+        if (!padded || at >= 0) qf[k] = *reinterpret_cast<const u32x4*>(src + at);
+        qf[k] ^= a.flip;
       }
     }
     f32x4 o[R][NB];
-    float m[RB], l[RB];
+    float m = -INFINITY, l = 0.f;
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
       for (int k = 0; k < NB; ++k) o[r][k] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int r = 0; r < RB; ++r) {
-      m[r] = -INFINITY;
-      l[r] = 0.f;
-    }
 
     for (int tl = t0; tl < t1; ++tl) {
       uint16_t* cur = tile[(tl - t0) & 1];
@@ -284,68 +285,59 @@ __global__ __launch_bounds__(R == 1 ? 256 : 512) void latent_kernel(Args a) {
       if (t < WR) moved[(tl - t0 + 1) & 1][t] = 0;
       if (tl + 1 < t1) valid = load_tile(tl + 1, tiles + ((tl - t0 + 1) & 1) * (kTile * C * 16));
 
-      f32x4 s[RB];
+      f32x4 s[TB];
 #pragma unroll
-      for (int r = 0; r < RB; ++r) s[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int j = 0; j < TB; ++j) s[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int k = 0; k < KS; ++k) {
-        const u32x4 kf = lds_read<u32x4>(here + krow[k & 1] + (k >> 1) * 128);
+      for (int k = 0; k < KS; ++k)
 #pragma unroll
-        for (int r = 0; r < RB; ++r) s[r] = T::mfma(kf, qf[r][k], s[r]);
-      }
+        for (int j = 0; j < TB; ++j)
+          s[j] = T::mfma(lds_read<u32x4>(here + krow[k & 1] + (k >> 1) * 128 + 16 * j * C * 16), qf[k], s[j]);
       // The products' results are taken up here, in the block that made them: the
       // compiler leaves too few wait states before a read behind a branch.
 #pragma unroll
-      for (int r = 0; r < RB; ++r) asm volatile("" : "+v"(s[r]));
-      const uint32_t seen = __builtin_amdgcn_readfirstlane(
-          WR == 1 ? (int)present[wt] : (int)(present[2 * wt % kWaves] | present[(2 * wt + 1) % kWaves] << 8));
-      const bool edge = (tl + 1) * kTile > lim_lo;
-      if (edge || seen != 0xffffu) {
-        const int j0 = tl * kTile + 16 * wt + 4 * g;
+      for (int j = 0; j < TB; ++j) asm volatile("" : "+v"(s[j]));
+      // which of the wavefront's tokens are there, TW bits from each that loaded them
+      constexpr int kFrom = 16 * TB / TW;
+      uint32_t seen = 0;
 #pragma unroll
-        for (int r = 0; r < RB; ++r)
+      for (int j = 0; j < kFrom; ++j) seen |= present[kFrom * wt + j] << (TW * j);
+      seen = (uint32_t)__builtin_amdgcn_readfirstlane((int)seen);
+      const bool edge = (tl + 1) * kTile > lim_lo;
+      if (edge || seen != (uint32_t)((1ull << (16 * TB)) - 1)) {
+        const int ahead = lim - (tl * kTile + 16 * TB * wt + 4 * g);  // its tokens from this lane's first on
+        const uint32_t have = seen >> (4 * g);
+#pragma unroll
+        for (int j = 0; j < TB; ++j)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            s[r][i] = j0 + i < lim[r] && (seen >> (4 * g + i) & 1u) ? s[r][i] : -INFINITY;
+            s[j][i] = 16 * j + i < ahead && (have & (1u << (16 * j + i))) ? s[j][i] : -INFINITY;
       }
+      // a NaN score makes the row's result NaN through its exponential; the maximum passes over it
+      float mx = -INFINITY;
 #pragma unroll
-      for (int r = 0; r < RB; ++r) {
-        // a NaN score makes the row's result NaN through its exponential; the maximum passes over it
-        float mx = fmaxf(fmaxf(s[r][0], s[r][1]), fmaxf(s[r][2], s[r][3]));
-        mx = fmaxf(mx, __shfl_xor(mx, 16));
-        mx = fmaxf(mx, __shfl_xor(mx, 32));
-        if (g == 0) red[wt][16 * (RB * wr + r) + n] = mx;
-      }
+      for (int j = 0; j < TB; ++j) mx = fmaxf(mx, fmaxf(fmaxf(s[j][0], s[j][1]), fmaxf(s[j][2], s[j][3])));
+      mx = quarter_max(mx);
+      if (g == 0) red[wt][16 * wr + n] = mx;
       __syncthreads();
-      float to[RB];
-      bool up = false;
 #pragma unroll
-      for (int r = 0; r < RB; ++r) {
-        const int row = 16 * (RB * wr + r) + n;
-        const float mx = fmaxf(fmaxf(red[0][row], red[1][row]), fmaxf(red[2][row], red[3][row])) * a.c;
-        const bool u = mx > m[r] + kSlack;
-        to[r] = u ? mx : m[r];
-        up |= u;
-      }
-      if (__any(up)) {
-#pragma unroll
-        for (int r = 0; r < RB; ++r) {
-          const float f = to[r] == m[r] ? 1.f : __builtin_amdgcn_exp2f(m[r] - to[r]);
-          m[r] = to[r];
-          l[r] *= f;
-          if (wt == 0 && g == 0) fac[16 * (RB * wr + r) + n] = f;
-        }
+      for (int j = 0; j < WT; ++j) mx = fmaxf(mx, red[j][16 * wr + n]);
+      mx *= a.c;
+      if (__any(mx > m + kSlack)) {
+        const float to = mx > m + kSlack ? mx : m, f = to == m ? 1.f : __builtin_amdgcn_exp2f(m - to);
+        m = to;
+        l *= f;
+        if (wt == 0 && g == 0) fac[16 * wr + n] = f;
         if (wt == 0) moved[(tl - t0) & 1][wr] = 1;
       }
+      const float ref = m == -INFINITY ? 0.f : m;
 #pragma unroll
-      for (int r = 0; r < RB; ++r) {
-        const float ref = m[r] == -INFINITY ? 0.f : m[r];
+      for (int j = 0; j < TB; ++j) {
         float p[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(__fmaf_rn(s[r][i], a.c, -ref));
-        l[r] += (p[0] + p[1]) + (p[2] + p[3]);
-        *(__attribute__((address_space(3))) u32x2*)(weights + pdst + 2048 * r) =
-            u32x2{T::pack(p[0], p[1]), T::pack(p[2], p[3])};
+        for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(__fmaf_rn(s[j][i], a.c, -ref));
+        l += (p[0] + p[1]) + (p[2] + p[3]);
+        *(__attribute__((address_space(3))) u32x2*)(weights + pdst[j]) = u32x2{T::pack(p[0], p[1]), T::pack(p[2], p[3])};
       }
       // A token that some rows see and others do not: their weight for it is 0, and 0
       // times an infinity or NaN is not.
@@ -363,11 +355,7 @@ __global__ __launch_bounds__(R == 1 ? 256 : 512) void latent_kernel(Args a) {
       for (int q = 0; q < WR; ++q)
         if (__builtin_amdgcn_readfirstlane(moved[(tl - t0) & 1][q])) {
 #pragma unroll
-          for (int r = RB * q; r < RB * (q + 1); ++r) {
-            const float f = fac[16 * r + n];
-#pragma unroll
-            for (int k = 0; k < NB; ++k) o[r][k] *= f;
-          }
+          for (int k = 0; k < NB; ++k) o[q][k] *= fac[16 * q + n];
         }
       if (odd) {
         // what the infinities and NaN give to the rows that see them, and zeros in their place
@@ -420,19 +408,16 @@ __global__ __launch_bounds__(R == 1 ? 256 : 512) void latent_kernel(Args a) {
 
     // the rows' sums over the lanes and wavefronts that hold their tokens
     __syncthreads();
-#pragma unroll
-    for (int r = 0; r < RB; ++r) {
-      const int row = 16 * (RB * wr + r) + n;
-      l[r] += __shfl_xor(l[r], 16);
-      l[r] += __shfl_xor(l[r], 32);
-      if (g == 0) red[wt][row] = l[r];
-      if (g == 0 && wt == 0) fac[row] = m[r];
-    }
+    l = quarter_sum(l);
+    if (g == 0) red[wt][16 * wr + n] = l;
+    if (g == 0 && wt == 0) fac[16 * wr + n] = m;
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       const int row = r0 + 16 * r + n;
-      const float sum = red[0][16 * r + n] + red[1][16 * r + n] + (red[2][16 * r + n] + red[3][16 * r + n]);
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < WT; ++j) sum += red[j][16 * r + n];
       const float ref = fac[16 * r + n];
       if (whole) {
         if (row > rlast) continue;

@@ -7,7 +7,9 @@
 #include <math.h>
 #include <stdint.h>
 
+#include "bufio.hpp"
 #include "common.hpp"
+#include "wavered.hpp"
 
 namespace sd {
 namespace latent {
@@ -71,6 +73,16 @@ __device__ __forceinline__ uint32_t lawless(uint32_t v) {
 // piece pairs of four tokens in a row.
 __device__ __forceinline__ int perm(int token) { return ((token & 3) << 1) | ((token >> 2) & 1); }
 
+// Over lanes 16 and 32 apart (in every one of them the same bits).
+__device__ __forceinline__ float across(float v, bool row32, bool max) {
+  uint32_t a = __builtin_bit_cast(uint32_t, v), b = a;
+  row32 ? swap32(a, b) : swap16(a, b);
+  const float x = __builtin_bit_cast(float, a), y = __builtin_bit_cast(float, b);
+  return max ? fmaxf(x, y) : x + y;
+}
+__device__ __forceinline__ float quarter_max(float v) { return across(across(v, false, true), true, true); }
+__device__ __forceinline__ float quarter_sum(float v) { return across(across(v, false, false), true, false); }
+
 // LDS by byte offsets: one base and immediate offsets for a lane's reads.
 typedef __attribute__((address_space(3))) char* Lds;
 __device__ __forceinline__ Lds lds_of(void* p) { return (Lds)p; }
@@ -85,6 +97,10 @@ __device__ __forceinline__ u32x2 lds_read_tr(Lds p) {
 typedef const __attribute__((address_space(1))) char* Global;
 __device__ __forceinline__ void load_lds(Global src, Lds dst) {
   __builtin_amdgcn_global_load_lds(src, dst, 16, 0, 0);
+}
+// The same from byte `off` of a view: one register an address, and none to compute.
+__device__ __forceinline__ void load_lds(__amdgpu_buffer_rsrc_t view, uint32_t off, Lds dst) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(view, dst, 16, off, 0, 0, 0);
 }
 
 }  // namespace latent

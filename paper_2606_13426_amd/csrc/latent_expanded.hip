@@ -134,8 +134,9 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_kernel(Expanded a) {
     const Global src = base + (int64_t)tl * kTile * stride * 2;
     const int last = nk - 1 - tl * kTile;  // places behind the last key repeat it; their weights are 0
     if (last >= kTile - 1 && !padded) {
+      const auto view = buf_view((const void*)src, 2 * ((kTile - 1) * stride + d));
 #pragma unroll
-      for (int i = 0; i < P / 4; ++i) load_lds(src + offs[i], dst + 1024 * (w + 4 * i));
+      for (int i = 0; i < P / 4; ++i) load_lds(view, offs[i], dst + 1024 * (w + 4 * i));
     } else {
 #pragma unroll
       for (int i = 0; i < P / 4; ++i) {
@@ -198,7 +199,7 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_kernel(Expanded a) {
     for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[0][i]);
 #pragma unroll
     for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[1][i]);
-    mx = fmaxf(mx, __shfl_xor(mx, 32)) * a.c;
+    mx = across(mx, true, true) * a.c;
     // (a NaN score passes the maximum over and makes its row NaN by its weight)
     const bool up = mx > m + kSlack || (m == -INFINITY && mx > -INFINITY);
     if (__any(up)) {
@@ -300,7 +301,7 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_kernel(Expanded a) {
     __builtin_amdgcn_sched_barrier(0);
   }
 
-  l += __shfl_xor(l, 32);
+  l = across(l, true, false);
   if (!real) return;
   const int64_t at = (int64_t)(qb + row) * a.H + head;
   if (a.split > 1) {
