@@ -110,7 +110,7 @@ __global__ __launch_bounds__(R == 1 ? 256 : 512) void latent_kernel(Args a) {
   __shared__ float red[WT][16 * R];
   __shared__ float fac[16 * R];
   __shared__ int limits[16 * R];
-  __shared__ int moved[2][WR];
+  __shared__ int moved[2][WR + 1];  // whose rows' reference moved; last: values that are no numbers
   __shared__ uint32_t present[kWaves];
 
   const int t = threadIdx.x, lane = t & 63, n = lane & 15, g = lane >> 4;
@@ -250,7 +250,7 @@ __global__ __launch_bounds__(R == 1 ? 256 : 512) void latent_kernel(Args a) {
         if (!(valid >> (i / C) & 1u)) *(__attribute__((address_space(3))) u32x4*)(dst + 16 * i) = u32x4{0u, 0u, 0u, 0u};
     };
     uint32_t valid = load_tile(t0, tiles);
-    if (t < 2 * WR) moved[t / WR][t % WR] = 0;
+    if (t < 2 * (WR + 1)) moved[t / (WR + 1)][t % (WR + 1)] = 0;
     if (t < 16 * R) limits[t] = r0 + t <= rlast ? len - nrow + (r0 + t) / a.H + 1 : 0;
 
     int lim;
@@ -282,17 +282,34 @@ __global__ __launch_bounds__(R == 1 ? 256 : 512) void latent_kernel(Args a) {
       if (valid != (1u << TW) - 1u) clear_rest(valid, here);
       if (lane == 0) present[w] = valid;
       __syncthreads();
-      if (t < WR) moved[(tl - t0 + 1) & 1][t] = 0;
+      if (t <= WR) moved[(tl - t0 + 1) & 1][t] = 0;
       if (tl + 1 < t1) valid = load_tile(tl + 1, tiles + ((tl - t0 + 1) & 1) * (kTile * C * 16));
 
       f32x4 s[TB];
 #pragma unroll
       for (int j = 0; j < TB; ++j) s[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      {
+        // two steps' pieces are read while the two before are multiplied
+        u32x4 kf[2][2][TB];
+        auto read = [&](int k) {
 #pragma unroll
-      for (int k = 0; k < KS; ++k)
+          for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int j = 0; j < TB; ++j)
-          s[j] = T::mfma(lds_read<u32x4>(here + krow[k & 1] + (k >> 1) * 128 + 16 * j * C * 16), qf[k], s[j]);
+            for (int j = 0; j < TB; ++j)
+              kf[(k >> 1) & 1][i][j] = lds_read<u32x4>(here + krow[i] + (k >> 1) * 128 + 16 * j * C * 16);
+        };
+        read(0);
+#pragma unroll
+        for (int k = 0; k < KS; k += 2) {
+          if (k + 2 < KS) read(k + 2);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < TB; ++j) s[j] = T::mfma(kf[(k >> 1) & 1][i][j], qf[k + i], s[j]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
       // The products' results are taken up here, in the block that made them: the
       // compiler leaves too few wait states before a read behind a branch.
 #pragma unroll
@@ -319,7 +336,7 @@ __global__ __launch_bounds__(R == 1 ? 256 : 512) void latent_kernel(Args a) {
       for (int j = 0; j < TB; ++j) mx = fmaxf(mx, fmaxf(fmaxf(s[j][0], s[j][1]), fmaxf(s[j][2], s[j][3])));
       mx = quarter_max(mx);
       if (g == 0) red[wt][16 * wr + n] = mx;
-      __syncthreads();
+      lds_barrier();
 #pragma unroll
       for (int j = 0; j < WT; ++j) mx = fmaxf(mx, red[j][16 * wr + n]);
       mx *= a.c;
@@ -341,23 +358,21 @@ __global__ __launch_bounds__(R == 1 ? 256 : 512) void latent_kernel(Args a) {
       }
       // A token that some rows see and others do not: their weight for it is 0, and 0
       // times an infinity or NaN is not.
-      bool odd = false;
       if (edge && lim_lo < lim_hi) {
         uint32_t bad = 0;
         const int from = max(lim_lo - tl * kTile, 0), to_j = min(lim_hi - tl * kTile, kTile);
         for (int i = t; i < (to_j - from) * DC / 2; i += kLanes)
           bad |= lawless<T>(reinterpret_cast<const uint32_t*>(cur + (from + i / (DC / 2)) * C * 8)[i % (DC / 2)]);
-        odd = __syncthreads_or((bad & 0x80008000u) != 0);
-      } else {
-        __syncthreads();
+        if (__any((bad & 0x80008000u) != 0) && lane == 0) moved[(tl - t0) & 1][WR] = 1;
       }
+      lds_barrier();
 #pragma unroll
       for (int q = 0; q < WR; ++q)
         if (__builtin_amdgcn_readfirstlane(moved[(tl - t0) & 1][q])) {
 #pragma unroll
           for (int k = 0; k < NB; ++k) o[q][k] *= fac[16 * q + n];
         }
-      if (odd) {
+      if (__builtin_amdgcn_readfirstlane(moved[(tl - t0) & 1][WR])) {
         // what the infinities and NaN give to the rows that see them, and zeros in their place
         const int first = tl * kTile, to_j = min(lim_hi - first, kTile);
 #pragma clang loop unroll(disable)
@@ -385,19 +400,27 @@ __global__ __launch_bounds__(R == 1 ? 256 : 512) void latent_kernel(Args a) {
         }
         __syncthreads();
       }
-      // O^T += C^T P^T over the tile's two steps of 32 tokens
-#pragma unroll
-      for (int st = 0; st < 2; ++st) {
-        u32x4 pf[R];
-#pragma unroll
-        for (int r = 0; r < R; ++r) pf[r] = lds_read<u32x4>(weights + prow[st] + 2048 * r);
-#pragma unroll
-        for (int k = 0; k < NB; ++k) {
-          const Lds src = here + vrow[k & 3] + (k >> 2) * 128 + 32 * st * C * 16;
+      // O^T += C^T P^T over the tile's two steps of 32 tokens; the next block's values are read while
+      // one is multiplied
+      {
+        u32x4 pf[R], vf[2];
+        auto read = [&](int i) {
+          const Lds src = here + vrow[i % NB & 3] + (i % NB >> 2) * 128 + 32 * (i / NB) * C * 16;
           const u32x2 lo = lds_read_tr(src), hi = lds_read_tr(src + 16 * C * 16);
-          const u32x4 vf = {lo[0], lo[1], hi[0], hi[1]};
+          vf[i & 1] = u32x4{lo[0], lo[1], hi[0], hi[1]};
+        };
+        read(0);
 #pragma unroll
-          for (int r = 0; r < R; ++r) o[r][k] = T::mfma(vf, pf[r], o[r][k]);
+        for (int i = 0; i < 2 * NB; ++i) {
+          if (i % NB == 0) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) pf[r] = lds_read<u32x4>(weights + prow[i / NB] + 2048 * r);
+          }
+          if (i + 1 < 2 * NB) read(i + 1);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int r = 0; r < R; ++r) o[r][i % NB] = T::mfma(vf[i & 1], pf[r], o[r][i % NB]);
+          __builtin_amdgcn_sched_barrier(0);
         }
       }
       // wait states for a read of the last results behind the loop's branch

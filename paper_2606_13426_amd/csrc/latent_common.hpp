@@ -93,6 +93,9 @@ __device__ __forceinline__ V lds_read(Lds p) {
 __device__ __forceinline__ u32x2 lds_read_tr(Lds p) {
   return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p));
 }
+// A barrier for what the wavefronts exchange through LDS themselves.  It does not wait
+// for loads that write LDS, as __syncthreads does: those are in flight across it.
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 // 16 bytes a lane from global memory to LDS at dst + 16 lane (dst uniform).
 typedef const __attribute__((address_space(1))) char* Global;
 __device__ __forceinline__ void load_lds(Global src, Lds dst) {
