@@ -84,9 +84,9 @@ struct Args {
   int32_t* last;   // [B][supers] the team that ends it
 };
 
-__device__ __forceinline__ int length_of(const Args& a, int b) { return min(max(a.lens[b], 0), a.capacity); }
+__device__ __forceinline__ int length_of(const Args& a, int b) { return min(max(load_global<int32_t>(a.lens + b), 0), a.capacity); }
 __device__ __forceinline__ int rows_of(const Args& a, int b) {
-  return a.rows ? min(max(a.rows[b], 0), a.Q) : a.Q;
+  return a.rows ? min(max(load_global<int32_t>(a.rows + b), 0), a.Q) : a.Q;
 }
 __device__ __forceinline__ int tiles_of(int len) { return (len + kTile - 1) / kTile; }
 // Team `team` of `teams` (a multiple of 8 that go round the XCDs) runs as workgroups group_of(.., 0..).
@@ -152,10 +152,16 @@ __global__ __launch_bounds__(R == 1 ? 256 : 512) void latent_kernel(Args a) {
   }
 
   // The pieces that this lane loads: piece 64 i + lane of the wavefront's TW tokens.
-  auto piece_token = [&](int i) { return (8 * i + (lane >> 3)) / (C / 8); };
-  auto piece_col = [&](int i) {  // its column in a token, -1 past d_latent or d_rope
-    const int tok = piece_token(i), pc = 64 * i + lane - tok * C, col = ((pc & ~7) | ((pc ^ perm(tok)) & 7)) * 8;
+  auto piece_token = [&](int i, int ln) { return (8 * i + (ln >> 3)) / (C / 8); };
+  auto piece_col = [&](int i, int ln) {  // its column in a token, -1 past d_latent or d_rope
+    const int tok = piece_token(i, ln), pc = 64 * i + ln - tok * C, col = ((pc & ~7) | ((pc ^ perm(tok)) & 7)) * 8;
     return col < DC ? (col < a.dc ? col : -1) : (col - DC < a.dr ? a.dc + col - DC : -1);
+  };
+  // The lane, for the loop's rare paths: what they compute from it is not kept in registers through
+  // the others.
+  auto rare = [&](int v) {
+    asm volatile("" : "+v"(v));
+    return v;
   };
   const bool padded = a.dc != DC || a.dr != kRope;
   // Where a wavefront's tokens lie one after another in one page, a tile's loads have one scalar
@@ -163,7 +169,7 @@ __global__ __launch_bounds__(R == 1 ? 256 : 512) void latent_kernel(Args a) {
   const bool rowed = (a.pages == nullptr || a.page_size % TW == 0) && a.token_stride < (1 << 24) && !padded;
   uint32_t off[NL];
 #pragma unroll
-  for (int i = 0; i < NL; ++i) off[i] = 2u * (uint32_t)(piece_token(i) * (int)a.token_stride + piece_col(i));
+  for (int i = 0; i < NL; ++i) off[i] = 2u * (uint32_t)(piece_token(i, lane) * (int)a.token_stride + piece_col(i, lane));
   // what a lane reads of a tile and of P, in bytes
   const int kx = g ^ perm(n);
   const int krow[2] = {((16 * TB * wt + n) * C + kx) * 16, ((16 * TB * wt + n) * C + (kx ^ 4)) * 16};
@@ -216,40 +222,60 @@ __global__ __launch_bounds__(R == 1 ? 256 : 512) void latent_kernel(Args a) {
     // Tile tl's part of this wavefront: tokens tl * 64 + TW w .. + TW - 1.  Returns which of them some
     // row sees and whose page exists; the others are not loaded.
     const int32_t* table = a.pages ? a.pages + (int64_t)b * a.pages_stride : nullptr;
-    auto load_tile = [&](int tl, Lds dst) -> uint32_t {
+    // (the page of a whole tile's part is asked for a tile ahead: it would be waited for)
+    auto page_of = [&](int tl) {
+      const int j0 = tl * kTile + TW * w;
+      return table && rowed && j0 < lim_hi ? load_global<int32_t>(table + j0 / a.page_size) : b;
+    };
+    // What a tile's loads need; `on` says that they go by the view, one after another (next_load), and
+    // valid which tokens they bring.  Tiles of another kind are loaded here.
+    struct Load {
+      u32x4 view;
+      uint32_t dst, valid;
+      uint64_t on;
+    };
+    auto start_load = [&](int tl, int ahead, Lds dst) -> Load {
+      Load ld{u32x4{0u, 0u, 0u, 0u}, 0u, 0u, 0ull};
       const int j0 = tl * kTile + TW * w, count = min(max(lim_hi - j0, 0), TW);
       dst += TW * w * C * 16;
       if (rowed && count == TW) {
-        const int pg = table ? j0 / a.page_size : 0, page = __builtin_amdgcn_readfirstlane(table ? table[pg] : b);
-        if (page < 0 || page >= a.n_pages) return 0u;
-        const auto view = buf_view(
-            a.cache + (int64_t)page * a.page_stride + (int64_t)(j0 - pg * a.page_size) * a.token_stride,
-            2 * ((TW - 1) * a.token_stride + a.dc + a.dr));
-#pragma unroll
-        for (int i = 0; i < NL; ++i) load_lds(view, off[i], dst + 1024 * i);
-        return (1u << TW) - 1u;
+        const int pg = table ? j0 / a.page_size : 0, page = __builtin_amdgcn_readfirstlane(ahead);
+        if (page < 0 || page >= a.n_pages) return ld;
+        ld.view = lds_view(a.cache + (int64_t)page * a.page_stride + (int64_t)(j0 - pg * a.page_size) * a.token_stride,
+                           2 * ((TW - 1) * a.token_stride + a.dc + a.dr));
+        ld.dst = lds_address(dst);
+        ld.valid = (1u << TW) - 1u;
+        ld.on = ~0ull;
+        return ld;
       }
-      const int j = j0 + lane % TW, pg = j / a.page_size;
-      const int page = lane % TW < count ? (table ? table[pg] : b) : -1;
+      const int ln = rare(lane), j = j0 + ln % TW, pg = j / a.page_size;
+      const int page = ln % TW < count ? (table ? load_global<int32_t>(table + pg) : b) : -1;
       const bool ok = page >= 0 && page < a.n_pages;
       const uint32_t valid = (uint32_t)__ballot(ok) & ((1u << TW) - 1u);
       const uint64_t adr = reinterpret_cast<uint64_t>(
           a.cache + (ok ? (int64_t)page * a.page_stride + (int64_t)(table ? j - pg * a.page_size : j) * a.token_stride : 0));
 #pragma unroll 1
       for (int i = 0; i < NL; ++i) {
-        const int tok = piece_token(i), col = piece_col(i);
+        const int tok = piece_token(i, ln), col = piece_col(i, ln);
         const uint32_t lo = __shfl((int)(uint32_t)adr, tok), hi = __shfl((int)(uint32_t)(adr >> 32), tok);
         if (col >= 0 && (valid >> tok & 1u)) load_lds((Global)(((uint64_t)hi << 32) | lo) + 2 * col, dst + 1024 * i);
       }
-      return valid;
+      ld.valid = valid;
+      return ld;
     };
     // tokens that no row sees, or of no page, become zero vectors
     auto clear_rest = [&](uint32_t valid, Lds dst) {
       dst += TW * w * C * 16;
-      for (int i = lane; i < TW * C; i += 64)
+      for (int i = rare(lane); i < TW * C; i += 64)
         if (!(valid >> (i / C) & 1u)) *(__attribute__((address_space(3))) u32x4*)(dst + 16 * i) = u32x4{0u, 0u, 0u, 0u};
     };
-    uint32_t valid = load_tile(t0, tiles);
+    int next = t0 + 1 < t1 ? page_of(t0 + 1) : 0;
+    uint32_t valid;
+    {
+      const Load ld = start_load(t0, page_of(t0), tiles);
+      valid = ld.valid;
+      each<NL>([&](auto i) { load_lds_view<1024 * decltype(i)::value>(ld.view, off[i], ld.dst, ld.on); });
+    }
     if (t < 2 * (WR + 1)) moved[t / (WR + 1)][t % (WR + 1)] = 0;
     if (t < 16 * R) limits[t] = r0 + t <= rlast ? len - nrow + (r0 + t) / a.H + 1 : 0;
 
@@ -263,8 +289,9 @@ __global__ __launch_bounds__(R == 1 ? 256 : 512) void latent_kernel(Args a) {
       for (int k = 0; k < KS; ++k) {
         const int col = 32 * k + 8 * g;
         const int at = col < DC ? (col < a.dc ? col : -1) : (col - DC < a.dr ? a.dc + col - DC : -1);
-        qf[k] = u32x4{0u, 0u, 0u, 0u};
-        if (!padded || at >= 0) qf[k] = *reinterpret_cast<const u32x4*>(src + at);
+        // (loads are not branched around, so that all are in flight together)
+        qf[k] = load_global<u32x4>(src + (at >= 0 ? at : 0));
+        qf[k] = at >= 0 ? qf[k] : u32x4{0u, 0u, 0u, 0u};
         qf[k] ^= a.flip;
       }
     }
@@ -283,13 +310,25 @@ __global__ __launch_bounds__(R == 1 ? 256 : 512) void latent_kernel(Args a) {
       if (lane == 0) present[w] = valid;
       __syncthreads();
       if (t <= WR) moved[(tl - t0 + 1) & 1][t] = 0;
-      if (tl + 1 < t1) valid = load_tile(tl + 1, tiles + ((tl - t0 + 1) & 1) * (kTile * C * 16));
+      Load ld{u32x4{0u, 0u, 0u, 0u}, 0u, 0u, 0ull};
+      if (tl + 1 < t1) {
+        const int page = next;
+        if (tl + 2 < t1) next = page_of(tl + 2);
+        ld = start_load(tl + 1, page, tiles + ((tl - t0 + 1) & 1) * (kTile * C * 16));
+        valid = ld.valid;
+      }
+      // the scalar registers of a uniform value that a branch chose
+      ld.view = u32x4{uniform(ld.view[0]), uniform(ld.view[1]), uniform(ld.view[2]), kBufferWord3};
+      ld.dst = uniform(ld.dst);
+      ld.on = (uint64_t)0 - (uint64_t)(uniform((uint32_t)ld.on) & 1u);
 
       f32x4 s[TB];
 #pragma unroll
       for (int j = 0; j < TB; ++j) s[j] = f32x4{0.f, 0.f, 0.f, 0.f};
       {
-        // two steps' pieces are read while the two before are multiplied
+        // Two steps' pieces are read while the two before are multiplied.  The next tile's loads go out
+        // between them: a load of 1 KB takes the unit that makes its addresses 16 cycles, so that
+        // 72 in a row would hold up the wavefronts for longer than the products take.
         u32x4 kf[2][2][TB];
         auto read = [&](int k) {
 #pragma unroll
@@ -299,16 +338,19 @@ __global__ __launch_bounds__(R == 1 ? 256 : 512) void latent_kernel(Args a) {
               kf[(k >> 1) & 1][i][j] = lds_read<u32x4>(here + krow[i] + (k >> 1) * 128 + 16 * j * C * 16);
         };
         read(0);
-#pragma unroll
-        for (int k = 0; k < KS; k += 2) {
+        each<KS / 2>([&](auto step) {
+          constexpr int h = decltype(step)::value, k = 2 * h;
           if (k + 2 < KS) read(k + 2);
           __builtin_amdgcn_sched_barrier(0);
+          each<NL>([&](auto i) {
+            if constexpr (i * (KS / 2) / NL == h) load_lds_view<1024 * decltype(i)::value>(ld.view, off[i], ld.dst, ld.on);
+          });
 #pragma unroll
           for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int j = 0; j < TB; ++j) s[j] = T::mfma(kf[(k >> 1) & 1][i][j], qf[k + i], s[j]);
+            for (int j = 0; j < TB; ++j) s[j] = T::mfma(kf[h & 1][i][j], qf[k + i], s[j]);
           __builtin_amdgcn_sched_barrier(0);
-        }
+        });
       }
       // The products' results are taken up here, in the block that made them: the
       // compiler leaves too few wait states before a read behind a branch.
@@ -361,7 +403,7 @@ __global__ __launch_bounds__(R == 1 ? 256 : 512) void latent_kernel(Args a) {
       if (edge && lim_lo < lim_hi) {
         uint32_t bad = 0;
         const int from = max(lim_lo - tl * kTile, 0), to_j = min(lim_hi - tl * kTile, kTile);
-        for (int i = t; i < (to_j - from) * DC / 2; i += kLanes)
+        for (int i = rare(t); i < (to_j - from) * DC / 2; i += kLanes)
           bad |= lawless<T>(reinterpret_cast<const uint32_t*>(cur + (from + i / (DC / 2)) * C * 8)[i % (DC / 2)]);
         if (__any((bad & 0x80008000u) != 0) && lane == 0) moved[(tl - t0) & 1][WR] = 1;
       }
@@ -374,7 +416,7 @@ __global__ __launch_bounds__(R == 1 ? 256 : 512) void latent_kernel(Args a) {
         }
       if (__builtin_amdgcn_readfirstlane(moved[(tl - t0) & 1][WR])) {
         // what the infinities and NaN give to the rows that see them, and zeros in their place
-        const int first = tl * kTile, to_j = min(lim_hi - first, kTile);
+        const int first = tl * kTile, to_j = min(lim_hi - first, kTile), ln = rare(lane), ng = ln >> 4, nn = ln & 15;
 #pragma clang loop unroll(disable)
         for (int j = max(lim_lo - first, 0); j < to_j; ++j) {
           const int blk = j >> 2, at = 4 * (blk >> 3) + (blk & 3), part = 4 * (blk >> 2 & 1) + (j & 3);
@@ -382,19 +424,19 @@ __global__ __launch_bounds__(R == 1 ? 256 : 512) void latent_kernel(Args a) {
           for (int k = 0; k < NB; ++k)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const int ch = (w * NB + k) * 2 + (g >> 1), pc = (ch & ~7) | ((ch ^ perm(j)) & 7);
-              const uint16_t v = cur[(j * C + pc) * 8 + 4 * (g & 1) + i];
+              const int ch = (w * NB + k) * 2 + (ng >> 1), pc = (ch & ~7) | ((ch ^ perm(j)) & 7);
+              const uint16_t v = cur[(j * C + pc) * 8 + 4 * (ng & 1) + i];
               if ((v & T::kExponent) == T::kExponent) {
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
-                  const float p = T::value(pl[(16 * r + n) * kTile + (at ^ (n & 7)) * 8 + part]);
-                  if (first + j < limits[16 * r + n]) o[r][k][i] += p * T::value(v);
+                  const float p = T::value(pl[(16 * r + nn) * kTile + (at ^ (nn & 7)) * 8 + part]);
+                  if (first + j < limits[16 * r + nn]) o[r][k][i] += p * T::value(v);
                 }
               }
             }
         }
         __syncthreads();
-        for (int i = t; i < to_j * DC; i += kLanes) {
+        for (int i = rare(t); i < to_j * DC; i += kLanes) {
           uint16_t* v = cur + (i / DC) * C * 8 + i % DC;
           if (first + i / DC >= lim_lo && (*v & T::kExponent) == T::kExponent) *v = 0;
         }

@@ -7,6 +7,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "bufio.hpp"
 #include "common.hpp"
 #include "wavered.hpp"
@@ -73,6 +75,23 @@ __device__ __forceinline__ uint32_t lawless(uint32_t v) {
 // piece pairs of four tokens in a row.
 __device__ __forceinline__ int perm(int token) { return ((token & 3) << 1) | ((token >> 2) & 1); }
 
+// f(0), f(1), .. f(N - 1) with the numbers as types' values.
+template <int N, int I = 0, class F>
+__device__ __forceinline__ void each(F&& f) {
+  if constexpr (I < N) {
+    f(std::integral_constant<int, I>{});
+    each<N, I + 1>(f);
+  }
+}
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
+
+// A load known to be from global memory.  (One that might be from LDS counts as both, and while
+// it is pending every wait for an LDS read is a wait for all of them.)
+template <class V, class P>
+__device__ __forceinline__ V load_global(const P* p) {
+  return *(const __attribute__((address_space(1))) V*)(uint64_t)p;
+}
+
 // Over lanes 16 and 32 apart (in every one of them the same bits).
 __device__ __forceinline__ float across(float v, bool row32, bool max) {
   uint32_t a = __builtin_bit_cast(uint32_t, v), b = a;
@@ -96,14 +115,37 @@ __device__ __forceinline__ u32x2 lds_read_tr(Lds p) {
 // A barrier for what the wavefronts exchange through LDS themselves.  It does not wait
 // for loads that write LDS, as __syncthreads does: those are in flight across it.
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
-// 16 bytes a lane from global memory to LDS at dst + 16 lane (dst uniform).
+// 16 bytes a lane from global memory to LDS at dst + 16 lane (dst uniform).  In
+// assembly, because the compiler takes a load that writes LDS for one that any LDS read
+// behind it may have to wait for, and then waits for all reads in flight where it should
+// for one.  Nothing is returned to registers; the caller waits for the loads (vmcnt)
+// before a barrier.  The wait states are those of a scalar register written by a vector
+// instruction, and of M0.
 typedef const __attribute__((address_space(1))) char* Global;
-__device__ __forceinline__ void load_lds(Global src, Lds dst) {
-  __builtin_amdgcn_global_load_lds(src, dst, 16, 0, 0);
+__device__ __forceinline__ uint32_t lds_address(Lds p) {
+  return (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint64_t)p);
 }
-// The same from byte `off` of a view: one register an address, and none to compute.
-__device__ __forceinline__ void load_lds(__amdgpu_buffer_rsrc_t view, uint32_t off, Lds dst) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(view, dst, 16, off, 0, 0, 0);
+__device__ __forceinline__ void load_lds(Global src, Lds dst) {
+  asm volatile("s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_address(dst)),
+               "v"((uint64_t)src)
+               : "memory", "m0");
+}
+// A view of global memory for loads that write LDS, in scalar registers.
+__device__ __forceinline__ u32x4 lds_view(const void* base, int64_t bytes) {
+  const uint64_t p = reinterpret_cast<uint64_t>(base);
+  return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)p),
+               (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(p >> 32)),
+               (uint32_t)__builtin_amdgcn_readfirstlane((int)bytes), kBufferWord3};
+}
+// The same from byte `off` of a view to dst + STEP + 16 lane: one register an address,
+// and none to compute.  on: all ones, or 0 for no load at all.
+template <int STEP>
+__device__ __forceinline__ void load_lds_view(u32x4 view, uint32_t off, uint32_t dst, uint64_t on) {
+  asm volatile(
+      "s_nop 1\n\ts_mov_b64 exec, %4\n\ts_add_i32 m0, %0, %1\n\ts_nop 0\n\t"
+      "buffer_load_dwordx4 %2, %3, 0 offen lds\n\ts_mov_b64 exec, -1" ::"s"(dst),
+      "n"(STEP), "v"(off), "s"(view), "s"(on)
+      : "memory", "m0", "scc");
 }
 
 }  // namespace latent

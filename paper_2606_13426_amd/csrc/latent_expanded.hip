@@ -54,7 +54,7 @@ struct Expanded {
   float2* stat;  // [split][Tq][H] (reference, sum)
 };
 
-__device__ __forceinline__ int offset_of(const int32_t* cu, int i, int total) { return min(max(cu[i], 0), total); }
+__device__ __forceinline__ int offset_of(const int32_t* cu, int i, int total) { return min(max(load_global<int32_t>(cu + i), 0), total); }
 
 template <class T, int DN, int DV>
 __global__ __launch_bounds__(kThreads, 2) void expanded_kernel(Expanded a) {
@@ -97,8 +97,9 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_kernel(Expanded a) {
     for (int k = 0; k < KS; ++k) {
       const int col = 16 * k + 8 * h;
       const int at = col < DN ? (col < a.dn ? col : -1) : (col - DN < a.dr ? a.dn + col - DN : -1);
-      qf[k] = u32x4{0u, 0u, 0u, 0u};
-      if (at >= 0) qf[k] = *reinterpret_cast<const u32x4*>(src + at);
+      // (loads are not branched around, so that all are in flight together)
+      qf[k] = load_global<u32x4>(src + (at >= 0 ? at : 0));
+      qf[k] = at >= 0 ? qf[k] : u32x4{0u, 0u, 0u, 0u};
       qf[k] ^= a.flip;
     }
   }
@@ -114,7 +115,7 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_kernel(Expanded a) {
   const Global gv = (Global)(a.v + (int64_t)kb * a.vt + (int64_t)head * a.vh);
   const Lds lds = lds_of(buf);
   const bool padded = a.dn != DN || a.dr != kRope || a.dv != DV;
-  uint32_t off[(CN + CR + CV) / 4];
+  uint32_t off_n[CN / 4], off_r[CR / 4], off_v[CV / 4];
   auto place = [&](int P, int i, int* tok) {
     const int s = 64 * (w + 4 * i) + lane, pc = s % P;
     *tok = s / P;
@@ -127,16 +128,18 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_kernel(Expanded a) {
       to[i] = 2u * (uint32_t)(tok * (int)stride + col);
     }
   };
-  set_offsets(CN, a.kt, off);
-  set_offsets(CR, a.krt, off + CN / 4);
-  set_offsets(CV, a.vt, off + (CN + CR) / 4);
-  auto load_part = [&](int P, const uint32_t* offs, Global base, int64_t stride, int d, int tl, Lds dst) {
+  set_offsets(CN, a.kt, off_n);
+  set_offsets(CR, a.krt, off_r);
+  set_offsets(CV, a.vt, off_v);
+  // piece i of a wavefront goes to 1024 (w + 4 i): four wavefronts side by side
+  auto load_part = [&](auto& offs, Global base, int64_t stride, int d, int tl, Lds dst) {
+    constexpr int P = 4 * (int)(sizeof(offs) / sizeof(offs[0]));
     const Global src = base + (int64_t)tl * kTile * stride * 2;
     const int last = nk - 1 - tl * kTile;  // places behind the last key repeat it; their weights are 0
     if (last >= kTile - 1 && !padded) {
-      const auto view = buf_view((const void*)src, 2 * ((kTile - 1) * stride + d));
-#pragma unroll
-      for (int i = 0; i < P / 4; ++i) load_lds(view, offs[i], dst + 1024 * (w + 4 * i));
+      const u32x4 view = lds_view((const void*)src, 2 * ((kTile - 1) * stride + d));
+      const uint32_t to = lds_address(dst + 1024 * w);
+      each<P / 4>([&](auto i) { load_lds_view<4096 * decltype(i)::value>(view, offs[i], to, ~0ull); });
     } else {
 #pragma unroll
       for (int i = 0; i < P / 4; ++i) {
@@ -147,9 +150,9 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_kernel(Expanded a) {
     }
   };
   auto load_tile = [&](int tl, Lds dst) {
-    load_part(CN, off, gk, a.kt, a.dn, tl, dst);
-    load_part(CR, off + CN / 4, gr, a.krt, a.dr, tl, dst + kKr);
-    load_part(CV, off + (CN + CR) / 4, gv, a.vt, a.dv, tl, dst + kV);
+    load_part(off_n, gk, a.kt, a.dn, tl, dst);
+    load_part(off_r, gr, a.krt, a.dr, tl, dst + kKr);
+    load_part(off_v, gv, a.vt, a.dv, tl, dst + kV);
   };
   if (padded) {
     // pieces that no load writes are zero in both buffers
