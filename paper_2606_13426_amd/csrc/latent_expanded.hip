@@ -62,7 +62,7 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_kernel(Expanded a) {
   constexpr int CN = DN / 8, CR = kRope / 8, CV = DV / 8;  // 16-byte pieces a token in the three parts
   constexpr int kKr = kTile * DN * 2, kV = kKr + kTile * kRope * 2, kStage = kV + kTile * DV * 2;
   __shared__ __align__(16) char buf[2 * kStage];
-  const int t = threadIdx.x, w = t >> 6, lane = t & 63, n = lane & 31, h = lane >> 5;
+  const int t = threadIdx.x, w = (int)uniform((uint32_t)t >> 6), lane = t & 63, n = lane & 31, h = lane >> 5;
 
   // the tiles of a head from the last to the first, a head's tiles on one XCD
   const int id = xcd_tile((int)(gridDim.x * gridDim.y * gridDim.z));
@@ -86,6 +86,9 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_kernel(Expanded a) {
   const int row = q0 + 32 * w + n;
   const bool real = row < nq;
   const int lim = real ? min(max(row + shift, 0), nk) : 0;
+  // the least limit of the workgroup's rows; tiles that reach past it have keys that not all its rows see
+  const int g_lo = min(max(q0 + shift, 0), nk);
+  auto mixed = [&](int tl) { return (tl + 1) * kTile > g_lo; };
   // the least and the largest limit of this wavefront's real rows
   const int w_lo = min(max(q0 + 32 * w + shift, 0), nk);
   const int w_hi = q0 + 32 * w < nq ? min(max(min(q0 + 32 * w + 31, nq - 1) + shift, 0), nk) : 0;
@@ -108,14 +111,17 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_kernel(Expanded a) {
   for (int k = 0; k < NV; ++k) o[k] = f32x16{};
   float m = -INFINITY, l = 0.f;
 
-  // Piece 64 (w + 4 i) + lane of each part of a tile: its token, and the column (permuted among
-  // eight; -1 past the part's own).
+  // Piece 64 (w + 4 i) + lane of each part of a tile: its token, and the column (permuted among eight).
   const Global gk = (Global)(a.k + (int64_t)kb * a.kt + (int64_t)head * a.kh);
   const Global gr = (Global)(a.kr + (int64_t)kb * a.krt);
   const Global gv = (Global)(a.v + (int64_t)kb * a.vt + (int64_t)head * a.vh);
   const Lds lds = lds_of(buf);
   const bool padded = a.dn != DN || a.dr != kRope || a.dv != DV;
   uint32_t off_n[CN / 4], off_r[CR / 4], off_v[CV / 4];
+  auto rare = [&](int v) {  // (what the loop's rare paths compute from it is not kept in registers)
+    asm volatile("" : "+v"(v));
+    return v;
+  };
   auto place = [&](int P, int i, int* tok) {
     const int s = 64 * (w + 4 * i) + lane, pc = s % P;
     *tok = s / P;
@@ -132,38 +138,61 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_kernel(Expanded a) {
   set_offsets(CR, a.krt, off_r);
   set_offsets(CV, a.vt, off_v);
   // piece i of a wavefront goes to 1024 (w + 4 i): four wavefronts side by side
-  auto load_part = [&](auto& offs, Global base, int64_t stride, int d, int tl, Lds dst) {
-    constexpr int P = 4 * (int)(sizeof(offs) / sizeof(offs[0]));
-    const Global src = base + (int64_t)tl * kTile * stride * 2;
-    const int last = nk - 1 - tl * kTile;  // places behind the last key repeat it; their weights are 0
-    if (last >= kTile - 1 && !padded) {
-      const u32x4 view = lds_view((const void*)src, 2 * ((kTile - 1) * stride + d));
-      const uint32_t to = lds_address(dst + 1024 * w);
-      each<P / 4>([&](auto i) { load_lds_view<4096 * decltype(i)::value>(view, offs[i], to, ~0ull); });
-    } else {
-#pragma unroll
-      for (int i = 0; i < P / 4; ++i) {
-        int tok;
-        const int col = place(P, i, &tok);
-        if (col < d) load_lds(src + 2u * (uint32_t)(min(tok, last) * (int)stride + col), dst + 1024 * (w + 4 * i));
-      }
+  // The three views of a tile, for loads that go out one after another (next_load); `on` is 0 where
+  // the tile is of another kind (its keys end in it, or columns are missing) and loaded here.
+  struct Load {
+    u32x4 n, r, v;
+    uint32_t dst;
+    uint64_t on;
+  };
+  auto base_of = [&](Global base, int64_t stride, int tl) { return base + (int64_t)tl * kTile * stride * 2; };
+  auto slow_part = [&](int P, Global base, int64_t stride, int d, int tl, Lds dst) {
+    const Global src = base_of(base, stride, tl);
+    const int last = nk - 1 - tl * kTile, ln = rare(lane);  // places behind the last key repeat it; their weights are 0
+#pragma unroll 1
+    for (int i = 0; i < P / 4; ++i) {
+      const int s = 64 * (w + 4 * i) + ln, pc = s % P, tok = s / P, col = ((pc & ~7) | ((pc ^ perm(tok)) & 7)) * 8;
+      if (col < d) load_lds(src + 2u * (uint32_t)(min(tok, last) * (int)stride + col), dst + 1024 * (w + 4 * i));
     }
   };
-  auto load_tile = [&](int tl, Lds dst) {
-    load_part(off_n, gk, a.kt, a.dn, tl, dst);
-    load_part(off_r, gr, a.krt, a.dr, tl, dst + kKr);
-    load_part(off_v, gv, a.vt, a.dv, tl, dst + kV);
+  auto start_load = [&](int tl, Lds dst, bool want) -> Load {
+    Load ld;
+    const bool fast = tl * kTile + kTile <= nk && !padded;
+    if (want && !fast) {
+      slow_part(CN, gk, a.kt, a.dn, tl, dst);
+      slow_part(CR, gr, a.krt, a.dr, tl, dst + kKr);
+      slow_part(CV, gv, a.vt, a.dv, tl, dst + kV);
+    }
+    ld.n = lds_view((const void*)base_of(gk, a.kt, tl), 2 * ((kTile - 1) * a.kt + a.dn));
+    ld.r = lds_view((const void*)base_of(gr, a.krt, tl), 2 * ((kTile - 1) * a.krt + a.dr));
+    ld.v = lds_view((const void*)base_of(gv, a.vt, tl), 2 * ((kTile - 1) * a.vt + a.dv));
+    ld.dst = lds_address(dst + 1024 * w);
+    ld.on = (uint64_t)0 - (uint64_t)uniform(fast && want ? 1u : 0u);
+    return ld;
+  };
+  constexpr int kLoads = (CN + CR + CV) / 4;
+  auto next_load = [&](const Load& ld, auto i) {
+    constexpr int I = decltype(i)::value;
+    if constexpr (I < CN / 4)
+      load_lds_view<4096 * I>(ld.n, off_n[I], ld.dst, ld.on);
+    else if constexpr (I < (CN + CR) / 4)
+      load_lds_view<4096 * (I - CN / 4) + kKr>(ld.r, off_r[I - CN / 4], ld.dst, ld.on);
+    else
+      load_lds_view<4096 * (I - (CN + CR) / 4) + kV>(ld.v, off_v[I - (CN + CR) / 4], ld.dst, ld.on);
   };
   if (padded) {
     // pieces that no load writes are zero in both buffers
     for (int i = t; i < 2 * kStage / 16; i += kThreads) reinterpret_cast<u32x4*>(buf)[i] = u32x4{0u, 0u, 0u, 0u};
     __syncthreads();
   }
-  if (t0 < t1) load_tile(t0, lds);
+  if (t0 < t1) {
+    const Load ld = start_load(t0, lds, true);
+    each<kLoads>([&](auto i) { next_load(ld, i); });
+  }
 
   // what a lane reads of a tile, in bytes: of key n (and n + 32) piece 2 k + h; of values four tokens by
   // sixteen columns, of which the lanes from 16 and 48 on take the upper sixteen of a block of 32
-  const int kx = h ^ perm(n);
+  const int kx = h ^ perm(n), krow = n * DN * 2 + kx * 16, rrow = kKr + n * kRope * 2 + kx * 16;
   const int vtok = 4 * h + ((lane & 15) >> 2), vch = 2 * (lane >> 4 & 1) + ((lane & 3) >> 1);
   const int vrow[2] = {vtok * DV * 2 + (vch ^ perm(vtok)) * 16 + 8 * (lane & 1),
                        vtok * DV * 2 + ((vch + 4) ^ perm(vtok)) * 16 + 8 * (lane & 1)};
@@ -171,21 +200,39 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_kernel(Expanded a) {
   for (int tl = t0; tl < t1; ++tl) {
     const Lds here = lds + (tl - t0 & 1) * kStage;
     __builtin_amdgcn_s_waitcnt(0);
-    __syncthreads();
-    if (tl + 1 < t1) load_tile(tl + 1, lds + (tl - t0 + 1 & 1) * kStage);
-    if (tl * kTile >= w_hi) continue;  // none of this wavefront's rows sees the tile
+    lds_barrier();
+    Load ld = start_load(min(tl + 1, t1 - 1), lds + (tl - t0 + 1 & 1) * kStage, tl + 1 < t1);
+    if (tl * kTile >= w_hi && !mixed(tl)) {
+      // none of this wavefront's rows sees the tile
+      each<kLoads>([&](auto i) { next_load(ld, i); });
+      continue;
+    }
 
-    f32x16 s[2];
+    f32x16 s[2] = {f32x16{}, f32x16{}};
+    {
+      // a step's pieces are read while the two before it are multiplied; the next tile's loads go out between
+      u32x4 kf[3][2];
+      auto read = [&](int k) {
+        const bool own = k < DN / 16;
+        const int kk = own ? k : k - DN / 16;
 #pragma unroll
-    for (int b2 = 0; b2 < 2; ++b2) {
-      s[b2] = f32x16{};
+        for (int b2 = 0; b2 < 2; ++b2)
+          kf[k % 3][b2] = lds_read<u32x4>(here + (own ? krow : rrow) + (own ? 32 * b2 * DN * 2 : 32 * b2 * kRope * 2) +
+                                          (kk >> 2) * 128 + (((2 * (kk & 3)) ^ kx) - kx) * 16);
+      };
+      read(0);
+      read(1);
+      each<KS>([&](auto step) {
+        constexpr int k = decltype(step)::value;
+        if (k + 2 < KS) read(k + 2);
+        __builtin_amdgcn_sched_barrier(0);
+        each<kLoads>([&](auto i) {
+          if constexpr (i * KS / kLoads == k) next_load(ld, i);
+        });
 #pragma unroll
-      for (int k = 0; k < KS; ++k) {
-        const int base = k < DN / 16 ? (32 * b2 + n) * DN * 2 : kKr + (32 * b2 + n) * kRope * 2;
-        const int kk = k < DN / 16 ? k : k - DN / 16;
-        const u32x4 kf = lds_read<u32x4>(here + base + (kk >> 2) * 128 + ((2 * (kk & 3)) ^ kx) * 16);
-        s[b2] = T::mfma32(kf, qf[k], s[b2]);
-      }
+        for (int b2 = 0; b2 < 2; ++b2) s[b2] = T::mfma32(kf[k % 3][b2], qf[k], s[b2]);
+        __builtin_amdgcn_sched_barrier(0);
+      });
     }
 #pragma unroll
     for (int b2 = 0; b2 < 2; ++b2) asm volatile("" : "+v"(s[b2]));  // taken up before any branch
@@ -227,77 +274,54 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_kernel(Expanded a) {
       }
     l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
 
-    auto values = [&](int st, int k) {
-      const Lds src = here + kV + st * 16 * DV * 2 + vrow[k & 1] + (k >> 1) * 128;
-      const u32x2 lo = lds_read_tr(src), hi = lds_read_tr(src + 8 * DV * 2);
-      return u32x4{lo[0], lo[1], hi[0], hi[1]};
-    };
-    // A key that some rows see and others do not: its weight for those is 0, and 0 times
-    // an infinity or NaN in its value is not.
-    if (edge) {
-      const int from = max(w_lo - tl * kTile, 0);
+    // A key that some rows of the workgroup see and others do not: its weight for those is 0, and 0
+    // times an infinity or NaN in its value is not.  All wavefronts look and find the same.
+    if (mixed(tl)) {
+      const int from = max(g_lo - tl * kTile, 0), ln = rare(lane);
       uint32_t bad = 0;
-      for (int i = lane; i < (kTile - from) * CV; i += 64) {
+      for (int i = ln; i < (kTile - from) * CV; i += 64) {
         const u32x4 v = lds_read<u32x4>(here + kV + from * DV * 2 + 16 * i);
         bad |= (lawless<T>(v[0]) | lawless<T>(v[1])) | (lawless<T>(v[2]) | lawless<T>(v[3]));
       }
       if (__any((bad & 0x80008000u) != 0)) {
-        // finite values as they are, and whether a row sees an infinity of either sign (a NaN counts as both)
-        u32x4 seen[4];
+        // what they give to the rows that see them, and zeros in their place
+        const int hh = ln >> 5, row_lim = lim - tl * kTile;
+#pragma clang loop unroll(disable)
+        for (int j = from; j < kTile; ++j)
 #pragma unroll
-        for (int st = 0; st < 4; ++st)
+          for (int k = 0; k < NV; ++k)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int key = tl * kTile + 16 * st + 8 * (j >> 1) + 4 * h + 2 * (j & 1);
-            seen[st][j] = (key < lim ? T::kOne : 0u) | (key + 1 < lim ? T::kOne << 16 : 0u);
-          }
-        auto sign = [&](uint32_t v, bool minus) {
-          uint32_t r = 0;
-#pragma unroll
-          for (int u = 0; u < 32; u += 16) {
-            const uint32_t x = v >> u & 0xffffu;
-            const bool inf = (x & 0x7fffu) == T::kExponent, nan = (x & 0x7fffu) > T::kExponent;
-            if (nan || (inf && (x >> 15 != 0) == minus)) r |= T::kOne << u;
-          }
-          return r;
-        };
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-          uint32_t mark = 0;  // bits i: an infinity, 16 + i: minus one
-#pragma unroll 1
-          for (int minus = 0; minus < 2; ++minus) {
-            f32x16 c = f32x16{};
-#pragma unroll
-            for (int st = 0; st < 4; ++st) {
-              const u32x4 v = values(st, k);
-              c = T::mfma32(u32x4{sign(v[0], minus), sign(v[1], minus), sign(v[2], minus), sign(v[3], minus)}, seen[st], c);
+            for (int i = 0; i < 16; ++i) {
+              const int col = 32 * k + 8 * (i >> 2) + 4 * hh + (i & 3), pc = (col >> 3 & ~7) | ((col >> 3 ^ perm(j)) & 7);
+              const uint32_t v = lds_read<uint16_t>(here + kV + j * DV * 2 + pc * 16 + 2 * (col & 7));
+              if ((v & T::kExponent) == T::kExponent && j < row_lim) o[k][i] += T::value((uint16_t)v);
             }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) mark |= c[i] > 0.f ? 1u << (16 * minus + i) : 0u;
-          }
-#pragma unroll
-          for (int st = 0; st < 4; ++st) {
-            u32x4 v = values(st, k);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const uint32_t x = lawless<T>(v[j]);
-              v[j] &= ((x & 0x8000u) ? 0u : 0xffffu) | ((x & 0x80000000u) ? 0u : 0xffff0000u);
-            }
-            o[k] = T::mfma32(v, pf[st], o[k]);
-          }
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            if (mark >> i & 1u) o[k][i] += INFINITY;
-            if (mark >> (16 + i) & 1u) o[k][i] -= INFINITY;
-          }
+        lds_barrier();
+        for (int i = from * DV + rare(t); i < kTile * DV; i += kThreads) {
+          const Lds at = here + kV + 2 * i;
+          if ((lds_read<uint16_t>(at) & T::kExponent) == T::kExponent) *(__attribute__((address_space(3))) uint16_t*)at = 0;
         }
-        continue;
+        lds_barrier();
       }
     }
+    {
+      // two blocks' values are read while one is multiplied
+      u32x4 vf[3];
+      auto read = [&](int i) {
+        const Lds src = here + kV + (i / NV) * 16 * DV * 2 + vrow[i % NV & 1] + (i % NV >> 1) * 128;
+        const u32x2 lo = lds_read_tr(src), hi = lds_read_tr(src + 8 * DV * 2);
+        vf[i % 3] = u32x4{lo[0], lo[1], hi[0], hi[1]};
+      };
+      read(0);
+      read(1);
 #pragma unroll
-    for (int st = 0; st < 4; ++st)
-#pragma unroll
-      for (int k = 0; k < NV; ++k) o[k] = T::mfma32(values(st, k), pf[st], o[k]);
+      for (int i = 0; i < 4 * NV; ++i) {
+        if (i + 2 < 4 * NV) read(i + 2);
+        __builtin_amdgcn_sched_barrier(0);
+        o[i % NV] = T::mfma32(vf[i % 3], pf[i / NV], o[i % NV]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
     // wait states for a read of the last results behind the loop's branch
     __builtin_amdgcn_sched_barrier(0);
     asm volatile("s_nop 15\n\ts_nop 15");
