@@ -410,12 +410,16 @@ def sd_run_plain_em(target, B, seed, y_out=None, ws=None, device="cuda"):
     return y_out
 
 
+_types = {}
+
+
 def _type(t):
-    import torch
-    types = {torch.float32: SD_TYPE_F32, torch.bfloat16: SD_TYPE_BF16, torch.float16: SD_TYPE_F16}
-    if t.dtype not in types:
+    if not _types:
+        import torch
+        _types.update({torch.float32: SD_TYPE_F32, torch.bfloat16: SD_TYPE_BF16, torch.float16: SD_TYPE_F16})
+    if t.dtype not in _types:
         raise SpecDiffError(SD_EINVAL, f"unsupported element type {t.dtype}")
-    return types[t.dtype]
+    return _types[t.dtype]
 
 
 def _need(cond, name, what):
@@ -423,22 +427,29 @@ def _need(cond, name, what):
         raise SpecDiffError(SD_EINVAL, f"{name}: {what}")
 
 
-def _operands(name, dtypes, tensors):
-    """Refuses operands that are not on the current device or not of the stated type."""
+def _operands(name, types, **tensors):
+    """Refuses operands that are not on the current device, or not of the type that `types` states.
+
+    Returns the current stream's handle."""
     import torch
-    dev = torch.cuda.current_device() if torch.cuda.is_available() else None
+    dev = torch.cuda.current_device() if next(iter(tensors.values())).is_cuda else 0
     for what, t in tensors.items():
-        if t is None:
-            continue
-        _need(t.device.type == "cuda" and t.device.index == dev, name,
-              f"{what} is on {t.device}, not on the current GPU")
-        want = dtypes.get(what)
-        _need(want is None or t.dtype == want, name, f"{what} must be {want}, not {t.dtype}")
+        if t is not None and (t.get_device() != dev or not t.is_cuda):
+            _need(False, name, f"{what} is on {t.device}, not on the current GPU")
+    for what, want in types.items():
+        t = tensors[what]
+        if t is not None and t.dtype != want:
+            _need(False, name, f"{what} must be {want}, not {t.dtype}")
+    return torch._C._cuda_getCurrentRawStream(dev)
 
 
-def _workspace(ws, need, device):
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _workspace(need, device):
     import torch
-    return torch.empty(need, dtype=torch.uint8, device=device) if ws is None else ws
+    return torch.empty(need, dtype=torch.uint8, device=device)
 
 
 def sd_latent_attention_workspace(B, Q, H, d_latent, d_rope):
@@ -462,22 +473,24 @@ def sd_latent_attention(q, cache, lens, d_latent, pages=None, rows=None, scale=N
         out = torch.empty(B, Q, H, d_latent, dtype=q.dtype, device=q.device)
     if lse is None:
         lse = torch.empty(B, Q, H, dtype=torch.float32, device=q.device)
-    _operands(name, dict(lens=i32, pages=i32, rows=i32, out=q.dtype, lse=torch.float32, ws=torch.uint8),
-              dict(q=q, cache=cache, lens=lens, pages=pages, rows=rows, out=out, lse=lse, ws=ws))
-    _need(tuple(lens.shape) == (B,) and lens.is_contiguous(), name, "lens must be contiguous [B]")
-    _need(rows is None or (tuple(rows.shape) == (B,) and rows.is_contiguous()), name, "rows must be contiguous [B]")
+    stream = _operands(name, dict(lens=i32, pages=i32, rows=i32, out=q.dtype, lse=torch.float32, ws=torch.uint8),
+                       q=q, cache=cache, lens=lens, pages=pages, rows=rows, out=out, lse=lse, ws=ws)
+    _need(lens.shape == (B,) and lens.is_contiguous(), name, "lens must be contiguous [B]")
+    _need(rows is None or (rows.shape == (B,) and rows.is_contiguous()), name, "rows must be contiguous [B]")
     _need(pages is None or (pages.dim() == 2 and pages.shape[0] == B and pages.stride(1) == 1), name,
           "pages must be [B][max_pages] with contiguous rows")
-    _need(tuple(out.shape) == (B, Q, H, d_latent) and out.stride(3) == 1, name, "out must be [B][Q][H][d_latent]")
-    _need(tuple(lse.shape) == (B, Q, H) and lse.is_contiguous(), name, "lse must be contiguous [B][Q][H]")
-    ws = _workspace(ws, sd_latent_attention_workspace(B, Q, H, d_latent, d - d_latent), q.device)
+    _need(out.shape == (B, Q, H, d_latent) and out.stride(3) == 1, name, "out must be [B][Q][H][d_latent]")
+    _need(lse.shape == (B, Q, H) and lse.is_contiguous(), name, "lse must be contiguous [B][Q][H]")
+    if ws is None:
+        ws = _workspace(sd_latent_attention_workspace(B, Q, H, d_latent, d - d_latent), q.device)
     _check(load().sd_latent_attention(B, Q, H, d_latent, d - d_latent, _type(q),
-                                      d ** -0.5 if scale is None else float(scale), _p(q),
-                                      sd_stride_h(*q.stride()[:3]), _p(cache), cache.stride(0), cache.stride(1),
-                                      cache.shape[0], cache.shape[1], _p(pages),
+                                      d ** -0.5 if scale is None else float(scale), q.data_ptr(),
+                                      sd_stride_h(*q.stride()[:3]), cache.data_ptr(), cache.stride(0), cache.stride(1),
+                                      cache.shape[0], cache.shape[1], _ptr(pages),
                                       0 if pages is None else pages.stride(0),
-                                      0 if pages is None else pages.shape[1], _p(lens), _p(rows), _p(out),
-                                      sd_stride_h(*out.stride()[:3]), _p(lse), _p(ws), ws.numel(), _stream()), name)
+                                      0 if pages is None else pages.shape[1], lens.data_ptr(), _ptr(rows),
+                                      out.data_ptr(), sd_stride_h(*out.stride()[:3]), lse.data_ptr(), ws.data_ptr(),
+                                      ws.numel(), stream), name)
     return out, lse
 
 
@@ -508,22 +521,22 @@ def sd_latent_attention_expanded(q, k, k_rope, v, cu_q, cu_k, scale=None, out=No
         out = torch.empty(Tq, H, dv, dtype=q.dtype, device=q.device)
     if lse is None:
         lse = torch.empty(Tq, H, dtype=torch.float32, device=q.device)
-    _operands(name, dict(cu_q=i32, cu_k=i32, out=q.dtype, lse=torch.float32, ws=torch.uint8),
-              dict(q=q, k=k, k_rope=k_rope, v=v, cu_q=cu_q, cu_k=cu_k, out=out, lse=lse, ws=ws))
+    stream = _operands(name, dict(cu_q=i32, cu_k=i32, out=q.dtype, lse=torch.float32, ws=torch.uint8),
+                       q=q, k=k, k_rope=k_rope, v=v, cu_q=cu_q, cu_k=cu_k, out=out, lse=lse, ws=ws)
     n = cu_q.numel() - 1
-    _need(cu_q.dim() == 1 and tuple(cu_k.shape) == (n + 1,) and cu_q.is_contiguous() and cu_k.is_contiguous(), name,
+    _need(cu_q.dim() == 1 and cu_k.shape == (n + 1,) and cu_q.is_contiguous() and cu_k.is_contiguous(), name,
           "cu_q and cu_k must be contiguous [n + 1]")
-    _need(tuple(out.shape) == (Tq, H, dv) and out.stride(2) == 1, name, "out must be [Tq][H][d_v]")
-    _need(tuple(lse.shape) == (Tq, H) and lse.is_contiguous(), name, "lse must be contiguous [Tq][H]")
-    need = sd_latent_attention_expanded_workspace(n, H, dn, dr, dv, Tq, Tk)
-    if need > 0:
-        ws = _workspace(ws, need, q.device)
-    strides = [sd_stride_h(0, x.stride(0), x.stride(1)) for x in (q, k, v, out)]
+    _need(out.shape == (Tq, H, dv) and out.stride(2) == 1, name, "out must be [Tq][H][d_v]")
+    _need(lse.shape == (Tq, H) and lse.is_contiguous(), name, "lse must be contiguous [Tq][H]")
+    if ws is None:
+        need = sd_latent_attention_expanded_workspace(n, H, dn, dr, dv, Tq, Tk)
+        ws = _workspace(need, q.device) if need > 0 else None
+    strides = [sd_stride_h(0, *x.stride()[:2]) for x in (q, k, v, out)]
     _check(load().sd_latent_attention_expanded(n, H, dn, dr, dv, _type(q), d ** -0.5 if scale is None else float(scale),
-                                               Tq, _p(q), strides[0], Tk, _p(k), strides[1], _p(k_rope),
-                                               k_rope.stride(0) if k_rope is not None else 0, _p(v), strides[2],
-                                               _p(cu_q), _p(cu_k), _p(out), strides[3], _p(lse), _p(ws),
-                                               ws.numel() if ws is not None else 0, _stream()), name)
+                                               Tq, q.data_ptr(), strides[0], Tk, k.data_ptr(), strides[1], _ptr(k_rope),
+                                               k_rope.stride(0) if k_rope is not None else 0, v.data_ptr(), strides[2],
+                                               cu_q.data_ptr(), cu_k.data_ptr(), out.data_ptr(), strides[3],
+                                               lse.data_ptr(), _ptr(ws), ws.numel() if ws is not None else 0, stream), name)
     return out, lse
 
 
@@ -541,24 +554,26 @@ def sd_token_logprobs(logits, tokens=None, n_top=0, temperature=1.0, ws=None):
     name, i32 = "sd_token_logprobs", torch.int32
     _need(logits.dim() == 2 and (logits.stride(1) == 1 or logits.shape[1] == 1), name, "logits must be [rows][V] with contiguous rows")
     rows, V = logits.shape
-    _operands(name, dict(tokens=i32, ws=torch.uint8), dict(logits=logits, tokens=tokens, ws=ws))
+    stream = _operands(name, dict(tokens=i32, ws=torch.uint8), logits=logits, tokens=tokens, ws=ws)
     n_tok = 0
     if tokens is not None:
         _need(tokens.dim() in (1, 2) and tokens.shape[0] == rows and tokens.is_contiguous(), name,
               "tokens must be contiguous [rows] or [rows][n_tok]")
         n_tok = 1 if tokens.dim() == 1 else tokens.shape[1]
-    f32 = dict(dtype=torch.float32, device=logits.device)
-    out = dict(lse=torch.empty(rows, **f32), entropy=torch.empty(rows, **f32))
+    f32, dev = torch.float32, logits.device
+    lse, entropy = torch.empty(rows, dtype=f32, device=dev), torch.empty(rows, dtype=f32, device=dev)
+    logprob = ids = tops = None
+    out = dict(lse=lse, entropy=entropy)
     if tokens is not None:
-        out["logprob"] = torch.empty(tokens.shape, **f32)
+        out["logprob"] = logprob = torch.empty(tokens.shape, dtype=f32, device=dev)
     if n_top > 0:
-        out["top_ids"] = torch.empty(rows, n_top, dtype=i32, device=logits.device)
-        out["top_logprobs"] = torch.empty(rows, n_top, **f32)
-    ws = _workspace(ws, sd_token_logprobs_workspace(rows, V, n_top), logits.device)
-    _check(load().sd_token_logprobs(rows, V, _type(logits), _p(logits), logits.stride(0) if rows > 1 else V,
-                                    float(temperature), n_tok, _p(tokens), _p(out.get("logprob")),
-                                    _p(out["entropy"]), _p(out["lse"]), n_top, _p(out.get("top_ids")),
-                                    _p(out.get("top_logprobs")), _p(ws), ws.numel(), _stream()), name)
+        out["top_ids"] = ids = torch.empty(rows, n_top, dtype=i32, device=dev)
+        out["top_logprobs"] = tops = torch.empty(rows, n_top, dtype=f32, device=dev)
+    if ws is None:
+        ws = _workspace(sd_token_logprobs_workspace(rows, V, n_top), dev)
+    _check(load().sd_token_logprobs(rows, V, _type(logits), logits.data_ptr(), logits.stride(0) if rows > 1 else V,
+                                    float(temperature), n_tok, _ptr(tokens), _ptr(logprob), entropy.data_ptr(),
+                                    lse.data_ptr(), n_top, _ptr(ids), _ptr(tops), ws.data_ptr(), ws.numel(), stream), name)
     return out
 
 
@@ -578,26 +593,34 @@ def sd_verify_tokens(draft, target, tokens, kb, uniforms=None, rnd=None, seed=0,
     name, i32, f32 = "sd_verify_tokens", torch.int32, torch.float32
     _need(draft.dim() == 3 and target.dim() == 3, name, "draft and target must be [B][K][V] and [B][K+1][V]")
     B, K, V = draft.shape
-    _need(tuple(target.shape) == (B, K + 1, V), name, "target must be [B][K+1][V]")
+    _need(target.shape == (B, K + 1, V), name, "target must be [B][K+1][V]")
     _need(draft.dtype == target.dtype, name, "draft and target must be of one type")
-    _operands(name, dict(tokens=i32, kb=i32, uniforms=torch.float64, ws=torch.uint8),
-              dict(draft=draft, target=target, tokens=tokens, kb=kb, uniforms=uniforms, rnd=rnd, ws=ws))
-    _need(tuple(tokens.shape) == (B, K) and tokens.is_contiguous(), name, "tokens must be contiguous [B][K]")
-    _need(tuple(kb.shape) == (B,) and kb.is_contiguous(), name, "kb must be contiguous [B]")
-    _need(uniforms is None or (tuple(uniforms.shape) == (B, K + 1) and uniforms.is_contiguous()), name,
+    stream = _operands(name, dict(tokens=i32, kb=i32, uniforms=torch.float64, ws=torch.uint8),
+                       draft=draft, target=target, tokens=tokens, kb=kb, uniforms=uniforms, rnd=rnd, ws=ws)
+    _need(tokens.shape == (B, K) and tokens.is_contiguous(), name, "tokens must be contiguous [B][K]")
+    _need(kb.shape == (B,) and kb.is_contiguous(), name, "kb must be contiguous [B]")
+    _need(uniforms is None or (uniforms.shape == (B, K + 1) and uniforms.is_contiguous()), name,
           "uniforms must be contiguous [B][K+1]")
-    _need(rnd is None or (tuple(rnd.shape) == (B,) and rnd.element_size() == 4 and rnd.is_contiguous()), name,
+    _need(rnd is None or (rnd.shape == (B,) and rnd.element_size() == 4 and rnd.is_contiguous()), name,
           "rnd must be contiguous [B] of 32 bits")
     if out is None:
-        out = dict(tau=torch.empty(B, dtype=i32, device=draft.device), token=torch.empty(B, dtype=i32, device=draft.device),
-                   log_alpha_res=torch.empty(B, dtype=f32, device=draft.device),
-                   log_ratio=torch.empty(B, K, dtype=f32, device=draft.device),
-                   coins=torch.empty(B, dtype=torch.int64, device=draft.device))
-    ws = _workspace(ws, sd_verify_tokens_workspace(B, K, V), draft.device)
-    _check(load().sd_verify_tokens(B, K, V, mode, _type(draft), float(temperature), _p(draft), stride3(draft),
-                                   _p(target), stride3(target), _p(tokens), _p(kb), _p(uniforms), _p(rnd), seed,
-                                   _p(out["tau"]), _p(out["token"]), _p(out["log_alpha_res"]), _p(out["log_ratio"]),
-                                   _p(out.get("coins")), _p(ws), ws.numel(), _stream()), name)
+        dev = draft.device
+        out = dict(tau=torch.empty(B, dtype=i32, device=dev), token=torch.empty(B, dtype=i32, device=dev),
+                   log_alpha_res=torch.empty(B, dtype=f32, device=dev), log_ratio=torch.empty(B, K, dtype=f32, device=dev),
+                   coins=torch.empty(B, dtype=torch.int64, device=dev))
+    else:
+        _operands(name, dict(tau=i32, token=i32, log_alpha_res=f32, log_ratio=f32, coins=torch.int64),
+                  **{k: out.get(k) for k in ("tau", "token", "log_alpha_res", "log_ratio", "coins")})
+        for k, o in out.items():
+            _need(o is None or (o.shape == ((B, K) if k == "log_ratio" else (B,)) and o.is_contiguous()), name,
+                  f"{k} must be contiguous [B][K]" if k == "log_ratio" else f"{k} must be contiguous [B]")
+    if ws is None:
+        ws = _workspace(sd_verify_tokens_workspace(B, K, V), draft.device)
+    _check(load().sd_verify_tokens(B, K, V, mode, _type(draft), float(temperature), draft.data_ptr(), stride3(draft),
+                                   target.data_ptr(), stride3(target), tokens.data_ptr(), kb.data_ptr(), _ptr(uniforms),
+                                   _ptr(rnd), seed, out["tau"].data_ptr(), out["token"].data_ptr(),
+                                   out["log_alpha_res"].data_ptr(), out["log_ratio"].data_ptr(), _ptr(out.get("coins")),
+                                   ws.data_ptr(), ws.numel(), stream), name)
     return out
 
 
