@@ -77,38 +77,45 @@ __device__ __forceinline__ u32x4 funnel(u32x4 lo, u32x4 hi, int words, bool half
   return u32x4{v[0], v[1], v[2], v[3]};
 }
 
-// Slice `slice`, as position() counts it with the lead a, of the row p[0..V):
-// x[i] is the element at position(i), -inf outside the row.  A row whose own lead
-// is another (the second of a pair) is read in its aligned vectors, two for each
-// vector of positions, and shifted.
+// Vector k of this thread in slice `slice`, as position() counts it with the lead a, of
+// the row p[0..V): its bits, -inf's outside the row.  A row whose own lead is another (the
+// second of a pair) is read in its aligned vectors, two for each vector of positions, and
+// shifted.
 // STREAM: rows that no later kernel reads pass by the caches.
+template <class T>
+union Vec {
+  u32x4 v;
+  typename T::raw r[T::kVec];
+};
+template <class T, int E, bool STREAM = false>
+__device__ __forceinline__ Vec<T> load_vector(const typename T::raw* __restrict__ p, int a, int V, int slice, int k) {
+  constexpr int VEC = T::kVec;
+  const int off = (lead<T>(p) - a) & (VEC - 1);  // elements from an aligned vector to a vector of positions
+  const int e0 = position<T, E>(slice, a, k * VEC);
+  Vec<T> w;
+  if (off == 0 && e0 >= 0 && e0 + VEC <= V) {
+    const u32x4* q = reinterpret_cast<const u32x4*>(p + e0);
+    w.v = STREAM ? __builtin_nontemporal_load(q) : *q;
+  } else if (off != 0 && e0 - off >= 0 && e0 - off + 2 * VEC <= V) {
+    const u32x4* q = reinterpret_cast<const u32x4*>(p + (e0 - off));
+    w.v = funnel(q[0], q[1], off * (int)sizeof(w.r[0]) >> 2, sizeof(w.r[0]) == 2 && (off & 1));
+  } else {
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) {
+      w.r[j] = T::kNone;
+      if (e0 + j >= 0 && e0 + j < V) w.r[j] = p[e0 + j];
+    }
+  }
+  return w;
+}
+// The slice's elements of this thread: x[i] is the one at position(i).
 template <class T, int E, bool STREAM = false>
 __device__ __forceinline__ void load_slice(const typename T::raw* __restrict__ p, int a, int V, int slice,
                                            float (&x)[E]) {
-  typedef typename T::raw raw;
   constexpr int VEC = T::kVec, NV = E / VEC;
-  const int off = (lead<T>(p) - a) & (VEC - 1);  // elements from an aligned vector to a vector of positions
-  union Vec {
-    u32x4 v;
-    raw r[VEC];
-  } w[NV];
+  Vec<T> w[NV];
 #pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    const int e0 = position<T, E>(slice, a, k * VEC);
-    if (off == 0 && e0 >= 0 && e0 + VEC <= V) {
-      const u32x4* q = reinterpret_cast<const u32x4*>(p + e0);
-      w[k].v = STREAM ? __builtin_nontemporal_load(q) : *q;
-    } else if (off != 0 && e0 - off >= 0 && e0 - off + 2 * VEC <= V) {
-      const u32x4* q = reinterpret_cast<const u32x4*>(p + (e0 - off));
-      w[k].v = funnel(q[0], q[1], off * (int)sizeof(raw) >> 2, sizeof(raw) == 2 && (off & 1));
-    } else {
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        w[k].r[j] = T::kNone;
-        if (e0 + j >= 0 && e0 + j < V) w[k].r[j] = p[e0 + j];
-      }
-    }
-  }
+  for (int k = 0; k < NV; ++k) w[k] = load_vector<T, E, STREAM>(p, a, V, slice, k);
 #pragma unroll
   for (int k = 0; k < NV; ++k)
 #pragma unroll

@@ -43,7 +43,7 @@ __device__ __forceinline__ float key_value(uint64_t k) {
   return __builtin_bit_cast(float, o ^ ((uint32_t)((int32_t)~o >> 31) | 0x80000000u));
 }
 template <int CTRL>
-__device__ __forceinline__ uint64_t dpp(uint64_t v) {
+__device__ __forceinline__ uint64_t dpp64(uint64_t v) {
   return ((uint64_t)dpp32<CTRL>((uint32_t)(v >> 32)) << 32) | dpp32<CTRL>((uint32_t)v);
 }
 __device__ __forceinline__ uint64_t max64(uint64_t a, uint64_t b) { return a > b ? a : b; }
@@ -52,19 +52,33 @@ __device__ __forceinline__ uint64_t lane_key(uint64_t v, int i) {
          (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, i);
 }
 __device__ __forceinline__ uint64_t wave_max(uint64_t v) {
-  v = max64(v, dpp<kDppXor1>(v));
-  v = max64(v, dpp<kDppXor2>(v));
-  v = max64(v, dpp<kDppHalfMirror>(v));
-  v = max64(v, dpp<kDppMirror>(v));
+  v = max64(v, dpp64<kDppXor1>(v));
+  v = max64(v, dpp64<kDppXor2>(v));
+  v = max64(v, dpp64<kDppHalfMirror>(v));
+  v = max64(v, dpp64<kDppMirror>(v));
   v = max64(v, (uint64_t)__shfl_xor((unsigned long long)v, 16));
   return max64(v, (uint64_t)__shfl_xor((unsigned long long)v, 32));
+}
+
+__device__ __forceinline__ float wave_max(float v) {
+  v = fmaxf(v, dpp<kDppXor1>(v));
+  v = fmaxf(v, dpp<kDppXor2>(v));
+  v = fmaxf(v, dpp<kDppHalfMirror>(v));
+  v = fmaxf(v, dpp<kDppMirror>(v));
+  uint32_t a = __builtin_bit_cast(uint32_t, v), b = a;
+  swap16(a, b);
+  a = b = __builtin_bit_cast(uint32_t, fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b)));
+  swap32(a, b);
+  return fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
 }
 
 constexpr int kPool = 1024;  // candidates a workgroup orders at once
 struct TopLds {
   uint64_t group[64];
+  float groupf[64];
   uint64_t pool[kPool];
   uint64_t bound;
+  float boundf;
   int count;
 };
 
@@ -80,28 +94,67 @@ __device__ __forceinline__ void write_ranked(const uint64_t* pool, int c, int n,
   for (int i = c + (int)threadIdx.x; i < n; i += kThreads) out[i] = 0;
 }
 
-// The n largest of the slice x to out[0..n) in falling order, 0 past its elements.
-// The largest keys of 64 groups of four threads give a bound: n groups hold a key
-// at or above the n-th largest of them, so the n largest elements are among those
-// not below it, which are few.  Where they do not fit the pool (an order made for
-// it) the n largest are taken one after another.
+// The n largest of the slice x to out[0..n) in falling order, 0 past its elements; best[k] is
+// the largest of vector k of this thread.  The largest values of 64 groups of four threads give a
+// bound: n groups hold one at or above the n-th largest of them, so the n largest elements
+// are among those not below it, which are few: most wavefronts find no candidate in a
+// compare or two an element.  Where equal values overflow the pool (few values that are
+// not -inf, a constant row) the groups' largest keys give the bound, which no two
+// elements share, and where that overflows it too (an order made for it) the n largest
+// are taken one after another.
 template <class T, int E>
-__device__ void slice_top(const float (&x)[E], int slice, int a, int V, int n, TopLds& sm, uint64_t* out) {
+__device__ __forceinline__ void slice_top(const float (&x)[E], const float (&best)[E / T::kVec], int slice, int a, int V, int n, TopLds& sm,
+                                          uint64_t* out) {
   const int t = threadIdx.x;
-  float best = x[0];
+  float g = best[0];
 #pragma unroll
-  for (int i = 1; i < E; ++i) best = fmaxf(best, x[i]);
-  int bi = 0;
+  for (int k = 1; k < E / T::kVec; ++k) g = fmaxf(g, best[k]);
+  g = fmaxf(g, dpp<kDppXor1>(g));
+  g = fmaxf(g, dpp<kDppXor2>(g));
+  if ((t & 3) == 0) sm.groupf[t >> 2] = g;
+  if (t == 0) sm.count = 0;
+  __syncthreads();
+  if (t < 64) {
+    const float k = sm.groupf[t];
+    int from = 0;  // groups not below this one
 #pragma unroll
-  for (int i = E - 1; i >= 0; --i) {
-    const int pos = position<T, E>(slice, a, i);
-    if (x[i] == best && pos >= 0) bi = i;
+    for (int i = 0; i < 64; ++i)
+      from += __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, k), i)) >= k;
+    const float b = wave_max(from >= n ? k : -INFINITY);
+    if (t == 0) sm.boundf = b;
   }
-  const int bpos = position<T, E>(slice, a, bi);
-  const uint64_t mine = bpos >= 0 && bpos < V ? key_of(best, bpos) : 0;
-  uint64_t g = max64(mine, dpp<kDppXor1>(mine));
-  g = max64(g, dpp<kDppXor2>(g));
-  if ((t & 3) == 0) sm.group[t >> 2] = g;
+  __syncthreads();
+  const float boundf = sm.boundf;
+  if (boundf > -INFINITY) {
+#pragma unroll
+    for (int k = 0; k < E / T::kVec; ++k)
+      if (__any(best[k] >= boundf))
+#pragma unroll
+        for (int i = k * T::kVec; i < (k + 1) * T::kVec; ++i) {
+          if (!__any(x[i] >= boundf)) continue;
+          const int pos = position<T, E>(slice, a, i);
+          if (x[i] >= boundf && pos >= 0 && pos < V) {
+            const int c = atomicAdd(&sm.count, 1);
+            if (c < kPool) sm.pool[c] = key_of(x[i], pos);
+          }
+        }
+    __syncthreads();
+    const int c = sm.count;
+    if (c <= kPool) {
+      write_ranked(sm.pool, c, n, out);
+      return;
+    }
+  }
+  uint64_t mine = 0;
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    const int pos = position<T, E>(slice, a, i);
+    if (pos >= 0 && pos < V) mine = max64(mine, key_of(x[i], pos));
+  }
+  uint64_t gk = max64(mine, dpp64<kDppXor1>(mine));
+  gk = max64(gk, dpp64<kDppXor2>(gk));
+  __syncthreads();
+  if ((t & 3) == 0) sm.group[t >> 2] = gk;
   if (t == 0) sm.count = 0;
   __syncthreads();
   if (t < 64) {
@@ -152,14 +205,21 @@ __device__ void slice_top(const float (&x)[E], int slice, int a, int V, int n, T
 }
 
 // ------------------------------------------------------------------- sums --
-// Sums of a workgroup's slice: m its maximum, S and (ENT) U.
+// Sums of a workgroup's slice: m its maximum, S and (ENT) U; best[k] the largest of vector k of this thread.
 template <class T, int E, bool ENT>
-__device__ __forceinline__ Part slice_sums(const float (&x)[E], float c, double* red, float* redm) {
+__device__ __forceinline__ Part slice_sums(const float (&x)[E], float c, double* red, float* redm,
+                                           float (&best)[E / T::kVec]) {
   const int t = threadIdx.x, w = t >> 6;
-  float m = x[0];
+  constexpr int NV = E / T::kVec;
+  float m = -INFINITY;
 #pragma unroll
-  for (int i = 1; i < E; ++i) m = fmaxf(m, x[i]);
-  m = (float)group_max((double)m, 64);
+  for (int k = 0; k < NV; ++k) {
+    best[k] = x[k * T::kVec];
+#pragma unroll
+    for (int j = 1; j < T::kVec; ++j) best[k] = fmaxf(best[k], x[k * T::kVec + j]);
+    m = fmaxf(m, best[k]);
+  }
+  m = wave_max(m);
   if ((t & 63) == 0) redm[w] = m;
   __syncthreads();
   m = fmaxf(fmaxf(redm[0], redm[1]), fmaxf(redm[2], redm[3]));
@@ -172,13 +232,10 @@ __device__ __forceinline__ Part slice_sums(const float (&x)[E], float c, double*
     s[i & 3] += e;
     if (ENT) u[i & 3] = __fmaf_rn(e, fmaxf(d, kLowest), u[i & 3]);
   }
-  const double S = wave_sum((double)s[0] + s[1] + ((double)s[2] + s[3]));
-  double U = 0.0;
-  if (ENT) U = wave_sum((double)u[0] + u[1] + ((double)u[2] + u[3]));
-  if ((t & 63) == 0) {
-    red[w] = S;
-    if (ENT) red[4 + w] = U;
-  }
+  const double S = (double)s[0] + s[1] + ((double)s[2] + s[3]), U = (double)u[0] + u[1] + ((double)u[2] + u[3]);
+  // with U the lower lanes add up the one, the upper lanes the other
+  const double v = ENT ? group_sum(swap_add<true>(S, U), 32) : wave_sum(S);
+  if ((t & 31) == 0 && (ENT || (t & 63) == 0)) red[(t & 32) / 8 + w] = v;
   __syncthreads();
   Part p;
   p.S = red[0] + red[1] + (red[2] + red[3]);
@@ -189,7 +246,7 @@ __device__ __forceinline__ Part slice_sums(const float (&x)[E], float c, double*
 }
 
 template <class T, int E>
-__global__ __launch_bounds__(kThreads) void logprobs_slice_kernel(const typename T::raw* __restrict__ x, int64_t ld,
+__global__ __launch_bounds__(kThreads, 4) void logprobs_slice_kernel(const typename T::raw* __restrict__ x, int64_t ld,
                                                                   int V, int S, float c, int n,
                                                                   Part* __restrict__ parts,
                                                                   uint64_t* __restrict__ keys) {
@@ -200,11 +257,11 @@ __global__ __launch_bounds__(kThreads) void logprobs_slice_kernel(const typename
   const int slice = (int)(id % S);
   const typename T::raw* p = x + (id / S) * ld;
   const int a = lead<T>(p);
-  float v[E];
+  float v[E], best[E / T::kVec];
   load_slice<T, E, true>(p, a, V, slice, v);
-  const Part r = slice_sums<T, E, true>(v, c, red, redm);
+  const Part r = slice_sums<T, E, true>(v, c, red, redm, best);
   if (threadIdx.x == 0) parts[id] = r;
-  if (n > 0) slice_top<T, E>(v, slice, a, V, n, top, keys + id * n);
+  if (n > 0) slice_top<T, E>(v, best, slice, a, V, n, top, keys + id * n);
 }
 
 // One workgroup a row: the slices' sums, the given tokens and the alternatives.
@@ -223,7 +280,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_join_kernel(
   const Part* p = parts + row * S;
   float m = -INFINITY;
   for (int i = t; i < S; i += kThreads) m = fmaxf(m, p[i].m);
-  m = (float)group_max((double)m, 64);
+  m = wave_max(m);
   if ((t & 63) == 0) redm[w] = m;
   __syncthreads();
   m = fmaxf(fmaxf(redm[0], redm[1]), fmaxf(redm[2], redm[3]));
@@ -349,9 +406,9 @@ __global__ __launch_bounds__(kThreads) void verify_sums_kernel(Rows rows, int K,
   const int n = drafts(kb, b, K);
   if (n == 0 || (i <= K ? i > n : i - K - 1 >= n)) return;
   const typename T::raw* p = row_of<T>(rows, b, i, K);
-  float v[E];
+  float v[E], best[E / T::kVec];
   load_slice<T, E>(p, lead<T>(p), V, slice, v);
-  const Part q = slice_sums<T, E, false>(v, c, red, redm);
+  const Part q = slice_sums<T, E, false>(v, c, red, redm, best);
   if (threadIdx.x == 0) parts[id] = q;
 }
 
@@ -361,10 +418,10 @@ __device__ __forceinline__ int first_rejected(uint64_t cm, int n) {
   return rej ? __ffsll((unsigned long long)rej) : n + 1;
 }
 
-// One wavefront a chain: the rows' laws, the log-ratios, log alpha_j; with token
-// verification also the decision.
+// One workgroup a chain: the rows' laws (16 lanes a row), the log-ratios, log alpha_j; with
+// token verification also the decision.
 template <class T>
-__global__ __launch_bounds__(64) void verify_join_kernel(Rows rows, int K, int V, int S, int mode, double inv_t,
+__global__ __launch_bounds__(kThreads) void verify_join_kernel(Rows rows, int K, int V, int S, int mode, double inv_t,
                                                          const int32_t* __restrict__ tokens,
                                                          const int32_t* __restrict__ kb,
                                                          const double* __restrict__ uniforms,
@@ -373,32 +430,46 @@ __global__ __launch_bounds__(64) void verify_join_kernel(Rows rows, int K, int V
                                                          double* __restrict__ la, int32_t* __restrict__ tau,
                                                          float* __restrict__ lar, float* __restrict__ ratio,
                                                          uint64_t* __restrict__ coins) {
-  const int b = blockIdx.x, lane = threadIdx.x;
+  __shared__ Law law[2 * SD_MAX_BLOCK + 1];
+  const int b = blockIdx.x, t = threadIdx.x, lane = t, in = t & 15;
   const int n = drafts(kb, b, K);
-  double qx = NAN, px = NAN;  // log q_j(x_j), log p_j(x_j) of draft j = lane + 1
+  // the draft's two logits are on their way while the rows' sums are joined
   const int tok = lane < n ? tokens[(int64_t)b * K + lane] : -1;
   const bool known = tok >= 0 && tok < V;
-  for (int i = lane; i < 2 * K + 1; i += 64) {
-    const int j = i <= K ? i : i - K - 1;
-    if (n == 0 || (i <= K ? j > n : j >= n)) continue;
-    const Part* p = parts + ((int64_t)b * (2 * K + 1) + i) * S;
-    float m = -INFINITY;
-    for (int s = 0; s < S; ++s) m = fmaxf(m, p[s].m);
-    double sum = 0.0;
-    for (int s = 0; s < S; ++s)
-      if (!(p[s].m == -INFINITY && p[s].S == 0.0)) sum += p[s].S * exp(((double)p[s].m - (double)m) * inv_t);
-    laws[(int64_t)b * (2 * K + 1) + i] = Law{sum, log(sum), m, 0.f};
+  float xq = -INFINITY, xp = -INFINITY;
+  if (known) {
+    xq = T::value(row_of<T>(rows, b, lane, K)[tok]);
+    xp = T::value(row_of<T>(rows, b, K + 1 + lane, K)[tok]);
   }
+  if (n > 0)
+    for (int i = t >> 4; i < 2 * K + 1; i += kThreads / 16) {
+      if (i <= K ? i > n : i - K - 1 >= n) continue;
+      const Part* p = parts + ((int64_t)b * (2 * K + 1) + i) * S;
+      float m = -INFINITY;
+      for (int s = in; s < S; s += 16) m = fmaxf(m, p[s].m);
+      m = (float)group_max((double)m, 16);
+      double sum = 0.0;
+      for (int s = in; s < S; s += 16) {
+        const Part q = p[s];
+        if (!(q.m == -INFINITY && q.S == 0.0)) sum += q.S * exp(((double)q.m - (double)m) * inv_t);
+      }
+      sum = group_sum(sum, 16);
+      if (in == 0) {
+        law[i] = Law{sum, log(sum), m, 0.f};
+        laws[(int64_t)b * (2 * K + 1) + i] = law[i];
+      }
+    }
   __syncthreads();
+  if (t >= 64) return;
+  double qx = NAN, px = NAN;  // log q_j(x_j), log p_j(x_j) of draft j = lane + 1
   if (lane < n) {
-    const Law q = laws[(int64_t)b * (2 * K + 1) + lane], p = laws[(int64_t)b * (2 * K + 1) + K + 1 + lane];
-    auto logp = [&](const Law& l, const typename T::raw* row) {
+    auto logp = [&](const Law& l, float x) {
       if (l.S == 0.0) return -(double)INFINITY;
       if (!(l.S > 0.0) || !isfinite(l.S)) return (double)NAN;
-      return known ? ((double)T::value(row[tok]) - (double)l.m) * inv_t - l.logS : -(double)INFINITY;
+      return known ? ((double)x - (double)l.m) * inv_t - l.logS : -(double)INFINITY;
     };
-    qx = logp(q, row_of<T>(rows, b, lane, K));
-    px = logp(p, row_of<T>(rows, b, K + 1 + lane, K));
+    qx = logp(law[lane], xq);
+    px = logp(law[K + 1 + lane], xp);
   }
   // log_ratio: -inf where q has nothing for the draft, whatever p has
   const double ell = qx == -(double)INFINITY && px == px ? -(double)INFINITY : qx - px;
@@ -440,7 +511,8 @@ __global__ __launch_bounds__(kThreads) void verify_excess_kernel(Rows rows, int 
                                                                  const double* __restrict__ la,
                                                                  double* __restrict__ excess) {
   __shared__ double red[4];
-  const int64_t id = blockIdx.x;
+  // from the last chain on: what the sums have read last is in the caches still
+  const int64_t id = gridDim.x - 1 - blockIdx.x;
   const int slice = (int)(id % S), r = (int)(id / S), b = r / (K - 1), j = r % (K - 1) + 1;
   if (j >= drafts(kb, b, K)) return;
   const Law q = laws[(int64_t)b * (2 * K + 1) + j], p = laws[(int64_t)b * (2 * K + 1) + K + 1 + j];
@@ -467,43 +539,50 @@ __global__ __launch_bounds__(kThreads) void verify_excess_kernel(Rows rows, int 
   if (threadIdx.x == 0) excess[((int64_t)b * K + j) * S + slice] = red[0] + red[1] + (red[2] + red[3]);
 }
 
-// One wavefront a chain: block verification's coins and tau.
-__global__ __launch_bounds__(64) void verify_decide_kernel(int K, int S, const int32_t* __restrict__ kb,
-                                                           const double* __restrict__ uniforms,
-                                                           const uint32_t* __restrict__ round, uint64_t seed,
-                                                           const double* __restrict__ la,
-                                                           const double* __restrict__ excess,
-                                                           int32_t* __restrict__ tau, float* __restrict__ lar,
-                                                           uint64_t* __restrict__ coins) {
-  const int b = blockIdx.x, lane = threadIdx.x;
-  const int n = drafts(kb, b, K);
-  if (n == 0) return;  // verify_join_kernel has written its outputs
-  double l = 0.0, h = 0.0, eta = 2.0;
-  if (lane < n) {
-    l = la[(int64_t)b * K + lane];
-    if (lane + 1 < n) {
-      double v = 0.0;
-      const double* e = excess + ((int64_t)b * K + lane + 1) * S;
-      for (int s = 0; s < S; ++s) v += e[s];
-      h = l >= 0.0 ? 1.0 : v / (v - expm1(l));
-    } else {
-      h = exp(l);
+// Block verification's coins and tau of a chain with n > 0 drafts, by the whole workgroup: 16
+// lanes add up the slices of a v_j.  The same bits in every workgroup that asks; `write`
+// says which one puts them out.
+__device__ __forceinline__ int decide(int b, int n, int K, int S, const double* __restrict__ uniforms,
+                                      const uint32_t* __restrict__ round, uint64_t seed, const double* __restrict__ la,
+                                      const double* __restrict__ excess, bool write, int32_t* __restrict__ tau,
+                                      float* __restrict__ lar, uint64_t* __restrict__ coins) {
+  __shared__ double vs[SD_MAX_BLOCK];
+  __shared__ int tau_s;
+  const int t = threadIdx.x, lane = t, in = t & 15;
+  for (int j = 1 + (t >> 4); j < n; j += kThreads / 16) {
+    const double* e = excess + ((int64_t)b * K + j) * S;
+    double v = 0.0;
+    for (int s = in; s < S; s += 16) v += e[s];
+    v = group_sum(v, 16);
+    if (in == 0) vs[j] = v;
+  }
+  __syncthreads();
+  if (t < 64) {
+    double l = 0.0, h = 0.0, eta = 2.0;
+    if (lane < n) {
+      l = la[(int64_t)b * K + lane];
+      h = lane + 1 == n ? exp(l) : l >= 0.0 ? 1.0 : vs[lane + 1] / (vs[lane + 1] - expm1(l));
+      if (uniforms) {
+        eta = uniforms[(int64_t)b * (K + 1) + lane];
+      } else {
+        const uint4 w = philox((uint32_t)(lane >> 2), (uint32_t)b, round[b], TAG_COIN << 24, seed);
+        eta = uniform64(pick(w, lane & 3));
+      }
     }
-    if (uniforms) {
-      eta = uniforms[(int64_t)b * (K + 1) + lane];
-    } else {
-      const uint4 w = philox((uint32_t)(lane >> 2), (uint32_t)b, round[b], TAG_COIN << 24, seed);
-      eta = uniform64(pick(w, lane & 3));
+    const uint64_t cm = __ballot(lane < n && eta < h);
+    const int at = cm ? 65 - __clzll((long long)cm) : 1;
+    const double res = at >= 2 ? __shfl(l, at - 2) : 0.0;
+    if (lane == 0) {
+      tau_s = at;
+      if (write) {
+        tau[b] = at;
+        lar[b] = (float)res;
+        if (coins) coins[b] = cm;
+      }
     }
   }
-  const uint64_t cm = __ballot(lane < n && eta < h);
-  const int t = cm ? 65 - __clzll((long long)cm) : 1;
-  const double res = t >= 2 ? __shfl(l, t - 2) : 0.0;
-  if (lane == 0) {
-    tau[b] = t;
-    lar[b] = (float)res;
-    if (coins) coins[b] = cm;
-  }
+  __syncthreads();
+  return tau_s;
 }
 
 // ---------------------------------------------------------------- the draw --
@@ -524,33 +603,56 @@ __device__ __forceinline__ Pair<T> drawn_rows(const Rows& rows, int b, int K, in
   return r;
 }
 
-// e^{(x - m) / T} of one element.
-__device__ __forceinline__ double weight(float x, float m, double inv_t) {
-  return exp(((double)x - (double)m) * inv_t);
+// 2^x for x <= 0 in float64, NaN for NaN: the whole part goes to the exponent (taken from the
+// low bits of x + 1.5 2^52, which end at the units), the rest, at most a half in size, is the
+// series of e^{r log 2} to its tenth power (the next is below 3e-13 of it).  0 below 2^-1000.
+__device__ __forceinline__ double pow2(double x) {
+  constexpr double magic = 0x1.8p52, k = 0.69314718055994530942;
+  const double z = x + magic, r = x - (z - magic);
+  double c[11] = {1.0};
+#pragma unroll
+  for (int i = 1; i < 11; ++i) c[i] = c[i - 1] * (k / i);
+  double p = c[10];
+#pragma unroll
+  for (int i = 9; i >= 0; --i) p = fma(p, r, c[i]);
+  const uint64_t v = __builtin_bit_cast(uint64_t, p) + ((uint64_t)(uint32_t)__builtin_bit_cast(uint64_t, z) << 52);
+  return x < -1000.0 ? 0.0 : __builtin_bit_cast(double, v);
 }
+// e^{(x - m) / T} of one element, c = log2(e) / T.
+__device__ __forceinline__ double weight(float x, float m, double c) { return pow2(((double)x - (double)m) * c); }
 
-// Slices of the two rows' sums.
+// Slices of the two rows' sums, behind block verification's decision where there is one (excess).
 template <class T, int E>
-__global__ __launch_bounds__(kThreads) void draw_sums_kernel(Rows rows, int K, int V, int S, double inv_t,
-                                                             const int32_t* __restrict__ kb,
-                                                             const int32_t* __restrict__ tau,
-                                                             const Law* __restrict__ laws, Mass* __restrict__ sums) {
+__global__ __launch_bounds__(kThreads) void draw_sums_kernel(
+    Rows rows, int K, int V, int S, double c, const int32_t* __restrict__ kb, const double* __restrict__ uniforms,
+    const uint32_t* __restrict__ round, uint64_t seed, const Law* __restrict__ laws, const double* __restrict__ la,
+    const double* __restrict__ excess, int Se, int32_t* __restrict__ tau, float* __restrict__ lar,
+    uint64_t* __restrict__ coins, Mass* __restrict__ sums, uint32_t* __restrict__ arrived) {
   __shared__ double red[8];
   const int slice = blockIdx.x % S, b = blockIdx.x / S, t = threadIdx.x;
-  const Pair<T> r = drawn_rows<T>(rows, b, K, drafts(kb, b, K), tau[b]);
-  if (!r.any) return;
+  const int n = drafts(kb, b, K);
+  if (slice == 0 && t == 0) arrived[b] = 0;
+  if (n == 0) return;
+  const int at = excess ? decide(b, n, K, Se, uniforms, round, seed, la, excess, slice == 0, tau, lar, coins) : tau[b];
+  const Pair<T> r = drawn_rows<T>(rows, b, K, n, at);
   const int a = lead<T>(r.q);
   double s[2] = {0.0, 0.0};
+  // (loops that are not unrolled: 20 KB of float64 code that every workgroup runs through once
+  // would wait for its instructions)
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const typename T::raw* p = h ? r.p : r.q;
     if (!p) continue;
     const float m = laws[(int64_t)b * (2 * K + 1) + (h ? r.ip : r.iq)].m;
-    float x[E];
-    load_slice<T, E>(p, a, V, slice, x);
-    if (m > -INFINITY)
+    if (m == -INFINITY) continue;
+    Vec<T> x = load_vector<T, E>(p, a, V, slice, 0);
+#pragma unroll 1
+    for (int k = 0; k < E / T::kVec; ++k) {
+      const Vec<T> next = k + 1 < E / T::kVec ? load_vector<T, E>(p, a, V, slice, k + 1) : x;
 #pragma unroll
-      for (int i = 0; i < E; ++i) s[h] += weight(x[i], m, inv_t);
+      for (int j = 0; j < T::kVec; ++j) s[h] += weight(T::value(x.r[j]), m, c);
+      x = next;
+    }
   }
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
@@ -628,77 +730,102 @@ __device__ __forceinline__ Residual residual_of(const Pair<T>& r, int b, int K, 
   if (f.mp == -INFINITY) f.mp = 0.f;
   return f;
 }
-__device__ __forceinline__ double residual_weight(const Residual& f, float x, float y, double inv_t) {
-  const double w = fma(f.A, weight(x, f.mq, inv_t), -(f.B * weight(y, f.mp, inv_t)));
+__device__ __forceinline__ double residual_weight(const Residual& f, float x, float y, double c) {
+  const double w = fma(f.A, weight(x, f.mq, c), -(f.B * weight(y, f.mp, c)));
   return w > 0.0 ? w : 0.0;
 }
 
-// Slices of the residual's mass.
+// Vector k of this thread in a slice of both rows.
+template <class T>
+struct Two {
+  Vec<T> x, y;
+};
 template <class T, int E>
-__global__ __launch_bounds__(kThreads) void draw_mass_kernel(Rows rows, int K, int V, int S, int mode, double inv_t,
-                                                             const int32_t* __restrict__ kb,
-                                                             const int32_t* __restrict__ tau,
-                                                             const Law* __restrict__ laws,
-                                                             const double* __restrict__ la,
-                                                             const Mass* __restrict__ sums,
-                                                             double* __restrict__ mass) {
-  __shared__ double red[4];
-  const int slice = blockIdx.x % S, b = blockIdx.x / S;
-  const Pair<T> r = drawn_rows<T>(rows, b, K, drafts(kb, b, K), tau[b]);
-  if (!r.any) return;
-  const Residual f = residual_of<T>(r, b, K, S, mode, tau[b], laws, la, sums, red);
+__device__ __forceinline__ Two<T> load_two(const Pair<T>& r, bool with_p, int V, int slice, int k) {
   const int a = lead<T>(r.q);
-  float x[E], y[E];
-  load_slice<T, E>(r.q, a, V, slice, x);
-  if (r.p) {
-    load_slice<T, E>(r.p, a, V, slice, y);
+  Two<T> v;
+  v.x = load_vector<T, E>(r.q, a, V, slice, k);
+  v.y = with_p ? load_vector<T, E>(r.p, a, V, slice, k) : v.x;
+  return v;
+}
+// The residual's weights of such a pair; their sum.
+template <class T>
+__device__ __forceinline__ double residual_vector(const Residual& f, const Two<T>& v, bool with_p, double c,
+                                                  double (&w)[T::kVec]) {
+  double sum = 0.0;
+  if (with_p) {
+#pragma unroll
+    for (int j = 0; j < T::kVec; ++j) sum += w[j] = residual_weight(f, T::value(v.x.r[j]), T::value(v.y.r[j]), c);
   } else {
 #pragma unroll
-    for (int i = 0; i < E; ++i) y[i] = -INFINITY;
+    for (int j = 0; j < T::kVec; ++j) {
+      const double g = f.A * weight(T::value(v.x.r[j]), f.mq, c);
+      sum += w[j] = g > 0.0 ? g : 0.0;
+    }
   }
-  double s = 0.0;
-#pragma unroll
-  for (int i = 0; i < E; ++i) s += residual_weight(f, x[i], y[i], inv_t);
-  s = block_sum(s, red);
-  if (threadIdx.x == 0) mass[blockIdx.x] = s;
+  return sum;
 }
 
-// One workgroup a chain: the slice that the uniform falls into, and the token in
-// it.  Here a thread takes E elements that follow one another.
+// Slices of the residual's mass.  The workgroup of a chain that is done last finds the slice
+// that the uniform falls into, and the token in it: the sums are read in the slices' order,
+// so which one it is changes nothing.
 template <class T, int E>
-__global__ __launch_bounds__(kThreads) void draw_pick_kernel(Rows rows, int K, int V, int S, int mode, double inv_t,
-                                                             const int32_t* __restrict__ kb,
-                                                             const int32_t* __restrict__ tau,
-                                                             const double* __restrict__ uniforms,
-                                                             const uint32_t* __restrict__ round, uint64_t seed,
-                                                             const Law* __restrict__ laws,
-                                                             const double* __restrict__ la,
-                                                             const Mass* __restrict__ sums,
-                                                             const double* __restrict__ mass,
-                                                             int32_t* __restrict__ token) {
-  __shared__ double red[4];
+__global__ __launch_bounds__(kThreads) void draw_token_kernel(
+    Rows rows, int K, int V, int S, int mode, double c, const int32_t* __restrict__ kb,
+    const int32_t* __restrict__ taus, const double* __restrict__ uniforms, const uint32_t* __restrict__ round,
+    uint64_t seed, const Law* __restrict__ laws, const double* __restrict__ la, const Mass* __restrict__ sums,
+    double* __restrict__ mass, uint32_t* __restrict__ arrived, int32_t* __restrict__ token) {
+  constexpr int VEC = T::kVec, NV = E / VEC;
+  __shared__ double red[4 * NV];
   __shared__ int ired[4];
   __shared__ double before_s;
-  __shared__ int slice_s, tok_s;
-  const int b = blockIdx.x, t = threadIdx.x;
-  const Pair<T> r = drawn_rows<T>(rows, b, K, drafts(kb, b, K), tau[b]);
+  __shared__ int slice_s, tok_s, last_s;
+  const int b = blockIdx.x / S, t = threadIdx.x;
+  const int n = drafts(kb, b, K), tau = n > 0 ? taus[b] : 0;
+  const Pair<T> r = drawn_rows<T>(rows, b, K, n, tau);
   if (!r.any) {
-    if (t == 0) token[b] = -1;
+    if (blockIdx.x % S == 0 && t == 0) token[b] = -1;
     return;
   }
-  Residual f = residual_of<T>(r, b, K, S, mode, tau[b], laws, la, sums, red);
+  Two<T> two = load_two<T, E>(r, r.p != nullptr, V, blockIdx.x % S, 0);
+  const Residual f = residual_of<T>(r, b, K, S, mode, tau, laws, la, sums, red);
+  double w[VEC];
+  {
+    double s = 0.0;
+#pragma unroll 1
+    for (int k = 0; k < NV; ++k) {
+      const Two<T> next = k + 1 < NV ? load_two<T, E>(r, r.p != nullptr, V, blockIdx.x % S, k + 1) : two;
+      s += residual_vector<T>(f, two, r.p != nullptr, c, w);
+      two = next;
+    }
+    s = block_sum(s, red);
+    if (t == 0) {
+      // Atomics of device scope go past what the XCDs' caches may hold of their own, so a wait for
+      // the store is all that orders it; a device-scope fence would write back the whole L2 here,
+      // once a workgroup (64 chains of 131072 tokens: 75 us in all with the fence).
+      __hip_atomic_store(&mass[blockIdx.x], s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      last_s = __hip_atomic_fetch_add(&arrived[b], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)S - 1u;
+    }
+  }
+  __syncthreads();
+  if (!last_s) return;
+  auto mass_of = [&](int s) {
+    return __hip_atomic_load(&mass[(int64_t)b * S + s], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  };
+
   double u;
   if (uniforms) {
     u = uniforms[(int64_t)b * (K + 1) + K];
   } else {
-    const uint4 w = philox(0u, (uint32_t)b, round[b], TAG_USAMPLE << 24, seed);
-    u = ((double)(((uint64_t)(w.x >> 6) << 26) | (w.y >> 6)) + 0.5) * 0x1p-52;
+    const uint4 x = philox(0u, (uint32_t)b, round[b], TAG_USAMPLE << 24, seed);
+    u = ((double)(((uint64_t)(x.x >> 6) << 26) | (x.y >> 6)) + 0.5) * 0x1p-52;
   }
   // Laws without mass or with a NaN: the residual's sums come out 0 (a NaN weight
   // counts 0), the target's are then taken, and those decide.
   const int per = (S + kThreads - 1) / kThreads, s0 = min(t * per, S), s1 = min(s0 + per, S);
   double v = 0.0;
-  for (int s = s0; s < s1; ++s) v += mass[(int64_t)b * S + s];
+  for (int s = s0; s < s1; ++s) v += mass_of(s);
   double cum = block_scan(v, red);
   __syncthreads();
   if (t == kThreads - 1) before_s = cum;
@@ -716,7 +843,6 @@ __global__ __launch_bounds__(kThreads) void draw_pick_kernel(Rows rows, int K, i
     return;
   }
   if (use_q) {
-    f.B = 0.0;
     v = 0.0;
     for (int s = s0; s < s1; ++s) v += sums[(int64_t)b * S + s].q * f.A;
     cum = block_scan(v, red);
@@ -734,47 +860,64 @@ __global__ __launch_bounds__(kThreads) void draw_pick_kernel(Rows rows, int K, i
   }
   __syncthreads();
   if (t == owner) {
-    double c = cum - v;
+    double at = cum - v;
     int last = s0;
     for (int s = s0; s < s1; ++s) {
-      const double g = use_q ? sums[(int64_t)b * S + s].q * f.A : mass[(int64_t)b * S + s];
+      const double g = use_q ? sums[(int64_t)b * S + s].q * f.A : mass_of(s);
       if (g > 0.0) {
         last = s;
-        before_s = c;
-        if (c + g > goal) break;
+        before_s = at;
+        if (at + g > goal) break;
       }
-      c += g;
+      at += g;
     }
     slice_s = last;
   }
   __syncthreads();
+  // the slice's weights again, in vectors of kThreads * VEC elements that follow one another
   const int slice = slice_s;
-  const double before = before_s;
-  const int a = lead<T>(r.q), e0 = slice * kThreads * E + t * E - a;
-  double w[E], mine = 0.0;
-#pragma unroll
-  for (int i = 0; i < E; ++i) {
-    const int e = e0 + i;
-    const bool in = e >= 0 && e < V;
-    w[i] = in ? residual_weight(f, T::value(r.q[e]), r.p && !use_q ? T::value(r.p[e]) : -INFINITY, inv_t) : 0.0;
-    mine += w[i];
+  const bool with_p = r.p && !use_q;
+  double mine = 0.0;
+  two = load_two<T, E>(r, with_p, V, slice, 0);
+#pragma unroll 1
+  for (int k = 0; k < NV; ++k) {
+    const Two<T> next = k + 1 < NV ? load_two<T, E>(r, with_p, V, slice, k + 1) : two;
+    mine = residual_vector<T>(f, two, with_p, c, w);
+    two = next;
+    const double s = wave_sum(mine);
+    if ((t & 63) == 0) red[4 * k + (t >> 6)] = s;
   }
-  const double upto = before + block_scan(mine, red);
-  int who = block_first(upto > goal, ired);
+  __syncthreads();
+  double before = before_s, upto = before;
+  int vec = 0;
+  bool past = false;
+  for (int k = 0; k < NV; ++k) {
+    const double g = red[4 * k] + red[4 * k + 1] + (red[4 * k + 2] + red[4 * k + 3]);
+    if (!past && g > 0.0) {
+      vec = k;
+      before = upto;
+      past = upto + g > goal;
+    }
+    upto += g;
+  }
+  if (vec != NV - 1) mine = residual_vector<T>(f, load_two<T, E>(r, with_p, V, slice, vec), with_p, c, w);
+  __syncthreads();
+  const double end = before + block_scan(mine, red);
+  int who = block_first(end > goal, ired);
   if (who == kThreads) who = block_last(mine > 0.0, ired);
   if (t == who) {
-    double c = upto - mine;
-    int at = -1;
+    double at = end - mine;
+    int tok = -1;
     bool found = false;
 #pragma unroll
-    for (int i = 0; i < E; ++i) {
-      c += w[i];
-      if (!found && w[i] > 0.0) {
-        at = e0 + i;
-        found = c > goal;
+    for (int j = 0; j < VEC; ++j) {
+      at += w[j];
+      if (!found && w[j] > 0.0) {
+        tok = position<T, E>(slice, lead<T>(r.q), vec * VEC + j);
+        found = at > goal;
       }
     }
-    tok_s = at;
+    tok_s = tok;
   }
   __syncthreads();
   if (t == 0) token[b] = tok_s;
@@ -801,7 +944,7 @@ hipError_t logprobs_run(int rows, int V, const void* x, int64_t ld, double inv_t
 }
 
 struct VerifyWs {
-  size_t parts, laws, la, excess, sums, mass, bytes;
+  size_t parts, laws, la, excess, sums, mass, arrived, bytes;
 };
 VerifyWs verify_layout(int B, int K, int V) {
   const int64_t rows = (int64_t)B * (2 * K + 1);
@@ -813,7 +956,8 @@ VerifyWs verify_layout(int B, int K, int V) {
   w.excess = w.la + up256(sizeof(double) * (size_t)B * K);
   w.sums = w.excess + up256(sizeof(double) * (size_t)B * K * S);
   w.mass = w.sums + up256(sizeof(Mass) * (size_t)B * Sd);
-  w.bytes = w.mass + up256(sizeof(double) * (size_t)B * Sd);
+  w.arrived = w.mass + up256(sizeof(double) * (size_t)B * Sd);
+  w.bytes = w.arrived + up256(sizeof(uint32_t) * (size_t)B);
   return w;
 }
 
@@ -829,36 +973,40 @@ hipError_t verify_run(const Rows& rows, int B, int K, int V, int mode, double in
   hipError_t e = launch_timed("verify_sums", verify_sums_kernel<T, E>, dim3((unsigned)((int64_t)B * (2 * K + 1) * S)),
                               dim3(kThreads), s, rows, K, V, S, c, kb, parts);
   if (e != hipSuccess) return e;
-  e = launch_timed("verify_join", verify_join_kernel<T>, dim3(B), dim3(64), s, rows, K, V, S, mode, inv_t, tokens, kb,
-                   uniforms, round, seed, (const Part*)parts, laws, la, tau, lar, ratio, coins);
-  if (e != hipSuccess || mode != SD_BLOCK) return e;
-  if (K > 1) {
-    e = launch_timed("verify_excess", verify_excess_kernel<T, E>, dim3((unsigned)((int64_t)B * (K - 1) * S)),
-                     dim3(kThreads), s, rows, K, V, S, c, kb, (const Law*)laws, (const double*)la, excess);
-    if (e != hipSuccess) return e;
-  }
-  return launch_timed("verify_decide", verify_decide_kernel, dim3(B), dim3(64), s, K, S, kb, uniforms, round, seed,
-                      (const double*)la, (const double*)excess, tau, lar, coins);
+  e = launch_timed("verify_join", verify_join_kernel<T>, dim3(B), dim3(kThreads), s, rows, K, V, S, mode, inv_t,
+                   tokens, kb, uniforms, round, seed, (const Part*)parts, laws, la, tau, lar, ratio, coins);
+  if (e != hipSuccess || mode != SD_BLOCK || K == 1) return e;
+  return launch_timed("verify_excess", verify_excess_kernel<T, E>, dim3((unsigned)((int64_t)B * (K - 1) * S)),
+                      dim3(kThreads), s, rows, K, V, S, c, kb, (const Law*)laws, (const double*)la, excess);
 }
 
+// Se: the slices of a row in verify_run.
 template <class T, int E>
-hipError_t draw_run(const Rows& rows, int B, int K, int V, int mode, double inv_t, const int32_t* kb,
-                    const double* uniforms, const uint32_t* round, uint64_t seed, const int32_t* tau, int32_t* token,
-                    char* ws, const VerifyWs& w, hipStream_t s) {
+hipError_t draw_run(const Rows& rows, int B, int K, int V, int Se, int mode, double inv_t, const int32_t* kb,
+                    const double* uniforms, const uint32_t* round, uint64_t seed, int32_t* tau, int32_t* token,
+                    float* lar, uint64_t* coins, char* ws, const VerifyWs& w, hipStream_t s) {
   const int S = slices(V, E);
+  const double c = inv_t * kLog2e;
   const Law* laws = reinterpret_cast<const Law*>(ws + w.laws);
-  const double* la = reinterpret_cast<const double*>(ws + w.la);
+  const double *la = reinterpret_cast<const double*>(ws + w.la),
+               *excess = reinterpret_cast<const double*>(ws + w.excess);
   Mass* sums = reinterpret_cast<Mass*>(ws + w.sums);
   double* mass = reinterpret_cast<double*>(ws + w.mass);
+  uint32_t* arrived = reinterpret_cast<uint32_t*>(ws + w.arrived);
   const dim3 grid((unsigned)((int64_t)B * S));
-  hipError_t e = launch_timed("draw_sums", draw_sums_kernel<T, E>, grid, dim3(kThreads), s, rows, K, V, S, inv_t, kb,
-                              tau, laws, sums);
+  hipError_t e = launch_timed("draw_sums", draw_sums_kernel<T, E>, grid, dim3(kThreads), s, rows, K, V, S, c, kb,
+                              uniforms, round, seed, laws, la, mode == SD_BLOCK ? excess : nullptr, Se, tau, lar,
+                              coins, sums, arrived);
   if (e != hipSuccess) return e;
-  e = launch_timed("draw_mass", draw_mass_kernel<T, E>, grid, dim3(kThreads), s, rows, K, V, S, mode, inv_t, kb, tau,
-                   laws, la, (const Mass*)sums, mass);
-  if (e != hipSuccess) return e;
-  return launch_timed("draw_pick", draw_pick_kernel<T, E>, dim3(B), dim3(kThreads), s, rows, K, V, S, mode, inv_t, kb,
-                      tau, uniforms, round, seed, laws, la, (const Mass*)sums, (const double*)mass, token);
+  return launch_timed("draw_token", draw_token_kernel<T, E>, grid, dim3(kThreads), s, rows, K, V, S, mode, c, kb,
+                      (const int32_t*)tau, uniforms, round, seed, laws, la, (const Mass*)sums, mass, arrived, token);
+}
+
+// Where each row is read for itself: eight vectors a thread instead of 32 elements, so that
+// more elements share a slice's reductions.
+template <class T>
+int per_thread_alone(int64_t rows, int V) {
+  return per_thread(rows, V) == 32 ? 8 * T::kVec : 8;
 }
 
 // f with the element type's tag.
@@ -870,7 +1018,7 @@ hipError_t by_type(sd_type type, F&& f) {
 }  // namespace
 
 size_t logprobs_ws_bytes(int rows, int V, int n) {
-  const size_t S = (size_t)slices(V, per_thread(rows, V));
+  const size_t S = (size_t)slices(V, per_thread(rows, V));  // (as many as any type has)
   return up256(sizeof(Part) * (size_t)rows * S) + up256(sizeof(uint64_t) * (size_t)rows * S * (size_t)n);
 }
 int64_t logprobs_groups(int rows, int V) { return (int64_t)rows * slices(V, per_thread(rows, V)); }
@@ -881,8 +1029,8 @@ hipError_t logprobs_launch(int rows, int V, sd_type type, const void* x, int64_t
   const double inv_t = 1.0 / temperature;
   return by_type(type, [&](auto tag) {
     typedef decltype(tag) T;
-    return per_thread(rows, V) == 32
-               ? logprobs_run<T, 32>(rows, V, x, ld, inv_t, n_tok, tokens, logprob, entropy, lse, n, ids, tops, ws, s)
+    return per_thread_alone<T>(rows, V) > 8
+               ? logprobs_run<T, 8 * T::kVec>(rows, V, x, ld, inv_t, n_tok, tokens, logprob, entropy, lse, n, ids, tops, ws, s)
                : logprobs_run<T, 8>(rows, V, x, ld, inv_t, n_tok, tokens, logprob, entropy, lse, n, ids, tops, ws, s);
   });
 }
@@ -910,10 +1058,11 @@ hipError_t verify_tokens_launch(int B, int K, int V, int mode, sd_type type, dou
                        : verify_run<T, 8>(rows, B, K, V, mode, inv_t, tokens, kb, uniforms, round, seed, tau, lar,
                                           ratio, coins, base, w, s);
     if (e != hipSuccess) return e;
-    return per_thread(B, V) == 32 ? draw_run<T, 32>(rows, B, K, V, mode, inv_t, kb, uniforms, round, seed, tau, token,
-                                                    base, w, s)
-                                  : draw_run<T, 8>(rows, B, K, V, mode, inv_t, kb, uniforms, round, seed, tau, token,
-                                                   base, w, s);
+    const int Se = slices(V, per_thread((int64_t)B * (2 * K + 1), V));
+    return per_thread(B, V) == 32 ? draw_run<T, 32>(rows, B, K, V, Se, mode, inv_t, kb, uniforms, round, seed, tau,
+                                                    token, lar, coins, base, w, s)
+                                  : draw_run<T, 8>(rows, B, K, V, Se, mode, inv_t, kb, uniforms, round, seed, tau,
+                                                   token, lar, coins, base, w, s);
   });
 }
 
