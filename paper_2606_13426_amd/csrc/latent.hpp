@@ -117,15 +117,21 @@ __global__ __launch_bounds__(R == 1 ? 256 : 512) void latent_kernel(Args a) {
   const int w = __builtin_amdgcn_readfirstlane(t >> 6), wt = w % WT, wr = w / WT;
   const int L = blockIdx.x, i8 = L / 8, team = i8 / a.p.team * 8 + L % 8, member = i8 % a.p.team;
 
-  // this team's run of the list of all sequences' tiles: found by each wavefront for itself
-  int total = 0;
-  for (int b0 = 0; b0 < a.B; b0 += 64) {
-    const int b = b0 + lane;
-    total += b < a.B ? tiles_of(length_of(a, b)) * a.p.supers : 0;
-  }
+  // this team's run of the list of all sequences' tiles: found by each wavefront for itself, in blocks
+  // of 64 sequences, the first of which stays in registers
+  auto tiles_at = [&](int len, int bb) { return bb < a.B ? tiles_of(len) * a.p.supers : 0; };
+  auto scan = [&](int v) {
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) total += __shfl_xor(total, d);
-  total = __builtin_amdgcn_readfirstlane(total);
+    for (int d = 1; d < 64; d <<= 1) {
+      const int o = __shfl_up(v, d);
+      if (lane >= d) v += o;
+    }
+    return v;
+  };
+  const int len0 = length_of(a, min(lane, a.B - 1)), tiles0 = tiles_at(len0, lane), upto0 = scan(tiles0);
+  int total = __builtin_amdgcn_readlane(upto0, 63);
+  for (int b0 = 64; b0 < a.B; b0 += 64)
+    total += __builtin_amdgcn_readlane(scan(tiles_at(length_of(a, min(b0 + lane, a.B - 1)), b0 + lane)), 63);
   const int teams = min(a.p.teams, total);
   if (team >= teams) return;
   const int share = total / teams, more = total - share * teams;
@@ -133,13 +139,8 @@ __global__ __launch_bounds__(R == 1 ? 256 : 512) void latent_kernel(Args a) {
   int left = share + (team < more ? 1 : 0);
   int b = 0, within = 0;
   for (int b0 = 0, at = 0;; b0 += 64) {
-    const int bb = b0 + lane, mine = bb < a.B ? tiles_of(length_of(a, bb)) * a.p.supers : 0;
-    int upto = mine;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int o = __shfl_up(upto, d);
-      if (lane >= d) upto += o;
-    }
+    const int mine = b0 == 0 ? tiles0 : tiles_at(length_of(a, min(b0 + lane, a.B - 1)), b0 + lane);
+    const int upto = b0 == 0 ? upto0 : scan(mine);
     const uint64_t hit = __ballot(at + upto > begin);
     if (hit) {
       const int i = __ffsll((unsigned long long)hit) - 1;
@@ -197,7 +198,7 @@ __global__ __launch_bounds__(R == 1 ? 256 : 512) void latent_kernel(Args a) {
   __syncthreads();
 
   for (int seg = 0; left > 0; ++seg) {
-    const int len = __builtin_amdgcn_readfirstlane(length_of(a, b)), nt = tiles_of(len), units = nt * a.p.supers;
+    const int len = b < 64 ? __builtin_amdgcn_readlane(len0, b) : __builtin_amdgcn_readfirstlane(length_of(a, b)), nt = tiles_of(len), units = nt * a.p.supers;
     if (within >= units) {
       within -= units;
       ++b;
@@ -511,24 +512,30 @@ __global__ __launch_bounds__(R == 1 ? 256 : 512) void latent_kernel(Args a) {
 }
 
 // The rows of sequences that no run did whole: parts joined against the largest
-// reference; rows without a token.  WAYS wavefronts take a row's parts in turn.
+// reference; rows without a token.  With WAYS = 1 a wavefront takes a row; with WAYS =
+// 4, for rows of many parts, the four of a workgroup take the parts of 128 columns of a
+// row in turn.
 template <class T, int DC, int WAYS>
 __global__ __launch_bounds__(kThreads) void latent_join_kernel(Args a) {
-  constexpr int NC = DC / 128;  // pairs of columns of a lane
-  __shared__ float acc[WAYS == 1 ? 1 : 4][DC];
+  constexpr int NC = WAYS == 1 ? DC / 128 : 1;   // pairs of columns of a lane
+  constexpr int CH = WAYS == 1 ? 1 : DC / 128;   // wavefronts that share a row by columns
+  __shared__ float2 acc[4][64];
   __shared__ float sums[4];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int way = WAYS == 1 ? 0 : w, per_group = 4 / WAYS;
-  const int rows = a.B * a.Q * a.H, R = a.p.R;
-  for (int base = blockIdx.x * per_group; base < rows; base += gridDim.x * per_group) {
-    const int id = base + (WAYS == 1 ? w : 0);
+  const int rows = a.B * a.Q * a.H, R = a.p.R;  // (times DC / 128 below 2^31: the rows have an output each)
+  for (int base = blockIdx.x * per_group; base < rows * CH; base += gridDim.x * per_group) {
+    const int unit = base + (WAYS == 1 ? w : 0), id = unit / CH, col0 = unit % CH * 128 + 2 * lane;
     if (id >= rows) break;
     const int b = id / (a.Q * a.H), row = id - b * a.Q * a.H, i = row / a.H, h = row - i * a.H;
     if (i >= rows_of(a, b)) continue;
     uint16_t* dst = a.out + (int64_t)b * a.os + (int64_t)i * a.orow + (int64_t)h * a.oh;
+    const bool says = a.lse && way == 0 && lane == 0 && unit % CH == 0;
     if (length_of(a, b) == 0) {
-      for (int c = lane; way == 0 && c < a.dc / 2; c += 64) reinterpret_cast<uint32_t*>(dst)[c] = 0u;
-      if (a.lse && way == 0 && lane == 0) a.lse[id] = -INFINITY;
+#pragma unroll
+      for (int k = 0; k < NC; ++k)
+        if (way == 0 && col0 + 128 * k < a.dc) *reinterpret_cast<uint32_t*>(dst + col0 + 128 * k) = 0u;
+      if (says) a.lse[id] = -INFINITY;
       continue;
     }
     const int block = row / (16 * R), super = block / a.p.team, member = block - super * a.p.team;
@@ -540,8 +547,10 @@ __global__ __launch_bounds__(kThreads) void latent_join_kernel(Args a) {
     };
     float m = -INFINITY;
     for (int k = ta + lane; k <= tb; k += 64) m = fmaxf(m, a.stat[part_of(k)].x);
+    m = across(m, true, true);
+    m = across(m, false, true);
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
+    for (int d = 1; d < 16; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
     const float ref = m == -INFINITY ? 0.f : m;
     float2 o[NC];
 #pragma unroll
@@ -554,13 +563,13 @@ __global__ __launch_bounds__(kThreads) void latent_join_kernel(Args a) {
       const float f = __builtin_amdgcn_exp2f(st.x - ref);
       sum += mine <= tb ? st.y * f : 0.f;
       const int count = min((tb - k0) / WAYS + 1, 64);
-#pragma unroll 4
+#pragma unroll(WAYS == 1 ? 4 : 16)
       for (int j = 0; j < count; ++j) {
         const float fj = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), j));
-        const float2* src = reinterpret_cast<const float2*>(a.part + (int64_t)__builtin_amdgcn_readlane(at, j) * DC) + lane;
+        const float* src = a.part + (int64_t)__builtin_amdgcn_readlane(at, j) * DC + col0;
 #pragma unroll
         for (int k = 0; k < NC; ++k) {
-          const float2 v = src[64 * k];
+          const float2 v = *reinterpret_cast<const float2*>(src + 128 * k);
           o[k].x = __fmaf_rn(v.x, fj, o[k].x);
           o[k].y = __fmaf_rn(v.y, fj, o[k].y);
         }
@@ -570,27 +579,22 @@ __global__ __launch_bounds__(kThreads) void latent_join_kernel(Args a) {
     for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
     if (WAYS > 1) {
       __syncthreads();
-#pragma unroll
-      for (int k = 0; k < NC; ++k) *reinterpret_cast<float2*>(&acc[way][2 * lane + 128 * k]) = o[k];
+      acc[way][lane] = o[0];
       if (lane == 0) sums[way] = sum;
       __syncthreads();
       if (way > 0) continue;
       sum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
-#pragma unroll
-      for (int k = 0; k < NC; ++k)
-        for (int q = 1; q < WAYS; ++q) {
-          const float2 v = *reinterpret_cast<const float2*>(&acc[q][2 * lane + 128 * k]);
-          o[k].x += v.x;
-          o[k].y += v.y;
-        }
+      for (int q = 1; q < WAYS; ++q) {
+        o[0].x += acc[q][lane].x;
+        o[0].y += acc[q][lane].y;
+      }
     }
     const float f = sum > 0.f ? 1.f / sum : sum != sum ? NAN : 0.f;
 #pragma unroll
-    for (int k = 0; k < NC; ++k) {
-      const int c = 2 * lane + 128 * k;
-      if (c < a.dc) *reinterpret_cast<uint32_t*>(dst + c) = T::pack(o[k].x * f, o[k].y * f);
-    }
-    if (a.lse && lane == 0) a.lse[id] = (m + __builtin_amdgcn_logf(sum)) * kLn2;
+    for (int k = 0; k < NC; ++k)
+      if (col0 + 128 * k < a.dc)
+        *reinterpret_cast<uint32_t*>(dst + col0 + 128 * k) = T::pack(o[k].x * f, o[k].y * f);
+    if (says) a.lse[id] = (m + __builtin_amdgcn_logf(sum)) * kLn2;
   }
 }
 
@@ -598,12 +602,13 @@ template <class T, int R, int DC>
 hipError_t run(const Args& a, hipStream_t s) {
   hipError_t e = launch_timed("latent_attention", latent_kernel<T, R, DC>, dim3(kGroups), dim3(R == 1 ? 256 : 512), s, a);
   if (e != hipSuccess) return e;
-  // four wavefronts a row where a sequence may have eight parts or more, else one
-  const int rows = a.B * a.Q * a.H;
+  // four wavefronts for 128 columns where a row may have eight parts or more, else one for the row
+  const int64_t rows = (int64_t)a.B * a.Q * a.H, many = rows * (DC / 128), few = (rows + 3) / 4;
   return a.p.teams >= 8 * (int64_t)a.B * a.p.supers
-             ? launch_timed("latent_join", latent_join_kernel<T, DC, 4>, dim3(rows < 4096 ? rows : 4096), dim3(kThreads), s, a)
-             : launch_timed("latent_join", latent_join_kernel<T, DC, 1>,
-                            dim3((rows + 3) / 4 < 4096 ? (rows + 3) / 4 : 4096), dim3(kThreads), s, a);
+             ? launch_timed("latent_join", latent_join_kernel<T, DC, 4>, dim3((unsigned)(many < 4096 ? many : 4096)),
+                            dim3(kThreads), s, a)
+             : launch_timed("latent_join", latent_join_kernel<T, DC, 1>, dim3((unsigned)(few < 4096 ? few : 4096)),
+                            dim3(kThreads), s, a);
 }
 
 template <class T>
