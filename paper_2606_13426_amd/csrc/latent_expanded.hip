@@ -211,6 +211,7 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_kernel(Expanded a) {
     f32x16 s[2] = {f32x16{}, f32x16{}};
     {
       // a step's pieces are read while the two before it are multiplied; the next tile's loads go out between
+      __builtin_amdgcn_s_setprio(1);
       u32x4 kf[3][2];
       auto read = [&](int k) {
         const bool own = k < DN / 16;
@@ -236,6 +237,7 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_kernel(Expanded a) {
     }
 #pragma unroll
     for (int b2 = 0; b2 < 2; ++b2) asm volatile("" : "+v"(s[b2]));  // taken up before any branch
+    __builtin_amdgcn_s_setprio(0);
     const bool edge = (tl + 1) * kTile > w_lo;
     if (edge) {
 #pragma unroll
@@ -262,17 +264,15 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_kernel(Expanded a) {
     const float ref = m == -INFINITY ? 0.f : m;
     u32x4 pf[4];
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    auto weigh = [&](int b2, int i) {  // scores i and i + 1 of a half
+      const float p0 = __builtin_amdgcn_exp2f(__fmaf_rn(s[b2][i], a.c, -ref));
+      const float p1 = __builtin_amdgcn_exp2f(__fmaf_rn(s[b2][i + 1], a.c, -ref));
+      sum[i & 2] += p0;
+      sum[(i & 2) + 1] += p1;
+      pf[2 * b2 + (i >> 3)][(i & 7) >> 1] = T::pack(p0, p1);
+    };
 #pragma unroll
-    for (int b2 = 0; b2 < 2; ++b2)
-#pragma unroll
-      for (int i = 0; i < 16; i += 2) {
-        const float p0 = __builtin_amdgcn_exp2f(__fmaf_rn(s[b2][i], a.c, -ref));
-        const float p1 = __builtin_amdgcn_exp2f(__fmaf_rn(s[b2][i + 1], a.c, -ref));
-        sum[i & 2] += p0;
-        sum[(i & 2) + 1] += p1;
-        pf[2 * b2 + (i >> 3)][(i & 7) >> 1] = T::pack(p0, p1);
-      }
-    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    for (int i = 0; i < 16; i += 2) weigh(0, i);
 
     // A key that some rows of the workgroup see and others do not: its weight for those is 0, and 0
     // times an infinity or NaN in its value is not.  All wavefronts look and find the same.
@@ -305,7 +305,10 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_kernel(Expanded a) {
       }
     }
     {
-      // two blocks' values are read while one is multiplied
+      // Two blocks' values are read while one is multiplied, and the second half's weights are made in
+      // the first half's products' time.  The products go first where both wavefronts of a SIMD have
+      // something to issue.
+      __builtin_amdgcn_s_setprio(1);
       u32x4 vf[3];
       auto read = [&](int i) {
         const Lds src = here + kV + (i / NV) * 16 * DV * 2 + vrow[i % NV & 1] + (i % NV >> 1) * 128;
@@ -319,12 +322,18 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_kernel(Expanded a) {
         if (i + 2 < 4 * NV) read(i + 2);
         __builtin_amdgcn_sched_barrier(0);
         o[i % NV] = T::mfma32(vf[i % 3], pf[i / NV], o[i % NV]);
+        if (i < 2 * NV) {
+#pragma unroll
+          for (int j = 0; j < 4 / NV; ++j) weigh(1, 2 * (i * (4 / NV) + j));
+        }
         __builtin_amdgcn_sched_barrier(0);
       }
     }
+    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
     // wait states for a read of the last results behind the loop's branch
     __builtin_amdgcn_sched_barrier(0);
     asm volatile("s_nop 15\n\ts_nop 15");
+    __builtin_amdgcn_s_setprio(0);
     __builtin_amdgcn_sched_barrier(0);
   }
 
