@@ -605,16 +605,16 @@ __device__ __forceinline__ Pair<T> drawn_rows(const Rows& rows, int b, int K, in
 
 // 2^x for x <= 0 in float64, NaN for NaN: the whole part goes to the exponent (taken from the
 // low bits of x + 1.5 2^52, which end at the units), the rest, at most a half in size, is the
-// series of e^{r log 2} to its tenth power (the next is below 3e-13 of it).  0 below 2^-1000.
+// series of e^{r log 2} to its eleventh power (the next is below 7e-15 of it).  0 below 2^-1000.
 __device__ __forceinline__ double pow2(double x) {
   constexpr double magic = 0x1.8p52, k = 0.69314718055994530942;
   const double z = x + magic, r = x - (z - magic);
-  double c[11] = {1.0};
+  double c[12] = {1.0};
 #pragma unroll
-  for (int i = 1; i < 11; ++i) c[i] = c[i - 1] * (k / i);
-  double p = c[10];
+  for (int i = 1; i < 12; ++i) c[i] = c[i - 1] * (k / i);
+  double p = c[11];
 #pragma unroll
-  for (int i = 9; i >= 0; --i) p = fma(p, r, c[i]);
+  for (int i = 10; i >= 0; --i) p = fma(p, r, c[i]);
   const uint64_t v = __builtin_bit_cast(uint64_t, p) + ((uint64_t)(uint32_t)__builtin_bit_cast(uint64_t, z) << 52);
   return x < -1000.0 ? 0.0 : __builtin_bit_cast(double, v);
 }
