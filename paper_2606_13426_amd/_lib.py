@@ -609,9 +609,12 @@ def sd_verify_tokens(draft, target, tokens, kb, uniforms=None, rnd=None, seed=0,
                    log_alpha_res=torch.empty(B, dtype=f32, device=dev), log_ratio=torch.empty(B, K, dtype=f32, device=dev),
                    coins=torch.empty(B, dtype=torch.int64, device=dev))
     else:
-        _operands(name, dict(tau=i32, token=i32, log_alpha_res=f32, log_ratio=f32, coins=torch.int64),
-                  **{k: out.get(k) for k in ("tau", "token", "log_alpha_res", "log_ratio", "coins")})
-        for k, o in out.items():
+        said = dict(tau=i32, token=i32, log_alpha_res=f32, log_ratio=f32, coins=torch.int64)
+        _need(all(out.get(k) is not None for k in said if k != "coins"), name,
+              "out must hold tau, token, log_alpha_res and log_ratio")
+        _operands(name, said, **{k: out.get(k) for k in said})
+        for k in said:
+            o = out.get(k)
             _need(o is None or (o.shape == ((B, K) if k == "log_ratio" else (B,)) and o.is_contiguous()), name,
                   f"{k} must be contiguous [B][K]" if k == "log_ratio" else f"{k} must be contiguous [B]")
     if ws is None:
