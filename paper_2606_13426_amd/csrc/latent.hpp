@@ -49,15 +49,26 @@ constexpr int kGroups = 256;  // workgroups: one a compute unit (the tiles fill 
 struct Plan {
   int R, blocks, team, supers, teams;
 };
-inline Plan plan(int Q, int H) {
-  const int64_t rows = (int64_t)Q * H;
+inline int most_r(int64_t rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }
+inline Plan plan_of(int64_t rows, int R) {
   Plan p;
-  p.R = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+  p.R = R;
   p.blocks = (int)((rows + 16 * p.R - 1) / (16 * p.R));
   p.team = p.blocks % 4 == 0 ? 4 : p.blocks % 2 == 0 ? 2 : p.blocks == 3 ? 3 : 1;
   p.supers = p.blocks / p.team;
   p.teams = 8 * (kGroups / 8 / p.team);
   return p;
+}
+// Many rows a workgroup read the cache less often, few leave smaller parts to join.  By the
+// tiles of 64 rows and 64 tokens that a compute unit has if every sequence is as long as its
+// pages allow; in us (both kernels) with R = 1 / 2 / 4, H heads of one row each:
+//   1 x 800 tokens, H = 64, 0.05 tiles:  20 / 21 / 25     4 x 4000, H = 128, 2:    41 / 40 / 46
+//   1 x 4000, H = 128, 0.5:              29 / 31 / 34     16 x 4000, H = 128, 8:   83 / 62 / 61
+//   8 x 4000, H = 64, 2:                 41 / 40 / 47     64 x 4000, H = 64, 16:   147 / 105 / 94
+inline Plan plan(int B, int Q, int H, int capacity) {
+  const int64_t rows = (int64_t)Q * H, tiles = ((int64_t)capacity + kTile - 1) / kTile * B * ((rows + 63) / 64);
+  const int most = most_r(rows);
+  return plan_of(rows, tiles < kGroups ? 1 : tiles < 8 * kGroups && most > 2 ? 2 : most);
 }
 
 struct Args {
@@ -602,9 +613,11 @@ template <class T, int R, int DC>
 hipError_t run(const Args& a, hipStream_t s) {
   hipError_t e = launch_timed("latent_attention", latent_kernel<T, R, DC>, dim3(kGroups), dim3(R == 1 ? 256 : 512), s, a);
   if (e != hipSuccess) return e;
-  // four wavefronts for 128 columns where a row may have eight parts or more, else one for the row
+  // One wavefront a row, or four for 128 columns of it where rows are few and may have eight parts or
+  // more.  In us, one / four: 64 rows of 128 parts 40 / 13, 512 rows of 16 parts 9.7 / 9.6, 2048
+  // rows of 4 parts 7 / 21, 8192 rows of 2 parts 13 / 67.
   const int64_t rows = (int64_t)a.B * a.Q * a.H, many = rows * (DC / 128), few = (rows + 3) / 4;
-  return a.p.teams >= 8 * (int64_t)a.B * a.p.supers
+  return rows < 1024 && a.p.teams >= 8 * (int64_t)a.B * a.p.supers
              ? launch_timed("latent_join", latent_join_kernel<T, DC, 4>, dim3((unsigned)(many < 4096 ? many : 4096)),
                             dim3(kThreads), s, a)
              : launch_timed("latent_join", latent_join_kernel<T, DC, 1>, dim3((unsigned)(few < 4096 ? few : 4096)),

@@ -23,7 +23,16 @@ Layout layout(int B, int dc, const latent::Plan& p) {
 }
 }  // namespace
 
-size_t latent_ws_bytes(int B, int Q, int H, int dc) { return layout(B, dc, latent::plan(Q, H)).bytes; }
+// (whatever the pages hold)
+size_t latent_ws_bytes(int B, int Q, int H, int dc) {
+  const int64_t rows = (int64_t)Q * H;
+  size_t most = 0;
+  for (int R = latent::most_r(rows); R >= 1; R /= 2) {
+    const size_t bytes = layout(B, dc, latent::plan_of(rows, R)).bytes;
+    most = bytes > most ? bytes : most;
+  }
+  return most;
+}
 
 hipError_t latent_launch(int B, int Q, int H, int dc, int dr, sd_type type, double scale, const void* q, sd_stride_h qs,
                          const void* cache, int64_t page_stride, int64_t token_stride, int n_pages, int page_size,
@@ -57,7 +66,7 @@ hipError_t latent_launch(int B, int Q, int H, int dc, int dr, sd_type type, doub
   a.orow = os.row;
   a.oh = os.head;
   a.lse = lse;
-  a.p = latent::plan(Q, H);
+  a.p = latent::plan(B, Q, H, a.capacity);
   const Layout l = layout(B, dc, a.p);
   char* base = static_cast<char*>(ws);
   a.part = reinterpret_cast<float*>(base + l.part);

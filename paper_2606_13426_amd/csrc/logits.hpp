@@ -127,6 +127,9 @@ inline int slices(int V, int E) { return (int)(((int64_t)V + 7 + (int64_t)kThrea
 
 // The elements a thread holds: 32, or 8 where rows of such slices would leave
 // compute units without a workgroup (256 compute units, four workgroups each).
+// In us, 8 / 32: one row of 32000 logits (float32, log-probabilities) 11 / 13, one chain
+// of 4 drafts over 32000 (bf16) 33 / 44, 16 rows of 131072 (bf16) 20 / 19, 2048 such rows
+// 306 / 161, 64 chains of 8 drafts over 131072 (bf16) 212 / 155.
 inline int per_thread(int64_t rows, int V) { return rows * slices(V, 32) >= 1024 ? 32 : 8; }
 
 }  // namespace logits

@@ -219,3 +219,26 @@ def test_calls_repeat_to_the_bit_and_replay_in_a_graph():
     graph.replay()
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(want, held))
+
+
+@pytest.mark.parametrize("tokens", [300, 2 ** 18, 2 ** 22])
+@pytest.mark.parametrize("B,Q,H,dc,dr,lens", [
+    (3, 1, 64, 512, 64, [515, 90, 0]), (2, 3, 33, 512, 64, [290, 3]), (1, 9, 32, 256, 64, [300]), (2, 2, 16, 128, 32, [64, 200]),
+    (2, 1, 200, 384, 64, [128, 129]), (5, 1, 17, 512, 64, [63, 0, 65, 1, 300])])
+def test_tables_of_every_width(B, Q, H, dc, dr, lens, tokens):
+    """The rows a workgroup takes go by what the table's pages could hold; what stands past the sequences' own
+    pages is never read."""
+    q, cache, ln, pages = _case(B, Q, H, dc, dr, lens, "bf16", 20 + B, page=16)
+    wide = torch.full((B, max(tokens // 16, pages.shape[1])), -7, dtype=torch.int32, device=DEV)
+    wide[:, :pages.shape[1]] = pages
+    ws = torch.full((_lib.sd_latent_attention_workspace(B, Q, H, dc, dr) + 4096,), 0x5A, dtype=torch.uint8, device=DEV)
+    got = _lib.sd_latent_attention(q, cache, ln, dc, pages=wide, ws=ws[:-4096])
+    _check(q, cache, ln, dc, pages, None, (dc + dr) ** -0.5, got, "bf16", heads=[0, 1, H // 2, H - 1])
+    assert (ws[-4096:] == 0x5A).all()
+    # an infinity in the last token: only the last row sees it
+    for b, n in enumerate(lens):
+        if n:
+            cache[pages[b, (n - 1) // 16], (n - 1) % 16, 3] = float("inf")
+    out, lse = _lib.sd_latent_attention(q, cache, ln, dc, pages=wide)
+    if Q > 1:
+        assert torch.isfinite(out[:, :-1].float()).all()
