@@ -15,8 +15,6 @@
 #include <math.h>
 #include <stdint.h>
 
-#include <type_traits>
-
 #include "common.hpp"
 
 namespace sd {
