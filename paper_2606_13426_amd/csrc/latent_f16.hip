@@ -23,11 +23,11 @@ Layout layout(int B, int dc, const latent::Plan& p) {
 }
 }  // namespace
 
-// (whatever the pages hold)
+// Enough for pages of any size (the smallest give the fewest rows a workgroup).
 size_t latent_ws_bytes(int B, int Q, int H, int dc) {
   const int64_t rows = (int64_t)Q * H;
   size_t most = 0;
-  for (int R = latent::most_r(rows); R >= 1; R /= 2) {
+  for (int R = latent::most_r(rows); R >= latent::plan(B, Q, H, 1).R; R /= 2) {
     const size_t bytes = layout(B, dc, latent::plan_of(rows, R)).bytes;
     most = bytes > most ? bytes : most;
   }

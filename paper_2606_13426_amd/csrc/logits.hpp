@@ -53,9 +53,9 @@ __device__ __forceinline__ int lead(const typename T::raw* p) {
 
 // The row position of element i of this thread's slice (negative, or V and
 // above, outside the row).
-template <class T, int E>
+template <class T, int E, int N = kThreads>
 __device__ __forceinline__ int position(int slice, int a, int i) {
-  return ((slice * (E / T::kVec) + i / T::kVec) * kThreads + (int)threadIdx.x) * T::kVec + i % T::kVec - a;
+  return ((slice * (E / T::kVec) + i / T::kVec) * N + (int)threadIdx.x) * T::kVec + i % T::kVec - a;
 }
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
@@ -85,11 +85,11 @@ union Vec {
   u32x4 v;
   typename T::raw r[T::kVec];
 };
-template <class T, int E, bool STREAM = false>
+template <class T, int E, bool STREAM = false, int N = kThreads>
 __device__ __forceinline__ Vec<T> load_vector(const typename T::raw* __restrict__ p, int a, int V, int slice, int k) {
   constexpr int VEC = T::kVec;
   const int off = (lead<T>(p) - a) & (VEC - 1);  // elements from an aligned vector to a vector of positions
-  const int e0 = position<T, E>(slice, a, k * VEC);
+  const int e0 = position<T, E, N>(slice, a, k * VEC);
   Vec<T> w;
   if (off == 0 && e0 >= 0 && e0 + VEC <= V) {
     const u32x4* q = reinterpret_cast<const u32x4*>(p + e0);
@@ -107,13 +107,13 @@ __device__ __forceinline__ Vec<T> load_vector(const typename T::raw* __restrict_
   return w;
 }
 // The slice's elements of this thread: x[i] is the one at position(i).
-template <class T, int E, bool STREAM = false>
+template <class T, int E, bool STREAM = false, int N = kThreads>
 __device__ __forceinline__ void load_slice(const typename T::raw* __restrict__ p, int a, int V, int slice,
                                            float (&x)[E]) {
   constexpr int VEC = T::kVec, NV = E / VEC;
   Vec<T> w[NV];
 #pragma unroll
-  for (int k = 0; k < NV; ++k) w[k] = load_vector<T, E, STREAM>(p, a, V, slice, k);
+  for (int k = 0; k < NV; ++k) w[k] = load_vector<T, E, STREAM, N>(p, a, V, slice, k);
 #pragma unroll
   for (int k = 0; k < NV; ++k)
 #pragma unroll
@@ -125,9 +125,9 @@ inline int slices(int V, int E) { return (int)(((int64_t)V + 7 + (int64_t)kThrea
 
 // The elements a thread holds: 32, or 8 where rows of such slices would leave
 // compute units without a workgroup (256 compute units, four workgroups each).
-// In us, 8 / 32: one row of 32000 logits (float32, log-probabilities) 11 / 13, one chain
-// of 4 drafts over 32000 (bf16) 33 / 44, 16 rows of 131072 (bf16) 20 / 19, 2048 such rows
-// 306 / 161, 64 chains of 8 drafts over 131072 (bf16) 212 / 155.
+// In us, 8 / 32: one chain of 4 drafts over 32000 (bf16) 33 / 44, 8 over 131072 40 / 46, 64
+// of 8 drafts 212 / 155; log-probabilities of 16 rows of 131072 (bf16) 20 / 19, of 2048
+// 306 / 161.
 inline int per_thread(int64_t rows, int V) { return rows * slices(V, 32) >= 1024 ? 32 : 8; }
 
 }  // namespace logits

@@ -16,8 +16,7 @@
 // products (22 and 38 us there, about 23 of them an element); log-probabilities by
 // vector instructions, about 14 an element with the alternatives (2048 rows of 131072
 // bf16: 145 us, 3.7 TB/s, 119 of them issuing).  Few rows are launches and trips to
-// memory: one row of 32000 takes 5 + 6 us in two kernels, one chain of 4 drafts 23 us
-// in five.
+// memory: one row of 32000 takes 9 us in one kernel, one chain of 4 drafts 23 us in five.
 #include "common.hpp"
 #include "logits.hpp"
 #include "philox.hpp"
@@ -91,34 +90,41 @@ struct TopLds {
 
 // The keys of pool[0..c) in falling order to out[0..n) (fewer than n: the rest 0).
 // Every key counts those above it; c is mostly little more than n.
+template <int N = kThreads>
 __device__ __forceinline__ void write_ranked(const uint64_t* pool, int c, int n, uint64_t* out) {
-  for (int i = threadIdx.x; i < c; i += kThreads) {
+  for (int i = threadIdx.x; i < c; i += N) {
     const uint64_t k = pool[i];
     int above = 0;
     for (int j = 0; j < c; ++j) above += pool[j] > k;
     if (above < n) out[above] = k;
   }
-  for (int i = c + (int)threadIdx.x; i < n; i += kThreads) out[i] = 0;
+  for (int i = c + (int)threadIdx.x; i < n; i += N) out[i] = 0;
 }
 
 // The n largest of the slice x to out[0..n) in falling order, 0 past its elements; best[k] is
-// the largest of vector k of this thread.  The largest values of 64 groups of four threads give a
+// the largest of vector k of this thread.  The largest values of 64 groups of threads give a
 // bound: n groups hold one at or above the n-th largest of them, so the n largest elements
 // are among those not below it, which are few: most wavefronts find no candidate in a
 // compare or two an element.  Where equal values overflow the pool (few values that are
 // not -inf, a constant row) the groups' largest keys give the bound, which no two
 // elements share, and where that overflows it too (an order made for it) the n largest
 // are taken one after another.
-template <class T, int E>
+template <class T, int E, int N = kThreads>
 __device__ __forceinline__ void slice_top(const float (&x)[E], const float (&best)[E / T::kVec], int slice, int a, int V, int n, TopLds& sm,
                                           uint64_t* out) {
+  constexpr int G = N / 64;  // threads a group
+  static_assert(G == 4 || G == 16, "groups of lanes side by side");
   const int t = threadIdx.x;
   float g = best[0];
 #pragma unroll
   for (int k = 1; k < E / T::kVec; ++k) g = fmaxf(g, best[k]);
   g = fmaxf(g, dpp<kDppXor1>(g));
   g = fmaxf(g, dpp<kDppXor2>(g));
-  if ((t & 3) == 0) sm.groupf[t >> 2] = g;
+  if (G == 16) {
+    g = fmaxf(g, dpp<kDppHalfMirror>(g));
+    g = fmaxf(g, dpp<kDppMirror>(g));
+  }
+  if (t % G == 0) sm.groupf[t / G] = g;
   if (t == 0) sm.count = 0;
   __syncthreads();
   if (t < 64) {
@@ -139,7 +145,7 @@ __device__ __forceinline__ void slice_top(const float (&x)[E], const float (&bes
 #pragma unroll
         for (int i = k * T::kVec; i < (k + 1) * T::kVec; ++i) {
           if (!__any(x[i] >= boundf)) continue;
-          const int pos = position<T, E>(slice, a, i);
+          const int pos = position<T, E, N>(slice, a, i);
           if (x[i] >= boundf && pos >= 0 && pos < V) {
             const int c = atomicAdd(&sm.count, 1);
             if (c < kPool) sm.pool[c] = key_of(x[i], pos);
@@ -148,20 +154,24 @@ __device__ __forceinline__ void slice_top(const float (&x)[E], const float (&bes
     __syncthreads();
     const int c = sm.count;
     if (c <= kPool) {
-      write_ranked(sm.pool, c, n, out);
+      write_ranked<N>(sm.pool, c, n, out);
       return;
     }
   }
   uint64_t mine = 0;
 #pragma unroll
   for (int i = 0; i < E; ++i) {
-    const int pos = position<T, E>(slice, a, i);
+    const int pos = position<T, E, N>(slice, a, i);
     if (pos >= 0 && pos < V) mine = max64(mine, key_of(x[i], pos));
   }
   uint64_t gk = max64(mine, dpp64<kDppXor1>(mine));
   gk = max64(gk, dpp64<kDppXor2>(gk));
+  if (G == 16) {
+    gk = max64(gk, dpp64<kDppHalfMirror>(gk));
+    gk = max64(gk, dpp64<kDppMirror>(gk));
+  }
   __syncthreads();
-  if ((t & 3) == 0) sm.group[t >> 2] = gk;
+  if (t % G == 0) sm.group[t / G] = gk;
   if (t == 0) sm.count = 0;
   __syncthreads();
   if (t < 64) {
@@ -178,7 +188,7 @@ __device__ __forceinline__ void slice_top(const float (&x)[E], const float (&bes
   if (mine != 0 && mine >= bound) {
 #pragma unroll
     for (int i = 0; i < E; ++i) {
-      const int pos = position<T, E>(slice, a, i);
+      const int pos = position<T, E, N>(slice, a, i);
       if (pos < 0 || pos >= V) continue;
       const uint64_t k = key_of(x[i], pos);
       if (k < bound) continue;
@@ -189,7 +199,7 @@ __device__ __forceinline__ void slice_top(const float (&x)[E], const float (&bes
   __syncthreads();
   const int c = sm.count;
   if (c <= kPool) {
-    write_ranked(sm.pool, c, n, out);
+    write_ranked<N>(sm.pool, c, n, out);
     return;
   }
   uint64_t last = ~0ull;
@@ -197,7 +207,7 @@ __device__ __forceinline__ void slice_top(const float (&x)[E], const float (&bes
     uint64_t k = 0;
 #pragma unroll
     for (int i = 0; i < E; ++i) {
-      const int pos = position<T, E>(slice, a, i);
+      const int pos = position<T, E, N>(slice, a, i);
       const uint64_t q = pos >= 0 && pos < V ? key_of(x[i], pos) : 0;
       if (q < last) k = max64(k, q);
     }
@@ -205,7 +215,8 @@ __device__ __forceinline__ void slice_top(const float (&x)[E], const float (&bes
     __syncthreads();
     if ((t & 63) == 0) sm.group[t >> 6] = k;
     __syncthreads();
-    k = max64(max64(sm.group[0], sm.group[1]), max64(sm.group[2], sm.group[3]));
+    k = sm.group[0];
+    for (int i = 1; i < N / 64; ++i) k = max64(k, sm.group[i]);
     if (t == 0) out[r] = k;
     last = k;
   }
@@ -213,11 +224,16 @@ __device__ __forceinline__ void slice_top(const float (&x)[E], const float (&bes
 
 // ------------------------------------------------------------------- sums --
 // Sums of a workgroup's slice: m its maximum, S and (ENT) U; best[k] the largest of vector k of this thread.
-template <class T, int E, bool ENT>
+template <int W>
+__device__ __forceinline__ double pairwise(const double* p) {
+  if constexpr (W == 1) return p[0];
+  else return pairwise<W / 2>(p) + pairwise<W / 2>(p + W / 2);
+}
+template <class T, int E, bool ENT, int N = kThreads>
 __device__ __forceinline__ Part slice_sums(const float (&x)[E], float c, double* red, float* redm,
                                            float (&best)[E / T::kVec]) {
   const int t = threadIdx.x, w = t >> 6;
-  constexpr int NV = E / T::kVec;
+  constexpr int NV = E / T::kVec, W = N / 64;
   float m = -INFINITY;
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
@@ -229,7 +245,9 @@ __device__ __forceinline__ Part slice_sums(const float (&x)[E], float c, double*
   m = wave_max(m);
   if ((t & 63) == 0) redm[w] = m;
   __syncthreads();
-  m = fmaxf(fmaxf(redm[0], redm[1]), fmaxf(redm[2], redm[3]));
+  m = redm[0];
+#pragma unroll
+  for (int i = 1; i < W; ++i) m = fmaxf(m, redm[i]);
   const float ref = m == -INFINITY ? 0.f : m;
   float s[4] = {0.f, 0.f, 0.f, 0.f}, u[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -242,11 +260,11 @@ __device__ __forceinline__ Part slice_sums(const float (&x)[E], float c, double*
   const double S = (double)s[0] + s[1] + ((double)s[2] + s[3]), U = (double)u[0] + u[1] + ((double)u[2] + u[3]);
   // with U the lower lanes add up the one, the upper lanes the other
   const double v = ENT ? group_sum(swap_add<true>(S, U), 32) : wave_sum(S);
-  if ((t & 31) == 0 && (ENT || (t & 63) == 0)) red[(t & 32) / 8 + w] = v;
+  if ((t & 31) == 0 && (ENT || (t & 63) == 0)) red[(t & 32 ? W : 0) + w] = v;
   __syncthreads();
   Part p;
-  p.S = red[0] + red[1] + (red[2] + red[3]);
-  p.U = ENT ? red[4] + red[5] + (red[6] + red[7]) : 0.0;
+  p.S = pairwise<W>(red);
+  p.U = ENT ? pairwise<W>(red + W) : 0.0;
   p.m = m;
   p.pad = 0.f;
   return p;
@@ -269,6 +287,61 @@ __global__ __launch_bounds__(kThreads, 4) void logprobs_slice_kernel(const typen
   const Part r = slice_sums<T, E, true>(v, c, red, redm, best);
   if (threadIdx.x == 0) parts[id] = r;
   if (n > 0) slice_top<T, E>(v, best, slice, a, V, n, top, keys + id * n);
+}
+
+// What a row's sums say, by a workgroup of N threads: the given tokens, and the alternatives whose keys are in
+// best[0..n) (LDS, behind a barrier).
+template <class T, int N = kThreads>
+__device__ __forceinline__ void write_row(const typename T::raw* __restrict__ x, int64_t ld, int V, double inv_t,
+                                          int64_t row, float m, double s, double u, int n_tok,
+                                          const int32_t* __restrict__ tokens, float* __restrict__ logprob,
+                                          float* __restrict__ entropy, float* __restrict__ lse, int n,
+                                          int32_t* __restrict__ ids, float* __restrict__ tops, const uint64_t* best) {
+  const int t = threadIdx.x;
+  const bool law = s > 0.0 && isfinite(s), none = s == 0.0;
+  const double logs = log(s);
+  auto logp = [&](float v) {
+    return law ? (float)(((double)v - (double)m) * inv_t - logs) : none ? -INFINITY : NAN;
+  };
+  if (t == 0) {
+    if (lse) lse[row] = law ? (float)((double)m * inv_t + logs) : none ? -INFINITY : NAN;
+    if (entropy) entropy[row] = law ? (float)(logs - u * inv_t / s) : none ? 0.f : NAN;
+  }
+  for (int i = t; i < n_tok; i += N) {
+    const int tok = tokens[row * n_tok + i];
+    logprob[row * n_tok + i] = logp(tok >= 0 && tok < V ? T::value(x[row * ld + tok]) : -INFINITY);
+  }
+  if (t < n) {
+    const uint64_t me = best[t];
+    const bool real = me != 0 && (law || none);
+    ids[row * n + t] = real ? key_pos(me) : -1;
+    tops[row * n + t] = law || none ? (me != 0 ? logp(key_value(me)) : -INFINITY) : NAN;
+  }
+}
+
+// A row that one workgroup holds at once: all of it in one kernel.
+constexpr int kRowThreads = 1024;
+template <class T, int E>
+__global__ __launch_bounds__(kRowThreads) void logprobs_row_kernel(
+    const typename T::raw* __restrict__ x, int64_t ld, int V, float c, double inv_t, int n_tok,
+    const int32_t* __restrict__ tokens, float* __restrict__ logprob, float* __restrict__ entropy,
+    float* __restrict__ lse, int n, int32_t* __restrict__ ids, float* __restrict__ tops) {
+  __shared__ double red[2 * kRowThreads / 64];
+  __shared__ float redm[kRowThreads / 64];
+  __shared__ TopLds top;
+  __shared__ uint64_t keys[SD_MAX_TOP];
+  const int64_t row = blockIdx.x;
+  const typename T::raw* p = x + row * ld;
+  const int a = lead<T>(p);
+  float v[E], best[E / T::kVec];
+  load_slice<T, E, true, kRowThreads>(p, a, V, 0, v);
+  const Part r = slice_sums<T, E, true, kRowThreads>(v, c, red, redm, best);
+  if (n > 0) {
+    slice_top<T, E, kRowThreads>(v, best, 0, a, V, n, top, keys);
+    __syncthreads();
+  }
+  write_row<T, kRowThreads>(x, ld, V, inv_t, row, r.m, r.S, r.U, n_tok, tokens, logprob, entropy, lse, n, ids, tops,
+                            keys);
 }
 
 // One workgroup a row: the slices' sums, the given tokens and the alternatives.
@@ -308,21 +381,13 @@ __global__ __launch_bounds__(kThreads) void logprobs_join_kernel(
   __syncthreads();
   s = red[0] + red[1] + (red[2] + red[3]);
   u = red[4] + red[5] + (red[6] + red[7]);
-  const bool law = s > 0.0 && isfinite(s), none = s == 0.0;
-  const double logs = log(s);
-  auto logp = [&](float v) {
-    return law ? (float)(((double)v - (double)m) * inv_t - logs) : none ? -INFINITY : NAN;
+  auto finish = [&]() {
+    write_row<T>(x, ld, V, inv_t, row, m, s, u, n_tok, tokens, logprob, entropy, lse, n, ids, tops, best);
   };
-  if (t == 0) {
-    if (lse) lse[row] = law ? (float)((double)m * inv_t + logs) : none ? -INFINITY : NAN;
-    if (entropy) entropy[row] = law ? (float)(logs - u * inv_t / s) : none ? 0.f : NAN;
+  if (n == 0) {
+    finish();
+    return;
   }
-  for (int i = t; i < n_tok; i += kThreads) {
-    const int tok = tokens[row * n_tok + i];
-    logprob[row * n_tok + i] =
-        logp(tok >= 0 && tok < V ? T::value(x[row * ld + tok]) : -INFINITY);
-  }
-  if (n == 0) return;
   // The slices' lists are ordered: the n-th largest of their first q elements, q
   // the least with S q >= n, bounds the n largest of all from below.
   const uint64_t* k = keys + row * S * n;
@@ -368,12 +433,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_join_kernel(
     }
   }
   __syncthreads();
-  if (t < n) {
-    const uint64_t me = best[t];
-    const bool real = me != 0 && (law || none);
-    ids[row * n + t] = real ? key_pos(me) : -1;
-    tops[row * n + t] = law || none ? (me != 0 ? logp(key_value(me)) : -INFINITY) : NAN;
-  }
+  finish();
 }
 
 // ------------------------------------------------------------ verification --
@@ -932,11 +992,21 @@ __global__ __launch_bounds__(kThreads) void draw_token_kernel(
 // The workspace's parts, each at a multiple of 256 bytes.
 inline size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
 
+// Short rows are each one workgroup's, in one kernel, where there is a compute unit for every
+// one.  In us, two kernels / one: a row of 32000 float32, 20 alternatives, 14.1 / 9.0, bf16
+// 11.5 / 7.4; 256 rows of 32000 bf16 15.7 / 9.8; 512 18.0 / 17.4, of 8000 16.1 / 18.0; 2048 of
+// 32000 float32 44 / 67.  (Longer rows of 16 bits, 64 elements a thread: 11.9 + 6.2 / 27 for 256 of 65000.)
+constexpr int kOneEach = 256;
+
 template <class T, int E>
 hipError_t logprobs_run(int rows, int V, const void* x, int64_t ld, double inv_t, int n_tok, const int32_t* tokens,
                         float* logprob, float* entropy, float* lse, int n, int32_t* ids, float* tops, void* ws,
                         hipStream_t s) {
   typedef typename T::raw raw;
+  if (rows <= kOneEach && V + 7 <= kRowThreads * 32)
+    return launch_timed("logprobs_row", logprobs_row_kernel<T, 32>, dim3((unsigned)rows), dim3(kRowThreads), s,
+                        static_cast<const raw*>(x), ld, V, (float)(inv_t * kLog2e), inv_t, n_tok, tokens, logprob,
+                        entropy, lse, n, ids, tops);
   const int S = slices(V, E);
   Part* parts = static_cast<Part*>(ws);
   uint64_t* keys = reinterpret_cast<uint64_t*>(static_cast<char*>(ws) + up256(sizeof(Part) * (size_t)rows * S));

@@ -331,3 +331,44 @@ def test_rows_of_a_view_are_read_where_they_lie():
     b = _lib.sd_verify_tokens(buf[:, K + 1:].contiguous(), buf[:, :K + 1].contiguous(), tokens, kb, uniforms=un)
     assert all(torch.equal(a[k], b[k]) for k in ("tau", "token", "coins"))
     assert torch.allclose(a["log_ratio"], b["log_ratio"], rtol=0, atol=1e-5)
+
+
+def _awkward(x, t):
+    inf, low, V = float("inf"), torch.finfo(TYPES[t]).min, x.shape[1]
+    x[0] = -inf
+    x[1] = low
+    x[2] = -inf
+    x[2, V // 2] = 1.5
+    x[3] = low
+    x[3, V - 1] = 2.0
+    x[4, V // 3] = inf
+    x[5, V - 1] = float("nan")
+    x[6] = 0.25
+    x[7] = -inf
+    x[7, 1::3] = 0.5
+    x[8] = torch.finfo(TYPES[t]).max
+    x[9] = inf
+    return x
+
+
+@pytest.mark.parametrize("t", list(TYPES))
+@pytest.mark.parametrize("rows,V", [(11, 32761), (11, 32762), (300, 700), (257, 9001), (256, 3000), (1100, 4001)])
+def test_logprobs_in_one_kernel_and_in_slices(rows, V, t):
+    """Both sides of the lengths and of the rows up to which a row is one workgroup's, with masks and lawless rows."""
+    x = _awkward(_rows(rows, V, t, 6, off=3), t)
+    tokens = torch.full((rows, 3), V // 2, dtype=torch.int32, device=DEV)
+    tokens[:, 1], tokens[:, 2] = 1, 2 ** 31 - 1
+    r = _lib.sd_token_logprobs(x, tokens, n_top=32)
+    _check_logprobs(x, tokens, 32, 1.0, r, list(range(11)) + [rows - 1])
+
+
+@pytest.mark.parametrize("rows,V", [(2, 40000), (300, 9000)])
+@pytest.mark.parametrize("order", ["rising", "falling", "blocks", "equal"])
+def test_alternatives_of_slices_in_an_order(V, rows, order):
+    """As above for slices of 8 elements a thread."""
+    i = torch.arange(V, device=DEV, dtype=torch.float32)
+    x = dict(rising=i / 512, falling=-i / 512, equal=i * 0,
+             blocks=torch.where((i.long() % 1024) < 31 * 4 * 4, 8.0 + (i.long() * 7919 % 4093).float() / 4096, i * 0))[order]
+    x = x[None].expand(rows, V).contiguous()
+    r = _lib.sd_token_logprobs(x, None, n_top=32)
+    _check_logprobs(x, None, 32, 1.0, r, [0, rows - 1])
