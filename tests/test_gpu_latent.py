@@ -242,3 +242,30 @@ def test_tables_of_every_width(B, Q, H, dc, dr, lens, tokens):
     out, lse = _lib.sd_latent_attention(q, cache, ln, dc, pages=wide)
     if Q > 1:
         assert torch.isfinite(out[:, :-1].float()).all()
+
+
+@pytest.mark.parametrize("tokens", [300, 2 ** 18, 2 ** 22])
+@pytest.mark.parametrize("B,Q,H,order", [(3, 2, 40, "heads first"), (2, 3, 31, "gaps"), (2, 1, 70, "gaps"), (1, 5, 13, "rows apart")])
+def test_views_of_q_and_of_the_output(B, Q, H, order, tokens):
+    """Orders and strides of q and out that a workgroup's rows do not lie level in, and such that they do."""
+    dc, dr, t = 256, 64, "bf16"
+    d = dc + dr
+    q, cache, ln, pages = _case(B, Q, H, dc, dr, [170, 65, 9][:B], t, 30 + B, page=16)
+    wide = torch.full((B, max(tokens // 16, pages.shape[1])), -7, dtype=torch.int32, device=DEV)
+    wide[:, :pages.shape[1]] = pages
+    if order == "heads first":
+        qv, shape = q.transpose(1, 2).contiguous().transpose(1, 2), (B, H, Q, dc)
+        ov = lambda x: x.transpose(1, 2)  # noqa: E731
+    elif order == "gaps":
+        qv = torch.full((B, Q, H, d + 24), 5.0, dtype=q.dtype, device=DEV)[..., 8:8 + d]
+        qv.copy_(q)
+        shape, ov = (B, Q, H, dc + 8), lambda x: x[..., :dc]
+    else:
+        qv = torch.full((B, 2 * Q + 1, H, d), 5.0, dtype=q.dtype, device=DEV)[:, 1::2]
+        qv.copy_(q)
+        shape, ov = (B, 2 * Q, H, dc), lambda x: x[:, ::2]
+    out = torch.full(shape, 3.0, dtype=q.dtype, device=DEV)
+    got = _lib.sd_latent_attention(qv, cache, ln, dc, pages=wide, out=ov(out))
+    _check(q, cache, ln, dc, pages, None, d ** -0.5, got, t, heads=[0, 1, H // 2, H - 1])
+    ov(out).fill_(3.0)
+    assert (out == 3.0).all()
