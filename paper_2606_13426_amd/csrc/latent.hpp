@@ -187,13 +187,17 @@ __global__ __launch_bounds__(R == 1 ? 256 : 512) void latent_kernel(Args a) {
   const bool padded = a.dc != DC || a.dr != kRope;
   // Where a wavefront's tokens lie one after another in one page, a tile's loads have one scalar
   // address and a lane's fixed offsets.
-  const bool rowed = (a.pages == nullptr || a.page_size % TW == 0) && a.token_stride < (1 << 24) && !padded;
+  const bool rowed = a.token_stride < (1 << 24);
   // The same of a sequence's rows of Q, heads side by side in every one (16 rows would be one wavefront's
   // then: 17 us instead of 15 for a short sequence).
-  const bool level = R > 1 && (a.Q == 1 || a.qr == a.H * a.qh) && a.qh < (1 << 24) && a.token_stride < (1 << 24) && !padded;
+  const bool level = R > 1 && (a.Q == 1 || a.qr == a.H * a.qh) && a.qh < (1 << 24) && rowed;
   uint32_t off[NL];
 #pragma unroll
-  for (int i = 0; i < NL; ++i) off[i] = 2u * (uint32_t)(piece_token(i, lane) * (int)a.token_stride + piece_col(i, lane));
+  for (int i = 0; i < NL; ++i) {
+    // (a column that is not there lies past every view's end: nothing is read for it)
+    const int col = piece_col(i, lane);
+    off[i] = col < 0 ? 0x80000000u : 2u * (uint32_t)(piece_token(i, lane) * (int)a.token_stride + col);
+  }
   // what a lane reads of a tile and of P, in bytes
   const int kx = g ^ perm(n);
   const int krow[2] = {((16 * TB * wt + n) * C + kx) * 16, ((16 * TB * wt + n) * C + (kx ^ 4)) * 16};
@@ -262,10 +266,11 @@ __global__ __launch_bounds__(R == 1 ? 256 : 512) void latent_kernel(Args a) {
       Load ld{u32x4{0u, 0u, 0u, 0u}, 0u, 0u, 0ull};
       const int j0 = tl * kTile + TW * w, count = min(max(lim_hi - j0, 0), TW);
       dst += TW * w * C * 16;
-      if (rowed && count == TW) {
-        const int pg = table ? j0 / a.page_size : 0, page = __builtin_amdgcn_readfirstlane(ahead);
+      const int pg0 = table ? j0 / a.page_size : 0, in = j0 - pg0 * a.page_size;
+      if (rowed && count == TW && (!table || in + TW <= a.page_size)) {
+        const int page = __builtin_amdgcn_readfirstlane(ahead);
         if (page < 0 || page >= a.n_pages) return ld;
-        ld.view = lds_view(a.cache + (int64_t)page * a.page_stride + (int64_t)(j0 - pg * a.page_size) * a.token_stride,
+        ld.view = lds_view(a.cache + (int64_t)page * a.page_stride + (int64_t)in * a.token_stride,
                            2 * ((TW - 1) * a.token_stride + a.dc + a.dr));
         ld.dst = lds_address(dst);
         ld.valid = (1u << TW) - 1u;

@@ -132,19 +132,20 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_kernel(Expanded a) {
     *tok = s / P;
     return ((pc & ~7) | ((pc ^ perm(*tok)) & 7)) * 8;
   };
-  auto set_offsets = [&](int P, int64_t stride, uint32_t* to) {
+  auto set_offsets = [&](int P, int64_t stride, int d, uint32_t* to) {
     for (int i = 0; i < P / 4; ++i) {
       int tok;
       const int col = place(P, i, &tok);
-      to[i] = 2u * (uint32_t)(tok * (int)stride + col);
+      // (a column that is not there lies past every view's end: nothing is read for it)
+      to[i] = col < d ? 2u * (uint32_t)(tok * (int)stride + col) : 0x80000000u;
     }
   };
-  set_offsets(CN, a.kt, off_n);
-  set_offsets(CR, a.krt, off_r);
-  set_offsets(CV, a.vt, off_v);
+  set_offsets(CN, a.kt, a.dn, off_n);
+  set_offsets(CR, a.krt, a.dr, off_r);
+  set_offsets(CV, a.vt, a.dv, off_v);
   // piece i of a wavefront goes to 1024 (w + 4 i): four wavefronts side by side
   // The three views of a tile, for loads that go out one after another (next_load); `on` is 0 where
-  // the tile is of another kind (its keys end in it, or columns are missing) and loaded here.
+  // the tile is of another kind (its keys end in it) and loaded here.
   struct Load {
     u32x4 n, r, v;
     uint32_t dst;
@@ -162,7 +163,7 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_kernel(Expanded a) {
   };
   auto start_load = [&](int tl, Lds dst, bool want) -> Load {
     Load ld;
-    const bool fast = tl * kTile + kTile <= nk && !padded;
+    const bool fast = tl * kTile + kTile <= nk;
     if (want && !fast) {
       slow_part(CN, gk, a.kt, a.dn, tl, dst);
       slow_part(CR, gr, a.krt, a.dr, tl, dst + kKr);
