@@ -31,13 +31,14 @@
 // latent_join_kernel.
 //
 // What bounds it, on MI355X.  Up to 32 rows: the cache's stream (2 sequences of 131072
-// tokens, 32 heads, bf16: 62 us, 4.9 TB/s, and 13 us for the join of 128 parts a row).
+// tokens, 32 heads, bf16: 59 us, 5.1 TB/s, and 13 us for the join of 128 parts a row).
 // With 64 rows the phases between a tile's three barriers: one workgroup fills a compute
 // unit's LDS, LDS is read in 40 % of the cycles, the matrix cores are busy in 26 %, vector
 // instructions issue in 22 %, and wavefronts wait for 42 % of their time (64 ragged
-// sequences of up to 6000 tokens, 128 heads: 130 us, 2.1 TB/s, 0.47 PFLOP/s).
+// sequences of up to 6000 tokens, 128 heads: 122 us, 2.2 TB/s, 0.5 PFLOP/s; a tile takes
+// 3800 cycles, a run's first tile and Q 16000, its stores 9000).
 // Wavefronts of 32 rows, which read K from LDS twice a tile instead of four times, were slower
-// (155 us): with Q in registers there is room for fewer operands ahead of the products.
+// (155 us where these took 130): with Q in registers there is room for fewer operands ahead of the products.
 // A short sequence is latency: 15 us for 777 tokens, 5 for the join.
 #pragma once
 
