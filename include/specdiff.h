@@ -7,6 +7,7 @@
  * with a closed-form Gaussian-mixture target; and the paper's alternatives:
  * sample (token) verification, the reflection residual, the Frozen Drafter,
  * temperature, and the plain Euler-Maruyama chain they are measured against.
+ * "Language-model verification" below is the same pass for the drafts of a language model.
  *
  * Conventions for every entry point:
  *  - Pointers are DEVICE pointers unless the comment says "host".
