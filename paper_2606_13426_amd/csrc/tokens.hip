@@ -570,6 +570,14 @@ __global__ __launch_bounds__(kThreads) void verify_join_kernel(Rows rows, int K,
   }
 }
 
+// max(0, eq A - ep B), NaN for NaN; exactly 0 where the two are the same numbers (both products rounded).
+__device__ __forceinline__ float excess_of(float eq, float A, float ep, float B) {
+#pragma clang fp contract(off)
+  const float q = eq * A, p = ep * B;
+  const float d = q - p;
+  return d > 0.f ? d : d != d ? d : 0.f;
+}
+
 // The slices of v_j for j = 1..K_b - 1: rows j (0-based) of target and draft.
 template <class T, int E>
 __global__ __launch_bounds__(kThreads) void verify_excess_kernel(Rows rows, int K, int V, int S, float c,
@@ -596,8 +604,7 @@ __global__ __launch_bounds__(kThreads) void verify_excess_kernel(Rows rows, int 
 #pragma unroll
   for (int i = 0; i < E; ++i) {
     const float eq = __builtin_amdgcn_exp2f((x[i] - mq) * c), ep = __builtin_amdgcn_exp2f((y[i] - mp) * c);
-    const float d = __fmaf_rn(eq, A, -(ep * B));
-    s[i & 3] += d > 0.f ? d : d != d ? d : 0.f;
+    s[i & 3] += excess_of(eq, A, ep, B);
   }
   const double sum = wave_sum((double)s[0] + s[1] + ((double)s[2] + s[3]));
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = sum;
@@ -796,8 +803,12 @@ __device__ __forceinline__ Residual residual_of(const Pair<T>& r, int b, int K, 
   if (f.mp == -INFINITY) f.mp = 0.f;
   return f;
 }
+// (two rounded products: equal laws differ by exactly 0.  One of them unrounded, in a fused
+// operation, would leave the other's rounding, of which half is positive and would be drawn from.)
 __device__ __forceinline__ double residual_weight(const Residual& f, float x, float y, double c) {
-  const double w = fma(f.A, weight(x, f.mq, c), -(f.B * weight(y, f.mp, c)));
+#pragma clang fp contract(off)
+  const double q = f.A * weight(x, f.mq, c), p = f.B * weight(y, f.mp, c);
+  const double w = q - p;
   return w > 0.0 ? w : 0.0;
 }
 
