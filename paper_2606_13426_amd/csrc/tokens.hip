@@ -716,8 +716,9 @@ __global__ __launch_bounds__(kThreads) void draw_sums_kernel(
   for (int h = 0; h < 2; ++h) {
     const typename T::raw* p = h ? r.p : r.q;
     if (!p) continue;
-    const float m = laws[(int64_t)b * (2 * K + 1) + (h ? r.ip : r.iq)].m;
-    if (m == -INFINITY) continue;
+    const Law& law = laws[(int64_t)b * (2 * K + 1) + (h ? r.ip : r.iq)];
+    if (law.S == 0.0) continue;  // (a row of -inf alone; with a NaN among them S is NaN, and so is its sum here)
+    const float m = law.m;
     Vec<T> x = load_vector<T, E>(p, a, V, slice, 0);
 #pragma unroll 1
     for (int k = 0; k < E / T::kVec; ++k) {
