@@ -930,7 +930,9 @@ __global__ __launch_bounds__(kThreads) void draw_token_kernel(
     all = before_s;
   }
   const double goal = u * all;
-  int owner = block_first(cum > goal, ired);
+  // (a thread without mass is never chosen: added up in another order, its sum may exceed the one
+  // before it, and the goal, by a bit)
+  int owner = block_first(v > 0.0 && cum > goal, ired);
   if (owner == kThreads) owner = block_last(v > 0.0, ired);  // u next to 1
   if (owner < 0) {
     if (t == 0) token[b] = -1;
@@ -981,7 +983,7 @@ __global__ __launch_bounds__(kThreads) void draw_token_kernel(
   if (vec != NV - 1) mine = residual_vector<T>(f, load_two<T, E>(r, with_p, V, slice, vec), with_p, c, w);
   __syncthreads();
   const double end = before + block_scan(mine, red);
-  int who = block_first(end > goal, ired);
+  int who = block_first(mine > 0.0 && end > goal, ired);
   if (who == kThreads) who = block_last(mine > 0.0, ired);
   if (t == who) {
     double at = end - mine;
