@@ -514,7 +514,8 @@ sd_status sd_token_logprobs(int32_t rows, int32_t V, sd_type type, const void* l
  * drafts x_1..x_{K_b} (kb is clamped to K; kb <= 0: an inactive chain), p_j and q_j
  * the laws of draft row j-1 and target row j-1 (softmaxes of logits /
  * temperature):
- *   log_ratio[b][j-1] = ell_j = log q_j(x_j) - log p_j(x_j)   (0 for j > K_b);
+ *   log_ratio[b][j-1] = ell_j = log q_j(x_j) - log p_j(x_j)   (0 for j > K_b), in float64
+ *          (as h_j too), rounded once; less than 2^-44 is 0, and an alpha_j that near to 1 is 1;
  *   block: log alpha_j = min(0, log alpha_{j-1} + ell_j),
  *          v_j = sum_x max(0, alpha_j q_{j+1}(x) - p_{j+1}(x)),
  *          h_j = v_j / (v_j + 1 - alpha_j) (1 where alpha_j = 1), h_{K_b} = alpha_{K_b},

@@ -6,17 +6,19 @@
 // a slice of a row in registers, so its maximum, sum, entropy term and largest
 // elements come from one read, and a second kernel joins a row's slices.  With
 // z = x / T and m the slice's maximum,
-//   S = sum e^{(x - m) / T},   U = sum (x - m) e^{(x - m) / T},
-// differences and exponentials in float32 (one instruction each), the sums of a
-// thread's elements too; everything across threads and slices is float64.
+//   S = sum e^{(x - m) / T},   U = sum (x - m) e^{(x - m) / T}.
+// Log-probabilities: differences and exponentials in float32 (one instruction each), the sums of a
+// thread's elements too; everything across threads and slices is float64.  Verification is
+// float64 from the difference on: with draft and target next to equal, h = v / (v + 1 - alpha) divides
+// differences of the two laws, and an error of 1e-7 of them would be one of 1e-7 / (1 - alpha).
 //
-// What bounds it, on MI355X: verification's two passes over all rows run at the rate of
-// a read-only stream (64 chains of 8 drafts over 131072 bf16 tokens: sums 45 us, 6.3
-// TB/s; excess 39 us, 6.0 TB/s); the draw's two passes over two rows a chain by float64
-// products (22 and 38 us there, about 23 of them an element); log-probabilities by
+// What bounds it, on MI355X: verification's two passes over all rows by float64 products, 17 an
+// element (64 chains of 8 drafts over 131072 bf16 tokens: sums 111 us, 2.6 TB/s; excess 100 us, 2.3
+// TB/s; in float32 they ran at the stream's rate, 45 and 39); the draw's two passes over two rows a chain
+// too (21 and 37 us there); log-probabilities by
 // vector instructions, about 14 an element with the alternatives (2048 rows of 131072
 // bf16: 145 us, 3.7 TB/s, 119 of them issuing).  Few rows are launches and trips to
-// memory: one row of 32000 takes 9 us in one kernel, one chain of 4 drafts 23 us in five.
+// memory: one row of 32000 takes 9 us in one kernel, one chain of 4 drafts 25 us in five.
 #include "common.hpp"
 #include "logits.hpp"
 #include "philox.hpp"
@@ -223,13 +225,13 @@ __device__ __forceinline__ void slice_top(const float (&x)[E], const float (&bes
 }
 
 // ------------------------------------------------------------------- sums --
-// Sums of a workgroup's slice: m its maximum, S and (ENT) U; best[k] the largest of vector k of this thread.
+// Sums of a workgroup's slice: m its maximum, S and U; best[k] the largest of vector k of this thread.
 template <int W>
 __device__ __forceinline__ double pairwise(const double* p) {
   if constexpr (W == 1) return p[0];
   else return pairwise<W / 2>(p) + pairwise<W / 2>(p + W / 2);
 }
-template <class T, int E, bool ENT, int N = kThreads>
+template <class T, int E, int N = kThreads>
 __device__ __forceinline__ Part slice_sums(const float (&x)[E], float c, double* red, float* redm,
                                            float (&best)[E / T::kVec]) {
   const int t = threadIdx.x, w = t >> 6;
@@ -255,19 +257,82 @@ __device__ __forceinline__ Part slice_sums(const float (&x)[E], float c, double*
     const float d = x[i] - ref;
     const float e = __builtin_amdgcn_exp2f(d * c);
     s[i & 3] += e;
-    if (ENT) u[i & 3] = __fmaf_rn(e, fmaxf(d, kLowest), u[i & 3]);
+    u[i & 3] = __fmaf_rn(e, fmaxf(d, kLowest), u[i & 3]);
   }
   const double S = (double)s[0] + s[1] + ((double)s[2] + s[3]), U = (double)u[0] + u[1] + ((double)u[2] + u[3]);
-  // with U the lower lanes add up the one, the upper lanes the other
-  const double v = ENT ? group_sum(swap_add<true>(S, U), 32) : wave_sum(S);
-  if ((t & 31) == 0 && (ENT || (t & 63) == 0)) red[(t & 32 ? W : 0) + w] = v;
+  // the lower lanes add up the one, the upper lanes the other
+  const double v = group_sum(swap_add<true>(S, U), 32);
+  if ((t & 31) == 0) red[(t & 32 ? W : 0) + w] = v;
   __syncthreads();
   Part p;
   p.S = pairwise<W>(red);
-  p.U = ENT ? pairwise<W>(red + W) : 0.0;
+  p.U = pairwise<W>(red + W);
   p.m = m;
   p.pad = 0.f;
   return p;
+}
+
+// The law's exponent: log2(e) / T, and the difference of logits below which a weight is 2^-1000 of the
+// largest and less.
+struct Scale {
+  double c, low;
+};
+// 2^{d c} for d c in [-1001, 1] in float64, NaN for NaN: the whole part goes to the exponent (taken from the
+// low bits of d c + 1.5 2^52, which end at the units), the rest, at most a half in size, to the
+// Chebyshev expansion of 2^r on [-1/2, 1/2] up to its tenth term (3.2e-16 off), as a polynomial.
+__device__ __forceinline__ double pow2(double d, double c) {
+  constexpr double magic = 0x1.8p52;
+  constexpr double k[11] = {1.0,
+                            0x1.62e42fefa3a19p-1,
+                            0x1.ebfbdff82c5aep-3,
+                            0x1.c6b08d703ce43p-5,
+                            0x1.3b2ab6fb9f1a3p-7,
+                            0x1.5d87fe9d7afb3p-10,
+                            0x1.430913112cb56p-13,
+                            0x1.ffcb54047bef3p-17,
+                            0x1.62bfc2c7ae40ep-20,
+                            0x1.b675be272450dp-24,
+                            0x1.e6228bff026d1p-28};
+  const double z = fma(d, c, magic), r = fma(d, c, magic - z);
+  double p = k[10];
+#pragma unroll
+  for (int i = 9; i >= 0; --i) p = fma(p, r, k[i]);
+  return __builtin_amdgcn_ldexp(p, (int)(uint32_t)__builtin_bit_cast(uint64_t, z));
+}
+// e^{(x - m) / T} of one element, 0 below 2^-1000.
+__device__ __forceinline__ double weight(float x, float m, Scale c) {
+  const double d = (double)x - (double)m, v = pow2(d, c.c);
+  return d < c.low ? 0.0 : v;
+}
+// The same with 2^-1000 for less and for NaN: for sums beside a weight of 1, whose caller looks for NaN.
+__device__ __forceinline__ double weight_or_tiny(float x, float m, Scale c) {
+  return pow2(fmax((double)x - (double)m, c.low), c.c);
+}
+
+// The same without U and in float64 throughout: verification divides differences of two laws by one another.
+template <class T, int E>
+__device__ __forceinline__ Part slice_sums64(const float (&x)[E], Scale c, double* red, float* redm) {
+  const int t = threadIdx.x, w = t >> 6;
+  float m = x[0];
+  bool nan = false;
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    m = fmaxf(m, x[i]);
+    nan |= x[i] != x[i];
+  }
+  m = wave_max(m);
+  if ((t & 63) == 0) redm[w] = m;
+  __syncthreads();
+  m = fmaxf(fmaxf(redm[0], redm[1]), fmaxf(redm[2], redm[3]));
+  double s[2] = {0.0, 0.0};
+  if (m > -INFINITY) {
+#pragma unroll
+    for (int i = 0; i < E; ++i) s[i & 1] += weight_or_tiny(x[i], m, c);
+  }
+  const double v = wave_sum(nan || m == INFINITY ? NAN : s[0] + s[1]);
+  if ((t & 63) == 0) red[w] = v;
+  __syncthreads();
+  return Part{red[0] + red[1] + (red[2] + red[3]), 0.0, m, 0.f};
 }
 
 template <class T, int E>
@@ -284,7 +349,7 @@ __global__ __launch_bounds__(kThreads, 4) void logprobs_slice_kernel(const typen
   const int a = lead<T>(p);
   float v[E], best[E / T::kVec];
   load_slice<T, E, true>(p, a, V, slice, v);
-  const Part r = slice_sums<T, E, true>(v, c, red, redm, best);
+  const Part r = slice_sums<T, E>(v, c, red, redm, best);
   if (threadIdx.x == 0) parts[id] = r;
   if (n > 0) slice_top<T, E>(v, best, slice, a, V, n, top, keys + id * n);
 }
@@ -335,7 +400,7 @@ __global__ __launch_bounds__(kRowThreads) void logprobs_row_kernel(
   const int a = lead<T>(p);
   float v[E], best[E / T::kVec];
   load_slice<T, E, true, kRowThreads>(p, a, V, 0, v);
-  const Part r = slice_sums<T, E, true, kRowThreads>(v, c, red, redm, best);
+  const Part r = slice_sums<T, E, kRowThreads>(v, c, red, redm, best);
   if (n > 0) {
     slice_top<T, E, kRowThreads>(v, best, 0, a, V, n, top, keys);
     __syncthreads();
@@ -463,19 +528,19 @@ struct Mass {
 
 // Sums of every valid row's slices.
 template <class T, int E>
-__global__ __launch_bounds__(kThreads) void verify_sums_kernel(Rows rows, int K, int V, int S, float c,
+__global__ __launch_bounds__(kThreads) void verify_sums_kernel(Rows rows, int K, int V, int S, Scale c,
                                                                const int32_t* __restrict__ kb,
                                                                Part* __restrict__ parts) {
-  __shared__ double red[8];
+  __shared__ double red[4];
   __shared__ float redm[4];
   const int64_t id = blockIdx.x;
   const int slice = (int)(id % S), r = (int)(id / S), b = r / (2 * K + 1), i = r % (2 * K + 1);
   const int n = drafts(kb, b, K);
   if (n == 0 || (i <= K ? i > n : i - K - 1 >= n)) return;
   const typename T::raw* p = row_of<T>(rows, b, i, K);
-  float v[E], best[E / T::kVec];
+  float v[E];
   load_slice<T, E>(p, lead<T>(p), V, slice, v);
-  const Part q = slice_sums<T, E, false>(v, c, red, redm, best);
+  const Part q = slice_sums64<T, E>(v, c, red, redm);
   if (threadIdx.x == 0) parts[id] = q;
 }
 
@@ -528,23 +593,33 @@ __global__ __launch_bounds__(kThreads) void verify_join_kernel(Rows rows, int K,
     }
   __syncthreads();
   if (t >= 64) return;
-  double qx = NAN, px = NAN;  // log q_j(x_j), log p_j(x_j) of draft j = lane + 1
+  // The log-ratio of draft j = lane + 1: -inf where q has nothing for the draft, whatever p has.  Rows of
+  // the same values (up to one offset) give exactly the same (x - m) / T; their sums differ by the
+  // order in which they were added, since rows start at other places of a 16-byte vector: at most
+  // 160 roundings each (the largest vocabulary's 2049 slices by 16 lanes, 25 inside a slice), 2^-44.6 of
+  // their ratio.  So less than kSame is a ratio of 1, and an alpha that near to 1 is 1: its h_j is then 1
+  // and not a quotient of roundings.
+  constexpr double kSame = 0x1p-44;
+  double ell = NAN;
   if (lane < n) {
-    auto logp = [&](const Law& l, float x) {
-      if (l.S == 0.0) return -(double)INFINITY;
-      if (!(l.S > 0.0) || !isfinite(l.S)) return (double)NAN;
-      return known ? ((double)x - (double)l.m) * inv_t - l.logS : -(double)INFINITY;
-    };
-    qx = logp(law[lane], xq);
-    px = logp(law[K + 1 + lane], xp);
+    const Law &lq = law[lane], &lp = law[K + 1 + lane];
+    const bool okq = lq.S >= 0.0 && isfinite(lq.S), okp = lp.S >= 0.0 && isfinite(lp.S);
+    if (okq && okp) {
+      if (lq.S == 0.0 || xq == -INFINITY)
+        ell = -(double)INFINITY;
+      else if (lp.S == 0.0 || xp == -INFINITY)
+        ell = (double)INFINITY;
+      else
+        ell = (((double)xq - (double)lq.m) * inv_t - ((double)xp - (double)lp.m) * inv_t) - (lq.logS - lp.logS);
+      if (fabs(ell) < kSame) ell = 0.0;
+    }
   }
-  // log_ratio: -inf where q has nothing for the draft, whatever p has
-  const double ell = qx == -(double)INFINITY && px == px ? -(double)INFINITY : qx - px;
   const double use = ell == ell ? ell : -(double)INFINITY;  // no law: rejected
   double acc = 0.0, mine = 0.0;
   for (int i = 0; i < n; ++i) {
     const double e = __shfl(use, i);
     acc = acc == -(double)INFINITY ? acc : fmin(0.0, acc + e);
+    if (acc > -kSame) acc = 0.0;
     if (i == lane) mine = acc;
   }
   if (lane < K) {
@@ -570,17 +645,16 @@ __global__ __launch_bounds__(kThreads) void verify_join_kernel(Rows rows, int K,
   }
 }
 
-// max(0, eq A - ep B), NaN for NaN; exactly 0 where the two are the same numbers (both products rounded).
-__device__ __forceinline__ float excess_of(float eq, float A, float ep, float B) {
+// max(0, A wq - B wp), exactly 0 where the two are the same numbers (both products rounded).
+__device__ __forceinline__ double excess_of(double A, double wq, double B, double wp) {
 #pragma clang fp contract(off)
-  const float q = eq * A, p = ep * B;
-  const float d = q - p;
-  return d > 0.f ? d : d != d ? d : 0.f;
+  const double q = A * wq, p = B * wp;
+  return fmax(q - p, 0.0);
 }
 
 // The slices of v_j for j = 1..K_b - 1: rows j (0-based) of target and draft.
 template <class T, int E>
-__global__ __launch_bounds__(kThreads) void verify_excess_kernel(Rows rows, int K, int V, int S, float c,
+__global__ __launch_bounds__(kThreads) void verify_excess_kernel(Rows rows, int K, int V, int S, Scale c,
                                                                  const int32_t* __restrict__ kb,
                                                                  const Law* __restrict__ laws,
                                                                  const double* __restrict__ la,
@@ -590,23 +664,18 @@ __global__ __launch_bounds__(kThreads) void verify_excess_kernel(Rows rows, int 
   const int slice = (int)(id % S), r = (int)(id / S), b = r / (K - 1), j = r % (K - 1) + 1;
   if (j >= drafts(kb, b, K)) return;
   const Law q = laws[(int64_t)b * (2 * K + 1) + j], p = laws[(int64_t)b * (2 * K + 1) + K + 1 + j];
-  // alpha q and p are products of an exponential against the row's maximum and
-  // one factor, so a factor's rounding (2^-24) is all that scales them
-  const float A = q.S == 0.0 ? 0.f : (float)(exp(la[(int64_t)b * K + j - 1]) / q.S);
-  const float B = p.S == 0.0 ? 0.f : (float)(1.0 / p.S);
+  const double A = q.S == 0.0 ? 0.0 : exp(la[(int64_t)b * K + j - 1]) / q.S;
+  const double B = p.S == 0.0 ? 0.0 : 1.0 / p.S;
   const float mq = q.S == 0.0 ? 0.f : q.m, mp = p.S == 0.0 ? 0.f : p.m;
   const typename T::raw *pq = row_of<T>(rows, b, j, K), *pp = row_of<T>(rows, b, K + 1 + j, K);
   float x[E], y[E];
   const int a = lead<T>(pq);
   load_slice<T, E>(pq, a, V, slice, x);
   load_slice<T, E>(pp, a, V, slice, y);
-  float s[4] = {0.f, 0.f, 0.f, 0.f};
+  double s[2] = {0.0, 0.0};
 #pragma unroll
-  for (int i = 0; i < E; ++i) {
-    const float eq = __builtin_amdgcn_exp2f((x[i] - mq) * c), ep = __builtin_amdgcn_exp2f((y[i] - mp) * c);
-    s[i & 3] += excess_of(eq, A, ep, B);
-  }
-  const double sum = wave_sum((double)s[0] + s[1] + ((double)s[2] + s[3]));
+  for (int i = 0; i < E; ++i) s[i & 1] += excess_of(A, weight_or_tiny(x[i], mq, c), B, weight_or_tiny(y[i], mp, c));
+  const double sum = wave_sum(isfinite(A) && isfinite(B) ? s[0] + s[1] : NAN);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = sum;
   __syncthreads();
   if (threadIdx.x == 0) excess[((int64_t)b * K + j) * S + slice] = red[0] + red[1] + (red[2] + red[3]);
@@ -676,28 +745,10 @@ __device__ __forceinline__ Pair<T> drawn_rows(const Rows& rows, int b, int K, in
   return r;
 }
 
-// 2^x for x <= 0 in float64, NaN for NaN: the whole part goes to the exponent (taken from the
-// low bits of x + 1.5 2^52, which end at the units), the rest, at most a half in size, is the
-// series of e^{r log 2} to its eleventh power (the next is below 7e-15 of it).  0 below 2^-1000.
-__device__ __forceinline__ double pow2(double x) {
-  constexpr double magic = 0x1.8p52, k = 0.69314718055994530942;
-  const double z = x + magic, r = x - (z - magic);
-  double c[12] = {1.0};
-#pragma unroll
-  for (int i = 1; i < 12; ++i) c[i] = c[i - 1] * (k / i);
-  double p = c[11];
-#pragma unroll
-  for (int i = 10; i >= 0; --i) p = fma(p, r, c[i]);
-  const uint64_t v = __builtin_bit_cast(uint64_t, p) + ((uint64_t)(uint32_t)__builtin_bit_cast(uint64_t, z) << 52);
-  return x < -1000.0 ? 0.0 : __builtin_bit_cast(double, v);
-}
-// e^{(x - m) / T} of one element, c = log2(e) / T.
-__device__ __forceinline__ double weight(float x, float m, double c) { return pow2(((double)x - (double)m) * c); }
-
 // Slices of the two rows' sums, behind block verification's decision where there is one (excess).
 template <class T, int E>
 __global__ __launch_bounds__(kThreads) void draw_sums_kernel(
-    Rows rows, int K, int V, int S, double c, const int32_t* __restrict__ kb, const double* __restrict__ uniforms,
+    Rows rows, int K, int V, int S, Scale c, const int32_t* __restrict__ kb, const double* __restrict__ uniforms,
     const uint32_t* __restrict__ round, uint64_t seed, const Law* __restrict__ laws, const double* __restrict__ la,
     const double* __restrict__ excess, int Se, int32_t* __restrict__ tau, float* __restrict__ lar,
     uint64_t* __restrict__ coins, Mass* __restrict__ sums, uint32_t* __restrict__ arrived) {
@@ -806,7 +857,7 @@ __device__ __forceinline__ Residual residual_of(const Pair<T>& r, int b, int K, 
 }
 // (two rounded products: equal laws differ by exactly 0.  One of them unrounded, in a fused
 // operation, would leave the other's rounding, of which half is positive and would be drawn from.)
-__device__ __forceinline__ double residual_weight(const Residual& f, float x, float y, double c) {
+__device__ __forceinline__ double residual_weight(const Residual& f, float x, float y, Scale c) {
 #pragma clang fp contract(off)
   const double q = f.A * weight(x, f.mq, c), p = f.B * weight(y, f.mp, c);
   const double w = q - p;
@@ -828,7 +879,7 @@ __device__ __forceinline__ Two<T> load_two(const Pair<T>& r, bool with_p, int V,
 }
 // The residual's weights of such a pair; their sum.
 template <class T>
-__device__ __forceinline__ double residual_vector(const Residual& f, const Two<T>& v, bool with_p, double c,
+__device__ __forceinline__ double residual_vector(const Residual& f, const Two<T>& v, bool with_p, Scale c,
                                                   double (&w)[T::kVec]) {
   double sum = 0.0;
   if (with_p) {
@@ -849,7 +900,7 @@ __device__ __forceinline__ double residual_vector(const Residual& f, const Two<T
 // so which one it is changes nothing.
 template <class T, int E>
 __global__ __launch_bounds__(kThreads) void draw_token_kernel(
-    Rows rows, int K, int V, int S, int mode, double c, const int32_t* __restrict__ kb,
+    Rows rows, int K, int V, int S, int mode, Scale c, const int32_t* __restrict__ kb,
     const int32_t* __restrict__ taus, const double* __restrict__ uniforms, const uint32_t* __restrict__ round,
     uint64_t seed, const Law* __restrict__ laws, const double* __restrict__ la, const Mass* __restrict__ sums,
     double* __restrict__ mass, uint32_t* __restrict__ arrived, int32_t* __restrict__ token) {
@@ -1051,12 +1102,14 @@ VerifyWs verify_layout(int B, int K, int V) {
   return w;
 }
 
+Scale scale_of(double inv_t) { return Scale{inv_t * kLog2e, -1000.0 / (inv_t * kLog2e)}; }
+
 template <class T, int E>
 hipError_t verify_run(const Rows& rows, int B, int K, int V, int mode, double inv_t, const int32_t* tokens,
                       const int32_t* kb, const double* uniforms, const uint32_t* round, uint64_t seed, int32_t* tau,
                       float* lar, float* ratio, uint64_t* coins, char* ws, const VerifyWs& w, hipStream_t s) {
   const int S = slices(V, E);
-  const float c = (float)(inv_t * kLog2e);
+  const Scale c = scale_of(inv_t);
   Part* parts = reinterpret_cast<Part*>(ws + w.parts);
   Law* laws = reinterpret_cast<Law*>(ws + w.laws);
   double *la = reinterpret_cast<double*>(ws + w.la), *excess = reinterpret_cast<double*>(ws + w.excess);
@@ -1076,7 +1129,7 @@ hipError_t draw_run(const Rows& rows, int B, int K, int V, int Se, int mode, dou
                     const double* uniforms, const uint32_t* round, uint64_t seed, int32_t* tau, int32_t* token,
                     float* lar, uint64_t* coins, char* ws, const VerifyWs& w, hipStream_t s) {
   const int S = slices(V, E);
-  const double c = inv_t * kLog2e;
+  const Scale c = scale_of(inv_t);
   const Law* laws = reinterpret_cast<const Law*>(ws + w.laws);
   const double *la = reinterpret_cast<const double*>(ws + w.la),
                *excess = reinterpret_cast<const double*>(ws + w.excess);

@@ -1,5 +1,11 @@
 """sd_verify_tokens where draft and target laws are equal, next to equal or none, and
 uniforms next to 1, against the float64 oracle.
+
+What the kernels compute in float64, with u = 2^-53: a weight e^{(x - m) / T} is off by
+4e-16 (the end of its series), 40 u (a rounded factor; |x - m| / T up to 40 matters) and 4 u
+relative, a row's sum of weights by that and 160 u (its additions, at most), so log S
+by less than 3e-14, a log-ratio by 6e-14 and log alpha_j by 6e-14 j.  Log-ratios and
+distances of alpha_j from 1 below 2^-44 = 5.7e-14 are taken for 0.
 """
 import numpy as np
 import pytest
@@ -109,3 +115,73 @@ def test_a_uniform_on_a_border_draws_a_token():
             x = int(r["token"][b])
             assert x in allowed[b], (b, u, x)
             assert abs(allowed[b].index(x) - u * n) <= 1.0 + 1e-9, (b, u, x)
+
+
+@pytest.mark.parametrize("t,near", [("f32", 1e-2), ("f32", 1e-3), ("f32", 1e-4), ("f32", 1e-6), ("f16", 1e-3), ("bf16", 1e-2)])
+@pytest.mark.parametrize("B,V", [(24, 30011), (200, 2049)])
+def test_coins_of_laws_that_are_next_to_equal(t, near, B, V):
+    """h = v / (v + 1 - alpha) divides two numbers of the laws' difference.
+
+    dh = ((1 - alpha) dv + v dalpha) / (v + 1 - alpha)^2 is at most (dv + dalpha) / (v + 1 - alpha);
+    dalpha is 12e-14 j (above), dv no more than dalpha and two sums' 3e-14 each: with j <= 3 and the
+    oracle's own share 1e-12 in all.  Every coin's uniform is put that far below or above its h."""
+    K = 3
+    draft, target, tokens, kb, un = tok._blocks(B, K, V, t, 61, near=near)
+    kb.fill_(K)
+    d, q = draft.double().cpu().numpy(), target.double().cpu().numpy()
+    x, u = tokens.cpu().numpy(), un.cpu().numpy()
+    moved = 0
+    for b in range(B):
+        w = otok.verify_chain(d[b], q[b], x[b], K, u[b, :K], 0.5)
+        la = [0.0]
+        for j in range(K):
+            la.append(min(0.0, la[j] + w["ell"][j]))
+        for j in range(1, K + 1):
+            a = np.exp(la[j])
+            if j < K and a < 1.0:
+                v = np.maximum(0.0, np.exp(otok.row_law(q[b, j]) + la[j]) - np.exp(otok.row_law(d[b, j]))).sum()
+                margin = 1e-12 / (v + 1.0 - a)
+            else:
+                margin = 1e-12
+            side = 1 if (b + j) % 2 else -1
+            u[b, j - 1] = min(max(w["h"][j - 1] + side * margin, 2.0 ** -60), 1.0 - 2.0 ** -53)
+            moved += 0.0 < w["h"][j - 1] < 1.0
+    assert moved > B
+    r = _lib.sd_verify_tokens(draft, target, tokens, kb, uniforms=torch.tensor(u, device=DEV))
+    coins, tau, lar = (r[k].cpu().numpy() for k in ("coins", "tau", "log_alpha_res"))
+    for b in range(B):
+        w = otok.verify_chain(d[b], q[b], x[b], K, u[b, :K], 0.5)
+        assert coins[b] == w["coins"] and tau[b] == w["tau"], (b, coins[b], w["coins"], w["h"], u[b])
+        assert abs(lar[b] - w["log_alpha_res"]) <= 2.0 ** -24 * abs(w["log_alpha_res"]) + 2e-13
+
+
+@pytest.mark.parametrize("mode", MODES)
+@pytest.mark.parametrize("t", list(tok.TYPES))
+@pytest.mark.parametrize("V", [2049, 50001])
+def test_equal_laws_at_other_alignments_are_equal(V, t, mode):
+    """Rows of an odd number of logits start at other places of a 16-byte vector, so that the sums of
+    equal rows differ by their order: alpha_j is 1 all the same, and h_j with it."""
+    B, K = 24, 4
+    draft, target, tokens, kb, un = _equal(B, K, V, t, 71)
+    kb[::3] = K - 1
+    last = kb.long() - 1
+    tokens[torch.arange(B, device=DEV), last] = V  # the block's last draft is rejected, and no other
+    un[:, :K] = 0.9
+    r = _lib.sd_verify_tokens(draft, target, tokens, kb, uniforms=un, mode=mode)
+    assert torch.equal(r["tau"], kb) and (r["log_alpha_res"] == 0).all()
+    held = r["log_ratio"][torch.arange(K, device=DEV)[None] < last[:, None]]
+    assert (held == 0).all()
+    assert tok._check_verify(draft, target, tokens, kb, un, mode, 1.0, r) == (B, B)
+
+
+@pytest.mark.parametrize("t,V", [("f32", 50001), ("f32", 131072), ("bf16", 50001), ("f16", 8193)])
+def test_log_ratios_are_rounded_once(t, V):
+    """What float64 gives (6e-14, above) rounded to float32: a coin's threshold has no fewer bits."""
+    draft, target, tokens, kb, un = tok._blocks(5, 4, V, t, 81)
+    kb.fill_(4)
+    got = _lib.sd_verify_tokens(draft, target, tokens, kb, uniforms=un)["log_ratio"].cpu().numpy()
+    d, q, x = draft.double().cpu().numpy(), target.double().cpu().numpy(), tokens.cpu().numpy()
+    for b in range(5):
+        for j in range(4):
+            want = otok.row_law(q[b, j])[x[b, j]] - otok.row_law(d[b, j])[x[b, j]]
+            assert abs(got[b, j] - want) <= 2.0 ** -24 * abs(want) + 1e-13, (b, j, got[b, j], want)
