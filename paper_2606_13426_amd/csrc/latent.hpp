@@ -16,8 +16,8 @@
 // step meet the instruction's k places is the one those loads give, and P is
 // stored to match.
 //
-// m is a reference and not the maximum: it moves when a score exceeds it by kSlack,
-// so the rescaling of O is left out of almost every tile.
+// m is a reference and not the maximum: it moves when a score exceeds it by more than it
+// is allowed to (reach), so the rescaling of O is left out of almost every tile.
 //
 // Tiles come by loads that write LDS directly, the next one while this one is
 // multiplied.  A token's 16-byte pieces are permuted inside each 128 bytes by
@@ -430,8 +430,8 @@ __global__ __launch_bounds__(R == 1 ? 256 : 512) void latent_kernel(Args a) {
 #pragma unroll
       for (int j = 0; j < WT; ++j) mx = fmaxf(mx, red[j][16 * wr + n]);
       mx *= a.c;
-      if (__any(mx > m + kSlack)) {
-        const float to = mx > m + kSlack ? mx : m, f = to == m ? 1.f : __builtin_amdgcn_exp2f(m - to);
+      if (const bool up = mx > reach<T>(m); __any(up)) {
+        const float to = up ? reference<T>(mx) : m, f = to == m ? 1.f : __builtin_amdgcn_exp2f(m - to);
         m = to;
         l *= f;
         if (wt == 0 && g == 0) fac[16 * wr + n] = f;

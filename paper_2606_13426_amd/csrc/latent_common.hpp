@@ -18,9 +18,6 @@ namespace latent {
 
 constexpr int kThreads = 256, kTile = 64;
 constexpr float kLn2 = 0.69314718f;
-// How far (in powers of 2) a score may exceed its row's reference: weights then reach 2^kSlack,
-// harmless in float32 sums and in fp16.
-constexpr float kSlack = 8.f;
 constexpr int kRope = 64;  // columns of the rotary part, zero past d_rope
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -44,6 +41,7 @@ struct Bf16 {
   }
   __device__ static float value(uint16_t v) { return __builtin_bit_cast(float, (uint32_t)v << 16); }
   static constexpr uint32_t kExponent = 0x7f80, kOne = 0x3f80;  // all exponent bits set: an infinity or NaN
+  static constexpr float kBelow = 0.f, kReach = 8.f;
 };
 struct F16 {
   typedef _Float16 x8 __attribute__((ext_vector_type(8)));
@@ -60,7 +58,25 @@ struct F16 {
   }
   __device__ static float value(uint16_t v) { return (float)__builtin_bit_cast(_Float16, v); }
   static constexpr uint32_t kExponent = 0x7c00, kOne = 0x3c00;
+  static constexpr float kBelow = 11.f, kReach = 15.f;
 };
+
+// A row's reference, in powers of 2: a weight is 2^{score - reference}.  It is set kBelow below the
+// largest score so far and moves when one exceeds it by more than kReach, so that weights reach
+// 2^kReach, harmless in float32 sums and in `type`.  fp16 has its normal range down to 2^-14 and steps of
+// 2^-24 below: with the largest weight between 2^11 and 2^15 those down to 2^-25 of it
+// keep half a step of 2^-11, and a smaller one loses 2^-36 of it at most (a reference at the largest score:
+// 2^-14 and 2^-25, so that thousands of keys 17 nats below one of value 0 were a third
+// off).  Scores of 2^20 and more, which are as coarse as an eighth, keep the margin of 2^8.
+constexpr float kCoarse = 0x1p20f;
+template <class T>
+__device__ __forceinline__ float reference(float mx) {
+  return T::kBelow > 0.f && fabsf(mx) < kCoarse ? mx - T::kBelow : mx;
+}
+template <class T>
+__device__ __forceinline__ float reach(float m) {
+  return m + (T::kReach > 8.f && fabsf(m) < kCoarse ? T::kReach : 8.f);
+}
 
 // Bits 15 and 31 of the result say which halves of v hold an infinity or NaN (one
 // more at the lowest place of a full exponent carries into the cleared sign).

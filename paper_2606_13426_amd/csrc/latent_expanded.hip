@@ -13,8 +13,8 @@
 // places along k are free to mean any keys as long as V^T, read by transposing LDS
 // loads, has the same order.  No value of S or P passes through LDS.
 //
-// m is a reference and not the maximum: it moves when a score exceeds it by
-// kSlack, so the rescaling of O is left out of almost every tile.
+// m is a reference and not the maximum: it moves when a score exceeds it by more than
+// it is allowed to (reach), so the rescaling of O is left out of almost every tile.
 //
 // Tiles (K rotary and not, V) come by loads that write LDS directly, into the other
 // of two buffers while this one is multiplied; one barrier a tile.  80 KB of LDS
@@ -259,9 +259,9 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_kernel(Expanded a) {
     for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[1][i]);
     mx = across(mx, true, true) * a.c;
     // (a NaN score passes the maximum over and makes its row NaN by its weight)
-    const bool up = mx > m + kSlack || (m == -INFINITY && mx > -INFINITY);
+    const bool up = mx > reach<T>(m);
     if (__any(up)) {
-      const float to = up ? mx : m, f = up ? __builtin_amdgcn_exp2f(m - to) : 1.f;
+      const float to = up ? reference<T>(mx) : m, f = up ? __builtin_amdgcn_exp2f(m - to) : 1.f;
 #pragma unroll
       for (int k = 0; k < NV; ++k) o[k] *= f;
       l *= f;
