@@ -435,7 +435,7 @@ typedef struct {
  *   s_j = scale q . c_j,  lse = log sum_j e^{s_j},  out = sum_j e^{s_j - lse} c_j[0..d_latent).
  * A row that sees no token has out 0 and lse -inf.  Rows i >= n_b are not read
  * or written.  Tokens that a row does not see have no part in it, whatever they
- * hold.
+ * hold; an infinite value that it sees gives NaN where its weight is rounded to 0.
  * Token j of sequence b lies in page pages[b][j / page_size], at place j % page_size;
  * with pages NULL in page b (n_pages >= B): a plain [B][page_size] cache.  A token
  * whose page is outside [0, n_pages) counts as unseen by every row.  lens is

@@ -293,15 +293,26 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_kernel(Expanded a) {
         // what they give to the rows that see them, and zeros in their place
         const int hh = ln >> 5, row_lim = lim - tl * kTile;
 #pragma clang loop unroll(disable)
-        for (int j = from; j < kTile; ++j)
+        for (int j = from; j < kTile; ++j) {
+          // the row's weight for key j, as the product takes it: its score is one of this lane's or of the
+          // row's other lane's
+          const int at = 16 * (j >> 5) + 4 * (j >> 3 & 3) + (j & 3);
+          float score = 0.f;
+#pragma unroll
+          for (int i = 0; i < 32; ++i) score = i == at ? s[i >> 4][i & 15] : score;
+          uint32_t lower = __builtin_bit_cast(uint32_t, score), upper = lower;
+          swap32(lower, upper);
+          score = __builtin_bit_cast(float, j >> 2 & 1 ? upper : lower);
+          const float p = T::value((uint16_t)T::pack(__builtin_amdgcn_exp2f(__fmaf_rn(score, a.c, -ref)), 0.f));
 #pragma unroll
           for (int k = 0; k < NV; ++k)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
               const int col = 32 * k + 8 * (i >> 2) + 4 * hh + (i & 3), pc = (col >> 3 & ~7) | ((col >> 3 ^ perm(j)) & 7);
               const uint32_t v = lds_read<uint16_t>(here + kV + j * DV * 2 + pc * 16 + 2 * (col & 7));
-              if ((v & T::kExponent) == T::kExponent && j < row_lim) o[k][i] += T::value((uint16_t)v);
+              if ((v & T::kExponent) == T::kExponent && j < row_lim) o[k][i] += p * T::value((uint16_t)v);
             }
+        }
         lds_barrier();
         for (int i = from * DV + rare(t); i < kTile * DV; i += kThreads) {
           const Lds at = here + kV + 2 * i;
