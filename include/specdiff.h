@@ -444,9 +444,10 @@ typedef struct {
  * [B][Q][H][d_latent] of `type` (SD_TYPE_BF16 or SD_TYPE_F16); lse [B][Q][H],
  * nullable.  d_latent a multiple of 8 in [8, 512], d_rope a multiple of 8 in
  * [0, 64]; q, cache and out at 16-byte addresses, their strides multiples of 8
- * elements and at least what they step over.  The products take q and cache as they
- * are and the softmax's weights rounded to `type`, and add in float32: half a step each,
- * in fp16 of the weights above 2^-25 of a row's largest (2^-36 of it for smaller ones).
+ * elements and at least what they step over (out's so that no two rows lie in one
+ * place).  The products take q and cache as they are and the softmax's weights rounded
+ * to `type` (half a step each, in fp16 of those above 2^-25 of a row's largest; 2^-36 of
+ * the largest for smaller ones), and add in float32.
  * ws: >= sd_latent_attention_workspace bytes, 256-byte aligned. */
 size_t sd_latent_attention_workspace(int32_t B, int32_t Q, int32_t H, int32_t d_latent, int32_t d_rope);
 sd_status sd_latent_attention(int32_t B, int32_t Q, int32_t H, int32_t d_latent, int32_t d_rope,

@@ -12,6 +12,7 @@
 #include <mutex>
 #include <string>
 #include <thread>
+#include <utility>
 #include <vector>
 
 #include "common.hpp"
@@ -1112,12 +1113,24 @@ static bool latent_shape_ok(int32_t B, int32_t Q, int32_t H, int32_t dc, int32_t
          dr >= 0 && dr <= 64 && dr % 8 == 0;
 }
 // Strides of a [seq][rows][heads][d] view: multiples of 8 elements, a head's d apart at least, and
-// no two rows in one place (rows over heads or heads over rows).
+// no two rows of a sequence in one place (rows over heads or heads over rows).
 static bool stride_h_ok(sd_stride_h s, int seqs, int rows, int heads, int d) {
   const int64_t row = rows == 1 ? 0 : s.row, head = heads == 1 ? 0 : s.head, seq = seqs == 1 ? 0 : s.seq;
   return row % 8 == 0 && head % 8 == 0 && seq % 8 == 0 && (heads == 1 || head >= d) && (rows == 1 || row >= d) &&
          (seqs == 1 || seq >= d) &&
          (heads == 1 || rows == 1 || row >= heads * head || head >= rows * row);
+}
+// No two heads of an output in one place: each stride steps over all that the smaller ones reach.
+static bool apart(sd_stride_h s, int seqs, int rows, int heads, int d) {
+  std::pair<int64_t, int64_t> by[3] = {{s.seq, seqs}, {s.row, rows}, {s.head, heads}};
+  std::sort(by, by + 3);
+  __int128 reach = d;
+  for (const auto& [stride, count] : by) {
+    if (count == 1) continue;
+    if (stride < reach) return false;
+    reach += (__int128)stride * (count - 1);
+  }
+  return true;
 }
 
 size_t sd_latent_attention_workspace(int32_t B, int32_t Q, int32_t H, int32_t d_latent, int32_t d_rope) {
@@ -1152,7 +1165,8 @@ sd_status sd_latent_attention(int32_t B, int32_t Q, int32_t H, int32_t d_latent,
                    (n_pages == 1 || page_stride >= (int64_t)page_size * token_stride),
                "sd_latent_attention: cache strides must be multiples of 8 elements that step over a token and a page");
   SD_CHECK_ARG(stride_h_ok(qs, B, Q, H, d), "sd_latent_attention: q strides must be multiples of 8 elements that step over a row");
-  SD_CHECK_ARG(stride_h_ok(os, B, Q, H, d_latent), "sd_latent_attention: out strides must be multiples of 8 elements that step over a row");
+  SD_CHECK_ARG(stride_h_ok(os, B, Q, H, d_latent) && apart(os, B, Q, H, d_latent),
+               "sd_latent_attention: out strides must be multiples of 8 elements that step over a row, no two rows in one place");
   SD_CHECK_ARG(aligned(q, 16) && aligned(cache, 16) && aligned(out, 16), "sd_latent_attention: q, cache and out must be 16-byte aligned");
   const size_t need = latent_ws_bytes(B, Q, H, d_latent);
   SD_CHECK_ARG(ws_bytes >= need, "sd_latent_attention: workspace %zu < %zu bytes", ws_bytes, need);
