@@ -468,8 +468,8 @@ sd_status sd_latent_attention(int32_t B, int32_t Q, int32_t H, int32_t d_latent,
  * A row that sees no key has out 0 and lse -inf; keys that a row does not see have no
  * part in it, whatever they hold.  Rows of no sequence are not read or written.
  * cu_q, cu_k [n+1] rise from >= 0 to <= Tq, <= Tk (values outside are clamped).
- * All of one 16-bit `type` with float32 sums as in sd_latent_attention; d_nope and d_v
- * multiples of 8 in [8, 128], d_rope of 8 in [0, 64]; pointers at 16-byte addresses
+ * All of one 16-bit `type` with float32 sums as in sd_latent_attention; H <= 65535, d_nope and
+ * d_v multiples of 8 in [8, 128], d_rope of 8 in [0, 64]; pointers at 16-byte addresses
  * (k_rope too, not read where d_rope = 0: NULL then), strides (row: a token's,
  * head; seq is not read) multiples of 8 elements below 2^24 that step over a head's
  * elements; out [Tq][H][d_v]; lse [Tq][H], nullable.

@@ -1106,7 +1106,9 @@ static bool type_ok(sd_type t) { return t == SD_TYPE_F32 || t == SD_TYPE_BF16 ||
 static size_t type_size(sd_type t) { return t == SD_TYPE_F32 ? 4 : 2; }
 static bool aligned(const void* p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 static bool temperature_ok(double t) { return t >= 0x1p-60 && t <= 0x1p60; }
-constexpr int64_t kMaxGroups = ((int64_t)1 << 31) - 1;  // workgroups of a launch
+// What a launch holds: fewer than 2^32 threads in its first dimension (workgroups of 256 here), and 65535
+// workgroups in its second.
+constexpr int64_t kMaxGroups = (((int64_t)1 << 32) - 1) / 256, kMaxGroupsY = 65535;
 
 static bool latent_shape_ok(int32_t B, int32_t Q, int32_t H, int32_t dc, int32_t dr) {
   return B >= 1 && Q >= 1 && H >= 1 && (int64_t)Q * H <= ((int64_t)1 << 30) / B && dc >= 8 && dc <= 512 && dc % 8 == 0 &&
@@ -1179,7 +1181,8 @@ sd_status sd_latent_attention(int32_t B, int32_t Q, int32_t H, int32_t d_latent,
 static bool expanded_shape_ok(int32_t n, int32_t H, int32_t dn, int32_t dr, int32_t dv, int32_t Tq, int32_t Tk) {
   return n >= 1 && H >= 1 && Tq >= 1 && Tk >= 1 && dn >= 8 && dn <= 128 && dn % 8 == 0 && dv >= 8 && dv <= 128 &&
          dv % 8 == 0 && dr >= 0 && dr <= 64 && dr % 8 == 0 && Tk < (1 << 30) && n < (1 << 24) &&
-         (int64_t)Tq * H <= ((int64_t)1 << 30) && expanded_groups(n, H, Tq, Tk) <= kMaxGroups;
+         (int64_t)Tq * H <= ((int64_t)1 << 30) && expanded_groups(n, H, Tq, Tk) <= kMaxGroups && H <= kMaxGroupsY &&
+         expanded_groups(n, H, Tq, Tk) * H < ((int64_t)1 << 31);
 }
 static bool token_stride_ok(sd_stride_h s, int tokens, int heads, int d) {
   return stride_h_ok(sd_stride_h{0, s.row, s.head}, 1, tokens, heads, d) && (tokens == 1 || s.row < (1 << 24)) &&
@@ -1246,7 +1249,7 @@ sd_status sd_token_logprobs(int32_t rows, int32_t V, sd_type type, const void* l
   const size_t need = logprobs_ws_bytes(rows, V, n_top);
   SD_CHECK_ARG(ws_bytes >= need, "sd_token_logprobs: workspace %zu < %zu bytes", ws_bytes, need);
   SD_CHECK_ARG(aligned(ws, 256), "sd_token_logprobs: workspace must be 256-byte aligned");
-  SD_CHECK_ARG(logprobs_groups(rows, V) <= kMaxGroups, "sd_token_logprobs: too many rows for one call");
+  SD_CHECK_ARG(logprobs_groups(rows, V, type) <= kMaxGroups, "sd_token_logprobs: too many rows for one call");
   SD_HIP(logprobs_launch(rows, V, type, logits, row_stride, temperature, n_tok, tokens, logprob, entropy, lse, n_top,
                          top_ids, top_logprob, ws, (hipStream_t)stream));
   return SD_OK;

@@ -289,7 +289,7 @@ hipError_t latent_launch(int B, int Q, int H, int dc, int dr, sd_type type, doub
                          const void* cache, int64_t page_stride, int64_t token_stride, int n_pages, int page_size,
                          const int32_t* pages, int64_t pages_stride, int max_pages, const int32_t* lens,
                          const int32_t* rows, void* out, sd_stride_h os, float* lse, void* ws, hipStream_t s);
-int64_t expanded_groups(int n, int H, int Tq, int Tk);
+int64_t expanded_groups(int n, int H, int Tq, int Tk);  // workgroups a head
 size_t expanded_ws_bytes(int n, int H, int dn, int dv, int Tq, int Tk);
 hipError_t expanded_launch(int n, int H, int dn, int dr, int dv, sd_type type, double scale, int Tq, const void* q,
                            sd_stride_h qs, int Tk, const void* k, sd_stride_h ks, const void* kr, int64_t kr_stride,
@@ -297,7 +297,7 @@ hipError_t expanded_launch(int n, int H, int dn, int dr, int dv, sd_type type, d
                            sd_stride_h os, float* lse, void* ws, hipStream_t s);
 // Workgroups of the widest launch, workspace and launches of sd_token_logprobs
 // and sd_verify_tokens.
-int64_t logprobs_groups(int rows, int V);
+int64_t logprobs_groups(int rows, int V, sd_type type);
 size_t logprobs_ws_bytes(int rows, int V, int n_top);
 hipError_t logprobs_launch(int rows, int V, sd_type type, const void* x, int64_t ld, double temperature, int n_tok,
                            const int32_t* tokens, float* logprob, float* entropy, float* lse, int n_top,

@@ -443,8 +443,9 @@ size_t expanded_ws_bytes(int n, int H, int dn, int dv, int Tq, int Tk) {
   const size_t rows = (size_t)split * Tq * H;
   return up256(rows * padded_dv(dn, dv) * sizeof(float)) + up256(rows * sizeof(float2));
 }
+// Workgroups a head.
 int64_t expanded_groups(int n, int H, int Tq, int Tk) {
-  return (int64_t)tiles_of(Tq, n) * H * split_of(n, H, Tq, Tk);
+  return (int64_t)tiles_of(Tq, n) * split_of(n, H, Tq, Tk);
 }
 
 hipError_t expanded_launch(int n, int H, int dn, int dr, int dv, sd_type type, double scale, int Tq, const void* q,

@@ -1154,7 +1154,7 @@ int per_thread_alone(int64_t rows, int V) {
 
 // f with the element type's tag.
 template <class F>
-hipError_t by_type(sd_type type, F&& f) {
+auto by_type(sd_type type, F&& f) {
   return type == SD_TYPE_F32 ? f(F32{}) : type == SD_TYPE_BF16 ? f(BF16{}) : f(F16{});
 }
 
@@ -1164,7 +1164,9 @@ size_t logprobs_ws_bytes(int rows, int V, int n) {
   const size_t S = (size_t)slices(V, per_thread(rows, V));  // (as many as any type has)
   return up256(sizeof(Part) * (size_t)rows * S) + up256(sizeof(uint64_t) * (size_t)rows * S * (size_t)n);
 }
-int64_t logprobs_groups(int rows, int V) { return (int64_t)rows * slices(V, per_thread(rows, V)); }
+int64_t logprobs_groups(int rows, int V, sd_type type) {
+  return (int64_t)rows * slices(V, by_type(type, [&](auto tag) { return per_thread_alone<decltype(tag)>(rows, V); }));
+}
 
 hipError_t logprobs_launch(int rows, int V, sd_type type, const void* x, int64_t ld, double temperature, int n_tok,
                            const int32_t* tokens, float* logprob, float* entropy, float* lse, int n, int32_t* ids,

@@ -17,3 +17,22 @@ def test_sequences_of_the_output_may_not_overlap(lib, os):
                                 S(512, 128, 1024), S(1536, 1024, 128)])
 def test_outputs_nested_in_any_order_do_not(lib, os):
     abi._refused(abi._latent(lib, os=os, ws_bytes=64), "workspace 64 <")  # the check behind
+
+
+def test_more_heads_than_a_grid_holds(lib):
+    a = dict(n=1, Tq=1, Tk=1, qs=S(0, 0, 192), ks=S(0, 0, 256), vs=S(0, 0, 256), os=S(0, 0, 128))
+    abi._refused(abi._expanded(lib, H=65536, **a), "too many rows")
+    abi._refused(abi._expanded(lib, H=65535, scale=float("nan"), **a), "scale")  # the check behind
+    assert lib.sd_latent_attention_expanded_workspace(1, 65536, 128, 64, 128, 1, 8000) == 0
+
+
+@pytest.mark.parametrize("call", ["logprobs", "verify", "expanded"])
+def test_more_workgroups_than_a_launch_holds(lib, call):
+    """A launch's first dimension holds fewer than 2^32 threads: 2^24 - 1 workgroups of 256."""
+    if call == "logprobs":
+        s = abi._logprobs(lib, rows=1 << 24, V=1, ld=1, n_tok=0, n_top=0, ws_bytes=2 ** 62)
+    elif call == "verify":
+        s = abi._verify(lib, B=(1 << 24) // 3 + 1, K=1, V=1, ds=_lib.sd_stride(1, 1), ts=_lib.sd_stride(2, 1), ws_bytes=2 ** 62)
+    else:
+        s = abi._expanded(lib, n=(1 << 24) - 1, H=1, Tq=256, Tk=1 << 20, qs=S(0, 192, 192), os=S(0, 128, 128))
+    abi._refused(s, "too many rows")
