@@ -601,8 +601,8 @@ def sd_verify_tokens(draft, target, tokens, kb, uniforms=None, rnd=None, seed=0,
     _need(kb.shape == (B,) and kb.is_contiguous(), name, "kb must be contiguous [B]")
     _need(uniforms is None or (uniforms.shape == (B, K + 1) and uniforms.is_contiguous()), name,
           "uniforms must be contiguous [B][K+1]")
-    _need(rnd is None or (rnd.shape == (B,) and rnd.element_size() == 4 and rnd.is_contiguous()), name,
-          "rnd must be contiguous [B] of 32 bits")
+    _need(rnd is None or (rnd.shape == (B,) and rnd.dtype in (torch.int32, torch.uint32) and rnd.is_contiguous()), name,
+          "rnd must be contiguous [B] of int32 or uint32")
     if out is None:
         dev = draft.device
         out = dict(tau=torch.empty(B, dtype=i32, device=dev), token=torch.empty(B, dtype=i32, device=dev),
