@@ -440,6 +440,8 @@ def _operands(name, types, **tensors):
         t = tensors[what]
         if t is not None and t.dtype != want:
             _need(False, name, f"{what} must be {want}, not {t.dtype}")
+    ws = tensors.get("ws")
+    _need(ws is None or ws.is_contiguous(), name, "ws must be contiguous")
     return torch._C._cuda_getCurrentRawStream(dev)
 
 
