@@ -471,6 +471,7 @@ def sd_latent_attention(q, cache, lens, d_latent, pages=None, rows=None, scale=N
           "q must be [B][Q][H][d] and cache [n_pages][page_size][d] with contiguous d")
     B, Q, H, d = q.shape
     _need(cache.shape[2] == d and cache.dtype == q.dtype, name, "q and cache must agree in d and type")
+    _need(0 < d_latent <= d, name, f"d_latent = {d_latent} is not in [1, {d}]")
     if out is None:
         out = torch.empty(B, Q, H, d_latent, dtype=q.dtype, device=q.device)
     if lse is None:
@@ -514,6 +515,7 @@ def sd_latent_attention_expanded(q, k, k_rope, v, cu_q, cu_k, scale=None, out=No
     Tq, H, d = q.shape
     Tk, _, dn = k.shape
     dr, dv = d - dn, v.shape[2]
+    _need(dn > 0, name, "d_nope = 0")
     _need(k.shape[1] == H and tuple(v.shape[:2]) == (Tk, H) and k.dtype == v.dtype == q.dtype, name,
           "q, k and v must agree in heads, tokens and type")
     _need((k_rope is None and dr == 0) or (k_rope is not None and tuple(k_rope.shape) == (Tk, dr) and

@@ -1,5 +1,6 @@
 """Views and sizes of the language-model calls that no launch may get; none reaches a HIP call."""
 import pytest
+import torch
 
 import test_abi_lm as abi
 from paper_2606_13426_amd import _lib
@@ -36,3 +37,12 @@ def test_more_workgroups_than_a_launch_holds(lib, call):
     else:
         s = abi._expanded(lib, n=(1 << 24) - 1, H=1, Tq=256, Tk=1 << 20, qs=S(0, 192, 192), os=S(0, 128, 128))
     abi._refused(s, "too many rows")
+
+
+def test_widths_that_the_binding_cannot_split():
+    h, i = (lambda *s: torch.zeros(*s).half()), torch.zeros(3, dtype=torch.int32)
+    for d_latent in (-8, 0, 200):
+        with pytest.raises(_lib.SpecDiffError, match="d_latent = "):
+            _lib.sd_latent_attention(h(1, 1, 2, 192), h(3, 16, 192), i[:1], d_latent, scale=0.1)
+    with pytest.raises(_lib.SpecDiffError, match="d_nope = 0"):
+        _lib.sd_latent_attention_expanded(h(5, 2, 0), h(9, 2, 0), None, h(9, 2, 128), i, i)
