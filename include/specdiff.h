@@ -432,7 +432,8 @@ typedef struct {
  * value the first d_latent elements.  With n_b = rows[b] (NULL: Q) rows of sequence b
  * and len_b = lens[b] cached tokens, the last n_b of them the rows' own, row i < n_b
  * of every head sees tokens j < len_b - n_b + i + 1:
- *   s_j = scale q . c_j,  lse = log sum_j e^{s_j},  out = sum_j e^{s_j - lse} c_j[0..d_latent).
+ *   s_j = scale q . c_j,  lse = log sum_j e^{s_j},  out = sum_j e^{s_j - lse} c_j[0..d_latent)
+ * (scale: the expanded form's, (d_nope + d_rope)^-1/2 for heads of width d_nope).
  * A row that sees no token has out 0 and lse -inf.  Rows i >= n_b are not read
  * or written.  Tokens that a row does not see have no part in it, whatever they
  * hold; an infinite value that it sees gives NaN where its weight is rounded to 0.

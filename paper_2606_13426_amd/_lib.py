@@ -7,6 +7,7 @@ fallback: if the library has not been built, loading raises.
 """
 import ctypes
 import os
+import warnings
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libspecdiff.so")
@@ -461,12 +462,20 @@ def sd_latent_attention_workspace(B, Q, H, d_latent, d_rope):
 def sd_latent_attention(q, cache, lens, d_latent, pages=None, rows=None, scale=None, out=None, lse=None, ws=None):
     """q [B][Q][H][d_latent + d_rope] and cache [n_pages][page_size][d_latent + d_rope] of one
     16-bit type (last dimension contiguous); lens [B], pages [B][max_pages] (None: page b is
-    sequence b), rows [B] (None: Q rows each) int32; scale defaults to (d_latent + d_rope)^-1/2.
+    sequence b), rows [B] (None: Q rows each) int32.
+
+    scale: a model's absorbed scores are those of its expanded form, whose scale is
+    (d_nope + d_rope)^-1/2 of the heads' own width d_nope; that cannot be read off the operands.
+    Without one (d_latent + d_rope)^-1/2 is taken, with a warning: attention to the cached
+    vectors for their own sake.
 
     Returns (out [B][Q][H][d_latent], lse [B][Q][H] float32).
     """
     import torch
     name, i32 = "sd_latent_attention", torch.int32
+    if scale is None:
+        warnings.warn(f"{name}: no scale given, (d_latent + d_rope)^-1/2 is taken; a model's absorbed attention has "
+                      "(d_nope + d_rope)^-1/2", stacklevel=2)
     _need(q.dim() == 4 and cache.dim() == 3 and q.stride(3) == 1 and cache.stride(2) == 1, name,
           "q must be [B][Q][H][d] and cache [n_pages][page_size][d] with contiguous d")
     B, Q, H, d = q.shape

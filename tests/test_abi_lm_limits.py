@@ -1,4 +1,7 @@
 """Views and sizes of the language-model calls that no launch may get; none reaches a HIP call."""
+import os
+import warnings
+
 import pytest
 import torch
 
@@ -46,3 +49,19 @@ def test_widths_that_the_binding_cannot_split():
             _lib.sd_latent_attention(h(1, 1, 2, 192), h(3, 16, 192), i[:1], d_latent, scale=0.1)
     with pytest.raises(_lib.SpecDiffError, match="d_nope = 0"):
         _lib.sd_latent_attention_expanded(h(5, 2, 0), h(9, 2, 0), None, h(9, 2, 128), i, i)
+
+
+def test_an_absorbed_call_without_a_scale_warns():
+    """The default, (d_latent + d_rope)^-1/2, is not the scale of any model's expanded form."""
+    q, c, n = torch.zeros(1, 1, 2, 192).half(), torch.zeros(3, 16, 192).half(), torch.ones(1, dtype=torch.int32)
+    with pytest.warns(UserWarning, match="d_nope"), pytest.raises(_lib.SpecDiffError):
+        _lib.sd_latent_attention(q, c, n, 128)
+    with warnings.catch_warnings(), pytest.raises(_lib.SpecDiffError, match="not on the current GPU"):
+        warnings.simplefilter("error")
+        _lib.sd_latent_attention(q, c, n, 128, scale=192 ** -0.5)
+
+
+def test_the_readmes_absorbed_call_has_a_scale():
+    with open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "README.md")) as f:
+        calls = [line for line in f if "sd_latent_attention(" in line]
+    assert calls and all("scale=" in line for line in calls)
