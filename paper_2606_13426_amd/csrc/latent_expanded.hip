@@ -94,9 +94,8 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_kernel(Expanded a) {
   // the least limit of the workgroup's rows; tiles that reach past it have keys that not all its rows see
   const int g_lo = min(max(q0 + shift, 0), nk);
   auto mixed = [&](int tl) { return (tl + 1) * kTile > g_lo; };
-  // the least and the largest limit of this wavefront's real rows
-  const int w_lo = min(max(q0 + 32 * w + shift, 0), nk);
-  const int w_hi = q0 + 32 * w < nq ? min(max(min(q0 + 32 * w + 31, nq - 1) + shift, 0), nk) : 0;
+  const int w_lo = min(max(q0 + 32 * w + shift, 0), nk);  // the least limit of this wavefront's rows
+  const bool idle = q0 + 32 * w >= nq;
 
   u32x4 qf[KS];
   {
@@ -208,8 +207,9 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_kernel(Expanded a) {
     __builtin_amdgcn_s_waitcnt(0);
     lds_barrier();
     Load ld = start_load(min(tl + 1, t1 - 1), lds + (tl - t0 + 1 & 1) * kStage, tl + 1 < t1);
-    if (tl * kTile >= w_hi && !mixed(tl)) {
-      // none of this wavefront's rows sees the tile
+    if (idle && !mixed(tl)) {
+      // a wavefront without rows only loads; in mixed tiles it takes part in the look for infinities below
+      // (where rows see nothing of a tile that others see, it is mixed)
       each<kLoads>([&](auto i) { next_load(ld, i); });
       continue;
     }
