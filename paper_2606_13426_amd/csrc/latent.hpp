@@ -18,6 +18,8 @@
 //
 // m is a reference and not the maximum: it moves when a score exceeds it by more than it
 // is allowed to (reach), so the rescaling of O is left out of almost every tile.
+// P is rounded to the operands' type, half a step a weight (the instruction takes both
+// operands of one type); the weights' sum is of the float32 ones.
 //
 // Tiles come by loads that write LDS directly, the next one while this one is
 // multiplied.  A token's 16-byte pieces are permuted inside each 128 bytes by
@@ -71,7 +73,8 @@ inline Plan plan_of(int64_t rows, int R) {
 }
 // Many rows a workgroup read the cache less often, few leave smaller parts to join.  By the
 // tiles of 64 rows and 64 tokens that a compute unit has if every sequence is as long as its
-// pages allow; in us (both kernels) with R = 1 / 2 / 4, H heads of one row each:
+// pages allow (the lengths are on the device: short sequences under a wide table get the rows of
+// long ones, in the first line 25 us for 20); in us (both kernels) with R = 1 / 2 / 4, H heads of one row each:
 //   1 x 800 tokens, H = 64, 0.05 tiles:  20 / 21 / 25     4 x 4000, H = 128, 2:    41 / 40 / 46
 //   1 x 4000, H = 128, 0.5:              29 / 31 / 34     16 x 4000, H = 128, 8:   83 / 62 / 61
 //   8 x 4000, H = 64, 2:                 41 / 40 / 47     64 x 4000, H = 64, 16:   147 / 105 / 94

@@ -15,6 +15,8 @@
 //
 // m is a reference and not the maximum: it moves when a score exceeds it by more than
 // it is allowed to (reach), so the rescaling of O is left out of almost every tile.
+// P is rounded to the operands' type, half a step a weight (the instruction takes both
+// operands of one type); the weights' sum is of the float32 ones.
 //
 // Tiles (K rotary and not, V) come by loads that write LDS directly, into the other
 // of two buffers while this one is multiplied; one barrier a tile.  80 KB of LDS

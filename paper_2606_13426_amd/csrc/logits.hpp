@@ -125,9 +125,9 @@ inline int slices(int V, int E) { return (int)(((int64_t)V + 7 + (int64_t)kThrea
 
 // The elements a thread holds: 32, or 8 where rows of such slices would leave
 // compute units without a workgroup (256 compute units, four workgroups each).
-// In us, 8 / 32: one chain of 4 drafts over 32000 (bf16) 33 / 44, 8 over 131072 40 / 46, 64
-// of 8 drafts 212 / 155; log-probabilities of 16 rows of 131072 (bf16) 20 / 19, of 2048
-// 306 / 161.
+// In us, 8 / 32: one chain of 4 drafts over 32000 (bf16) 28 / 35, of 8 over 131072 35 / 47, 8
+// of 8 67 / 69, 64 of 8 295 / 245, 32 of 5 over 50001 (f32) 51 / 61; log-probabilities of 16 rows of
+// 131072 (bf16) 20 / 19, of 2048 306 / 161.
 inline int per_thread(int64_t rows, int V) { return rows * slices(V, 32) >= 1024 ? 32 : 8; }
 
 }  // namespace logits

@@ -12,13 +12,13 @@
 // float64 from the difference on: with draft and target next to equal, h = v / (v + 1 - alpha) divides
 // differences of the two laws, and an error of 1e-7 of them would be one of 1e-7 / (1 - alpha).
 //
-// What bounds it, on MI355X: verification's two passes over all rows by float64 products, 17 an
-// element (64 chains of 8 drafts over 131072 bf16 tokens: sums 111 us, 2.6 TB/s; excess 100 us, 2.3
-// TB/s; in float32 they ran at the stream's rate, 45 and 39); the draw's two passes over two rows a chain
-// too (21 and 37 us there); log-probabilities by
-// vector instructions, about 14 an element with the alternatives (2048 rows of 131072
-// bf16: 145 us, 3.7 TB/s, 119 of them issuing).  Few rows are launches and trips to
-// memory: one row of 32000 takes 9 us in one kernel, one chain of 4 drafts 25 us in five.
+// What bounds it, on MI355X: verification's two passes over all rows by float64 products, 17
+// instructions an element (64 chains of 8 drafts over 131072 bf16 tokens: sums 94 to 117 us from a
+// cool to a warm card, 3.0 to 2.4 TB/s; excess 86 to 106 us; float32 exponentials ran at the stream's
+// rate, 45 and 39), and so the draw's two passes over two rows a chain (18 to 22 and 33 to 39 us
+// there); log-probabilities by vector instructions, about 14 an element with the alternatives (2048
+// rows of 131072 bf16: 145 us, 3.7 TB/s, 119 of them issuing).  Few rows are launches and trips to
+// memory: one row of 32000 takes 8 us in one kernel, one chain of 4 drafts 24 us in five.
 #include "common.hpp"
 #include "logits.hpp"
 #include "philox.hpp"
