@@ -74,11 +74,17 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_kernel(Expanded a) {
   // the tiles of a head from the last to the first, a head's tiles on one XCD
   const int id = xcd_tile((int)(gridDim.x * gridDim.y * gridDim.z));
   const int part = id % a.split, tile = a.tiles - 1 - id / a.split % a.tiles, head = id / a.split / a.tiles;
-  // sequence b's tiles are numbered from cu_q[b] / 128 + b
+  // Sequence b's tiles are numbered from cu_q[b] / 128 + b, which rises: the sequences that begin at or before
+  // this one's are counted by the last of 64 parts of those in question at a time.  (Every workgroup over
+  // all sequences: 26.5 ms for 16384 of 64 rows, 16 heads.)
   int before = 0;
-  for (int b0 = 0; b0 < a.n; b0 += 64) {
-    const int b = b0 + lane;
-    before += __popcll(__ballot(b < a.n && offset_of(a.cu_q, b < a.n ? b : 0, a.Tq) / kRows + b <= tile));
+  for (int left = a.n, step; left > 0; left = step > 1 ? min(step, left) : 0) {
+    step = (left + 63) / 64;
+    const int at = before + (lane + 1) * step - 1;
+    const bool here = (lane + 1) * step <= left;
+    const int parts = __popcll(__ballot(here && offset_of(a.cu_q, here ? at : 0, a.Tq) / kRows + at <= tile));
+    before += parts * step;
+    left -= parts * step;
   }
   const int b = __builtin_amdgcn_readfirstlane(max(before - 1, 0));
   const int qb = offset_of(a.cu_q, b, a.Tq), kb = offset_of(a.cu_k, b, a.Tk);
