@@ -185,3 +185,30 @@ def test_log_ratios_are_rounded_once(t, V):
         for j in range(4):
             want = otok.row_law(q[b, j])[x[b, j]] - otok.row_law(d[b, j])[x[b, j]]
             assert abs(got[b, j] - want) <= 2.0 ** -24 * abs(want) + 1e-13, (b, j, got[b, j], want)
+
+
+@pytest.mark.parametrize("mode", MODES)
+@pytest.mark.parametrize("t", list(tok.TYPES))
+@pytest.mark.parametrize("power", [-60, -20, -5, 5, 20])
+def test_temperatures(power, t, mode):
+    """From laws of one token to laws of equal ones, next to equal."""
+    draft, target, tokens, kb, un = tok._blocks(30, 4, 3001, t, 5)
+    r = _lib.sd_verify_tokens(draft, target, tokens, kb, uniforms=un, mode=mode, temperature=2.0 ** power)
+    decided, drawn = tok._check_verify(draft, target, tokens, kb, un, mode, 2.0 ** power, r)
+    assert decided >= 29 and drawn >= decided - 1
+
+
+def test_the_largest_vocabulary():
+    V = 1 << 24
+    draft, target, tokens, kb, un = tok._blocks(2, 1, V, "bf16", 5)
+    kb.fill_(1)
+    r = _lib.sd_verify_tokens(draft, target, tokens, kb, uniforms=un)
+    d, q = draft.double().cpu().numpy(), target.double().cpu().numpy()
+    x, u = tokens.cpu().numpy(), un.cpu().numpy()
+    for b in range(2):
+        w = otok.verify_chain(d[b], q[b], x[b], 1, u[b, :1], u[b, 1])
+        assert abs(u[b, 0] - w["h"][0]) > 1e-9 and r["tau"][b] == w["tau"]
+        c = np.cumsum(w["w"])
+        # (the oracle's sums are off by V u = 1.9e-9 of the whole at most)
+        at, goal = int(r["token"][b]), u[b, 1] * c[-1]
+        assert w["w"][at] > 0 and c[at] >= goal - 4e-9 * c[-1] and c[at] - w["w"][at] <= goal + 4e-9 * c[-1]
