@@ -552,6 +552,133 @@ sd_status sd_verify_tokens(int32_t B, int32_t K, int32_t V, sd_verify_mode mode,
                            float* log_ratio, uint64_t* coins, void* ws, size_t ws_bytes,
                            sd_stream stream);
 
+/* ---------------------------------------------------------- tree drafts --
+ * The same round with a tree of drafted tokens instead of a chain: several
+ * candidates a position, of which at most one branch is accepted.  A tree of
+ * sequence b has n_b = rows[b] nodes (NULL: Q), at most SD_MAX_TREE; node 0 is
+ * the root, the last token that is part of the text, and parents[b][i] (int32
+ * [B][Q]) is an earlier node, 0 <= parents[b][i] < i.  A node of any other value
+ * has no parent: it sees the prefix and itself, and no walk from the root
+ * reaches it.  A round is
+ *   sd_latent_append (every layer: the nodes' vectors into the cache, their
+ *   rotary parts turned) -> sd_latent_attention_tree (every layer) -> the
+ *   caller's products -> sd_verify_tree -> sd_latent_keep (the accepted branch's
+ *   vectors behind the prefix, and the lengths).
+ * The calls share sd_latent_attention's conventions: lens[b] counts the rows of the
+ * call, the last rows[b] of the cached tokens; pages as there. */
+#define SD_MAX_TREE 64
+
+/* Which elements of a rotary part of d make pair i < d / 2: (2 i, 2 i + 1) or
+ * (i, i + d / 2). */
+typedef enum { SD_ROPE_PAIRS = 0, SD_ROPE_HALVES = 1 } sd_rope;
+
+/* New tokens' vectors into a paged cache, with the position rotation on the way.
+ * Row i of sequence b's n_b goes to token place len_b - n_b + i as
+ *   [ latent, R(pos) k_rope ],  pos = len_b - n_b + i, or with parents
+ *   len_b - n_b + depth_i (the root's depth is 0, a child's one more than its
+ *   parent's);
+ * R(pos) turns pair p of a rotary part by the angle a = pos freq[p], a product in
+ * float64: (x, y) -> (x cos a - y sin a, x sin a + y cos a), computed in float32 and
+ * rounded once.  With q (nullable: H = 0 then) the rotary parts of the rows' H
+ * queries are turned by the same angles into q_out, which may be q itself; with
+ * k_out (nullable; may be k_rope itself) the turned k_rope is also put there.
+ * cu NULL: rows are views [B][Q], n_b = rows[b] (NULL: Q) clamped to [0, Q].  cu
+ * [B+1]: Q rows in all, those of sequence b being [cu[b], cu[b+1]) (values clamped
+ * to [0, Q], rising); rows and parents must be NULL, seq and chain strides are not read.
+ * With parents Q <= SD_MAX_TREE.  Rows of no sequence (i >= n_b) are neither stored
+ * nor turned.  A row whose place is negative, past the table's (the page's) tokens or
+ * in a page outside [0, n_pages) is not stored; its q_out and k_out are written.
+ * Outputs may not overlap one another or, other than as said, the inputs.
+ * latent, k_rope, cache, q, q_out, k_out of `type` (SD_TYPE_BF16 or SD_TYPE_F16) at
+ * 16-byte addresses, strides multiples of 8 elements that step over a row (d contiguous);
+ * freq [d_rope / 2] float64.  d_latent and d_rope as in sd_latent_attention (d_rope =
+ * 0: k_rope and freq are not read).  No workspace. */
+sd_status sd_latent_append(int32_t B, int32_t Q, int32_t H, int32_t d_latent, int32_t d_rope,
+                           sd_type type, sd_rope rope, const double* freq, const void* latent,
+                           sd_stride ls, const void* k_rope, sd_stride krs, const int32_t* cu,
+                           const int32_t* parents, const int32_t* lens, const int32_t* rows,
+                           void* cache, int64_t page_stride, int64_t token_stride, int32_t n_pages,
+                           int32_t page_size, const int32_t* pages, int64_t pages_stride,
+                           int32_t max_pages, void* k_out, sd_stride kos, const void* q,
+                           sd_stride_h qs, void* q_out, sd_stride_h qos, sd_stream stream);
+
+/* sd_latent_attention where row i of a sequence's n_b sees the prefix (tokens j <
+ * len_b - n_b), itself (token len_b - n_b + i) and its ancestors in the tree.  Q <=
+ * SD_MAX_TREE; everything else as there. */
+size_t sd_latent_attention_tree_workspace(int32_t B, int32_t Q, int32_t H, int32_t d_latent,
+                                          int32_t d_rope);
+sd_status sd_latent_attention_tree(int32_t B, int32_t Q, int32_t H, int32_t d_latent,
+                                   int32_t d_rope, sd_type type, double scale, const void* q,
+                                   sd_stride_h qs, const void* cache, int64_t page_stride,
+                                   int64_t token_stride, int32_t n_pages, int32_t page_size,
+                                   const int32_t* pages, int64_t pages_stride, int32_t max_pages,
+                                   const int32_t* lens, const int32_t* rows, const int32_t* parents,
+                                   void* out, sd_stride_h os, float* lse, void* ws, size_t ws_bytes,
+                                   sd_stream stream);
+
+/* How a node's children were drafted: independently from the draft law of the node
+ * (SD_TREE_IID), one after another from it without those before
+ * (SD_TREE_DISTINCT), or without any chance (SD_TREE_GIVEN: the likeliest tokens, say). */
+typedef enum { SD_TREE_IID = 0, SD_TREE_DISTINCT = 1, SD_TREE_GIVEN = 2 } sd_tree_draws;
+
+/* Verification of B trees of drafted tokens: token verification (Alg. 2) along the
+ * branches, with every child of a node as one more try at what the ones before
+ * have left, and the draw of the token that follows the accepted branch.  The next
+ * token so follows the target's law, however many candidates there are.
+ * q_i and p_i are the laws of target row i and draft row i (softmaxes of logits /
+ * temperature) at node i, from which its children were drafted.  From the root on, a
+ * node's children x_0, x_1, .. in the order of their numbers:
+ *   r_0 = q_i;  x_k is accepted if eta < h_k = r_k(x_k) / p_k(x_k), and the walk goes on
+ *   at its node; else r_{k+1} is proportional to max(0, r_k - p_k);
+ *   p_k = p_i (IID), p_i without x_0 .. x_{k-1} and rescaled (DISTINCT), or all
+ *   of it on x_k (GIVEN: h_k = r_k(x_k); draft is NULL);
+ * where no child is left token[b] is drawn from the last r: the lowest x whose
+ * cumulative sum exceeds u times the whole, in float64 as all of this (from q_i where
+ * the last r has no mass).  With p_k = p_i, r_k = max(0, q_i - a_k p_i) / S_k: a_0 = 0,
+ * S_k = sum_x max(0, q_i - a_k p_i), a_{k+1} = a_k + S_k (DISTINCT: S_k over the mass
+ * that the tries have left of p_i), so a try costs one sum over the vocabulary.
+ * A log-ratio log q_i - log p_i below 2^-44 is 0.
+ * max_children in [1, Q]: at most so many children of a node are tried (the calls'
+ * number grows with it).
+ * tau[b] = 1 + accepted drafts; path[b][0..tau-1] their nodes, the root first, -1
+ * behind; accept[b][i] (nullable) = min(1, h) of the nodes that were tried, -1 of others.
+ * A draft outside [0, V), of target probability 0, a sibling's token once more
+ * (DISTINCT, GIVEN) or of a node whose target or draft row has no law (a NaN or +inf)
+ * is rejected; one of draft probability 0 and r > 0 is accepted.  token is -1 where no
+ * law is left to draw from (target row all -inf; a NaN or +inf), and for sequences
+ * without rows, whose tau is 0 and path -1.
+ * eta of node i = uniforms[b][i-1] and u = uniforms[b][Q-1] (float64 in (0, 1), [B][Q]),
+ * or with uniforms NULL as in sd_verify_tokens, node i in the place of draft i (so a
+ * chain of nodes, IID, has the results of token verification).
+ * draft, target [B][Q][V] views of `type` (rows contiguous, aligned to their element;
+ * draft rows of nodes without children and rows past n_b are not read); tokens, parents
+ * [B][Q] (the root's are not read); 1 <= Q <= SD_MAX_TREE.
+ * ws: >= sd_verify_tree_workspace bytes, 256-byte aligned. */
+size_t sd_verify_tree_workspace(int32_t B, int32_t Q, int32_t V);
+sd_status sd_verify_tree(int32_t B, int32_t Q, int32_t V, sd_tree_draws draws, sd_type type,
+                         double temperature, int32_t max_children, const void* draft, sd_stride ds,
+                         const void* target, sd_stride ts, const int32_t* tokens,
+                         const int32_t* parents, const int32_t* rows, const double* uniforms,
+                         const uint32_t* round, uint64_t seed, int32_t* tau, int32_t* token,
+                         int32_t* path, float* accept, void* ws, size_t ws_bytes, sd_stream stream);
+
+/* The cached vectors of an accepted branch, moved up behind the prefix: in every layer,
+ * place len_b - n_b + j takes what place len_b - n_b + path[b][j] holds, j < tau_b, in
+ * place; new_lens[b] = len_b - n_b + tau_b.  tau is clamped to [0, n_b], and the branch
+ * ends before the first entry of path that does not rise from the one before or is
+ * outside [0, n_b).  Moves from or to a place that does not exist (as in
+ * sd_latent_append) are left out; len_b - n_b below 0 counts as it is, new_lens from 0.
+ * cache [layers][n_pages][page_size][d] of 16-bit `type`, layers layer_stride elements
+ * apart, one page table for all; d a multiple of 8 in [8, 576]; strides multiples of 8
+ * elements, 16-byte addresses.  path [B][Q], tau, lens, rows (NULL: Q) [B]; new_lens [B],
+ * nullable, may not overlap lens.  No workspace. */
+sd_status sd_latent_keep(int32_t layers, int32_t B, int32_t Q, int32_t d, sd_type type, void* cache,
+                         int64_t layer_stride, int64_t page_stride, int64_t token_stride,
+                         int32_t n_pages, int32_t page_size, const int32_t* pages,
+                         int64_t pages_stride, int32_t max_pages, const int32_t* lens,
+                         const int32_t* rows, const int32_t* tau, const int32_t* path,
+                         int32_t* new_lens, sd_stream stream);
+
 /* ------------------------------------------------------------- profiling --
  * Per-kernel timing with HIP events recorded around every launch on the
  * launch's own stream.  sd_profile_enable(1) clears and starts collection,

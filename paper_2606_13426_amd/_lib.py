@@ -19,7 +19,10 @@ SD_USAMPLE_EXACT, SD_USAMPLE_PAPER = 0, 1
 SD_RESIDUAL_DECOMPOSITION, SD_RESIDUAL_REFLECTION = 0, 1
 SD_DRAFTER_FREE, SD_DRAFTER_FROZEN = 0, 1
 SD_TYPE_F32, SD_TYPE_BF16, SD_TYPE_F16 = 0, 1, 2
+SD_ROPE_PAIRS, SD_ROPE_HALVES = 0, 1
+SD_TREE_IID, SD_TREE_DISTINCT, SD_TREE_GIVEN = 0, 1, 2
 SD_MAX_BLOCK = 64
+SD_MAX_TREE = 64
 SD_MAX_TOP, SD_MAX_VOCAB = 32, 1 << 24
 TAG_INIT, TAG_DRAFT, TAG_COIN, TAG_USAMPLE, TAG_RESID, TAG_TARGET = 1, 2, 3, 4, 5, 6
 
@@ -116,6 +119,17 @@ SIGNATURES = [
     ("sd_verify_tokens_workspace", c_size_t, [c_int32, c_int32, c_int32]),
     ("sd_verify_tokens", c_int32, [c_int32, c_int32, c_int32, c_int32, c_int32, c_double, P, S, P, S, P, P, P, P,
                                    c_uint64, P, P, P, P, P, P, c_size_t, P]),
+    ("sd_latent_append", c_int32, [c_int32] * 7 + [P, P, S, P, S, P, P, P, P, P, c_int64, c_int64, c_int32, c_int32, P,
+                                                   c_int64, c_int32, P, S, P, SH, P, SH, P]),
+    ("sd_latent_attention_tree_workspace", c_size_t, [c_int32] * 5),
+    ("sd_latent_attention_tree", c_int32, [c_int32, c_int32, c_int32, c_int32, c_int32, c_int32, c_double, P, SH, P,
+                                           c_int64, c_int64, c_int32, c_int32, P, c_int64, c_int32, P, P, P, P, SH, P, P,
+                                           c_size_t, P]),
+    ("sd_verify_tree_workspace", c_size_t, [c_int32, c_int32, c_int32]),
+    ("sd_verify_tree", c_int32, [c_int32, c_int32, c_int32, c_int32, c_int32, c_double, c_int32, P, S, P, S, P, P, P, P, P,
+                                 c_uint64, P, P, P, P, P, c_size_t, P]),
+    ("sd_latent_keep", c_int32, [c_int32] * 5 + [P, c_int64, c_int64, c_int64, c_int32, c_int32, P, c_int64, c_int32, P, P,
+                                                 P, P, P, P]),
     ("sd_profile_enable", c_int32, [c_int32]),
     ("sd_profile_only", c_int32, [c_char_p]),
     ("sd_profile_every", c_int32, [c_int32]),
@@ -471,11 +485,15 @@ def sd_latent_attention(q, cache, lens, d_latent, pages=None, rows=None, scale=N
 
     Returns (out [B][Q][H][d_latent], lse [B][Q][H] float32).
     """
+    return _attention("sd_latent_attention", q, cache, lens, None, d_latent, pages, rows, scale, out, lse, ws)
+
+
+def _attention(name, q, cache, lens, parents, d_latent, pages, rows, scale, out, lse, ws):
     import torch
-    name, i32 = "sd_latent_attention", torch.int32
+    i32, tree = torch.int32, parents is not None
     if scale is None:
         warnings.warn(f"{name}: no scale given, (d_latent + d_rope)^-1/2 is taken; a model's absorbed attention has "
-                      "(d_nope + d_rope)^-1/2", stacklevel=2)
+                      "(d_nope + d_rope)^-1/2", stacklevel=3)
     _need(q.dim() == 4 and cache.dim() == 3 and q.stride(3) == 1 and cache.stride(2) == 1, name,
           "q must be [B][Q][H][d] and cache [n_pages][page_size][d] with contiguous d")
     B, Q, H, d = q.shape
@@ -485,24 +503,27 @@ def sd_latent_attention(q, cache, lens, d_latent, pages=None, rows=None, scale=N
         out = torch.empty(B, Q, H, d_latent, dtype=q.dtype, device=q.device)
     if lse is None:
         lse = torch.empty(B, Q, H, dtype=torch.float32, device=q.device)
-    stream = _operands(name, dict(lens=i32, pages=i32, rows=i32, out=q.dtype, lse=torch.float32, ws=torch.uint8),
-                       q=q, cache=cache, lens=lens, pages=pages, rows=rows, out=out, lse=lse, ws=ws)
+    stream = _operands(name, dict(lens=i32, pages=i32, rows=i32, out=q.dtype, lse=torch.float32, ws=torch.uint8,
+                                  parents=i32),
+                       q=q, cache=cache, lens=lens, pages=pages, rows=rows, out=out, lse=lse, ws=ws, parents=parents)
     _need(lens.shape == (B,) and lens.is_contiguous(), name, "lens must be contiguous [B]")
+    _need(not tree or (parents.shape == (B, Q) and parents.is_contiguous()), name, "parents must be contiguous [B][Q]")
     _need(rows is None or (rows.shape == (B,) and rows.is_contiguous()), name, "rows must be contiguous [B]")
     _need(pages is None or (pages.dim() == 2 and pages.shape[0] == B and pages.stride(1) == 1), name,
           "pages must be [B][max_pages] with contiguous rows")
     _need(out.shape == (B, Q, H, d_latent) and out.stride(3) == 1, name, "out must be [B][Q][H][d_latent]")
     _need(lse.shape == (B, Q, H) and lse.is_contiguous(), name, "lse must be contiguous [B][Q][H]")
+    lib = load()
+    size, call = (lib.sd_latent_attention_tree_workspace, lib.sd_latent_attention_tree) if tree else \
+        (lib.sd_latent_attention_workspace, lib.sd_latent_attention)
     if ws is None:
-        ws = _workspace(sd_latent_attention_workspace(B, Q, H, d_latent, d - d_latent), q.device)
-    _check(load().sd_latent_attention(B, Q, H, d_latent, d - d_latent, _type(q),
-                                      d ** -0.5 if scale is None else float(scale), q.data_ptr(),
-                                      sd_stride_h(*q.stride()[:3]), cache.data_ptr(), cache.stride(0), cache.stride(1),
-                                      cache.shape[0], cache.shape[1], _ptr(pages),
-                                      0 if pages is None else pages.stride(0),
-                                      0 if pages is None else pages.shape[1], lens.data_ptr(), _ptr(rows),
-                                      out.data_ptr(), sd_stride_h(*out.stride()[:3]), lse.data_ptr(), ws.data_ptr(),
-                                      ws.numel(), stream), name)
+        ws = _workspace(size(B, Q, H, d_latent, d - d_latent), q.device)
+    _check(call(B, Q, H, d_latent, d - d_latent, _type(q), d ** -0.5 if scale is None else float(scale), q.data_ptr(),
+                sd_stride_h(*q.stride()[:3]), cache.data_ptr(), cache.stride(0), cache.stride(1), cache.shape[0],
+                cache.shape[1], _ptr(pages), 0 if pages is None else pages.stride(0),
+                0 if pages is None else pages.shape[1], lens.data_ptr(), _ptr(rows),
+                *((parents.data_ptr(),) if tree else ()), out.data_ptr(), sd_stride_h(*out.stride()[:3]),
+                lse.data_ptr(), ws.data_ptr(), ws.numel(), stream), name)
     return out, lse
 
 
@@ -638,6 +659,156 @@ def sd_verify_tokens(draft, target, tokens, kb, uniforms=None, rnd=None, seed=0,
                                    out["log_alpha_res"].data_ptr(), out["log_ratio"].data_ptr(), _ptr(out.get("coins")),
                                    ws.data_ptr(), ws.numel(), stream), name)
     return out
+
+
+def sd_latent_append(latent, k_rope, cache, lens, freq, pages=None, rows=None, cu=None, parents=None, q=None, q_out=None,
+                     k_out=None, rope=SD_ROPE_PAIRS):
+    """latent [B][Q][d_latent], k_rope [B][Q][d_rope] (None: d_rope = 0) into cache [n_pages][page_size][d_latent +
+    d_rope], all of one 16-bit type (last dimension contiguous); lens [B], rows [B] (None: Q each), parents [B][Q] (None:
+    a chain), pages [B][max_pages] (None: page b is sequence b) int32; freq [d_rope / 2] float64.  With cu [B + 1]
+    int32 the rows are ragged: [T][..] in the place of [B][Q][..].
+    q [B][Q][H][d_rope]: turned by the rows' positions too, into q_out (None: a new tensor; q: in place).
+    k_out [B][Q][d_rope] (k_rope: in place): the turned k_rope once more.
+
+    Returns q_out (None without q).
+    """
+    import torch
+    name, i32, f64 = "sd_latent_append", torch.int32, torch.float64
+    lead = 1 if cu is not None else 2
+    _need(latent.dim() == lead + 1 and cache.dim() == 3 and latent.stride(lead) == 1 and cache.stride(2) == 1, name,
+          "latent must be [B][Q][d_latent], or [T][d_latent] with cu, and cache [n_pages][page_size][d] with contiguous d")
+    dc, dr, t = latent.shape[lead], cache.shape[2] - latent.shape[lead], latent.dtype
+    _need((k_rope is None and dr == 0) or (k_rope is not None and tuple(k_rope.shape) == (*latent.shape[:lead], dr) and
+                                           k_rope.stride(lead) == 1), name,
+          "k_rope must be as latent with the rest of the cache's d, contiguous")
+    _need(q is not None or q_out is None, name, "q_out goes with q")
+    H = 0
+    if q is not None:
+        _need(q.dim() == lead + 2 and q.shape[:lead] == latent.shape[:lead] and q.shape[lead + 1] == dr and
+              q.stride(lead + 1) == 1 and q.shape[lead] > 0, name, "q must be [B][Q][H][d_rope], or [T][H][d_rope] with cu, contiguous in d")
+        H = q.shape[lead]
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        _need(q_out.shape == q.shape and q_out.stride(lead + 1) == 1, name, "q_out must be as q, contiguous in d")
+    _need(k_out is None or (k_rope is not None and k_out.shape == k_rope.shape and k_out.stride(lead) == 1), name,
+          "k_out must be as k_rope, contiguous in d")
+    stream = _operands(name, dict(k_rope=t, cache=t, q=t, q_out=t, k_out=t, lens=i32, freq=f64, pages=i32, rows=i32, cu=i32,
+                                  parents=i32),
+                       latent=latent, k_rope=k_rope, cache=cache, lens=lens, freq=freq, pages=pages, rows=rows, cu=cu,
+                       parents=parents, q=q, q_out=q_out, k_out=k_out)
+    _need(lens.dim() == 1 and lens.is_contiguous(), name, "lens must be contiguous [B]")
+    B = lens.shape[0]
+    Q = latent.shape[0] if cu is not None else latent.shape[1]
+    _need(cu is not None or latent.shape[0] == B, name, "latent and lens must agree in B")
+    _need(cu is None or (cu.shape == (B + 1,) and cu.is_contiguous()), name, "cu must be contiguous [B + 1]")
+    _need(dr == 0 or (freq is not None and freq.shape == (dr // 2,) and freq.is_contiguous()), name,
+          "freq must be contiguous [d_rope / 2]")
+    _need(rows is None or (rows.shape == (B,) and rows.is_contiguous()), name, "rows must be contiguous [B]")
+    _need(parents is None or (parents.shape == (B, Q) and parents.is_contiguous()), name, "parents must be contiguous [B][Q]")
+    _need(pages is None or (pages.dim() == 2 and pages.shape[0] == B and pages.stride(1) == 1), name,
+          "pages must be [B][max_pages] with contiguous rows")
+
+    def stride(x):
+        return sd_stride(0, 0) if x is None else sd_stride(*((0, x.stride(0)) if cu is not None else x.stride()[:2]))
+
+    def stride_h(x):
+        return sd_stride_h(0, 0, 0) if x is None else sd_stride_h(*((0, *x.stride()[:2]) if cu is not None else x.stride()[:3]))
+
+    _check(load().sd_latent_append(B, Q, H, dc, dr, _type(latent), rope, _ptr(freq), latent.data_ptr(), stride(latent),
+                                   _ptr(k_rope), stride(k_rope), _ptr(cu), _ptr(parents), lens.data_ptr(), _ptr(rows),
+                                   cache.data_ptr(), cache.stride(0), cache.stride(1), cache.shape[0], cache.shape[1],
+                                   _ptr(pages), 0 if pages is None else pages.stride(0),
+                                   0 if pages is None else pages.shape[1], _ptr(k_out), stride(k_out), _ptr(q),
+                                   stride_h(q), _ptr(q_out), stride_h(q_out), stream), name)
+    return q_out
+
+
+def sd_latent_attention_tree_workspace(B, Q, H, d_latent, d_rope):
+    return load().sd_latent_attention_tree_workspace(B, Q, H, d_latent, d_rope)
+
+
+def sd_latent_attention_tree(q, cache, lens, parents, d_latent, pages=None, rows=None, scale=None, out=None, lse=None,
+                             ws=None):
+    """sd_latent_attention where row i sees the prefix, itself and its ancestors: parents [B][Q] int32, an
+    earlier node's number (any other value: none)."""
+    _need(parents is not None, "sd_latent_attention_tree", "parents must be contiguous [B][Q]")
+    return _attention("sd_latent_attention_tree", q, cache, lens, parents, d_latent, pages, rows, scale, out, lse, ws)
+
+
+def sd_verify_tree_workspace(B, Q, V):
+    return load().sd_verify_tree_workspace(B, Q, V)
+
+
+def sd_verify_tree(draft, target, tokens, parents, rows=None, draws=SD_TREE_IID, max_children=None, uniforms=None, rnd=None,
+                   seed=0, temperature=1.0, ws=None, out=None):
+    """draft (None with SD_TREE_GIVEN) and target [B][Q][V] logits of one type (rows contiguous); tokens, parents
+    [B][Q], rows [B] (None: Q each) int32; uniforms [B][Q] float64, or rnd [B] int32/uint32 and the seed.
+    max_children: how many children of a node are tried (None: all; each one more is one more kernel).
+
+    Returns dict of device tensors tau, token [B], path [B][Q] int32, accept [B][Q] float32.
+    """
+    import torch
+    name, i32, f32 = "sd_verify_tree", torch.int32, torch.float32
+    _need(target.dim() == 3, name, "target must be [B][Q][V]")
+    B, Q, V = target.shape
+    _need(draft is None or (draft.shape == target.shape and draft.dtype == target.dtype), name,
+          "draft and target must be [B][Q][V] of one type")
+    stream = _operands(name, dict(tokens=i32, parents=i32, rows=i32, uniforms=torch.float64, ws=torch.uint8),
+                       target=target, draft=draft, tokens=tokens, parents=parents, rows=rows, uniforms=uniforms, rnd=rnd,
+                       ws=ws)
+    for what, x in (("tokens", tokens), ("parents", parents), ("uniforms", uniforms)):
+        _need(x is None or (x.shape == (B, Q) and x.is_contiguous()), name, f"{what} must be contiguous [B][Q]")
+    _need(rows is None or (rows.shape == (B,) and rows.is_contiguous()), name, "rows must be contiguous [B]")
+    _need(rnd is None or (rnd.shape == (B,) and rnd.dtype in (torch.int32, torch.uint32) and rnd.is_contiguous()), name,
+          "rnd must be contiguous [B] of int32 or uint32")
+    if out is None:
+        dev = target.device
+        out = dict(tau=torch.empty(B, dtype=i32, device=dev), token=torch.empty(B, dtype=i32, device=dev),
+                   path=torch.empty(B, Q, dtype=i32, device=dev), accept=torch.empty(B, Q, dtype=f32, device=dev))
+    else:
+        said = dict(tau=i32, token=i32, path=i32, accept=f32)
+        _need(all(out.get(k) is not None for k in said if k != "accept"), name, "out must hold tau, token and path")
+        _operands(name, said, **{k: out.get(k) for k in said})
+        for k in said:
+            o, wide = out.get(k), k in ("path", "accept")
+            _need(o is None or (o.shape == ((B, Q) if wide else (B,)) and o.is_contiguous()), name,
+                  f"{k} must be contiguous {'[B][Q]' if wide else '[B]'}")
+    if ws is None:
+        ws = _workspace(sd_verify_tree_workspace(B, Q, V), target.device)
+    _check(load().sd_verify_tree(B, Q, V, draws, _type(target), float(temperature), Q if max_children is None else max_children,
+                                 _ptr(draft), sd_stride(0, 0) if draft is None else stride3(draft), target.data_ptr(),
+                                 stride3(target), tokens.data_ptr(), parents.data_ptr(), _ptr(rows), _ptr(uniforms),
+                                 _ptr(rnd), seed, out["tau"].data_ptr(), out["token"].data_ptr(), out["path"].data_ptr(),
+                                 _ptr(out.get("accept")), ws.data_ptr(), ws.numel(), stream), name)
+    return out
+
+
+def sd_latent_keep(cache, lens, tau, path, pages=None, rows=None, new_lens=None):
+    """cache [n_pages][page_size][d] or [layers][n_pages][page_size][d] of a 16-bit type (d contiguous); lens, tau [B],
+    path [B][Q] (sd_verify_tree's), rows [B] (None: Q each), pages [B][max_pages] (None: page b is sequence b) int32.
+
+    Returns new_lens [B] int32 (None: a new tensor; not lens itself).
+    """
+    import torch
+    name, i32 = "sd_latent_keep", torch.int32
+    _need(cache.dim() in (3, 4) and cache.stride(-1) == 1, name, "cache must be [layers][n_pages][page_size][d] with contiguous d")
+    _need(path.dim() == 2 and path.is_contiguous(), name, "path must be contiguous [B][Q]")
+    B, Q = path.shape
+    if new_lens is None:
+        new_lens = torch.empty(B, dtype=i32, device=cache.device)
+    stream = _operands(name, dict(lens=i32, tau=i32, path=i32, pages=i32, rows=i32, new_lens=i32),
+                       cache=cache, lens=lens, tau=tau, path=path, pages=pages, rows=rows, new_lens=new_lens)
+    for what, x in (("lens", lens), ("tau", tau), ("rows", rows), ("new_lens", new_lens)):
+        _need(x is None or (x.shape == (B,) and x.is_contiguous()), name, f"{what} must be contiguous [B]")
+    _need(pages is None or (pages.dim() == 2 and pages.shape[0] == B and pages.stride(1) == 1), name,
+          "pages must be [B][max_pages] with contiguous rows")
+    many = cache.dim() == 4
+    _check(load().sd_latent_keep(cache.shape[0] if many else 1, B, Q, cache.shape[-1], _type(cache), cache.data_ptr(),
+                                 cache.stride(0) if many else 0, cache.stride(-3), cache.stride(-2), cache.shape[-3],
+                                 cache.shape[-2], _ptr(pages), 0 if pages is None else pages.stride(0),
+                                 0 if pages is None else pages.shape[1], lens.data_ptr(), _ptr(rows), tau.data_ptr(),
+                                 path.data_ptr(), new_lens.data_ptr(), stream), name)
+    return new_lens
 
 
 def sd_profile_enable(on=True):

@@ -1139,43 +1139,60 @@ size_t sd_latent_attention_workspace(int32_t B, int32_t Q, int32_t H, int32_t d_
   return latent_shape_ok(B, Q, H, d_latent, d_rope) ? latent_ws_bytes(B, Q, H, d_latent) : 0;
 }
 
+// sd_latent_attention (parents NULL) and sd_latent_attention_tree.
+static sd_status attention(const char* name, int32_t B, int32_t Q, int32_t H, int32_t d_latent, int32_t d_rope,
+                           sd_type type, double scale, const void* q, sd_stride_h qs, const void* cache,
+                           int64_t page_stride, int64_t token_stride, int32_t n_pages, int32_t page_size,
+                           const int32_t* pages, int64_t pages_stride, int32_t max_pages, const int32_t* lens,
+                           const int32_t* rows, const int32_t* parents, void* out, sd_stride_h os, float* lse,
+                           void* ws, size_t ws_bytes, sd_stream stream) {
+  SD_CHECK_ARG(B >= 1 && Q >= 1 && H >= 1, "%s: need B >= 1, Q >= 1 and H >= 1", name);
+  SD_CHECK_ARG(d_latent >= 8 && d_latent <= 512 && d_latent % 8 == 0, "%s: d_latent = %d is no multiple of 8 in [8, 512]", name, d_latent);
+  SD_CHECK_ARG(d_rope >= 0 && d_rope <= 64 && d_rope % 8 == 0, "%s: d_rope = %d is no multiple of 8 in [0, 64]", name, d_rope);
+  SD_CHECK_ARG(latent_shape_ok(B, Q, H, d_latent, d_rope), "%s: more than 2^30 rows", name);
+  SD_CHECK_ARG(type == SD_TYPE_BF16 || type == SD_TYPE_F16, "%s: type must be SD_TYPE_BF16 or SD_TYPE_F16", name);
+  SD_CHECK_ARG(isfinite(scale) && fabs(scale) <= 0x1p60, "%s: scale must be finite", name);
+  SD_CHECK_ARG(q && cache && lens && out && ws, "%s: NULL pointer argument", name);
+  SD_CHECK_ARG(n_pages >= 1 && page_size >= 1, "%s: need n_pages >= 1 and page_size >= 1", name);
+  if (pages) {
+    SD_CHECK_ARG(max_pages >= 1 && pages_stride >= max_pages, "%s: need max_pages >= 1 and pages_stride >= max_pages", name);
+    SD_CHECK_ARG((int64_t)max_pages * page_size < ((int64_t)1 << 30), "%s: a sequence's pages hold 2^30 tokens or more", name);
+  } else {
+    SD_CHECK_ARG(n_pages >= B, "%s: without a table n_pages = %d must be >= B = %d", name, n_pages, B);
+    SD_CHECK_ARG(page_size < (1 << 30), "%s: a page holds 2^30 tokens or more", name);
+  }
+  // (a sequence's rows are walked by at most one workgroup for every 64 of them)
+  SD_CHECK_ARG(((int64_t)(pages ? max_pages : 1) * page_size / 64 + 1) * B * ((int64_t)Q * H / 64 + 1) < ((int64_t)1 << 31),
+               "%s: too many rows and tokens for one call", name);
+  const int d = d_latent + d_rope;
+  SD_CHECK_ARG(token_stride >= d && token_stride % 8 == 0 && page_stride % 8 == 0 &&
+                   (n_pages == 1 || page_stride >= (int64_t)page_size * token_stride),
+               "%s: cache strides must be multiples of 8 elements that step over a token and a page", name);
+  SD_CHECK_ARG(stride_h_ok(qs, B, Q, H, d), "%s: q strides must be multiples of 8 elements that step over a row", name);
+  SD_CHECK_ARG(stride_h_ok(os, B, Q, H, d_latent) && apart(os, B, Q, H, d_latent),
+               "%s: out strides must be multiples of 8 elements that step over a row, no two rows in one place", name);
+  SD_CHECK_ARG(aligned(q, 16) && aligned(cache, 16) && aligned(out, 16), "%s: q, cache and out must be 16-byte aligned", name);
+  const size_t need = latent_ws_bytes(B, Q, H, d_latent);
+  SD_CHECK_ARG(ws_bytes >= need, "%s: workspace %zu < %zu bytes", name, ws_bytes, need);
+  SD_CHECK_ARG(aligned(ws, 256), "%s: workspace must be 256-byte aligned", name);
+  if (parents)
+    SD_HIP(latent_tree_launch(B, Q, H, d_latent, d_rope, type, scale, q, qs, cache, page_stride, token_stride, n_pages,
+                              page_size, pages, pages_stride, max_pages, lens, rows, parents, out, os, lse, ws,
+                              (hipStream_t)stream));
+  else
+    SD_HIP(latent_launch(B, Q, H, d_latent, d_rope, type, scale, q, qs, cache, page_stride, token_stride, n_pages,
+                         page_size, pages, pages_stride, max_pages, lens, rows, out, os, lse, ws, (hipStream_t)stream));
+  return SD_OK;
+}
+
 sd_status sd_latent_attention(int32_t B, int32_t Q, int32_t H, int32_t d_latent, int32_t d_rope, sd_type type,
                               double scale, const void* q, sd_stride_h qs, const void* cache, int64_t page_stride,
                               int64_t token_stride, int32_t n_pages, int32_t page_size, const int32_t* pages,
                               int64_t pages_stride, int32_t max_pages, const int32_t* lens, const int32_t* rows,
                               void* out, sd_stride_h os, float* lse, void* ws, size_t ws_bytes, sd_stream stream) {
-  SD_CHECK_ARG(B >= 1 && Q >= 1 && H >= 1, "sd_latent_attention: need B >= 1, Q >= 1 and H >= 1");
-  SD_CHECK_ARG(d_latent >= 8 && d_latent <= 512 && d_latent % 8 == 0, "sd_latent_attention: d_latent = %d is no multiple of 8 in [8, 512]", d_latent);
-  SD_CHECK_ARG(d_rope >= 0 && d_rope <= 64 && d_rope % 8 == 0, "sd_latent_attention: d_rope = %d is no multiple of 8 in [0, 64]", d_rope);
-  SD_CHECK_ARG(latent_shape_ok(B, Q, H, d_latent, d_rope), "sd_latent_attention: more than 2^30 rows");
-  SD_CHECK_ARG(type == SD_TYPE_BF16 || type == SD_TYPE_F16, "sd_latent_attention: type must be SD_TYPE_BF16 or SD_TYPE_F16");
-  SD_CHECK_ARG(isfinite(scale) && fabs(scale) <= 0x1p60, "sd_latent_attention: scale must be finite");
-  SD_CHECK_ARG(q && cache && lens && out && ws, "sd_latent_attention: NULL pointer argument");
-  SD_CHECK_ARG(n_pages >= 1 && page_size >= 1, "sd_latent_attention: need n_pages >= 1 and page_size >= 1");
-  if (pages) {
-    SD_CHECK_ARG(max_pages >= 1 && pages_stride >= max_pages, "sd_latent_attention: need max_pages >= 1 and pages_stride >= max_pages");
-    SD_CHECK_ARG((int64_t)max_pages * page_size < ((int64_t)1 << 30), "sd_latent_attention: a sequence's pages hold 2^30 tokens or more");
-  } else {
-    SD_CHECK_ARG(n_pages >= B, "sd_latent_attention: without a table n_pages = %d must be >= B = %d", n_pages, B);
-    SD_CHECK_ARG(page_size < (1 << 30), "sd_latent_attention: a page holds 2^30 tokens or more");
-  }
-  // (a sequence's rows are walked by at most one workgroup for every 64 of them)
-  SD_CHECK_ARG(((int64_t)(pages ? max_pages : 1) * page_size / 64 + 1) * B * ((int64_t)Q * H / 64 + 1) < ((int64_t)1 << 31),
-               "sd_latent_attention: too many rows and tokens for one call");
-  const int d = d_latent + d_rope;
-  SD_CHECK_ARG(token_stride >= d && token_stride % 8 == 0 && page_stride % 8 == 0 &&
-                   (n_pages == 1 || page_stride >= (int64_t)page_size * token_stride),
-               "sd_latent_attention: cache strides must be multiples of 8 elements that step over a token and a page");
-  SD_CHECK_ARG(stride_h_ok(qs, B, Q, H, d), "sd_latent_attention: q strides must be multiples of 8 elements that step over a row");
-  SD_CHECK_ARG(stride_h_ok(os, B, Q, H, d_latent) && apart(os, B, Q, H, d_latent),
-               "sd_latent_attention: out strides must be multiples of 8 elements that step over a row, no two rows in one place");
-  SD_CHECK_ARG(aligned(q, 16) && aligned(cache, 16) && aligned(out, 16), "sd_latent_attention: q, cache and out must be 16-byte aligned");
-  const size_t need = latent_ws_bytes(B, Q, H, d_latent);
-  SD_CHECK_ARG(ws_bytes >= need, "sd_latent_attention: workspace %zu < %zu bytes", ws_bytes, need);
-  SD_CHECK_ARG(aligned(ws, 256), "sd_latent_attention: workspace must be 256-byte aligned");
-  SD_HIP(latent_launch(B, Q, H, d_latent, d_rope, type, scale, q, qs, cache, page_stride, token_stride, n_pages,
-                       page_size, pages, pages_stride, max_pages, lens, rows, out, os, lse, ws, (hipStream_t)stream));
-  return SD_OK;
+  return attention("sd_latent_attention", B, Q, H, d_latent, d_rope, type, scale, q, qs, cache, page_stride, token_stride,
+                   n_pages, page_size, pages, pages_stride, max_pages, lens, rows, nullptr, out, os, lse, ws, ws_bytes,
+                   stream);
 }
 
 static bool expanded_shape_ok(int32_t n, int32_t H, int32_t dn, int32_t dr, int32_t dv, int32_t Tq, int32_t Tk) {
@@ -1284,6 +1301,180 @@ sd_status sd_verify_tokens(int32_t B, int32_t K, int32_t V, sd_verify_mode mode,
   SD_CHECK_ARG(verify_tokens_groups(B, K, V) <= kMaxGroups, "sd_verify_tokens: too many rows for one call");
   SD_HIP(verify_tokens_launch(B, K, V, mode, type, temperature, draft, ds, target, ts, tokens, kb, uniforms, round,
                               seed, tau, token, log_alpha_res, log_ratio, coins, ws, (hipStream_t)stream));
+  return SD_OK;
+}
+
+// ------------------------------------------------------------- tree drafts --
+static bool tree_rows_ok(int32_t B, int32_t Q) { return B >= 1 && Q >= 1 && Q <= SD_MAX_TREE; }
+
+size_t sd_latent_attention_tree_workspace(int32_t B, int32_t Q, int32_t H, int32_t d_latent, int32_t d_rope) {
+  return Q <= SD_MAX_TREE ? sd_latent_attention_workspace(B, Q, H, d_latent, d_rope) : 0;
+}
+
+sd_status sd_latent_attention_tree(int32_t B, int32_t Q, int32_t H, int32_t d_latent, int32_t d_rope, sd_type type,
+                                   double scale, const void* q, sd_stride_h qs, const void* cache, int64_t page_stride,
+                                   int64_t token_stride, int32_t n_pages, int32_t page_size, const int32_t* pages,
+                                   int64_t pages_stride, int32_t max_pages, const int32_t* lens, const int32_t* rows,
+                                   const int32_t* parents, void* out, sd_stride_h os, float* lse, void* ws,
+                                   size_t ws_bytes, sd_stream stream) {
+  SD_CHECK_ARG(Q <= SD_MAX_TREE, "sd_latent_attention_tree: Q = %d > %d", Q, SD_MAX_TREE);
+  SD_CHECK_ARG(parents, "sd_latent_attention_tree: NULL pointer argument");
+  return attention("sd_latent_attention_tree", B, Q, H, d_latent, d_rope, type, scale, q, qs, cache, page_stride,
+                   token_stride, n_pages, page_size, pages, pages_stride, max_pages, lens, rows, parents, out, os, lse,
+                   ws, ws_bytes, stream);
+}
+
+// A paged cache of vectors of d elements that a call writes.
+static sd_status pages_of(const char* name, void* cache, int d, int32_t B, int64_t page_stride, int64_t token_stride,
+                          int32_t n_pages, int32_t page_size, const int32_t* pages, int64_t pages_stride,
+                          int32_t max_pages, Pages* out) {
+  SD_CHECK_ARG(n_pages >= 1 && page_size >= 1, "%s: need n_pages >= 1 and page_size >= 1", name);
+  if (pages) {
+    SD_CHECK_ARG(max_pages >= 1 && pages_stride >= max_pages, "%s: need max_pages >= 1 and pages_stride >= max_pages", name);
+    SD_CHECK_ARG((int64_t)max_pages * page_size < ((int64_t)1 << 30), "%s: a sequence's pages hold 2^30 tokens or more", name);
+  } else {
+    SD_CHECK_ARG(n_pages >= B, "%s: without a table n_pages = %d must be >= B = %d", name, n_pages, B);
+    SD_CHECK_ARG(page_size < (1 << 30), "%s: a page holds 2^30 tokens or more", name);
+  }
+  SD_CHECK_ARG(token_stride >= d && token_stride % 8 == 0 && page_stride % 8 == 0 &&
+                   (n_pages == 1 || page_stride >= (int64_t)page_size * token_stride),
+               "%s: cache strides must be multiples of 8 elements that step over a token and a page", name);
+  *out = Pages{static_cast<uint16_t*>(cache), page_stride, token_stride, n_pages, page_size, pages, pages_stride,
+               pages ? max_pages * page_size : page_size};
+  return SD_OK;
+}
+// Strides of a [B][Q][d] view, or of a [Q][d] one (ragged).
+static bool rows_ok(sd_stride s, int B, int Q, int d, bool ragged) {
+  return (Q == 1 || (s.row % 8 == 0 && s.row >= d)) &&
+         (ragged || B == 1 || (s.chain % 8 == 0 && s.chain >= d && (Q == 1 || s.chain >= Q * s.row || s.row >= B * s.chain)));
+}
+
+sd_status sd_latent_append(int32_t B, int32_t Q, int32_t H, int32_t d_latent, int32_t d_rope, sd_type type, sd_rope rope,
+                           const double* freq, const void* latent, sd_stride ls, const void* k_rope, sd_stride krs,
+                           const int32_t* cu, const int32_t* parents, const int32_t* lens, const int32_t* rows,
+                           void* cache, int64_t page_stride, int64_t token_stride, int32_t n_pages, int32_t page_size,
+                           const int32_t* pages, int64_t pages_stride, int32_t max_pages, void* k_out, sd_stride kos,
+                           const void* q, sd_stride_h qs, void* q_out, sd_stride_h qos, sd_stream stream) {
+  SD_CHECK_ARG(B >= 1 && Q >= 1 && H >= 0, "sd_latent_append: need B >= 1, Q >= 1 and H >= 0");
+  SD_CHECK_ARG(d_latent >= 8 && d_latent <= 512 && d_latent % 8 == 0, "sd_latent_append: d_latent = %d is no multiple of 8 in [8, 512]", d_latent);
+  SD_CHECK_ARG(d_rope >= 0 && d_rope <= 64 && d_rope % 8 == 0, "sd_latent_append: d_rope = %d is no multiple of 8 in [0, 64]", d_rope);
+  SD_CHECK_ARG(type == SD_TYPE_BF16 || type == SD_TYPE_F16, "sd_latent_append: type must be SD_TYPE_BF16 or SD_TYPE_F16");
+  SD_CHECK_ARG(rope == SD_ROPE_PAIRS || rope == SD_ROPE_HALVES, "sd_latent_append: unknown rope");
+  SD_CHECK_ARG(latent && lens && cache && (d_rope == 0 || (k_rope && freq)), "sd_latent_append: NULL pointer argument");
+  SD_CHECK_ARG((H == 0) == (q == nullptr) && (H == 0) == (q_out == nullptr), "sd_latent_append: q and q_out go with H > 0");
+  SD_CHECK_ARG(d_rope > 0 || (H == 0 && !k_out), "sd_latent_append: q and k_out need d_rope > 0");
+  SD_CHECK_ARG(!cu || (!rows && !parents), "sd_latent_append: rows and parents must be NULL with cu");
+  SD_CHECK_ARG(!parents || Q <= SD_MAX_TREE, "sd_latent_append: Q = %d > %d", Q, SD_MAX_TREE);
+  AppendArgs a;
+  const sd_status st = pages_of("sd_latent_append", cache, d_latent + d_rope, B, page_stride, token_stride, n_pages,
+                                page_size, pages, pages_stride, max_pages, &a.pages);
+  if (st != SD_OK) return st;
+  const bool ragged = cu != nullptr;
+  SD_CHECK_ARG(rows_ok(ls, B, Q, d_latent, ragged), "sd_latent_append: latent strides must be multiples of 8 elements that step over a row");
+  SD_CHECK_ARG(d_rope == 0 || rows_ok(krs, B, Q, d_rope, ragged), "sd_latent_append: k_rope strides must be multiples of 8 elements that step over a row");
+  SD_CHECK_ARG(!k_out || rows_ok(kos, B, Q, d_rope, ragged), "sd_latent_append: k_out strides must be multiples of 8 elements that step over a row");
+  if (H > 0) {
+    const int n = ragged ? 1 : B;
+    SD_CHECK_ARG(stride_h_ok(qs, n, Q, H, d_rope), "sd_latent_append: q strides must be multiples of 8 elements that step over a row");
+    SD_CHECK_ARG(stride_h_ok(qos, n, Q, H, d_rope) && apart(qos, n, Q, H, d_rope),
+                 "sd_latent_append: q_out strides must be multiples of 8 elements that step over a row, no two rows in one place");
+  }
+  SD_CHECK_ARG(aligned(latent, 16) && (d_rope == 0 || aligned(k_rope, 16)) && aligned(cache, 16) && aligned(k_out, 16) &&
+                   aligned(q, 16) && aligned(q_out, 16),
+               "sd_latent_append: latent, k_rope, cache, k_out, q and q_out must be 16-byte aligned");
+  const int64_t tokens = ragged ? Q : (int64_t)B * Q;
+  SD_CHECK_ARG(tokens < ((int64_t)1 << 31) && append_groups(tokens, H, d_rope) <= kMaxGroups, "sd_latent_append: too many rows for one call");
+  a.B = B;
+  a.Q = Q;
+  a.H = H;
+  a.dc = d_latent;
+  a.dr = d_rope;
+  a.halves = rope == SD_ROPE_HALVES;
+  a.freq = freq;
+  a.latent = static_cast<const uint16_t*>(latent);
+  a.ls = ls;
+  a.k_rope = static_cast<const uint16_t*>(k_rope);
+  a.krs = krs;
+  a.cu = cu;
+  a.parents = parents;
+  a.lens = lens;
+  a.rows = rows;
+  a.k_out = static_cast<uint16_t*>(k_out);
+  a.kos = kos;
+  a.q = static_cast<const uint16_t*>(q);
+  a.qs = qs;
+  a.q_out = static_cast<uint16_t*>(q_out);
+  a.qos = qos;
+  SD_HIP(append_launch(a, tokens, type, (hipStream_t)stream));
+  return SD_OK;
+}
+
+size_t sd_verify_tree_workspace(int32_t B, int32_t Q, int32_t V) {
+  if (!tree_rows_ok(B, Q) || V < 1 || V > SD_MAX_VOCAB) return 0;
+  return verify_tree_ws_bytes(B, Q, V);
+}
+
+sd_status sd_verify_tree(int32_t B, int32_t Q, int32_t V, sd_tree_draws draws, sd_type type, double temperature,
+                         int32_t max_children, const void* draft, sd_stride ds, const void* target, sd_stride ts,
+                         const int32_t* tokens, const int32_t* parents, const int32_t* rows, const double* uniforms,
+                         const uint32_t* round, uint64_t seed, int32_t* tau, int32_t* token, int32_t* path,
+                         float* accept, void* ws, size_t ws_bytes, sd_stream stream) {
+  SD_CHECK_ARG(B >= 1, "sd_verify_tree: B = %d < 1", B);
+  SD_CHECK_ARG(Q >= 1 && Q <= SD_MAX_TREE, "sd_verify_tree: Q = %d not in [1, %d]", Q, SD_MAX_TREE);
+  SD_CHECK_ARG(V >= 1 && V <= SD_MAX_VOCAB, "sd_verify_tree: V = %d not in [1, %d]", V, SD_MAX_VOCAB);
+  SD_CHECK_ARG(draws == SD_TREE_IID || draws == SD_TREE_DISTINCT || draws == SD_TREE_GIVEN, "sd_verify_tree: unknown draws");
+  SD_CHECK_ARG(type_ok(type), "sd_verify_tree: unknown type");
+  SD_CHECK_ARG(temperature_ok(temperature), "sd_verify_tree: temperature must be in [2^-60, 2^60]");
+  SD_CHECK_ARG(max_children >= 1 && max_children <= Q, "sd_verify_tree: max_children = %d not in [1, Q = %d]", max_children, Q);
+  SD_CHECK_ARG((draft == nullptr) == (draws == SD_TREE_GIVEN), "sd_verify_tree: draft must be NULL with SD_TREE_GIVEN and only then");
+  SD_CHECK_ARG(target && tokens && parents && tau && token && path && ws, "sd_verify_tree: NULL pointer argument");
+  SD_CHECK_ARG(uniforms || round, "sd_verify_tree: one of uniforms and round must be non-NULL");
+  SD_CHECK_ARG(!draft || stride_ok(ds, V, Q), "sd_verify_tree: draft stride too small for [B][Q][V]");
+  SD_CHECK_ARG(stride_ok(ts, V, Q), "sd_verify_tree: target stride too small for [B][Q][V]");
+  SD_CHECK_ARG(aligned(draft, type_size(type)) && aligned(target, type_size(type)),
+               "sd_verify_tree: draft and target must be aligned to their element");
+  const size_t need = verify_tree_ws_bytes(B, Q, V);
+  SD_CHECK_ARG(ws_bytes >= need, "sd_verify_tree: workspace %zu < %zu bytes", ws_bytes, need);
+  SD_CHECK_ARG(aligned(ws, 256), "sd_verify_tree: workspace must be 256-byte aligned");
+  SD_CHECK_ARG(verify_tree_groups(B, Q, V) <= kMaxGroups, "sd_verify_tree: too many rows for one call");
+  const VerifyTreeArgs a{B, Q, V, draws, max_children, draft, ds, target, ts, tokens, parents, rows, uniforms, round,
+                         seed, tau, token, path, accept};
+  SD_HIP(verify_tree_launch(a, type, temperature, ws, (hipStream_t)stream));
+  return SD_OK;
+}
+
+sd_status sd_latent_keep(int32_t layers, int32_t B, int32_t Q, int32_t d, sd_type type, void* cache, int64_t layer_stride,
+                         int64_t page_stride, int64_t token_stride, int32_t n_pages, int32_t page_size,
+                         const int32_t* pages, int64_t pages_stride, int32_t max_pages, const int32_t* lens,
+                         const int32_t* rows, const int32_t* tau, const int32_t* path, int32_t* new_lens,
+                         sd_stream stream) {
+  SD_CHECK_ARG(layers >= 1 && B >= 1 && Q >= 1, "sd_latent_keep: need layers >= 1, B >= 1 and Q >= 1");
+  SD_CHECK_ARG(d >= 8 && d <= 576 && d % 8 == 0, "sd_latent_keep: d = %d is no multiple of 8 in [8, 576]", d);
+  SD_CHECK_ARG(type == SD_TYPE_BF16 || type == SD_TYPE_F16, "sd_latent_keep: type must be SD_TYPE_BF16 or SD_TYPE_F16");
+  SD_CHECK_ARG(cache && lens && tau && path, "sd_latent_keep: NULL pointer argument");
+  KeepArgs a;
+  const sd_status st = pages_of("sd_latent_keep", cache, d, B, page_stride, token_stride, n_pages, page_size, pages,
+                                pages_stride, max_pages, &a.pages);
+  if (st != SD_OK) return st;
+  // (layers over pages or pages over layers, but no two vectors in one place)
+  SD_CHECK_ARG(layers == 1 || (layer_stride % 8 == 0 && layer_stride >= d &&
+                               apart(sd_stride_h{layer_stride, page_stride, token_stride}, layers, n_pages, page_size, d)),
+               "sd_latent_keep: layer stride must be a multiple of 8 elements that leaves no two vectors in one place");
+  SD_CHECK_ARG(aligned(cache, 16), "sd_latent_keep: cache must be 16-byte aligned");
+  SD_CHECK_ARG(!new_lens || (uintptr_t)(new_lens + B) <= (uintptr_t)lens || (uintptr_t)(lens + B) <= (uintptr_t)new_lens,
+               "sd_latent_keep: new_lens overlaps lens");
+  SD_CHECK_ARG((int64_t)B * Q < ((int64_t)1 << 31) && keep_groups(layers, B, d / 8) <= kMaxGroups, "sd_latent_keep: too many rows for one call");
+  a.layers = layers;
+  a.B = B;
+  a.Q = Q;
+  a.pieces = d / 8;
+  a.layer_stride = layer_stride;
+  a.lens = lens;
+  a.rows = rows;
+  a.tau = tau;
+  a.path = path;
+  a.new_lens = new_lens;
+  SD_HIP(keep_launch(a, (hipStream_t)stream));
   return SD_OK;
 }
 

@@ -310,6 +310,66 @@ hipError_t verify_tokens_launch(int B, int K, int V, int mode, sd_type type, dou
                                 int32_t* tau, int32_t* token, float* log_alpha_res, float* log_ratio,
                                 uint64_t* coins, void* ws, hipStream_t s);
 
+// ------------------------------------------------------------- tree drafts --
+// A paged cache of 16-bit vectors as the kernels that write it see it.
+struct Pages {
+  uint16_t* cache;
+  int64_t page_stride, token_stride;
+  int n_pages, page_size;
+  const int32_t* table;  // null: page b is sequence b
+  int64_t table_stride;
+  int capacity;  // tokens that a sequence's pages hold
+};
+struct AppendArgs {
+  int B, Q, H, dc, dr;
+  bool halves;
+  const double* freq;
+  const uint16_t* latent;
+  sd_stride ls;
+  const uint16_t* k_rope;
+  sd_stride krs;
+  const int32_t *cu, *parents, *lens, *rows;
+  Pages pages;
+  uint16_t* k_out;
+  sd_stride kos;
+  const uint16_t* q;
+  sd_stride_h qs;
+  uint16_t* q_out;
+  sd_stride_h qos;
+};
+struct KeepArgs {
+  int layers, B, Q, pieces;  // pieces: 16 bytes of a vector
+  int64_t layer_stride;
+  Pages pages;
+  const int32_t *lens, *rows, *tau, *path;
+  int32_t* new_lens;
+};
+int64_t append_groups(int64_t tokens, int H, int dr);
+hipError_t append_launch(const AppendArgs& a, int64_t tokens, sd_type type, hipStream_t s);
+int64_t keep_groups(int layers, int B, int pieces);
+hipError_t keep_launch(const KeepArgs& a, hipStream_t s);
+hipError_t latent_tree_launch(int B, int Q, int H, int dc, int dr, sd_type type, double scale, const void* q, sd_stride_h qs,
+                              const void* cache, int64_t page_stride, int64_t token_stride, int n_pages, int page_size,
+                              const int32_t* pages, int64_t pages_stride, int max_pages, const int32_t* lens,
+                              const int32_t* rows, const int32_t* parents, void* out, sd_stride_h os, float* lse,
+                              void* ws, hipStream_t s);
+int64_t verify_tree_groups(int B, int Q, int V);
+size_t verify_tree_ws_bytes(int B, int Q, int V);
+struct VerifyTreeArgs {
+  int B, Q, V, draws, max_children;
+  const void* draft;
+  sd_stride ds;
+  const void* target;
+  sd_stride ts;
+  const int32_t *tokens, *parents, *rows;
+  const double* uniforms;
+  const uint32_t* round;
+  uint64_t seed;
+  int32_t *tau, *token, *path;
+  float* accept;
+};
+hipError_t verify_tree_launch(const VerifyTreeArgs& a, sd_type type, double temperature, void* ws, hipStream_t s);
+
 inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 
 // Whether a kernel that writes a block of `bytes` of draft rows uses

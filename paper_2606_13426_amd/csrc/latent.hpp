@@ -32,6 +32,12 @@
 // inside a sequence: its part is left in the workspace and joined by
 // latent_join_kernel.
 //
+// With TREE the rows of a sequence are nodes of a tree: a row sees the prefix, itself and its
+// ancestors.  A node's ancestors are 64 bits, found from the parents by the first wavefront
+// of a workgroup whose run reaches behind the prefix, in six doublings (a node's set, joined with that
+// of the node its chain of parents has reached so far), and kept in LDS beside the
+// rows; only tiles behind the prefix look at them.
+//
 // What bounds it, on MI355X.  Up to 32 rows: the cache's stream (2 sequences of 131072
 // tokens, 32 heads, bf16: 59 us, 5.1 TB/s, and 13 us for the join of 128 parts a row).
 // With 64 rows the phases between a tile's three barriers: one workgroup fills a compute
@@ -106,6 +112,7 @@ struct Args {
   float2* stat;    // [kGroups][2][16 R] (reference in log2 units, sum)
   int32_t* first;  // [B][supers] 2 team + slot of the run that starts the sequence; -1: one run did it all
   int32_t* last;   // [B][supers] the team that ends it
+  const int32_t* parents;  // [B][Q], with TREE
 };
 
 __device__ __forceinline__ int length_of(const Args& a, int b) { return min(max(load_global<int32_t>(a.lens + b), 0), a.capacity); }
@@ -118,7 +125,21 @@ __device__ __forceinline__ int group_of(int team, int member, int size) {
   return (team / 8 * size + member) * 8 + team % 8;
 }
 
-template <class T, int R, int DC>
+// The nodes that node `lane` of sequence b sees, itself among them; up: its parent in the tree.
+__device__ __forceinline__ uint64_t ancestors(int up, int lane) {
+  uint64_t set = 1ull << lane;
+#pragma unroll
+  for (int i = 0; i < 6; ++i) {
+    const int from = up < 0 ? lane : up;
+    const uint64_t more = (uint64_t)__shfl((unsigned long long)set, from);
+    const int next = __shfl(up, from);
+    set |= more;
+    up = up < 0 ? -1 : next;
+  }
+  return set;
+}
+
+template <class T, int R, int DC, bool TREE>
 __global__ __launch_bounds__(R == 1 ? 256 : 512) void latent_kernel(Args a) {
   constexpr int kWaves = R == 1 ? 4 : 8, kLanes = 64 * kWaves;
   constexpr int WR = R, WT = kWaves / WR, TB = kTile / 16 / WT;  // row groups of 16, token groups of 16 TB
@@ -134,6 +155,7 @@ __global__ __launch_bounds__(R == 1 ? 256 : 512) void latent_kernel(Args a) {
   __shared__ float red[WT][16 * R];
   __shared__ float fac[16 * R];
   __shared__ int limits[16 * R];
+  __shared__ uint64_t kin[TREE ? 16 * R : 1];  // a row's node and its ancestors
   __shared__ int moved[2][WR + 1];  // whose rows' reference moved; last: values that are no numbers
   __shared__ uint32_t present[kWaves];
 
@@ -249,7 +271,12 @@ __global__ __launch_bounds__(R == 1 ? 256 : 512) void latent_kernel(Args a) {
     if (r0 >= nrow * a.H) continue;
     // query rows' limits: row i of n sees len - n + i + 1 tokens
     const int rlast = min(r0 + 16 * R, nrow * a.H) - 1;
-    const int lim_lo = max(len - nrow + r0 / a.H + 1, 0), lim_hi = max(len - nrow + rlast / a.H + 1, 0);
+    // (a tree's rows all see the prefix; what they see of the rest their nodes say)
+    const int lim_lo = TREE ? max(len - nrow, 0) : max(len - nrow + r0 / a.H + 1, 0), lim_hi = max(len - nrow + rlast / a.H + 1, 0);
+    [[maybe_unused]] int up = -1;
+    if constexpr (TREE) {
+      if (w == 0 && t1 * kTile > lim_lo && lane < nrow) up = load_global<int32_t>(a.parents + (int64_t)b * a.Q + lane);
+    }
 
     // Tile tl's part of this wavefront: tokens tl * 64 + TW w .. + TW - 1.  Returns which of them some
     // row sees and whose page exists; the others are not loaded.
@@ -338,7 +365,15 @@ __global__ __launch_bounds__(R == 1 ? 256 : 512) void latent_kernel(Args a) {
         __builtin_amdgcn_s_waitcnt(0);
     }
     if (t < 2 * (WR + 1)) moved[t / (WR + 1)][t % (WR + 1)] = 0;
-    if (t < 16 * R) limits[t] = r0 + t <= rlast ? len - nrow + (r0 + t) / a.H + 1 : 0;
+    if constexpr (TREE) {
+      if (w == 0 && t1 * kTile > lim_lo) {
+        const uint64_t set = ancestors(up < lane ? up : -1, lane);
+        const uint64_t mine = (uint64_t)__shfl((unsigned long long)set, min(r0 + lane, rlast) / a.H);
+        if (lane < 16 * R) kin[lane] = mine;
+      }
+    } else {
+      if (t < 16 * R) limits[t] = r0 + t <= rlast ? len - nrow + (r0 + t) / a.H + 1 : 0;
+    }
     lds_barrier();
 
     u32x4 qf[KS];
@@ -416,7 +451,18 @@ __global__ __launch_bounds__(R == 1 ? 256 : 512) void latent_kernel(Args a) {
       const bool edge = (tl + 1) * kTile > lim_lo;
       if (edge || seen != (uint32_t)((1ull << (16 * TB)) - 1)) {
         const int ahead = lim - (tl * kTile + 16 * TB * wt + 4 * g);  // its tokens from this lane's first on
-        const uint32_t have = seen >> (4 * g);
+        uint32_t have = seen >> (4 * g);
+        if constexpr (TREE) {
+          if (edge) {
+            const int ln = rare(lane);
+            const uint64_t set = kin[16 * wr + (ln & 15)];
+            const int node = tl * kTile + 16 * TB * wt + 4 * (ln >> 4) - (len - nrow);  // of this lane's first token
+            have &= node >= 64   ? 0u
+                    : node >= 0  ? (uint32_t)(set >> node)
+                    : node > -32 ? ((uint32_t)set << -node) | ((1u << -node) - 1u)
+                                 : ~0u;
+          }
+        }
 #pragma unroll
         for (int j = 0; j < TB; ++j)
 #pragma unroll
@@ -481,7 +527,12 @@ __global__ __launch_bounds__(R == 1 ? 256 : 512) void latent_kernel(Args a) {
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
                   const float p = T::value(pl[(16 * r + nn) * kTile + (at ^ (nn & 7)) * 8 + part]);
-                  if (first + j < limits[16 * r + nn]) o[r][k][i] += p * T::value(v);
+                  if constexpr (TREE) {
+                    const int node = first + j - (len - nrow);  // (in [0, 64): from the prefix's end to the last row's)
+                    if (kin[16 * r + nn] >> node & 1u) o[r][k][i] += p * T::value(v);
+                  } else {
+                    if (first + j < limits[16 * r + nn]) o[r][k][i] += p * T::value(v);
+                  }
                 }
               }
             }
@@ -648,9 +699,9 @@ __global__ __launch_bounds__(kThreads) void latent_join_kernel(Args a) {
   }
 }
 
-template <class T, int R, int DC>
+template <class T, int R, int DC, bool TREE>
 hipError_t run(const Args& a, hipStream_t s) {
-  hipError_t e = launch_timed("latent_attention", latent_kernel<T, R, DC>, dim3(kGroups), dim3(R == 1 ? 256 : 512), s, a);
+  hipError_t e = launch_timed(TREE ? "latent_tree" : "latent_attention", latent_kernel<T, R, DC, TREE>, dim3(kGroups), dim3(R == 1 ? 256 : 512), s, a);
   if (e != hipSuccess) return e;
   // One wavefront a row, or four for 128 columns of it where rows are few and may have eight parts or
   // more.  In us, one / four: 64 rows of 128 parts 40 / 13, 512 rows of 16 parts 9.7 / 9.6, 2048
@@ -663,11 +714,11 @@ hipError_t run(const Args& a, hipStream_t s) {
                             dim3(kThreads), s, a);
 }
 
-template <class T>
+template <class T, bool TREE = false>
 hipError_t run_type(const Args& a, hipStream_t s) {
   auto by_rows = [&](auto dc) {
     constexpr int DC = decltype(dc)::value;
-    return a.p.R == 1 ? run<T, 1, DC>(a, s) : a.p.R == 2 ? run<T, 2, DC>(a, s) : run<T, 4, DC>(a, s);
+    return a.p.R == 1 ? run<T, 1, DC, TREE>(a, s) : a.p.R == 2 ? run<T, 2, DC, TREE>(a, s) : run<T, 4, DC, TREE>(a, s);
   };
   return a.dc <= 128   ? by_rows(std::integral_constant<int, 128>{})
          : a.dc <= 256 ? by_rows(std::integral_constant<int, 256>{})

@@ -1,9 +1,11 @@
-// sd_latent_attention's kernels for fp16 queries and caches, and the choice of type.
+// sd_latent_attention's kernels for fp16 queries and caches, and the choice of type and form.
 #include "latent.hpp"
 
 namespace sd {
 
 hipError_t latent_bf16_launch(const latent::Args& a, hipStream_t s);
+hipError_t latent_tree_bf16_launch(const latent::Args& a, hipStream_t s);
+hipError_t latent_tree_f16_launch(const latent::Args& a, hipStream_t s);
 
 namespace {
 inline size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
@@ -34,10 +36,11 @@ size_t latent_ws_bytes(int B, int Q, int H, int dc) {
   return most;
 }
 
-hipError_t latent_launch(int B, int Q, int H, int dc, int dr, sd_type type, double scale, const void* q, sd_stride_h qs,
-                         const void* cache, int64_t page_stride, int64_t token_stride, int n_pages, int page_size,
-                         const int32_t* pages, int64_t pages_stride, int max_pages, const int32_t* lens,
-                         const int32_t* rows, void* out, sd_stride_h os, float* lse, void* ws, hipStream_t s) {
+static latent::Args args_of(int B, int Q, int H, int dc, int dr, double scale, const void* q, sd_stride_h qs,
+                            const void* cache, int64_t page_stride, int64_t token_stride, int n_pages, int page_size,
+                            const int32_t* pages, int64_t pages_stride, int max_pages, const int32_t* lens,
+                            const int32_t* rows, const int32_t* parents, void* out, sd_stride_h os, float* lse,
+                            void* ws) {
   latent::Args a;
   a.B = B;
   a.Q = Q;
@@ -61,6 +64,7 @@ hipError_t latent_launch(int B, int Q, int H, int dc, int dr, sd_type type, doub
   a.capacity = pages ? max_pages * page_size : page_size;
   a.lens = lens;
   a.rows = rows;
+  a.parents = parents;
   a.out = static_cast<uint16_t*>(out);
   a.os = os.seq;
   a.orow = os.row;
@@ -73,7 +77,26 @@ hipError_t latent_launch(int B, int Q, int H, int dc, int dr, sd_type type, doub
   a.stat = reinterpret_cast<float2*>(base + l.stat);
   a.first = reinterpret_cast<int32_t*>(base + l.first);
   a.last = reinterpret_cast<int32_t*>(base + l.last);
+  return a;
+}
+
+hipError_t latent_launch(int B, int Q, int H, int dc, int dr, sd_type type, double scale, const void* q, sd_stride_h qs,
+                         const void* cache, int64_t page_stride, int64_t token_stride, int n_pages, int page_size,
+                         const int32_t* pages, int64_t pages_stride, int max_pages, const int32_t* lens,
+                         const int32_t* rows, void* out, sd_stride_h os, float* lse, void* ws, hipStream_t s) {
+  const latent::Args a = args_of(B, Q, H, dc, dr, scale, q, qs, cache, page_stride, token_stride, n_pages, page_size, pages,
+                                 pages_stride, max_pages, lens, rows, nullptr, out, os, lse, ws);
   return type == SD_TYPE_BF16 ? latent_bf16_launch(a, s) : latent::run_type<latent::F16>(a, s);
+}
+
+hipError_t latent_tree_launch(int B, int Q, int H, int dc, int dr, sd_type type, double scale, const void* q, sd_stride_h qs,
+                              const void* cache, int64_t page_stride, int64_t token_stride, int n_pages, int page_size,
+                              const int32_t* pages, int64_t pages_stride, int max_pages, const int32_t* lens,
+                              const int32_t* rows, const int32_t* parents, void* out, sd_stride_h os, float* lse,
+                              void* ws, hipStream_t s) {
+  const latent::Args a = args_of(B, Q, H, dc, dr, scale, q, qs, cache, page_stride, token_stride, n_pages, page_size, pages,
+                                 pages_stride, max_pages, lens, rows, parents, out, os, lse, ws);
+  return type == SD_TYPE_BF16 ? latent_tree_bf16_launch(a, s) : latent_tree_f16_launch(a, s);
 }
 
 }  // namespace sd

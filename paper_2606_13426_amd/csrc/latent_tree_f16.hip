@@ -1,0 +1,6 @@
+// sd_latent_attention_tree's kernels for fp16 queries and caches.
+#include "latent.hpp"
+
+namespace sd {
+hipError_t latent_tree_f16_launch(const latent::Args& a, hipStream_t s) { return latent::run_type<latent::F16, true>(a, s); }
+}  // namespace sd

@@ -1,0 +1,144 @@
+"""sd_latent_attention_tree against the float64 oracle; the bounds are those of test_gpu_latent.py,
+a row's tokens being the prefix, itself and its ancestors."""
+import numpy as np
+import pytest
+import torch
+
+import test_gpu_latent as chain
+from oracle import latent as olat
+from oracle import tree
+from paper_2606_13426_amd import _lib
+
+pytestmark = pytest.mark.gpu
+DEV, U, TYPES = "cuda", chain.U, chain.TYPES
+
+
+def _grown(seed, B, Q, wide=3):
+    r = np.random.default_rng(seed)
+    return [[-1] + [int(r.integers(max(0, (i - 1) // wide - 1), i)) for i in range(1, Q)] for _ in range(B)]
+
+
+def _i32(v):
+    return torch.tensor(v, dtype=torch.int32, device=DEV)
+
+
+def _check(q, cache, lens, parents, dc, pages, rows, scale, got, t, seqs=None, heads=None):
+    out, lse = (x.double().cpu().numpy() for x in got)
+    qn, cn = q.double().cpu().numpy(), cache.double().cpu().numpy()
+    B, Q, H, d = qn.shape
+    e = chain._half_step(t)
+    for b in range(B) if seqs is None else seqs:
+        n = min(max(int(lens[b]), 0), cn.shape[1] if pages is None else pages.shape[1] * cn.shape[1])
+        nb = Q if rows is None else min(max(int(rows[b]), 0), Q)
+        c, have = olat.gather(cn, [b] if pages is None else pages[b].cpu().numpy(), n)
+        kin = tree.sees([int(p) for p in parents[b]], nb)
+        for i in range(nb):
+            see = np.zeros(n, bool)
+            see[:max(n - nb, 0)] = True
+            for j in np.nonzero(kin[i])[0]:
+                if n - nb + j >= 0:
+                    see[n - nb + j] = True
+            see &= have
+            k = c[see]
+            for h in range(H) if heads is None else heads:
+                w, wl, mag = (x[0] for x in olat.attend(qn[b, i, h][None], k, k[:, :dc], scale, [len(k)]))
+                if len(k) == 0:
+                    assert (out[b, i, h] == 0).all() and lse[b, i, h] == -np.inf, (b, i, h)
+                    continue
+                if np.isnan(wl):
+                    assert np.isnan(lse[b, i, h]) and np.isnan(out[b, i, h]).all()
+                    continue
+                ds = (d + 5) * U * abs(scale) * (np.abs(k) @ np.abs(qn[b, i, h])).max()
+                assert abs(lse[b, i, h] - wl) <= ds + (len(k) + 4) * U + U * abs(wl), (b, i, h, lse[b, i, h], wl)
+                tol = 2 * (ds + e + (len(k) + 4) * U) * mag + e * np.abs(w) + (2.0 ** -24 if t == "f16" else 0.0)
+                same = (out[b, i, h] == w) | (np.isnan(out[b, i, h]) & np.isnan(w))  # (infinite values)
+                with np.errstate(invalid="ignore"):
+                    assert (same | (np.abs(out[b, i, h] - w) <= tol)).all(), (b, i, h)
+
+
+@pytest.mark.parametrize("t", list(TYPES))
+@pytest.mark.parametrize("B,Q,H,dc,dr,page,lens", [
+    (1, 1, 1, 8, 0, 4, [1]), (1, 2, 16, 512, 64, 64, [2]), (3, 5, 5, 128, 64, 16, [0, 5, 64]), (2, 16, 16, 512, 64, 1, [63, 130]),
+    (2, 64, 4, 256, 32, 48, [64, 150]), (1, 9, 4, 512, 64, 100, [3]), (4, 33, 3, 384, 64, 64, [200, 97, 128, 33]),
+    (2, 7, 13, 136, 40, 7, [129, 300]), (2, 20, 32, 512, 64, 64, [515, 90]), (3, 64, 1, 64, 16, 5, [70, -4, 91]),
+    (150, 3, 4, 128, 0, 16, [(37 * i) % 150 for i in range(150)]), (1, 31, 64, 504, 8, 33, [1000]),
+    (5, 9, 48, 256, 64, 64, [700, 9, 64, 650, 73])])
+def test_tree_attention(B, Q, H, dc, dr, page, lens, t):
+    q, cache, ln, pages = chain._case(B, Q, H, dc, dr, lens, t, B * 10 + Q, page)
+    parents = _grown(B + Q, B, Q)
+    got = _lib.sd_latent_attention_tree(q, cache, ln, _i32(parents), dc, pages=pages, scale=(dc + dr) ** -0.5)
+    _check(q, cache, lens, parents, dc, pages, None, (dc + dr) ** -0.5, got, t, seqs=None if B < 10 else range(0, B, 23),
+           heads=None if H < 10 else [0, H // 2, H - 1])
+
+
+@pytest.mark.parametrize("B,Q,H,lens", [(1, 16, 4, [20000]), (2, 32, 32, [9000, 4133])])
+def test_long_sequences_are_split_and_joined(B, Q, H, lens):
+    q, cache, ln, pages = chain._case(B, Q, H, 512, 64, lens, "bf16", 3, page=64)
+    parents = _grown(5, B, Q)
+    got = _lib.sd_latent_attention_tree(q, cache, ln, _i32(parents), 512, pages=pages, scale=0.07)
+    _check(q, cache, lens, parents, 512, pages, None, 0.07, got, "bf16", heads=[0, H - 1])
+
+
+def test_a_chain_of_nodes_is_the_chain_form():
+    for B, Q, H, lens in ((2, 9, 32, [700, 64]), (3, 64, 2, [64, 128, 65]), (1, 5, 4, [130])):
+        q, cache, ln, pages = chain._case(B, Q, H, 512, 64, lens, "bf16", 7, page=48)
+        parents = _i32([list(range(-1, Q - 1))] * B)
+        want = _lib.sd_latent_attention(q, cache, ln, 512, pages=pages, scale=0.07)
+        got = _lib.sd_latent_attention_tree(q, cache, ln, parents, 512, pages=pages, scale=0.07)
+        assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
+
+
+def test_parents_of_no_node_and_rows_past_a_sequences_own():
+    B, Q, H, dc = 5, 6, 6, 128
+    parents = [[7, 0, 5, -1, 3, 2 ** 31 - 1], [-2 ** 31, 1, 0, 2, 4, 4], [0, 0, 0, 0, 0, 0], [-1, 0, 1, 2, 3, 4], [9, 9, 9, 9, 9, 9]]
+    lens, rows = [300, 4, 0, 65, 40], [6, 4, 3, 0, 99]
+    q, cache, ln, pages = chain._case(B, Q, H, dc, 64, lens, "bf16", 4)
+    q[1, 4:] = float("nan")
+    q[3] = float("nan")
+    out, lse = torch.full((B, Q, H, dc), 7.0, dtype=torch.bfloat16, device=DEV), torch.full((B, Q, H), 7.0, device=DEV)
+    got = _lib.sd_latent_attention_tree(q, cache, ln, _i32(parents), dc, pages=pages, rows=_i32(rows), scale=0.07, out=out, lse=lse)
+    _check(q, cache, lens, parents, dc, pages, rows, 0.07, got, "bf16")
+    assert (out[1, 4:] == 7).all() and (lse[1, 4:] == 7).all() and (out[3] == 7).all() and (lse[3] == 7).all()
+
+
+@pytest.mark.parametrize("t", list(TYPES))
+@pytest.mark.parametrize("H", [2, 40])
+def test_values_that_are_no_numbers_in_nodes_others_do_not_see(H, t):
+    """Nodes hold NaN, infinities and the type's largest value: only they and their descendants know of them."""
+    B, Q, dc = 2, 12, 256
+    lens = [150, 12]
+    q, cache, ln, pages = chain._case(B, Q, H, dc, 64, lens, t, 6)
+    parents = [[-1, 0, 0, 1, 1, 2, 2, 3, 5, 5, 8, 4]] * 2
+    for b in range(B):
+        for node, value in ((3, float("nan")), (6, float("inf")), (9, -float("inf")), (11, torch.finfo(TYPES[t]).min)):
+            j = lens[b] - Q + node
+            cache[pages[b, j // 16], j % 16, 5::64] = value
+    got = _lib.sd_latent_attention_tree(q, cache, ln, _i32(parents), dc, pages=pages, scale=0.05)
+    clean = [i for i in range(Q) if i not in (3, 7, 6, 9, 11)]
+    assert torch.isfinite(got[0][:, clean].float()).all() and torch.isfinite(got[1][:, clean]).all()
+    assert torch.isnan(got[0][:, [3, 7]].float()).all()
+    keep = cache.clone()
+    keep[~torch.isfinite(keep)] = 0  # what the clean rows see does not depend on it
+    keep[keep == torch.finfo(TYPES[t]).min] = 0
+    again = _lib.sd_latent_attention_tree(q, keep, ln, _i32(parents), dc, pages=pages, scale=0.05)
+    assert torch.equal(again[0][:, clean], got[0][:, clean]) and torch.equal(again[1][:, clean], got[1][:, clean])
+    _check(q[:, clean[:3]], cache, [n - Q + 3 for n in lens], [p[:3] for p in parents], dc, pages, None, 0.05,
+           tuple(x[:, clean[:3]] for x in got), t)
+
+
+def test_pages_that_do_not_exist_plain_caches_and_views():
+    q, cache, ln, pages = chain._case(3, 8, 5, 128, 64, [150, 150, 40], "bf16", 6)
+    parents = _grown(3, 3, 8)
+    pages[0, 9], pages[0, 2], pages[1, 0], pages[2, 2] = -1, cache.shape[0], 2 ** 31 - 1, -2 ** 31
+    got = _lib.sd_latent_attention_tree(q, cache, ln, _i32(parents), 128, pages=pages, scale=-0.1)
+    _check(q, cache, [150, 150, 40], parents, 128, pages, None, -0.1, got, "bf16")
+    B, Q, H, dc, L = 3, 6, 4, 256, 200
+    g = torch.Generator(device=DEV)
+    g.manual_seed(8)
+    q = torch.randn(B, H, Q, dc + 72, generator=g, device=DEV).half()[..., 8:].transpose(1, 2)
+    cache = torch.randn(B + 1, L, 2, dc + 64, generator=g, device=DEV).half()[:B, :, 1]
+    out = torch.full((B, H, Q, dc + 16), 9.0, dtype=torch.float16, device=DEV)
+    parents, lens = _grown(9, B, Q), [200, 131, 900]
+    got = _lib.sd_latent_attention_tree(q, cache, _i32(lens), _i32(parents), dc, scale=0.05, out=out[..., 16:].transpose(1, 2))
+    _check(q, cache, lens, parents, dc, None, None, 0.05, got, "f16")
+    assert (out[..., :16] == 9.0).all()
