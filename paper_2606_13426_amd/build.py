@@ -22,6 +22,13 @@ FLAGS = [
     "-Wno-unused-command-line-argument",
 ]
 
+# Sources with flags of their own: matrix products whose results are ordinary registers where a kernel keeps
+# the accumulation registers to itself.
+MORE_FLAGS = {
+    "latent_wide_bf16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+    "latent_wide_f16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+}
+
 
 def _hipcc():
     return os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -29,7 +36,7 @@ def _hipcc():
 
 def _compile(src):
     obj = os.path.join(BUILD_DIR, os.path.basename(src) + ".o")
-    cmd = [_hipcc(), *FLAGS, "-I", os.path.join(ROOT, "include"), "-I", os.path.join(HERE, "csrc"),
+    cmd = [_hipcc(), *FLAGS, *MORE_FLAGS.get(os.path.basename(src), []), "-I", os.path.join(ROOT, "include"), "-I", os.path.join(HERE, "csrc"),
            "-c", src, "-o", obj]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:

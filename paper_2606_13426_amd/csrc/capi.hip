@@ -1172,7 +1172,7 @@ static sd_status attention(const char* name, int32_t B, int32_t Q, int32_t H, in
   SD_CHECK_ARG(stride_h_ok(os, B, Q, H, d_latent) && apart(os, B, Q, H, d_latent),
                "%s: out strides must be multiples of 8 elements that step over a row, no two rows in one place", name);
   SD_CHECK_ARG(aligned(q, 16) && aligned(cache, 16) && aligned(out, 16), "%s: q, cache and out must be 16-byte aligned", name);
-  const size_t need = latent_ws_bytes(B, Q, H, d_latent);
+  const size_t need = parents ? latent_tree_ws_bytes(B, Q, H, d_latent, d_rope) : latent_ws_bytes(B, Q, H, d_latent);
   SD_CHECK_ARG(ws_bytes >= need, "%s: workspace %zu < %zu bytes", name, ws_bytes, need);
   SD_CHECK_ARG(aligned(ws, 256), "%s: workspace must be 256-byte aligned", name);
   if (parents)
@@ -1308,7 +1308,7 @@ sd_status sd_verify_tokens(int32_t B, int32_t K, int32_t V, sd_verify_mode mode,
 static bool tree_rows_ok(int32_t B, int32_t Q) { return B >= 1 && Q >= 1 && Q <= SD_MAX_TREE; }
 
 size_t sd_latent_attention_tree_workspace(int32_t B, int32_t Q, int32_t H, int32_t d_latent, int32_t d_rope) {
-  return Q <= SD_MAX_TREE ? sd_latent_attention_workspace(B, Q, H, d_latent, d_rope) : 0;
+  return Q <= SD_MAX_TREE && latent_shape_ok(B, Q, H, d_latent, d_rope) ? latent_tree_ws_bytes(B, Q, H, d_latent, d_rope) : 0;
 }
 
 sd_status sd_latent_attention_tree(int32_t B, int32_t Q, int32_t H, int32_t d_latent, int32_t d_rope, sd_type type,

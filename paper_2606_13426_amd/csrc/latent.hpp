@@ -32,7 +32,7 @@
 // inside a sequence: its part is left in the workspace and joined by
 // latent_join_kernel.
 //
-// With TREE the rows of a sequence are nodes of a tree: a row sees the prefix, itself and its
+// With TREE (and fewer rows than latent_wide.hpp is for) the rows of a sequence are nodes of a tree: a row sees the prefix, itself and its
 // ancestors.  A node's ancestors are 64 bits, found from the parents by the first wavefront
 // of a workgroup whose run reaches behind the prefix, in six doublings (a node's set, joined with that
 // of the node its chain of parents has reached so far), and kept in LDS beside the
@@ -88,6 +88,22 @@ inline Plan plan(int B, int Q, int H, int capacity) {
   const int64_t rows = (int64_t)Q * H, tiles = ((int64_t)capacity + kTile - 1) / kTile * B * ((rows + 63) / 64);
   const int most = most_r(rows);
   return plan_of(rows, tiles < kGroups ? 1 : tiles < 8 * kGroups && most > 2 ? 2 : most);
+}
+
+// The kernel of 128 rows a workgroup (latent_wide.hpp), for trees: by its tiles of 128 rows and 64 tokens, 20 a
+// compute unit where sequences are cut (its parts to join are twice as large), 2 where blocks of rows are as
+// many as compute units and mostly done whole.  In us (all kernels), at most 64 rows a workgroup / 128:
+//   1 tree of 64 nodes, 16 heads, 25600 tokens, 12.5 tiles a unit:   97 / 108    100000, 49: 307 / 248
+//   64 trees of 16 nodes, 16 heads, 1600 tokens, 12.5:               91 / 121    6400, 50:   313 / 262
+//   24 trees of 20 nodes, 32 heads, 1600 tokens, 12:                105 / 115    6400, 47:   302 / 264
+//   8 trees of 32 nodes, 128 heads (256 blocks), 100 tokens, 2:      66 / 55     6400, 100:  596 / 439
+constexpr int kWideRows = 128, kWideR = kWideRows / 16;
+inline bool wide_fits(int64_t rows, int dc, int dr) { return rows >= kWideRows && dc == 512 && dr == kRope; }
+inline Plan tree_plan(int B, int Q, int H, int dc, int dr, int capacity) {
+  const int64_t rows = (int64_t)Q * H, blocks = (rows + kWideRows - 1) / kWideRows * B;
+  const int64_t tiles = ((int64_t)capacity + kTile - 1) / kTile * blocks;
+  const bool many = tiles >= 20 * kGroups || (blocks >= kGroups && tiles >= 2 * kGroups);
+  return many && wide_fits(rows, dc, dr) ? plan_of(rows, kWideR) : plan(B, Q, H, capacity);
 }
 
 struct Args {
@@ -699,19 +715,24 @@ __global__ __launch_bounds__(kThreads) void latent_join_kernel(Args a) {
   }
 }
 
-template <class T, int R, int DC, bool TREE>
-hipError_t run(const Args& a, hipStream_t s) {
-  hipError_t e = launch_timed(TREE ? "latent_tree" : "latent_attention", latent_kernel<T, R, DC, TREE>, dim3(kGroups), dim3(R == 1 ? 256 : 512), s, a);
-  if (e != hipSuccess) return e;
-  // One wavefront a row, or four for 128 columns of it where rows are few and may have eight parts or
-  // more.  In us, one / four: 64 rows of 128 parts 40 / 13, 512 rows of 16 parts 9.7 / 9.6, 2048
-  // rows of 4 parts 7 / 21, 8192 rows of 2 parts 13 / 67.
+// One wavefront a row, or four for 128 columns of it where rows are few and may have eight parts or
+// more.  In us, one / four: 64 rows of 128 parts 40 / 13, 512 rows of 16 parts 9.7 / 9.6, 2048
+// rows of 4 parts 7 / 21, 8192 rows of 2 parts 13 / 67.
+template <class T, int DC>
+hipError_t join(const Args& a, hipStream_t s) {
   const int64_t rows = (int64_t)a.B * a.Q * a.H, many = rows * (DC / 128), few = (rows + 3) / 4;
   return rows < 1024 && a.p.teams >= 8 * (int64_t)a.B * a.p.supers
              ? launch_timed("latent_join", latent_join_kernel<T, DC, 4>, dim3((unsigned)(many < 4096 ? many : 4096)),
                             dim3(kThreads), s, a)
              : launch_timed("latent_join", latent_join_kernel<T, DC, 1>, dim3((unsigned)(few < 4096 ? few : 4096)),
                             dim3(kThreads), s, a);
+}
+
+template <class T, int R, int DC, bool TREE>
+hipError_t run(const Args& a, hipStream_t s) {
+  const hipError_t e = launch_timed(TREE ? "latent_tree" : "latent_attention", latent_kernel<T, R, DC, TREE>, dim3(kGroups),
+                                    dim3(R == 1 ? 256 : 512), s, a);
+  return e != hipSuccess ? e : join<T, DC>(a, s);
 }
 
 template <class T, bool TREE = false>

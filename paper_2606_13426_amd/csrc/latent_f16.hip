@@ -35,12 +35,19 @@ size_t latent_ws_bytes(int B, int Q, int H, int dc) {
   }
   return most;
 }
+size_t latent_tree_ws_bytes(int B, int Q, int H, int dc, int dr) {
+  const size_t few = latent_ws_bytes(B, Q, H, dc);
+  if (!latent::wide_fits((int64_t)Q * H, dc, dr)) return few;
+  const size_t wide = layout(B, dc, latent::plan_of((int64_t)Q * H, latent::kWideR)).bytes;
+  return few > wide ? few : wide;
+}
 
 static latent::Args args_of(int B, int Q, int H, int dc, int dr, double scale, const void* q, sd_stride_h qs,
                             const void* cache, int64_t page_stride, int64_t token_stride, int n_pages, int page_size,
                             const int32_t* pages, int64_t pages_stride, int max_pages, const int32_t* lens,
                             const int32_t* rows, const int32_t* parents, void* out, sd_stride_h os, float* lse,
                             void* ws) {
+  // (parents: the tree form)
   latent::Args a;
   a.B = B;
   a.Q = Q;
@@ -70,7 +77,7 @@ static latent::Args args_of(int B, int Q, int H, int dc, int dr, double scale, c
   a.orow = os.row;
   a.oh = os.head;
   a.lse = lse;
-  a.p = latent::plan(B, Q, H, a.capacity);
+  a.p = parents ? latent::tree_plan(B, Q, H, dc, dr, a.capacity) : latent::plan(B, Q, H, a.capacity);
   const Layout l = layout(B, dc, a.p);
   char* base = static_cast<char*>(ws);
   a.part = reinterpret_cast<float*>(base + l.part);

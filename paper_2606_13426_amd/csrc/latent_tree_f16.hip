@@ -2,5 +2,8 @@
 #include "latent.hpp"
 
 namespace sd {
-hipError_t latent_tree_f16_launch(const latent::Args& a, hipStream_t s) { return latent::run_type<latent::F16, true>(a, s); }
+hipError_t latent_wide_f16_launch(const latent::Args& a, hipStream_t s);
+hipError_t latent_tree_f16_launch(const latent::Args& a, hipStream_t s) {
+  return a.p.R == latent::kWideR ? latent_wide_f16_launch(a, s) : latent::run_type<latent::F16, true>(a, s);
+}
 }  // namespace sd

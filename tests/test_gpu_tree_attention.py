@@ -142,3 +142,107 @@ def test_pages_that_do_not_exist_plain_caches_and_views():
     got = _lib.sd_latent_attention_tree(q, cache, _i32(lens), _i32(parents), dc, scale=0.05, out=out[..., 16:].transpose(1, 2))
     _check(q, cache, lens, parents, dc, None, None, 0.05, got, "f16")
     assert (out[..., :16] == 9.0).all()
+
+
+# The kernel of 128 rows a workgroup is chosen by the tokens that the table has room for, which
+# these sequences do not fill.
+def _roomy(pages, page, B, rows):
+    blocks = B * (-(-rows // 128))
+    width = -(-64 * (5120 // blocks + 1) // page)
+    return torch.cat([pages, torch.full((B, max(0, width - pages.shape[1])), -7, dtype=torch.int32, device=DEV)], 1)
+
+
+@pytest.mark.parametrize("t", list(TYPES))
+@pytest.mark.parametrize("B,Q,H,page,lens,rows", [
+    (1, 16, 8, 64, [16], None), (1, 16, 8, 64, [31], None), (1, 16, 8, 33, [150], None), (2, 17, 9, 7, [200, 61], None),
+    (3, 64, 2, 1, [64, 97, 130], None), (5, 20, 16, 48, [515, 20, 0, 7, -3], [20, 3, 9, 20, 5]), (2, 33, 4, 100, [1000, 40], [33, 1]),
+    (70, 8, 16, 16, [(37 * b) % 150 + 3 for b in range(70)], [b % 10 - 1 for b in range(70)]), (1, 64, 128, 64, [3000], None),
+    (4, 32, 12, 64, [700, 641, 32, 2100], [32, 7, 32, 20])])
+def test_many_rows(B, Q, H, page, lens, rows, t):
+    q, cache, ln, pages = chain._case(B, Q, H, 512, 64, lens, t, B * 10 + Q, page)
+    pages = _roomy(pages, page, B, Q * H)
+    parents = _grown(B + Q, B, Q)
+    out, lse = torch.full((B, Q, H, 512), 7.0, dtype=TYPES[t], device=DEV), torch.full((B, Q, H), 7.0, device=DEV)
+    _lib.sd_profile_enable(True)
+    got = _lib.sd_latent_attention_tree(q, cache, ln, _i32(parents), 512, pages=pages, scale=0.06, out=out, lse=lse,
+                                        rows=None if rows is None else _i32(rows))
+    torch.cuda.synchronize()
+    _lib.sd_profile_enable(False)
+    assert "latent_wide" in _lib.sd_profile_read()
+    _check(q, cache, lens, parents, 512, pages, rows, 0.06, got, t, seqs=None if B < 10 else range(0, B, 9),
+           heads=None if H < 5 else [0, H // 2, H - 1])
+    for b in range(B):
+        n = Q if rows is None else min(max(rows[b], 0), Q)
+        assert (out[b, n:] == 7).all() and (lse[b, n:] == 7).all()
+
+
+@pytest.mark.parametrize("t", list(TYPES))
+def test_many_rows_values_that_are_no_numbers(t):
+    """As above with nodes that hold NaN, infinities and the lowest value, in cut and in whole blocks."""
+    for lens in ([150, 16], [1000, 90]):
+        B, Q, H = 2, 16, 24
+        q, cache, ln, pages = chain._case(B, Q, H, 512, 64, lens, t, 6)
+        pages = _roomy(pages, 16, B, Q * H)
+        parents = [[-1, 0, 0, 1, 1, 2, 2, 3, 5, 5, 8, 4, 10, 12, 9, 6]] * B
+        bad = {3: float("nan"), 6: float("inf"), 9: -float("inf"), 11: torch.finfo(TYPES[t]).min}
+        for b in range(B):
+            for node, value in bad.items():
+                j = lens[b] - Q + node
+                cache[pages[b, j // 16], j % 16, 5::64] = value
+        got = _lib.sd_latent_attention_tree(q, cache, ln, _i32(parents), 512, pages=pages, scale=0.05)
+        kin = tree.sees(parents[0], Q)
+        clean = [i for i in range(Q) if not any(kin[i, n] for n in bad)]
+        assert torch.isfinite(got[0][:, clean].float()).all() and torch.isfinite(got[1][:, clean]).all()
+        assert torch.isnan(got[0][:, [3, 7]].float()).all()
+        keep = cache.clone()
+        keep[~torch.isfinite(keep) | (keep == torch.finfo(TYPES[t]).min)] = 0
+        again = _lib.sd_latent_attention_tree(q, keep, ln, _i32(parents), 512, pages=pages, scale=0.05)
+        assert torch.equal(again[0][:, clean], got[0][:, clean]) and torch.equal(again[1][:, clean], got[1][:, clean])
+        _check(q[:, :3], keep, [n - Q + 3 for n in lens], [p[:3] for p in parents], 512, pages, None, 0.05,
+               tuple(x[:, :3] for x in got), t, heads=[0, 23])
+        # an infinite value of positive weight stays one: only the latent part of node 9 is, not what its scores are of
+        cache[~torch.isfinite(cache) | (cache == torch.finfo(TYPES[t]).min)] = 0
+        q[..., 7] = 0
+        for b in range(B):
+            j = lens[b] - Q + 5
+            cache[pages[b, j // 16], j % 16, 7] = float("inf")
+        sees5 = [i for i in range(Q) if kin[i, 5]]
+        got = _lib.sd_latent_attention_tree(q, cache, ln, _i32(parents), 512, pages=pages, scale=0.05)
+        rest = [i for i in range(Q) if not kin[i, 5]]
+        assert torch.isfinite(got[0][:, rest].float()).all() and torch.isnan(got[0][:, sees5].float()).all()
+
+
+def test_many_rows_missing_pages_views_and_scales():
+    B, Q, H, dc, t = 2, 24, 6, 512, "f16"
+    g = torch.Generator(device=DEV)
+    g.manual_seed(8)
+    for scale in (-0.04, 0.0):
+        q = torch.randn(B, H, Q, dc + 72, generator=g, device=DEV).half()[..., 8:].transpose(1, 2)
+        cache = torch.randn(40, 16, 2, dc + 64, generator=g, device=DEV).half()[:, :, 1]
+        out = torch.full((B, H, Q, dc + 16), 9.0, dtype=torch.float16, device=DEV)
+        pages = torch.randperm(40, generator=g, device=DEV)[:36].view(B, 18).int()
+        pages[0, 3], pages[0, 16], pages[1, 0] = -1, 40, 2 ** 31 - 1
+        pages = _roomy(pages, 16, B, Q * H)
+        parents, lens = _grown(9, B, Q), [280, 131]
+        got = _lib.sd_latent_attention_tree(q, cache, _i32(lens), _i32(parents), dc, pages=pages, scale=scale,
+                                            out=out[..., 16:].transpose(1, 2))
+        _check(q, cache, lens, parents, dc, pages, None, scale, got, t)
+        assert (out[..., :16] == 9.0).all()
+
+
+def test_many_rows_of_many_trees():
+    """256 blocks of rows, mostly whole, and strides of 2^24 elements."""
+    B, Q, H = 8, 32, 128
+    lens = [150, 40, 32, 700, 90, 64, 33, 500]
+    q, cache, ln, pages = chain._case(B, Q, H, 512, 64, lens, "bf16", 12, page=64)
+    parents = _grown(3, B, Q)
+    got = _lib.sd_latent_attention_tree(q, cache, ln, _i32(parents), 512, pages=pages, scale=0.06)
+    _check(q, cache, lens, parents, 512, pages, None, 0.06, got, "bf16", seqs=[0, 2, 3, 6], heads=[0, 77, 127])
+    far = torch.empty(40, 1 << 24, dtype=torch.bfloat16, device=DEV)[:, :576]
+    far.copy_(torch.randn(40, 576, device=DEV))
+    q = q[:1, :16, :8].contiguous()
+    table = _roomy(_i32([[(7 * j) % 40 for j in range(40)]]), 1, 1, 128)
+    got = _lib.sd_latent_attention_tree(q, far[:, None], _i32([40]), _i32(_grown(4, 1, 16)), 512, pages=table, scale=0.06)
+    _check(q, far[:, None], [40], _grown(4, 1, 16), 512, table, None, 0.06, got, "bf16")
+    got = _lib.sd_latent_attention_tree(q, far[None], _i32([40]), _i32(_grown(4, 1, 16)), 512, scale=0.06)
+    _check(q, far[None], [40], _grown(4, 1, 16), 512, None, None, 0.06, got, "bf16")
