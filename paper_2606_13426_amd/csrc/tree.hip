@@ -11,12 +11,18 @@
 // first costs one sum over the vocabulary.  Given candidates cost none: r_k is q without
 // the tried ones, h_k = q(x) / (1 - their mass).
 //
-// Kernels: the trees (who has which children); both laws of every node with children, whose
-// last workgroup tries the first child; a sum a round for the nodes that are
-// undecided, whose last workgroup tries the next child; the draw, which walks the
-// decided nodes from the root, sums the last r in slices and finds the token.  Nodes off the
-// accepted branch are decided too: they are not known to be off it before.  All in
-// float64, as every border is compared with a uniform.
+// Kernels: the trees (who has which children); steps, each of which makes the next sum of every open
+// node that the walk may still come to (both laws, then S_k), slices of a row a workgroup, and the last of
+// a node's workgroups does the tries that the sum allows; the draw, which walks the decided
+// nodes from the root, sums the last r in slices and finds the token.  How many steps there are is
+// known on the host: one for the laws (three where they are much work) and one for every child behind
+// the first, and a node that is out by then costs nothing.  All in float64, as every border is
+// compared with a uniform.
+//
+// What bounds it: float64 exponentials, 16 products each (1.2e12 a second reached), where laws are summed, and for
+// small calls launches and each one's trips to memory (5 us for the trees, 7 to 10 a step, 12 the draw).  1 tree
+// of 12 over 32000 36 us, 24 of 24 over 50001 (given) 46, 32 of 32 over 131072 (distinct) 141: 194 with
+// every node's laws at once.
 #include "common.hpp"
 #include "laws.hpp"
 #include "logits.hpp"
@@ -29,7 +35,7 @@ namespace {
 using namespace laws;
 
 constexpr int kNodes = SD_MAX_TREE;
-constexpr int kOpen = -2, kNone = -1;  // Node::next: not decided yet; no child accepted
+constexpr int kOpen = 0, kNone = 1;  // Node::state: not decided yet; no child accepted; the accepted child + 1
 
 struct Node {
   double Sq, Sp;  // the laws' sums against mq and mp: 0 for a row of -inf, NaN for no law
@@ -37,13 +43,13 @@ struct Node {
   double rest;    // rest_k; GIVEN: what the tried tokens leave of q
   uint64_t kids;  // children, bits
   float mq, mp;
-  int32_t next, tried;  // the accepted child, kNone or kOpen; how many children were tried
+  int32_t state;  // in one word, as others read it while it changes: the decision, 256 times the children tried
+  int32_t steps;  // sums that were made for it
 };
+__device__ __forceinline__ int decided(int state) { return state & 255; }
 
 struct Tree {
   Node* nodes;       // [B][Q]
-  int32_t* list;     // [B][Q] nodes with children, rising
-  int32_t* count;    // [B]
   uint32_t* arrived; // [B][Q + 1] workgroups that are done with a node, with the draw
   float* chance;     // [B][Q] min(1, h) of tried nodes
   double* sums;      // [B][Q][S][2] slices' sums of q and p, then of max(0, q - a p) and of p
@@ -66,6 +72,9 @@ __device__ __forceinline__ void put(double* p, double v) {
   __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 __device__ __forceinline__ void put(float* p, float v) {
+  __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void put(uint32_t* p, uint32_t v) {
   __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 template <class V>
@@ -100,14 +109,12 @@ __global__ __launch_bounds__(64) void tree_plan_kernel(VerifyTreeArgs a, Tree w)
     const int p = __builtin_amdgcn_readlane(up, j);
     if (lane == j && p >= 0 && (so_far >> p & 1u)) reached = true;
   }
-  const uint64_t inner = __ballot(lane < n && reached && kids != 0);
-  if (inner >> lane & 1u) w.list[(int64_t)b * a.Q + __popcll(inner & ((1ull << lane) - 1ull))] = lane;
-  if (lane == 0) w.count[b] = __popcll(inner);
+  if (!reached) kids = 0;
   if (lane < a.Q) {
     Node v{};
     v.kids = kids;
     v.S = v.rest = 1.0;
-    v.next = kids ? kOpen : kNone;
+    v.state = kids ? kOpen : kNone;
     w.nodes[(int64_t)b * a.Q + lane] = v;
     w.arrived[(int64_t)b * (a.Q + 1) + lane] = 0;
     w.chance[(int64_t)b * a.Q + lane] = -1.f;
@@ -127,17 +134,33 @@ __device__ __forceinline__ double draw_of(const VerifyTreeArgs& a, int b) {
   return ((double)(((uint64_t)(x.x >> 6) << 26) | (x.y >> 6)) + 0.5) * 0x1p-52;
 }
 
-// The tries of node i that need no further sum, by one wavefront; v is its state, S_k in it.
+// What a child brings to its try, a lane each: its token, the logits there, its coin.
+struct Child {
+  double eta;
+  int x;
+  bool known;
+  float xq, xp;
+};
 template <class T>
-__device__ __forceinline__ void tries(const VerifyTreeArgs& a, const Tree& w, int b, int i, Node v, double inv_t) {
+__device__ __forceinline__ Child child_of(const VerifyTreeArgs& a, int b, int i, uint64_t kids) {
   const int lane = threadIdx.x & 63;
-  const bool mine = v.kids >> lane & 1u;
-  // every child's token, coin, log-ratio and draft probability, a lane each
-  const int x = mine ? a.tokens[(int64_t)b * a.Q + lane] : -1;
-  const bool known = x >= 0 && x < a.V;
-  const float xq = known ? T::value(row_of<T>(a.target, a.ts, b, i)[x]) : -INFINITY;
-  const float xp = known && a.draft ? T::value(row_of<T>(a.draft, a.ds, b, i)[x]) : -INFINITY;
-  const double eta = mine ? eta_of(a, b, lane) : 2.0;
+  const bool mine = kids >> lane & 1u;
+  Child k;
+  k.x = mine ? a.tokens[(int64_t)b * a.Q + lane] : -1;
+  k.eta = mine ? eta_of(a, b, lane) : 2.0;
+  k.known = k.x >= 0 && k.x < a.V;
+  k.xq = k.known ? T::value(row_of<T>(a.target, a.ts, b, i)[k.x]) : -INFINITY;
+  k.xp = k.known && a.draft ? T::value(row_of<T>(a.draft, a.ds, b, i)[k.x]) : -INFINITY;
+  return k;
+}
+
+// The tries of node i that need no further sum, by one wavefront; v is its state, S_k in it.
+__device__ __forceinline__ void tries(const VerifyTreeArgs& a, const Tree& w, int b, int i, Node v, const Child& child, double inv_t) {
+  const int lane = threadIdx.x & 63, x = child.x;
+  const bool mine = v.kids >> lane & 1u, known = child.known;
+  const float xq = child.xq, xp = child.xp;
+  const double eta = child.eta;
+  // every child's log-ratio and draft probability
   const bool okq = v.Sq >= 0.0 && isfinite(v.Sq), okp = a.draws == SD_TREE_GIVEN || (v.Sp >= 0.0 && isfinite(v.Sp));
   // (a log-ratio below 2^-44 is one of sums added in another order: 0)
   double ratio = 0.0, q = 0.0;  // q / p, q
@@ -153,14 +176,14 @@ __device__ __forceinline__ void tries(const VerifyTreeArgs& a, const Tree& w, in
       ratio = fabs(ell) < 0x1p-44 ? 1.0 : exp(ell);
     }
   }
+  int tried = v.state >> 8, next = kOpen;
   uint64_t left = v.kids;
-  for (int k = 0; k < v.tried; ++k) left &= left - 1;
+  for (int k = 0; k < tried; ++k) left &= left - 1;
   float chance = -1.f;
-  v.next = kOpen;
   while (left) {
     const int j = __ffsll((unsigned long long)left) - 1;
     left &= left - 1;
-    ++v.tried;
+    ++tried;
     const int tok = __shfl(x, j);
     const bool valid = __shfl((int)known, j) != 0 && okq && okp;
     const bool again = __ballot(mine && lane < j && x == tok) != 0;
@@ -183,110 +206,50 @@ __device__ __forceinline__ void tries(const VerifyTreeArgs& a, const Tree& w, in
     }
     if (lane == j) chance = (float)fmin(h, 1.0);
     if (coin < h) {
-      v.next = j;
+      next = j + 1;
       break;
     }
     if (spent && left) break;  // the next try needs S of the new a
   }
-  if (v.next == kOpen && !left) v.next = kNone;
+  if (next == kOpen && !left) next = kNone;
+  v.state = tried << 8 | next;
+  ++v.steps;
   if (chance >= 0.f) w.chance[(int64_t)b * a.Q + lane] = chance;
   if (lane == 0) w.nodes[(int64_t)b * a.Q + i] = v;
 }
 
-// Node r of the list of sequence b, or -1.
-__device__ __forceinline__ int listed(const VerifyTreeArgs& a, const Tree& w, int b, int r) {
-  return r < w.count[b] ? w.list[(int64_t)b * a.Q + r] : -1;
-}
-
-// Slices of both laws' sums of a node with children.
-template <class T, int E>
-__global__ __launch_bounds__(kThreads) void tree_sums_kernel(VerifyTreeArgs a, Tree w, int S, int R, Scale c, double inv_t) {
-  __shared__ double red[4], joined[2];
+enum { kLaws = 1, kExcess = 2, kBoth = 3 };
+// One sum of a node, the next that it needs: of both laws, or S_k (SUMS: the ones that there may be).  Its workgroups hold a slice each, and
+// the one that is done last goes on to the tries that the sum allows.
+template <class T, int E, int SUMS>
+__device__ __forceinline__ void node_step(const VerifyTreeArgs& a, const Tree& w, int b, int i, const Node& v, int slice, int S,
+                                          Scale c, double inv_t) {
+  __shared__ double red[8], joined[2];
   __shared__ float redm[4], peaks[2];
   __shared__ int last_s;
-  const int slice = blockIdx.x % S, t = threadIdx.x;
-  const int64_t id = blockIdx.x / S;
-  const int b = (int)(id / R);
-  for (int r = (int)(id % R); r < a.Q; r += R) {
-    const int i = listed(a, w, b, r);
-    if (i < 0) return;
-    const typename T::raw* pq = row_of<T>(a.target, a.ts, b, i);
-    const typename T::raw* pp = a.draft ? row_of<T>(a.draft, a.ds, b, i) : nullptr;
-    const int lead_q = lead<T>(pq);
-    // (both rows by the target's vectors: equal rows have equal sums)
-    float x[E], y[E];
-    load_slice<T, E>(pq, lead_q, a.V, slice, x);
-    if (pp) load_slice<T, E>(pp, lead_q, a.V, slice, y);
-    const Part q = slice_sums64<T, E>(x, c, red, redm);
+  const int t = threadIdx.x;
+  const bool first = SUMS == kLaws || (SUMS == kBoth && v.steps == 0), distinct = a.draws == SD_TREE_DISTINCT;
+  const typename T::raw* pq = row_of<T>(a.target, a.ts, b, i);
+  const typename T::raw* pp = a.draft ? row_of<T>(a.draft, a.ds, b, i) : nullptr;
+  const int lead_q = lead<T>(pq);
+  // (both rows by the target's vectors: equal rows have equal sums)
+  float x[E], y[E];
+  load_slice<T, E>(pq, lead_q, a.V, slice, x);
+  if (pp) load_slice<T, E>(pp, lead_q, a.V, slice, y);
+  // (read by every workgroup, for the last one: behind its count they would be two more trips to memory)
+  Child child{};
+  if (t < 64) child = child_of<T>(a, b, i, v.kids);
+  Part q, p{0.0, 0.0, -INFINITY, 0.f};
+  if (first) {
+    q = slice_sums64<T, E>(x, c, red, redm);
     __syncthreads();
-    Part p{0.0, 0.0, -INFINITY, 0.f};
     if (pp) p = slice_sums64<T, E>(y, c, red, redm);
-    const int64_t at = ((int64_t)b * a.Q + i) * S;
-    if (t == 0) {
-      put(&w.sums[2 * (at + slice)], q.S);
-      put(&w.sums[2 * (at + slice) + 1], p.S);
-      put(&w.maxima[2 * (at + slice)], q.m);
-      put(&w.maxima[2 * (at + slice) + 1], p.m);
-      last_s = last_of(&w.arrived[(int64_t)b * (a.Q + 1) + i], (uint32_t)S);
-    }
-    __syncthreads();
-    if (last_s) {
-      // the first wavefront joins q's slices, the second p's
-      const int h = t >> 6, lane = t & 63;
-      if (h < 2) {
-        float m = -INFINITY;
-        for (int s = lane; s < S; s += 64) m = fmaxf(m, get(&w.maxima[2 * (at + s) + h]));
-        m = wave_max(m);
-        double sum = 0.0;
-        for (int s = lane; s < S; s += 64) {
-          const float ms = get(&w.maxima[2 * (at + s) + h]);
-          const double v = get(&w.sums[2 * (at + s) + h]);
-          if (!(ms == -INFINITY && v == 0.0)) sum += v * exp(((double)ms - (double)m) * inv_t);
-        }
-        sum = wave_sum(sum);
-        if (lane == 0) {
-          joined[h] = sum;
-          peaks[h] = m;
-        }
-      }
-      __syncthreads();
-      if (t < 64) {
-        Node v = w.nodes[(int64_t)b * a.Q + i];
-        v.Sq = joined[0];
-        v.Sp = joined[1];
-        v.mq = peaks[0] == -INFINITY ? 0.f : peaks[0];
-        v.mp = peaks[1] == -INFINITY ? 0.f : peaks[1];
-        tries<T>(a, w, b, i, v, inv_t);
-      }
-    }
-    __syncthreads();
-  }
-}
-
-// Slices of S_k of the nodes that need it for their next child; round k >= 1.
-template <class T, int E>
-__global__ __launch_bounds__(kThreads) void tree_round_kernel(VerifyTreeArgs a, Tree w, int S, int R, int k, Scale c, double inv_t) {
-  __shared__ double red[8];
-  __shared__ int last_s;
-  const int slice = blockIdx.x % S, t = threadIdx.x;
-  const int64_t id = blockIdx.x / S;
-  const int b = (int)(id / R);
-  for (int r = (int)(id % R); r < a.Q; r += R) {
-    const int i = listed(a, w, b, r);
-    if (i < 0) return;
-    const Node v = w.nodes[(int64_t)b * a.Q + i];
-    if (v.next != kOpen) continue;
-    const typename T::raw *pq = row_of<T>(a.target, a.ts, b, i), *pp = row_of<T>(a.draft, a.ds, b, i);
+  } else {
     const double A = v.Sq == 0.0 ? 0.0 : 1.0 / v.Sq, B = v.Sp == 0.0 ? 0.0 : v.a / v.Sp;
-    const int lead_q = lead<T>(pq);
-    float x[E], y[E];
-    load_slice<T, E>(pq, lead_q, a.V, slice, x);
-    load_slice<T, E>(pp, lead_q, a.V, slice, y);
-    const bool distinct = a.draws == SD_TREE_DISTINCT;
     if (distinct) {
       // the tried tokens are out of p's sum, and have no part in the other
       uint64_t left = v.kids;
-      for (int j = 0; j < v.tried; ++j, left &= left - 1) {
+      for (int j = v.state >> 8; j > 0; --j, left &= left - 1) {
         const int tok = a.tokens[(int64_t)b * a.Q + __ffsll((unsigned long long)left) - 1];
         const int at = tok + lead_q, vec = at / T::kVec - slice * (E / T::kVec) * kThreads;
         if (tok < 0 || tok >= a.V || vec < 0 || vec % kThreads != t || vec / kThreads >= E / T::kVec) continue;
@@ -302,34 +265,124 @@ __global__ __launch_bounds__(kThreads) void tree_round_kernel(VerifyTreeArgs a, 
       s[e & 1] += excess_of(A, weight_or_tiny(x[e], v.mq, c), B, wp);
       if (distinct) rest += wp;
     }
-    const double sum = wave_sum(s[0] + s[1]);
-    rest = wave_sum(rest);
+    q.S = wave_sum(s[0] + s[1]);
+    p.S = wave_sum(rest);
     if ((t & 63) == 0) {
-      red[t >> 6] = sum;
-      red[4 + (t >> 6)] = rest;
+      red[t >> 6] = q.S;
+      red[4 + (t >> 6)] = p.S;
     }
     __syncthreads();
-    const int64_t at = ((int64_t)b * a.Q + i) * S;
-    if (t == 0) {
-      put(&w.sums[2 * (at + slice)], red[0] + red[1] + (red[2] + red[3]));
-      put(&w.sums[2 * (at + slice) + 1], red[4] + red[5] + (red[6] + red[7]));
-      last_s = last_of(&w.arrived[(int64_t)b * (a.Q + 1) + i], (uint32_t)(k + 1) * (uint32_t)S);
+    q.S = red[0] + red[1] + (red[2] + red[3]);
+    p.S = red[4] + red[5] + (red[6] + red[7]);
+  }
+  const int64_t at = ((int64_t)b * a.Q + i) * S;
+  if (t == 0) {
+    put(&w.sums[2 * (at + slice)], q.S);
+    put(&w.sums[2 * (at + slice) + 1], p.S);
+    if (first) {
+      put(&w.maxima[2 * (at + slice)], q.m);
+      put(&w.maxima[2 * (at + slice) + 1], p.m);
     }
-    __syncthreads();
-    if (last_s && t < 64) {
-      double sum = 0.0, rest = 0.0;
-      for (int j = t; j < S; j += 64) {
-        sum += get(&w.sums[2 * (at + j)]);
-        rest += get(&w.sums[2 * (at + j) + 1]);
+    last_s = last_of(&w.arrived[(int64_t)b * (a.Q + 1) + i], (uint32_t)S);
+  }
+  __syncthreads();
+  if (last_s) {
+    if (t == 0) put(&w.arrived[(int64_t)b * (a.Q + 1) + i], 0u);
+    // the first wavefront joins q's slices, the second p's
+    const int h = t >> 6, lane = t & 63;
+    if (h < 2) {
+      // (a slice of -inf alone has no maximum, and one with NaN no sum)
+      float m = -INFINITY;
+      double sum = 0.0;
+      for (int s = lane; s < S; s += 64) {
+        const double g = get(&w.sums[2 * (at + s) + h]);
+        if (!first) {
+          sum += g;
+          continue;
+        }
+        const float ms = get(&w.maxima[2 * (at + s) + h]), up = fmaxf(m, ms);
+        if (m < up) sum = m == -INFINITY ? sum : sum * exp(((double)m - (double)up) * inv_t);
+        if (!(ms == -INFINITY && g == 0.0)) sum += ms == up ? g : g * exp(((double)ms - (double)up) * inv_t);
+        m = up;
       }
-      Node u = v;
-      u.S = wave_sum(sum);
-      rest = wave_sum(rest);
-      // (weights below 2^-1000 are 0, for which the sum has 2^-1000)
-      if (distinct) u.rest = v.Sp > 0.0 && rest > 0x1p-960 ? rest / v.Sp : 0.0;
-      tries<T>(a, w, b, i, u, inv_t);
+      if (first) {
+        const float up = wave_max(m);
+        if (m < up && m > -INFINITY) sum *= exp(((double)m - (double)up) * inv_t);
+        m = up;
+      }
+      sum = wave_sum(sum);
+      if (lane == 0) {
+        joined[h] = sum;
+        peaks[h] = m;
+      }
     }
     __syncthreads();
+    if (t < 64) {
+      Node u = v;
+      if (first) {
+        u.Sq = joined[0];
+        u.Sp = joined[1];
+        u.mq = peaks[0] == -INFINITY ? 0.f : peaks[0];
+        u.mp = peaks[1] == -INFINITY ? 0.f : peaks[1];
+      } else {
+        u.S = joined[0];
+        // (weights below 2^-1000 are 0, for which the sum has 2^-1000)
+        if (distinct) u.rest = v.Sp > 0.0 && joined[1] > 0x1p-960 ? joined[1] / v.Sp : 0.0;
+      }
+      tries(a, w, b, i, u, child, inv_t);
+    }
+  }
+  __syncthreads();
+}
+
+// A step of every open node that the walk may come to: of all of them, or of the root (kRoot) or of it and its
+// children (kNear) alone.  A node is out once another child of its parent is accepted or it is rejected.
+// That may happen while this runs, and a workgroup that sees it leaves its slice out: then the node's
+// count of slices never fills, and it stays open.
+enum { kRoot, kNear, kAll };
+template <class T, int E, int SUMS>
+__global__ __launch_bounds__(kThreads) void tree_step_kernel(VerifyTreeArgs a, Tree w, int S, int R, int which, Scale c, double inv_t) {
+  const int slice = blockIdx.x % S, lane = threadIdx.x & 63;
+  const int64_t id = blockIdx.x / S;
+  const int b = (int)(id / R), worker = (int)(id % R);
+  const Node* nodes = w.nodes + (int64_t)b * a.Q;
+  const int state = lane < a.Q ? get(&nodes[lane].state) : kNone;
+  const uint64_t kids_of = lane < a.Q ? nodes[lane].kids : 0;
+  uint64_t open = kids_of;  // the children of node `lane` that are not out
+  if (decided(state) != kOpen) open = decided(state) == kNone ? 0ull : 1ull << (decided(state) - 1);
+  else
+    for (int k = state >> 8; k > 0; --k) open &= open - 1;
+  auto of = [](uint64_t v, int i) {
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, i) |
+           (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), i) << 32;
+  };
+  auto state_of = [&](int i) { return __builtin_amdgcn_readlane(state, i); };
+  const uint64_t inner = __ballot(open != 0);
+  uint64_t alive = 1, todo = inner & 1;  // (a parent comes before its children)
+  while (todo) {
+    const int i = __ffsll((unsigned long long)todo) - 1;
+    const uint64_t more = of(open, i);
+    alive |= more;
+    todo = (todo & (todo - 1)) | (more & inner);
+    if (which != kAll && (which == kRoot || i == 0)) todo = 0;
+  }
+  // (a node's workgroup is told by its place among all nodes with children, which does not change)
+  const uint64_t kids = __ballot(kids_of != 0);
+  uint64_t mine = __ballot(decided(state) == kOpen) & kids & alive;
+  if (which == kRoot) mine &= 1;
+  for (; mine; mine &= mine - 1) {
+    const int i = __ffsll((unsigned long long)mine) - 1;
+    if (__popcll(kids & ((1ull << i) - 1ull)) % R != worker) continue;
+    Node v{};
+    if (SUMS == kLaws) {  // (nothing more is known of it yet)
+      if (state_of(i) >> 8) continue;
+      v.S = v.rest = 1.0;
+      v.kids = of(kids_of, i);
+    } else {
+      v = nodes[i];
+      if (SUMS == kExcess && !v.steps) continue;
+    }
+    node_step<T, E, SUMS>(a, w, b, i, v, slice, S, c, inv_t);
   }
 }
 
@@ -385,7 +438,7 @@ __global__ __launch_bounds__(kThreads) void tree_draw_kernel(VerifyTreeArgs a, T
   if (t < 64) {
     // the walk, by one wavefront: a lane holds a node
     const Node* nodes = w.nodes + (int64_t)b * a.Q;
-    const int next = t < n ? nodes[t].next : kNone;
+    const int state = t < n ? decided(nodes[t].state) : kNone, next = state > kNone ? state - 1 : -1;
     const uint64_t kids = t < n ? nodes[t].kids : 0;
     int at = 0, steps = 1, mine = t == 0 ? 0 : -1;
     uint64_t seen = 0;  // children of the nodes that were passed
@@ -483,10 +536,17 @@ __global__ __launch_bounds__(kThreads) void tree_draw_kernel(VerifyTreeArgs a, T
   // the slices' masses against one maximum, a range of them a thread
   const int per = (S + kThreads - 1) / kThreads, s0 = min(t * per, S), s1 = min(s0 + per, S);
   const int64_t base = (int64_t)b * S;
+  // (a thread's first slice, mostly its only one, is read once)
+  const double draw = draw_of(a, b), left0 = s0 < s1 ? get(&w.mass[2 * (base + s0)]) : 0.0,
+               whole0 = s0 < s1 ? get(&w.mass[2 * (base + s0) + 1]) : 0.0;
+  const float peak0 = s0 < s1 ? get(&w.peak[base + s0]) : 0.f;
+  auto left_of = [&](int s) { return s == s0 ? left0 : get(&w.mass[2 * (base + s)]); };
+  auto whole_of = [&](int s) { return s == s0 ? whole0 : get(&w.mass[2 * (base + s) + 1]); };
+  auto peak_of = [&](int s) { return s == s0 ? peak0 : get(&w.peak[base + s]); };
   float m = -INFINITY;
   if (!inner) {
     for (int s = s0; s < s1; ++s)
-      if (get(&w.mass[2 * (base + s) + 1]) != 0.0) m = fmaxf(m, get(&w.peak[base + s]));
+      if (whole_of(s) != 0.0) m = fmaxf(m, peak_of(s));
     m = wave_max(m);
     if ((t & 63) == 0) redm[t >> 6] = m;
     __syncthreads();
@@ -494,12 +554,12 @@ __global__ __launch_bounds__(kThreads) void tree_draw_kernel(VerifyTreeArgs a, T
   }
   auto factor = [&](int s) {
     if (inner) return 1.0;
-    const double z = ((double)get(&w.peak[base + s]) - (double)m) * inv_t;
+    const double z = ((double)peak_of(s) - (double)m) * inv_t;
     return z < -700.0 ? 0.0 : exp(z);
   };
   bool use_q = false;
   auto mass_of = [&](int s) {
-    const double g = get(&w.mass[2 * (base + s) + (use_q ? 1 : 0)]);
+    const double g = use_q ? whole_of(s) : left_of(s);
     return g == 0.0 ? 0.0 : g * factor(s);  // (a slice of -inf alone has no maximum)
   };
   double mass = 0.0, cum = 0.0, all = 0.0;
@@ -521,7 +581,7 @@ __global__ __launch_bounds__(kThreads) void tree_draw_kernel(VerifyTreeArgs a, T
     if (t == 0) a.token[b] = -1;
     return;
   }
-  const double goal = draw_of(a, b) * all;
+  const double goal = draw * all;
   // (a thread without mass is never chosen: added up in another order, its sum may exceed the one
   // before it, and the goal, by a bit)
   int owner = block_first(mass > 0.0 && cum > goal, ired);
@@ -594,40 +654,63 @@ __global__ __launch_bounds__(kThreads) void tree_draw_kernel(VerifyTreeArgs a, T
   if (t == 0) a.token[b] = tok_s;
 }
 
-// Workgroups share a tree's nodes with children, of which branching trees have few: half as many as nodes
-// take all of them, in two turns where the tree is a chain.
-inline int workers(int Q) { return Q > 1 ? Q / 2 : 1; }
-inline int64_t law_rows(int B, int Q) { return (int64_t)B * workers(Q); }
+// Workgroups share a tree's nodes with children: half as many as nodes take all of them, in two turns where the
+// tree is a chain, and four the ones that a walk may still come to.
+inline int many(int Q) { return Q > 1 ? Q / 2 : 1; }
+inline int few(int Q) { return Q > 4 ? 4 : Q > 1 ? Q - 1 : 1; }
+// Whether the root's law comes first, then its children's that are left, then the rest's: two launches more, and
+// most nodes out before they are summed.  In us, at once / in stages, by B Q V: 32000 x 12 36 / 51; 2^24 51 / 59,
+// 91 / 90; 2^25 93 / 95, 100 / 98; 46 x 2^20 132 / 121, 132 / 133; 2^26 127 / 115; 70 x 2^20 (given)
+// 82 / 70; 2^27 194 / 141; 2^29 (given) 450 / 116.
+inline bool in_stages(const VerifyTreeArgs& a) { return (int64_t)a.B * a.Q * a.V >= 40ll << 20; }
 
 struct TreeWs {
-  size_t nodes, list, count, arrived, chance, sums, maxima, mass, peak, bytes;
+  size_t nodes, arrived, chance, sums, maxima, mass, peak, bytes;
 };
 TreeWs tree_layout(int B, int Q, int V) {
-  const size_t S = (size_t)slices(V, per_thread(law_rows(B, Q), V)), Sd = (size_t)slices(V, per_thread(B, V));
-  const size_t n = (size_t)B * Q;
+  const size_t S = (size_t)slices(V, per_thread(B, V)), n = (size_t)B * Q;  // (the most: more rows have no smaller slices)
   TreeWs w;
   w.nodes = 0;
-  w.list = w.nodes + up256(sizeof(Node) * n);
-  w.count = w.list + up256(sizeof(int32_t) * n);
-  w.arrived = w.count + up256(sizeof(int32_t) * (size_t)B);
+  w.arrived = w.nodes + up256(sizeof(Node) * n);
   w.chance = w.arrived + up256(sizeof(uint32_t) * (n + B));
   w.sums = w.chance + up256(sizeof(float) * n);
   w.maxima = w.sums + up256(2 * sizeof(double) * n * S);
   w.mass = w.maxima + up256(2 * sizeof(float) * n * S);
-  w.peak = w.mass + up256(2 * sizeof(double) * (size_t)B * Sd);
-  w.bytes = w.peak + up256(sizeof(float) * (size_t)B * Sd);
+  w.peak = w.mass + up256(2 * sizeof(double) * (size_t)B * S);
+  w.bytes = w.peak + up256(sizeof(float) * (size_t)B * S);
   return w;
 }
 
-template <class T, int E>
+// A step of the nodes that `which` says, by `workers` slices' workgroups a tree.
+template <class T, int E, int SUMS>
+hipError_t step_run(const char* name, const VerifyTreeArgs& a, const Tree& w, int which, int workers, double inv_t, hipStream_t s) {
+  const int S = slices(a.V, E);
+  return launch_timed(name, tree_step_kernel<T, E, SUMS>, dim3((unsigned)((int64_t)a.B * workers * S)), dim3(kThreads), s, a, w, S,
+                      workers, which, scale_of(inv_t), inv_t);
+}
+template <class T, int SUMS>
+hipError_t step_of(const char* name, const VerifyTreeArgs& a, const Tree& w, int which, int workers, double inv_t, hipStream_t s) {
+  return per_thread((int64_t)a.B * workers, a.V) == 32 ? step_run<T, 32, SUMS>(name, a, w, which, workers, inv_t, s)
+                                                       : step_run<T, 8, SUMS>(name, a, w, which, workers, inv_t, s);
+}
+template <class T>
 hipError_t laws_run(const VerifyTreeArgs& a, const Tree& w, double inv_t, hipStream_t s) {
-  const int S = slices(a.V, E), R = workers(a.Q);
-  const Scale c = scale_of(inv_t);
-  const dim3 grid((unsigned)((int64_t)a.B * R * S));
-  hipError_t e = launch_timed("tree_sums", tree_sums_kernel<T, E>, grid, dim3(kThreads), s, a, w, S, R, c, inv_t);
-  if (a.draws == SD_TREE_GIVEN) return e;
+  const bool given = a.draws == SD_TREE_GIVEN;  // (no sum behind the laws')
+  hipError_t e;
+  if (in_stages(a)) {
+    e = step_of<T, kLaws>("tree_root", a, w, kRoot, 1, inv_t, s);
+    if (e == hipSuccess)
+      e = given ? step_of<T, kLaws>("tree_near", a, w, kNear, few(a.Q), inv_t, s)
+                : step_of<T, kBoth>("tree_near", a, w, kNear, few(a.Q), inv_t, s);
+    if (e == hipSuccess)
+      e = given ? step_of<T, kLaws>("tree_rest", a, w, kAll, few(a.Q), inv_t, s)
+                : step_of<T, kBoth>("tree_rest", a, w, kAll, few(a.Q), inv_t, s);
+  } else {
+    e = step_of<T, kLaws>("tree_laws", a, w, kAll, many(a.Q), inv_t, s);
+  }
+  if (given) return e;
   for (int k = 1; k < a.max_children && k < a.Q - 1 && e == hipSuccess; ++k)
-    e = launch_timed("tree_round", tree_round_kernel<T, E>, grid, dim3(kThreads), s, a, w, S, R, k, c, inv_t);
+    e = step_of<T, kExcess>("tree_round", a, w, kAll, few(a.Q), inv_t, s);
   return e;
 }
 template <class T, int E>
@@ -641,25 +724,22 @@ hipError_t draw_run(const VerifyTreeArgs& a, const Tree& w, double inv_t, hipStr
 
 size_t verify_tree_ws_bytes(int B, int Q, int V) { return tree_layout(B, Q, V).bytes; }
 int64_t verify_tree_groups(int B, int Q, int V) {
-  const int64_t laws = law_rows(B, Q) * slices(V, per_thread(law_rows(B, Q), V));
-  return laws > (int64_t)B * slices(V, per_thread(B, V)) ? laws : (int64_t)B * slices(V, per_thread(B, V));
+  return (int64_t)B * (many(Q) > few(Q) ? many(Q) : few(Q)) * slices(V, per_thread(B, V));
 }
 
 hipError_t verify_tree_launch(const VerifyTreeArgs& a, sd_type type, double temperature, void* ws, hipStream_t s) {
   const double inv_t = 1.0 / temperature;
   const TreeWs l = tree_layout(a.B, a.Q, a.V);
   char* base = static_cast<char*>(ws);
-  const Tree w{reinterpret_cast<Node*>(base + l.nodes),       reinterpret_cast<int32_t*>(base + l.list),
-               reinterpret_cast<int32_t*>(base + l.count),    reinterpret_cast<uint32_t*>(base + l.arrived),
-               reinterpret_cast<float*>(base + l.chance),     reinterpret_cast<double*>(base + l.sums),
-               reinterpret_cast<float*>(base + l.maxima),     reinterpret_cast<double*>(base + l.mass),
+  const Tree w{reinterpret_cast<Node*>(base + l.nodes),   reinterpret_cast<uint32_t*>(base + l.arrived),
+               reinterpret_cast<float*>(base + l.chance), reinterpret_cast<double*>(base + l.sums),
+               reinterpret_cast<float*>(base + l.maxima), reinterpret_cast<double*>(base + l.mass),
                reinterpret_cast<float*>(base + l.peak)};
   hipError_t e = launch_timed("tree_plan", tree_plan_kernel, dim3((unsigned)a.B), dim3(64), s, a, w);
   if (e != hipSuccess) return e;
   return by_type(type, [&](auto tag) {
     typedef decltype(tag) T;
-    hipError_t e = hipSuccess;
-    if (a.Q > 1) e = per_thread(law_rows(a.B, a.Q), a.V) == 32 ? laws_run<T, 32>(a, w, inv_t, s) : laws_run<T, 8>(a, w, inv_t, s);
+    const hipError_t e = a.Q > 1 ? laws_run<T>(a, w, inv_t, s) : hipSuccess;
     if (e != hipSuccess) return e;
     return per_thread(a.B, a.V) == 32 ? draw_run<T, 32>(a, w, inv_t, s) : draw_run<T, 8>(a, w, inv_t, s);
   });

@@ -315,3 +315,33 @@ def test_the_next_token_follows_the_targets_law(draws):
     want = (q.double() / q.double().sum()) * B
     assert float(((n - want) ** 2 / want).sum()) < 31
     assert 0.3 < float((got["tau"] > 1).double().mean()) < 1.0
+
+
+# 40 * 2^20 logits and more: the root's law comes first, then its children's, then what the walk may still come to.
+@pytest.mark.parametrize("near", [1.0, 4.0])
+@pytest.mark.parametrize("draws,t", [("iid", "f32"), ("distinct", "bf16"), ("given", "f16"), ("distinct", "f16")])
+def test_much_work_in_stages(draws, t, near):
+    B, Q, V, wide = 24, 32, 60001, 4
+    draft, target, tokens, trees, un = _inputs(B, Q, V, wide, draws, t, 90 + int(near), near=near)
+    rows = [(7 * b) % 33 for b in range(B)]
+    got = _lib.sd_verify_tree(draft, target, tokens, _i32(trees), draws=DRAWS[draws], max_children=wide, uniforms=un, rows=_i32(rows))
+    _check(draft, target, tokens, trees, un, got, draws, rows=rows, wide=wide, seqs=range(0, B, 3))
+    again = _lib.sd_verify_tree(draft, target, tokens, _i32(trees), draws=DRAWS[draws], max_children=wide, uniforms=un, rows=_i32(rows))
+    for key, value in got.items():
+        assert torch.equal(value, again[key]), key
+    # the same trees a few at a time, whose nodes are all summed at once (in slices of another size)
+    part = slice(8, 11)
+    few = _lib.sd_verify_tree(None if draft is None else draft[part], target[part], tokens[part], _i32(trees[part]), draws=DRAWS[draws],
+                              max_children=wide, uniforms=un[part], rows=_i32(rows[part]))
+    assert torch.equal(few["tau"], got["tau"][part]) and torch.equal(few["path"], got["path"][part])
+
+
+def test_a_long_chain_in_stages():
+    B, K, V = 12, 63, 60001
+    draft, target, tokens, trees, un = _inputs(B, K + 1, V, 1, "iid", "bf16", 95, near=0.02)
+    trees = [[j - 1 for j in range(K + 1)]] * B
+    tokens[:, 1:] = draft[:, :K].float().argmax(-1).to(torch.int32)
+    un[:, :K] *= 0.9
+    got = _lib.sd_verify_tree(draft, target, tokens, _i32(trees), uniforms=un)
+    _check(draft, target, tokens, trees, un, got, "iid", seqs=[0, 5, 11])
+    assert (got["tau"] > 3).any()
