@@ -449,7 +449,7 @@ def _operands(name, types, **tensors):
     import torch
     dev = torch.cuda.current_device() if next(iter(tensors.values())).is_cuda else 0
     for what, t in tensors.items():
-        if t is not None and (t.get_device() != dev or not t.is_cuda):
+        if t is not None and t.get_device() != dev:  # (-1: in the host's memory)
             _need(False, name, f"{what} is on {t.device}, not on the current GPU")
     for what, want in types.items():
         t = tensors[what]
@@ -661,6 +661,15 @@ def sd_verify_tokens(draft, target, tokens, kb, uniforms=None, rnd=None, seed=0,
     return out
 
 
+def _table(name, pages, B):
+    """Width and row stride of a page table."""
+    if pages is None:
+        return 0, 0
+    shape, stride = pages.shape, pages.stride()
+    _need(len(shape) == 2 and shape[0] == B and stride[1] == 1, name, "pages must be [B][max_pages] with contiguous rows")
+    return shape[1], stride[0]
+
+
 def sd_latent_append(latent, k_rope, cache, lens, freq, pages=None, rows=None, cu=None, parents=None, q=None, q_out=None,
                      k_out=None, rope=SD_ROPE_PAIRS):
     """latent [B][Q][d_latent], k_rope [B][Q][d_rope] (None: d_rope = 0) into cache [n_pages][page_size][d_latent +
@@ -674,52 +683,53 @@ def sd_latent_append(latent, k_rope, cache, lens, freq, pages=None, rows=None, c
     """
     import torch
     name, i32, f64 = "sd_latent_append", torch.int32, torch.float64
-    lead = 1 if cu is not None else 2
-    _need(latent.dim() == lead + 1 and cache.dim() == 3 and latent.stride(lead) == 1 and cache.stride(2) == 1, name,
+    # (shapes and strides are read once: each reading is as long as several comparisons)
+    lead, ls, cs = 1 if cu is not None else 2, latent.shape, cache.shape
+    lst, cst = latent.stride(), cache.stride()
+    _need(len(ls) == lead + 1 and len(cs) == 3 and lst[lead] == 1 and cst[2] == 1, name,
           "latent must be [B][Q][d_latent], or [T][d_latent] with cu, and cache [n_pages][page_size][d] with contiguous d")
-    dc, dr, t = latent.shape[lead], cache.shape[2] - latent.shape[lead], latent.dtype
-    _need((k_rope is None and dr == 0) or (k_rope is not None and tuple(k_rope.shape) == (*latent.shape[:lead], dr) and
-                                           k_rope.stride(lead) == 1), name,
+    dc, t, tokens = ls[lead], latent.dtype, ls[:lead]
+    dr, H, none = cs[2] - dc, 0, sd_stride_h(0, 0, 0)
+    kst = None if k_rope is None else k_rope.stride()
+    _need((k_rope is None and dr == 0) or (k_rope is not None and k_rope.shape == (*tokens, dr) and kst[lead] == 1), name,
           "k_rope must be as latent with the rest of the cache's d, contiguous")
     _need(q is not None or q_out is None, name, "q_out goes with q")
-    H = 0
+    qst = ost = none
     if q is not None:
-        _need(q.dim() == lead + 2 and q.shape[:lead] == latent.shape[:lead] and q.shape[lead + 1] == dr and
-              q.stride(lead + 1) == 1 and q.shape[lead] > 0, name, "q must be [B][Q][H][d_rope], or [T][H][d_rope] with cu, contiguous in d")
-        H = q.shape[lead]
+        qs, qst = q.shape, q.stride()
+        _need(len(qs) == lead + 2 and qs[:lead] == tokens and qs[lead + 1] == dr and qst[lead + 1] == 1 and qs[lead] > 0, name,
+              "q must be [B][Q][H][d_rope], or [T][H][d_rope] with cu, contiguous in d")
+        H = qs[lead]
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        _need(q_out.shape == q.shape and q_out.stride(lead + 1) == 1, name, "q_out must be as q, contiguous in d")
-    _need(k_out is None or (k_rope is not None and k_out.shape == k_rope.shape and k_out.stride(lead) == 1), name,
+            q_out = torch.empty(qs, dtype=q.dtype, device=q.device)
+        ost = q_out.stride()
+        _need(q_out.shape == qs and ost[lead + 1] == 1, name, "q_out must be as q, contiguous in d")
+        qst = sd_stride_h(0, qst[0], qst[1]) if lead == 1 else sd_stride_h(qst[0], qst[1], qst[2])
+        ost = sd_stride_h(0, ost[0], ost[1]) if lead == 1 else sd_stride_h(ost[0], ost[1], ost[2])
+    ko = None if k_out is None else k_out.stride()
+    _need(k_out is None or (k_rope is not None and k_out.shape == k_rope.shape and ko[lead] == 1), name,
           "k_out must be as k_rope, contiguous in d")
     stream = _operands(name, dict(k_rope=t, cache=t, q=t, q_out=t, k_out=t, lens=i32, freq=f64, pages=i32, rows=i32, cu=i32,
                                   parents=i32),
                        latent=latent, k_rope=k_rope, cache=cache, lens=lens, freq=freq, pages=pages, rows=rows, cu=cu,
                        parents=parents, q=q, q_out=q_out, k_out=k_out)
     _need(lens.dim() == 1 and lens.is_contiguous(), name, "lens must be contiguous [B]")
-    B = lens.shape[0]
-    Q = latent.shape[0] if cu is not None else latent.shape[1]
-    _need(cu is not None or latent.shape[0] == B, name, "latent and lens must agree in B")
+    B, Q = lens.shape[0], ls[lead - 1]
+    _need(cu is not None or ls[0] == B, name, "latent and lens must agree in B")
     _need(cu is None or (cu.shape == (B + 1,) and cu.is_contiguous()), name, "cu must be contiguous [B + 1]")
     _need(dr == 0 or (freq is not None and freq.shape == (dr // 2,) and freq.is_contiguous()), name,
           "freq must be contiguous [d_rope / 2]")
     _need(rows is None or (rows.shape == (B,) and rows.is_contiguous()), name, "rows must be contiguous [B]")
     _need(parents is None or (parents.shape == (B, Q) and parents.is_contiguous()), name, "parents must be contiguous [B][Q]")
-    _need(pages is None or (pages.dim() == 2 and pages.shape[0] == B and pages.stride(1) == 1), name,
-          "pages must be [B][max_pages] with contiguous rows")
+    width, pst = _table(name, pages, B)
 
     def stride(x):
-        return sd_stride(0, 0) if x is None else sd_stride(*((0, x.stride(0)) if cu is not None else x.stride()[:2]))
+        return sd_stride(0, 0) if x is None else sd_stride(0, x[0]) if lead == 1 else sd_stride(x[0], x[1])
 
-    def stride_h(x):
-        return sd_stride_h(0, 0, 0) if x is None else sd_stride_h(*((0, *x.stride()[:2]) if cu is not None else x.stride()[:3]))
-
-    _check(load().sd_latent_append(B, Q, H, dc, dr, _type(latent), rope, _ptr(freq), latent.data_ptr(), stride(latent),
-                                   _ptr(k_rope), stride(k_rope), _ptr(cu), _ptr(parents), lens.data_ptr(), _ptr(rows),
-                                   cache.data_ptr(), cache.stride(0), cache.stride(1), cache.shape[0], cache.shape[1],
-                                   _ptr(pages), 0 if pages is None else pages.stride(0),
-                                   0 if pages is None else pages.shape[1], _ptr(k_out), stride(k_out), _ptr(q),
-                                   stride_h(q), _ptr(q_out), stride_h(q_out), stream), name)
+    _check(load().sd_latent_append(B, Q, H, dc, dr, _type(latent), rope, _ptr(freq), latent.data_ptr(), stride(lst),
+                                   _ptr(k_rope), stride(kst), _ptr(cu), _ptr(parents), lens.data_ptr(), _ptr(rows),
+                                   cache.data_ptr(), cst[0], cst[1], cs[0], cs[1], _ptr(pages), pst, width, _ptr(k_out),
+                                   stride(ko), _ptr(q), qst, _ptr(q_out), ost, stream), name)
     return q_out
 
 
@@ -791,7 +801,8 @@ def sd_latent_keep(cache, lens, tau, path, pages=None, rows=None, new_lens=None)
     """
     import torch
     name, i32 = "sd_latent_keep", torch.int32
-    _need(cache.dim() in (3, 4) and cache.stride(-1) == 1, name, "cache must be [layers][n_pages][page_size][d] with contiguous d")
+    shape, strides = cache.shape, cache.stride()
+    _need(len(shape) in (3, 4) and strides[-1] == 1, name, "cache must be [layers][n_pages][page_size][d] with contiguous d")
     _need(path.dim() == 2 and path.is_contiguous(), name, "path must be contiguous [B][Q]")
     B, Q = path.shape
     if new_lens is None:
@@ -799,14 +810,12 @@ def sd_latent_keep(cache, lens, tau, path, pages=None, rows=None, new_lens=None)
     stream = _operands(name, dict(lens=i32, tau=i32, path=i32, pages=i32, rows=i32, new_lens=i32),
                        cache=cache, lens=lens, tau=tau, path=path, pages=pages, rows=rows, new_lens=new_lens)
     for what, x in (("lens", lens), ("tau", tau), ("rows", rows), ("new_lens", new_lens)):
-        _need(x is None or (x.shape == (B,) and x.is_contiguous()), name, f"{what} must be contiguous [B]")
-    _need(pages is None or (pages.dim() == 2 and pages.shape[0] == B and pages.stride(1) == 1), name,
-          "pages must be [B][max_pages] with contiguous rows")
-    many = cache.dim() == 4
-    _check(load().sd_latent_keep(cache.shape[0] if many else 1, B, Q, cache.shape[-1], _type(cache), cache.data_ptr(),
-                                 cache.stride(0) if many else 0, cache.stride(-3), cache.stride(-2), cache.shape[-3],
-                                 cache.shape[-2], _ptr(pages), 0 if pages is None else pages.stride(0),
-                                 0 if pages is None else pages.shape[1], lens.data_ptr(), _ptr(rows), tau.data_ptr(),
+        if x is not None and not (x.shape == (B,) and x.is_contiguous()):
+            _need(False, name, f"{what} must be contiguous [B]")
+    width, pst = _table(name, pages, B)
+    layers, layer = (shape[0], strides[0]) if len(shape) == 4 else (1, 0)
+    _check(load().sd_latent_keep(layers, B, Q, shape[-1], _type(cache), cache.data_ptr(), layer, strides[-3], strides[-2],
+                                 shape[-3], shape[-2], _ptr(pages), pst, width, lens.data_ptr(), _ptr(rows), tau.data_ptr(),
                                  path.data_ptr(), new_lens.data_ptr(), stream), name)
     return new_lens
 
