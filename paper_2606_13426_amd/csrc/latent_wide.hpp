@@ -24,9 +24,9 @@
 // What bounds it, on MI355X: the matrix cores at the clock that they leave.  A tile takes 1.83 to 2.1 us
 // (1.25 to 1.09 PFLOP/s; the library's product of 8192^3 reaches 1.23), and 2.0 to 2.25 with the
 // exponentials, the reads of K or V or the tile loads left out.  Beside the tiles a workgroup's Q (147 KB) and
-// its O cost 30 to 40 us a call, most of it memory time, and the join of the parts of cut blocks 10 to 25: 8 trees of
-// 32 nodes, 128 heads, up to 6000 tokens 275 + 24 us (405 + 17 with 64 rows a workgroup), 1 of 64
-// nodes, 16 heads, 100000 tokens 228 + 15 (287 + 10).
+// its O (262 KB where it is a part) cost as much as 16 tiles, which the dealing of the tiles counts (kWideFixedTiles),
+// and the join of the parts of cut blocks 15 to 25 us: 8 trees of 32 nodes, 128 heads, up to 6000 tokens
+// 250 + 24 us (405 + 17 with 64 rows a workgroup), 1 of 64 nodes, 16 heads, 100000 tokens 215 + 15 (287 + 10).
 #pragma once
 
 #include "latent.hpp"
@@ -77,9 +77,17 @@ __device__ __forceinline__ float acc_read() {
   asm volatile("v_accvgpr_read_b32 %0, a[%1]" : "=v"(y) : "n"(I));
   return y;
 }
+// A run of tiles starts with Q and ends with its part of O, whatever its length.  So where the list of tiles is
+// dealt out, every block of rows has in front of its tiles a place as long as these take: a workgroup that comes
+// into the next block gets fewer tiles.  In tiles of 64 tokens; in us (both kernels) with 0 / 4 / 8 / 12:
+//   24 trees of 20 nodes, 32 heads, up to 5003: 183 / 152 / 143 / 144    8 of 32, 128 heads, up to 6000: 326 / 287 / 274 / 280
+//   1 of 64, 16 heads, 100000: 270 / 252 / 250 / 253                     64 of 16, 16 heads, up to 6400: 222 / 204 / 186 / 191
+// (In the kernel of few rows it gives 1 to 9 % and takes from a chain of nodes that its sums are
+// the chain form's bit by bit: not there.)
+constexpr int kWideFixedTiles = 8;
 template <class T>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) void latent_wide_kernel(Args a) {
-  constexpr int DC = 512, C = (DC + kRope) / 8, TK = 32, kRing = 4, TW = TK / 4, NL = TW * C / 64, KS = C / 2;
+  constexpr int DC = 512, C = (DC + kRope) / 8, TK = 32, kFixed = kWideFixedTiles, kRing = 4, TW = TK / 4, NL = TW * C / 64, KS = C / 2;
   constexpr int kTok = 16 * C, kBuf = TK * kTok;  // bytes of a token, of a tile
   constexpr int kAhead = 3, kFrags = 4;           // steps that K's operands are read ahead
   constexpr int kBehind = 6;                      // steps of S behind the barrier
@@ -99,9 +107,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
 
   // this team's run of the list of all sequences' tiles of 64 tokens
   auto supers_of = [&](int rows) { return (rows * a.H + kWideRows * a.p.team - 1) / (kWideRows * a.p.team); };
+  auto units_of = [&](int tiles, int rows) { return (tiles + (tiles > 0 ? kFixed : 0)) * supers_of(rows); };
   auto tiles_at = [&](int b0) {
     const int bb = min(b0 + lane, a.B - 1);
-    return b0 + lane < a.B ? tiles_of(length_of(a, bb)) * supers_of(rows_of(a, bb)) : 0;
+    return b0 + lane < a.B ? units_of(tiles_of(length_of(a, bb)), rows_of(a, bb)) : 0;
   };
   auto scan = [&](int v) {
 #pragma unroll
@@ -166,16 +175,21 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
 
   for (int seg = 0; left > 0; ++seg) {
     const int len = __builtin_amdgcn_readfirstlane(length_of(a, b)), nt = tiles_of(len);
-    const int nrow = __builtin_amdgcn_readfirstlane(rows_of(a, b)), units = nt * supers_of(nrow);
+    const int nrow = __builtin_amdgcn_readfirstlane(rows_of(a, b)), units = units_of(nt, nrow);
     if (within >= units) {
       within -= units;
       ++b;
       --seg;
       continue;
     }
-    const int super = within / nt, t0 = within - super * nt, t1 = min(t0 + left, nt);
-    within += t1 - t0;
-    left -= t1 - t0;
+    const int super = within / (nt + kFixed), u0 = within - super * (nt + kFixed), u1 = min(u0 + left, nt + kFixed);
+    const int t0 = max(u0 - kFixed, 0), t1 = max(u1 - kFixed, 0);
+    within += u1 - u0;
+    left -= u1 - u0;
+    if (t0 == t1) {
+      --seg;
+      continue;
+    }
     const int slot = seg == 0 ? 0 : 1;
     const bool whole = t0 == 0 && t1 == nt;
     if (member == 0 && t == 0) {
