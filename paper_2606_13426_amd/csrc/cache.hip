@@ -7,10 +7,15 @@
 // there, with sine and cosine by their power series in float32 (the first terms left out,
 // r^11 / 11! and r^12 / 12!, are below 2^-29); its heads share them.
 //
-// Keep.  A wavefront takes 64 pieces of 16 bytes of one sequence's vectors in one layer.
-// A kept vector's place is never behind its source (path rises), and a lane moves the
-// same piece of all of them, in order, eight at a time: no vector is overwritten before
-// it was read.
+// Keep.  A wavefront takes one sequence in one layer, eight vectors at a time: their pieces of
+// 16 bytes are dealt out to its lanes one after another.  A kept vector's place is never
+// behind its source (path rises), and eight are read before the first of them is written: no
+// vector is overwritten before it was read.
+//
+// What bounds them, on MI355X: memory, behind three or four trips that a token's place takes (lengths, parents,
+// page).  Append: 10766 tokens of 32 heads 24 us, 5.4 TB/s; 64 trees of up to 24 nodes, 128 heads 12.3 us, 3.4
+// TB/s (with the vectors asked for before the angles 12.6); one token 3.2.  Keep: 61 layers of 64
+// sequences of up to 24 nodes 11.2 us (13.2 where a wavefront took 64 pieces of every vector); one 3.5.
 #include "common.hpp"
 
 namespace sd {
@@ -185,19 +190,16 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, int64_t 
     if (h0 + k * slots < a.H) store_four(out + (h0 + k * slots) * a.qos.head, g, half, a.halves, turned<T>(f[k], t));
 }
 
-// Pieces of 64 to a wavefront.
-__host__ __device__ inline int chunks_of(int pieces) { return (pieces + 63) / 64; }
+constexpr int kBatch = 8, kMost = 72;  // vectors that a wavefront holds at once; pieces of a vector
 
 __global__ __launch_bounds__(kThreads) void keep_kernel(KeepArgs a, int64_t waves) {
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t unit = (int64_t)blockIdx.x * (kThreads / 64) + w;
   if (unit >= waves) return;
-  const int chunks = chunks_of(a.pieces);
-  const int chunk = (int)(unit % chunks), b = (int)(unit / chunks % a.B);
-  const int64_t layer = unit / chunks / a.B;
+  const int b = (int)(unit % a.B);
+  const int64_t layer = unit / a.B;
   const int n = a.rows ? min(max(a.rows[b], 0), a.Q) : a.Q, tau = min(max(a.tau[b], 0), n);
   const int64_t first = (int64_t)max(a.lens[b], 0) - n;
-  const int piece = chunk * 64 + lane;
   uint16_t* base = a.pages.cache;
   int before = -1, kept = 0;
   bool whole = true;
@@ -217,22 +219,23 @@ __global__ __launch_bounds__(kThreads) void keep_kernel(KeepArgs a, int64_t wave
       to = place_of(a.pages, b, first + j);
     }
     const int64_t src = from && to ? from - base : -1, dst = from && to ? to - base : -1;
-    uint16_t* mine = base + layer * a.layer_stride + 8 * piece;
-    for (int k0 = 0; k0 < count; k0 += 8) {
-      u32x4 held[8];
-      int64_t at[8];
+    uint16_t* mine = base + layer * a.layer_stride;
+    for (int k0 = 0; k0 < count; k0 += kBatch) {
+      u32x4 held[kBatch * kMost / 64];
+      int64_t at[kBatch * kMost / 64];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const int64_t f = k0 + k < count ? __shfl(src, k0 + k) : -1;
-        at[k] = k0 + k < count ? __shfl(dst, k0 + k) : -1;
-        if (f >= 0 && piece < a.pieces) held[k] = *reinterpret_cast<const u32x4*>(mine + f);
+      for (int i = 0; i < kBatch * kMost / 64; ++i) {
+        const int id = 64 * i + lane, v = id / a.pieces, piece = id - v * a.pieces, k = k0 + v;
+        const int64_t f = __shfl(src, k & 63), d = __shfl(dst, k & 63);
+        at[i] = v < kBatch && k < count && f >= 0 ? d + 8 * piece : -1;
+        if (at[i] >= 0) held[i] = *reinterpret_cast<const u32x4*>(mine + f + 8 * piece);
       }
 #pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (at[k] >= 0 && piece < a.pieces) *reinterpret_cast<u32x4*>(mine + at[k]) = held[k];
+      for (int i = 0; i < kBatch * kMost / 64; ++i)
+        if (at[i] >= 0) *reinterpret_cast<u32x4*>(mine + at[i]) = held[i];
     }
   }
-  if (a.new_lens && layer == 0 && chunk == 0 && lane == 0) a.new_lens[b] = (int)max(first + kept, (int64_t)0);
+  if (a.new_lens && layer == 0 && lane == 0) a.new_lens[b] = (int)max(first + kept, (int64_t)0);
 }
 
 }  // namespace
@@ -247,12 +250,10 @@ hipError_t append_launch(const AppendArgs& a, int64_t tokens, sd_type type, hipS
                               : launch_timed("latent_append", append_kernel<F16>, grid, dim3(kThreads), s, a, tokens);
 }
 
-int64_t keep_groups(int layers, int B, int pieces) {
-  return ((int64_t)layers * B * chunks_of(pieces) + kThreads / 64 - 1) / (kThreads / 64);
-}
+int64_t keep_groups(int layers, int B) { return ((int64_t)layers * B + kThreads / 64 - 1) / (kThreads / 64); }
 hipError_t keep_launch(const KeepArgs& a, hipStream_t s) {
-  const int64_t waves = (int64_t)a.layers * a.B * chunks_of(a.pieces);
-  return launch_timed("latent_keep", keep_kernel, dim3((unsigned)keep_groups(a.layers, a.B, a.pieces)), dim3(kThreads),
+  const int64_t waves = (int64_t)a.layers * a.B;
+  return launch_timed("latent_keep", keep_kernel, dim3((unsigned)keep_groups(a.layers, a.B)), dim3(kThreads),
                       s, a, waves);
 }
 

@@ -1463,7 +1463,7 @@ sd_status sd_latent_keep(int32_t layers, int32_t B, int32_t Q, int32_t d, sd_typ
   SD_CHECK_ARG(aligned(cache, 16), "sd_latent_keep: cache must be 16-byte aligned");
   SD_CHECK_ARG(!new_lens || (uintptr_t)(new_lens + B) <= (uintptr_t)lens || (uintptr_t)(lens + B) <= (uintptr_t)new_lens,
                "sd_latent_keep: new_lens overlaps lens");
-  SD_CHECK_ARG((int64_t)B * Q < ((int64_t)1 << 31) && keep_groups(layers, B, d / 8) <= kMaxGroups, "sd_latent_keep: too many rows for one call");
+  SD_CHECK_ARG((int64_t)B * Q < ((int64_t)1 << 31) && keep_groups(layers, B) <= kMaxGroups, "sd_latent_keep: too many rows for one call");
   a.layers = layers;
   a.B = B;
   a.Q = Q;

@@ -346,7 +346,7 @@ struct KeepArgs {
 };
 int64_t append_groups(int64_t tokens, int H, int dr);
 hipError_t append_launch(const AppendArgs& a, int64_t tokens, sd_type type, hipStream_t s);
-int64_t keep_groups(int layers, int B, int pieces);
+int64_t keep_groups(int layers, int B);
 hipError_t keep_launch(const KeepArgs& a, hipStream_t s);
 size_t latent_tree_ws_bytes(int B, int Q, int H, int dc, int dr);
 hipError_t latent_tree_launch(int B, int Q, int H, int dc, int dr, sd_type type, double scale, const void* q, sd_stride_h qs,
