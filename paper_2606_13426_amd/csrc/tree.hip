@@ -15,7 +15,7 @@
 // node that the walk may still come to (both laws, then S_k), slices of a row a workgroup, and the last of
 // a node's workgroups does the tries that the sum allows; the draw, which walks the decided
 // nodes from the root, sums the last r in slices and finds the token.  How many steps there are is
-// known on the host: one for the laws (three where they are much work) and one for every child behind
+// known on the host: one for the laws (three and more where they are much work) and one for every child behind
 // the first, and a node that is out by then costs nothing.  All in float64, as every border is
 // compared with a uniform.
 //
@@ -335,13 +335,11 @@ __device__ __forceinline__ void node_step(const VerifyTreeArgs& a, const Tree& w
   __syncthreads();
 }
 
-// A step of every open node that the walk may come to: of all of them, or of the root (kRoot) or of it and its
-// children (kNear) alone.  A node is out once another child of its parent is accepted or it is rejected.
+// A step of every open node that the walk may come to and that lies at most `deep` steps below the root.  A node is out once another child of its parent is accepted or it is rejected.
 // That may happen while this runs, and a workgroup that sees it leaves its slice out: then the node's
 // count of slices never fills, and it stays open.
-enum { kRoot, kNear, kAll };
 template <class T, int E, int SUMS>
-__global__ __launch_bounds__(kThreads) void tree_step_kernel(VerifyTreeArgs a, Tree w, int S, int R, int which, Scale c, double inv_t) {
+__global__ __launch_bounds__(kThreads) void tree_step_kernel(VerifyTreeArgs a, Tree w, int S, int R, int deep, Scale c, double inv_t) {
   const int slice = blockIdx.x % S, lane = threadIdx.x & 63;
   const int64_t id = blockIdx.x / S;
   const int b = (int)(id / R), worker = (int)(id % R);
@@ -359,18 +357,17 @@ __global__ __launch_bounds__(kThreads) void tree_step_kernel(VerifyTreeArgs a, T
   auto state_of = [&](int i) { return __builtin_amdgcn_readlane(state, i); };
   const uint64_t inner = __ballot(open != 0);
   uint64_t alive = 1, todo = inner & 1;  // (a parent comes before its children)
+  int depth = 0;
   while (todo) {
-    const int i = __ffsll((unsigned long long)todo) - 1;
-    const uint64_t more = of(open, i);
+    const int i = __ffsll((unsigned long long)todo) - 1, below = __builtin_amdgcn_readlane(depth, i) + 1;
+    const uint64_t more = below <= deep ? of(open, i) : 0;
     alive |= more;
+    if (more >> lane & 1u) depth = below;
     todo = (todo & (todo - 1)) | (more & inner);
-    if (which != kAll && (which == kRoot || i == 0)) todo = 0;
   }
   // (a node's workgroup is told by its place among all nodes with children, which does not change)
   const uint64_t kids = __ballot(kids_of != 0);
-  uint64_t mine = __ballot(decided(state) == kOpen) & kids & alive;
-  if (which == kRoot) mine &= 1;
-  for (; mine; mine &= mine - 1) {
+  for (uint64_t mine = __ballot(decided(state) == kOpen) & kids & alive; mine; mine &= mine - 1) {
     const int i = __ffsll((unsigned long long)mine) - 1;
     if (__popcll(kids & ((1ull << i) - 1ull)) % R != worker) continue;
     Node v{};
@@ -659,10 +656,14 @@ __global__ __launch_bounds__(kThreads) void tree_draw_kernel(VerifyTreeArgs a, T
 inline int many(int Q) { return Q > 1 ? Q / 2 : 1; }
 inline int few(int Q) { return Q > 4 ? 4 : Q > 1 ? Q - 1 : 1; }
 // Whether the root's law comes first, then its children's that are left, then the rest's: two launches more, and
-// most nodes out before they are summed.  In us, at once / in stages, by B Q V: 32000 x 12 36 / 51; 2^24 51 / 59,
+// most nodes out before they are summed.  A chain's next node is never out before the last one is summed: there the
+// stages go to depths 1, 3, 7 and so on.  In us, at once / in stages, by B Q V: 32000 x 12 36 / 51; 2^24 51 / 59,
 // 91 / 90; 2^25 93 / 95, 100 / 98; 46 x 2^20 132 / 121, 132 / 133; 2^26 127 / 115; 70 x 2^20 (given)
-// 82 / 70; 2^27 194 / 141; 2^29 (given) 450 / 116.
-inline bool in_stages(const VerifyTreeArgs& a) { return (int64_t)a.B * a.Q * a.V >= 40ll << 20; }
+// 82 / 70; 2^27 194 / 141; 2^29 (given) 450 / 116.  Chains: 20 x 2^20 (18 nodes) 87 / 92; 2^25 (64) 130 / 63;
+// 51 x 2^20 (32) 139 / 144; 91 x 2^20 (26) 195 / 145, with children of the root and the rest alone 174.
+inline bool in_stages(const VerifyTreeArgs& a) {
+  return (int64_t)a.B * a.Q * a.V >= (a.max_children == 1 ? 24ll << 20 : 40ll << 20);
+}
 
 struct TreeWs {
   size_t nodes, arrived, chance, sums, maxima, mass, peak, bytes;
@@ -681,36 +682,38 @@ TreeWs tree_layout(int B, int Q, int V) {
   return w;
 }
 
-// A step of the nodes that `which` says, by `workers` slices' workgroups a tree.
+// A step, by `workers` slices' workgroups a tree.
 template <class T, int E, int SUMS>
-hipError_t step_run(const char* name, const VerifyTreeArgs& a, const Tree& w, int which, int workers, double inv_t, hipStream_t s) {
+hipError_t step_run(const char* name, const VerifyTreeArgs& a, const Tree& w, int deep, int workers, double inv_t, hipStream_t s) {
   const int S = slices(a.V, E);
   return launch_timed(name, tree_step_kernel<T, E, SUMS>, dim3((unsigned)((int64_t)a.B * workers * S)), dim3(kThreads), s, a, w, S,
-                      workers, which, scale_of(inv_t), inv_t);
+                      workers, deep, scale_of(inv_t), inv_t);
 }
 template <class T, int SUMS>
-hipError_t step_of(const char* name, const VerifyTreeArgs& a, const Tree& w, int which, int workers, double inv_t, hipStream_t s) {
-  return per_thread((int64_t)a.B * workers, a.V) == 32 ? step_run<T, 32, SUMS>(name, a, w, which, workers, inv_t, s)
-                                                       : step_run<T, 8, SUMS>(name, a, w, which, workers, inv_t, s);
+hipError_t step_of(const char* name, const VerifyTreeArgs& a, const Tree& w, int deep, int workers, double inv_t, hipStream_t s) {
+  return per_thread((int64_t)a.B * workers, a.V) == 32 ? step_run<T, 32, SUMS>(name, a, w, deep, workers, inv_t, s)
+                                                       : step_run<T, 8, SUMS>(name, a, w, deep, workers, inv_t, s);
 }
 template <class T>
 hipError_t laws_run(const VerifyTreeArgs& a, const Tree& w, double inv_t, hipStream_t s) {
   const bool given = a.draws == SD_TREE_GIVEN;  // (no sum behind the laws')
   hipError_t e;
   if (in_stages(a)) {
-    e = step_of<T, kLaws>("tree_root", a, w, kRoot, 1, inv_t, s);
-    if (e == hipSuccess)
-      e = given ? step_of<T, kLaws>("tree_near", a, w, kNear, few(a.Q), inv_t, s)
-                : step_of<T, kBoth>("tree_near", a, w, kNear, few(a.Q), inv_t, s);
-    if (e == hipSuccess)
-      e = given ? step_of<T, kLaws>("tree_rest", a, w, kAll, few(a.Q), inv_t, s)
-                : step_of<T, kBoth>("tree_rest", a, w, kAll, few(a.Q), inv_t, s);
+    const bool chain = a.max_children == 1;
+    auto stage = [&](const char* name, int deep) {
+      if (e == hipSuccess)
+        e = given || chain ? step_of<T, kLaws>(name, a, w, deep, few(a.Q), inv_t, s)
+                           : step_of<T, kBoth>(name, a, w, deep, few(a.Q), inv_t, s);
+    };
+    e = step_of<T, kLaws>("tree_root", a, w, 0, 1, inv_t, s);
+    for (int deep = 1; deep < (chain ? a.Q - 2 : 2); deep = 2 * deep + 1) stage("tree_near", deep);
+    stage("tree_rest", a.Q);
   } else {
-    e = step_of<T, kLaws>("tree_laws", a, w, kAll, many(a.Q), inv_t, s);
+    e = step_of<T, kLaws>("tree_laws", a, w, a.Q, many(a.Q), inv_t, s);
   }
   if (given) return e;
   for (int k = 1; k < a.max_children && k < a.Q - 1 && e == hipSuccess; ++k)
-    e = step_of<T, kExcess>("tree_round", a, w, kAll, few(a.Q), inv_t, s);
+    e = step_of<T, kExcess>("tree_round", a, w, a.Q, few(a.Q), inv_t, s);
   return e;
 }
 template <class T, int E>

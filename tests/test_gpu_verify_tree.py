@@ -345,3 +345,22 @@ def test_a_long_chain_in_stages():
     got = _lib.sd_verify_tree(draft, target, tokens, _i32(trees), uniforms=un)
     _check(draft, target, tokens, trees, un, got, "iid", seqs=[0, 5, 11])
     assert (got["tau"] > 3).any()
+
+
+@pytest.mark.parametrize("draws", list(DRAWS))
+@pytest.mark.parametrize("B,K", [(11, 40), (210, 2)])
+def test_chains_in_stages_of_rising_depth(B, K, draws):
+    """One child a node is tried: of chains, and of trees whose other children are no part of it."""
+    V = 60001
+    draft, target, tokens, trees, un = _inputs(B, K + 1, V, 2, draws, "f16", 97, near=0.05)
+    trees = [[j - 1 for j in range(K + 1)] if b % 3 else trees[b] for b in range(B)]
+    for b in range(B):
+        for i in range(1, K + 1):
+            if b % 3 and draws != "given":
+                tokens[b, i] = draft[b, i - 1].float().argmax()
+            elif b % 3:
+                tokens[b, i] = target[b, i - 1].float().argmax()
+    un[:, :K] *= 0.9 if draws != "given" else 0.05
+    got = _lib.sd_verify_tree(draft, target, tokens, _i32(trees), draws=DRAWS[draws], max_children=1, uniforms=un)
+    _check(draft, target, tokens, trees, un, got, draws, wide=1, seqs=[0, 1, 2, 5, B - 1])
+    assert (got["tau"] > 2).any()
