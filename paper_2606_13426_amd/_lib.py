@@ -759,15 +759,19 @@ def sd_verify_tree(draft, target, tokens, parents, rows=None, draws=SD_TREE_IID,
     """
     import torch
     name, i32, f32 = "sd_verify_tree", torch.int32, torch.float32
-    _need(target.dim() == 3, name, "target must be [B][Q][V]")
-    B, Q, V = target.shape
-    _need(draft is None or (draft.shape == target.shape and draft.dtype == target.dtype), name,
+    shape, tst = target.shape, target.stride()
+    _need(len(shape) == 3, name, "target must be [B][Q][V]")
+    B, Q, V = shape
+    _need(draft is None or (draft.shape == shape and draft.dtype == target.dtype), name,
           "draft and target must be [B][Q][V] of one type")
+    dst = tst if draft is None else draft.stride()
+    _need(tst[2] == 1 and dst[2] == 1, name, "draft and target must have contiguous rows")
     stream = _operands(name, dict(tokens=i32, parents=i32, rows=i32, uniforms=torch.float64, ws=torch.uint8),
                        target=target, draft=draft, tokens=tokens, parents=parents, rows=rows, uniforms=uniforms, rnd=rnd,
                        ws=ws)
     for what, x in (("tokens", tokens), ("parents", parents), ("uniforms", uniforms)):
-        _need(x is None or (x.shape == (B, Q) and x.is_contiguous()), name, f"{what} must be contiguous [B][Q]")
+        if x is not None and not (x.shape == (B, Q) and x.is_contiguous()):
+            _need(False, name, f"{what} must be contiguous [B][Q]")
     _need(rows is None or (rows.shape == (B,) and rows.is_contiguous()), name, "rows must be contiguous [B]")
     _need(rnd is None or (rnd.shape == (B,) and rnd.dtype in (torch.int32, torch.uint32) and rnd.is_contiguous()), name,
           "rnd must be contiguous [B] of int32 or uint32")
@@ -786,8 +790,8 @@ def sd_verify_tree(draft, target, tokens, parents, rows=None, draws=SD_TREE_IID,
     if ws is None:
         ws = _workspace(sd_verify_tree_workspace(B, Q, V), target.device)
     _check(load().sd_verify_tree(B, Q, V, draws, _type(target), float(temperature), Q if max_children is None else max_children,
-                                 _ptr(draft), sd_stride(0, 0) if draft is None else stride3(draft), target.data_ptr(),
-                                 stride3(target), tokens.data_ptr(), parents.data_ptr(), _ptr(rows), _ptr(uniforms),
+                                 _ptr(draft), sd_stride(dst[0], dst[1]), target.data_ptr(),
+                                 sd_stride(tst[0], tst[1]), tokens.data_ptr(), parents.data_ptr(), _ptr(rows), _ptr(uniforms),
                                  _ptr(rnd), seed, out["tau"].data_ptr(), out["token"].data_ptr(), out["path"].data_ptr(),
                                  _ptr(out.get("accept")), ws.data_ptr(), ws.numel(), stream), name)
     return out

@@ -139,3 +139,11 @@ def test_the_binding_refuses():
             (lambda: _lib.sd_latent_keep(cache, i(2), i(2), i(2, 4)), "not on the current GPU")):
         with pytest.raises(_lib.SpecDiffError, match=match):
             call()
+
+
+def test_the_binding_refuses_logits_whose_rows_are_not_contiguous():
+    x, i = torch.zeros(2, 10, 3), torch.zeros(2, 3, dtype=torch.int32)
+    with pytest.raises(_lib.SpecDiffError, match="contiguous rows"):
+        _lib.sd_verify_tree(x.transpose(1, 2), x.transpose(1, 2), i, i, uniforms=torch.zeros(2, 3, dtype=torch.float64))
+    with pytest.raises(_lib.SpecDiffError, match="contiguous rows"):
+        _lib.sd_verify_tree(x.transpose(1, 2), torch.zeros(2, 3, 10), i, i, uniforms=torch.zeros(2, 3, dtype=torch.float64))
