@@ -82,7 +82,11 @@ __device__ __forceinline__ float acc_read() {
 // into the next block gets fewer tiles.  In tiles of 64 tokens; in us (both kernels) with 0 / 4 / 8 / 12:
 //   24 trees of 20 nodes, 32 heads, up to 5003: 183 / 152 / 143 / 144    8 of 32, 128 heads, up to 6000: 326 / 287 / 274 / 280
 //   1 of 64, 16 heads, 100000: 270 / 252 / 250 / 253                     64 of 16, 16 heads, up to 6400: 222 / 204 / 186 / 191
-// (In the kernel of few rows it gives 1 to 9 % and takes from a chain of nodes that its sums are
+// And where the longest block is no longer than a workgroup's share, and as many blocks as a workgroup gets at most take no
+// longer than a share with a cut block's cost, none is cut: 8 trees of 32 nodes, 128 heads, up to 400 tokens 77 / 62,
+// 30 of 46, 16 heads, up to 383 tokens 65 / 57, 48 of 64, 16 heads, 300 tokens 113 / 105 (with longer ones
+// uncut too, 8 of 32, 128 heads, up to 1600 117 / 130).
+// (In the kernel of few rows the first gives 1 to 9 % and takes from a chain of nodes that its sums are
 // the chain form's bit by bit: not there.)
 constexpr int kWideFixedTiles = 8;
 template <class T>
@@ -100,6 +104,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
   __shared__ uint32_t present[kRing];             // which tokens of a tile are there
   __shared__ uint32_t offs[NL][64];               // the byte offsets of a wavefront's pieces from its first token
   __shared__ float sums[kWideRows], refs[kWideRows];
+  __shared__ int uncut;  // (in LDS: it is asked once a run, and registers are short)
 
   const int t = threadIdx.x, lane = t & 63, n = lane & 31, hf = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(t >> 6);
@@ -120,13 +125,23 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
     }
     return v;
   };
-  int total = 0;
-  for (int b0 = 0; b0 < a.B; b0 += 64) total += __builtin_amdgcn_readlane(scan(tiles_at(b0)), 63);
+  int total = 0, blocks = 0, longest = 0;
+  for (int b0 = 0; b0 < a.B; b0 += 64) {
+    total += __builtin_amdgcn_readlane(scan(tiles_at(b0)), 63);
+    const int bb = min(b0 + lane, a.B - 1), nt = tiles_of(length_of(a, bb));
+    blocks += __builtin_amdgcn_readlane(scan(b0 + lane < a.B && nt > 0 ? supers_of(rows_of(a, bb)) : 0), 63);
+    longest = max(longest, nt);
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) longest = max(longest, __shfl_xor(longest, d));
   const int teams = min(a.p.teams, total);
   if (team >= teams) return;
   const int share = total / teams, more = total - share * teams;
   const int begin = team * share + min(team, more);
   int left = share + (team < more ? 1 : 0);
+  // Short blocks are not cut where that takes no longer: an end that falls into a block goes to its nearer end.
+  const int most = (blocks + teams - 1) / teams;
+  if (t == 0) uncut = longest <= share && (int64_t)most * total <= (int64_t)blocks * (share + kFixed);
   int b = 0, within = 0;
   for (int b0 = 0, at = 0;; b0 += 64) {
     const int mine = tiles_at(b0), upto = scan(mine);
@@ -183,9 +198,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
       continue;
     }
     const int super = within / (nt + kFixed), u0 = within - super * (nt + kFixed), u1 = min(u0 + left, nt + kFixed);
-    const int t0 = max(u0 - kFixed, 0), t1 = max(u1 - kFixed, 0);
+    int t0 = max(u0 - kFixed, 0), t1 = max(u1 - kFixed, 0);
     within += u1 - u0;
     left -= u1 - u0;
+    if (uniform((uint32_t)uncut)) {
+      t0 = 2 * u0 >= nt + kFixed ? nt : 0;
+      t1 = 2 * u1 >= nt + kFixed ? nt : 0;
+    }
     if (t0 == t1) {
       --seg;
       continue;
