@@ -753,7 +753,7 @@ def sd_verify_tree(draft, target, tokens, parents, rows=None, draws=SD_TREE_IID,
                    seed=0, temperature=1.0, ws=None, out=None):
     """draft (None with SD_TREE_GIVEN) and target [B][Q][V] logits of one type (rows contiguous); tokens, parents
     [B][Q], rows [B] (None: Q each) int32; uniforms [B][Q] float64, or rnd [B] int32/uint32 and the seed.
-    max_children: how many children of a node are tried (None: all; each one more is one more kernel).
+    max_children: how many children of a node are tried at most (None, Q or more: all; each one more is one more kernel).
 
     Returns dict of device tensors tau, token [B], path [B][Q] int32, accept [B][Q] float32.
     """
@@ -789,7 +789,7 @@ def sd_verify_tree(draft, target, tokens, parents, rows=None, draws=SD_TREE_IID,
                   f"{k} must be contiguous {'[B][Q]' if wide else '[B]'}")
     if ws is None:
         ws = _workspace(sd_verify_tree_workspace(B, Q, V), target.device)
-    _check(load().sd_verify_tree(B, Q, V, draws, _type(target), float(temperature), Q if max_children is None else max_children,
+    _check(load().sd_verify_tree(B, Q, V, draws, _type(target), float(temperature), Q if max_children is None else min(max_children, Q),
                                  _ptr(draft), sd_stride(dst[0], dst[1]), target.data_ptr(),
                                  sd_stride(tst[0], tst[1]), tokens.data_ptr(), parents.data_ptr(), _ptr(rows), _ptr(uniforms),
                                  _ptr(rnd), seed, out["tau"].data_ptr(), out["token"].data_ptr(), out["path"].data_ptr(),

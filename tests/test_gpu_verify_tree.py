@@ -364,3 +364,13 @@ def test_chains_in_stages_of_rising_depth(B, K, draws):
     got = _lib.sd_verify_tree(draft, target, tokens, _i32(trees), draws=DRAWS[draws], max_children=1, uniforms=un)
     _check(draft, target, tokens, trees, un, got, draws, wide=1, seqs=[0, 1, 2, 5, B - 1])
     assert (got["tau"] > 2).any()
+
+
+@pytest.mark.parametrize("draws", list(DRAWS))
+def test_more_children_than_nodes_are_all(draws):
+    draft, target, tokens, trees, un = _inputs(4, 3, 900, 6, draws, "f32", 99)
+    want = _lib.sd_verify_tree(draft, target, tokens, _i32(trees), draws=DRAWS[draws], uniforms=un)
+    for most in (2, 3, 6, 1000):
+        got = _lib.sd_verify_tree(draft, target, tokens, _i32(trees), draws=DRAWS[draws], uniforms=un, max_children=most)
+        assert all(torch.equal(got[k], want[k]) for k in want)
+    _check(draft, target, tokens, trees, un, want, draws)
