@@ -7,9 +7,10 @@
 // max(0, r_k - p / rest_k) has the positive part where q > (a_k + S_k / rest_k) p.  rest_k is 1
 // for independent draws; for draws without replacement what the tries so far leave of p, summed
 // beside S_k (1 less their mass is no number where p is all but one token), and a tried x
-// needs no care in S_k: it was rejected, so q(x) < a_{k+1} p(x), and a only grows.  The k-th child is accepted with h_k = max(0, q/p - a_k) rest_k / S_k.  So a try behind the
-// first costs one sum over the vocabulary.  Given candidates cost none: r_k is q without
-// the tried ones, h_k = q(x) / (1 - their mass).
+// needs no care in S_k: it was rejected, so q(x) < a_{k+1} p(x), and a only grows.  The k-th
+// child is accepted with h_k = max(0, q/p - a_k) rest_k / S_k.  So a try behind the first costs
+// one sum over the vocabulary.  Given candidates cost none: r_k is q without the tried
+// ones, h_k = q(x) / (1 - their mass).
 //
 // Kernels: the trees (who has which children); steps, each of which makes the next sum of every open
 // node that the walk may still come to (both laws, then S_k), slices of a row a workgroup, and the last of
@@ -21,7 +22,7 @@
 //
 // What bounds it: float64 exponentials, 16 products each (1.2e12 a second reached), where laws are summed, and for
 // small calls launches and each one's trips to memory (5 us for the trees, 7 to 10 a step, 12 the draw).  1 tree
-// of 12 over 32000 36 us, 24 of 24 over 50001 (given) 46, 32 of 32 over 131072 (distinct) 141: 194 with
+// of 12 over 32000 36 us, 24 of 24 over 50001 (given) 46, 32 of 32 over 131072 (distinct) 141 (in graphs): 194 with
 // every node's laws at once.
 #include "common.hpp"
 #include "laws.hpp"
