@@ -246,3 +246,61 @@ def test_many_rows_of_many_trees():
     _check(q, far[:, None], [40], _grown(4, 1, 16), 512, table, None, 0.06, got, "bf16")
     got = _lib.sd_latent_attention_tree(q, far[None], _i32([40]), _i32(_grown(4, 1, 16)), 512, scale=0.06)
     _check(q, far[None], [40], _grown(4, 1, 16), 512, None, None, 0.06, got, "bf16")
+
+
+@pytest.mark.parametrize("B,Q,H,longest", [(48, 64, 16, 300), (130, 33, 12, 200), (20, 60, 32, 520), (300, 16, 8, 90)])
+def test_many_rows_in_blocks_that_are_not_cut(B, Q, H, longest):
+    lens = [longest - (b * 41) % (longest - 3) if b % 7 else [0, Q, -2, longest][b // 7 % 4] for b in range(B)]
+    rows = [Q - (b * 5) % Q if b % 5 else [Q, 0, Q + 3, -1][b // 5 % 4] for b in range(B)]
+    q, cache, ln, pages = chain._case(B, Q, H, 512, 64, lens, "bf16", 31, page=16)
+    pages = _roomy(pages, 16, B, Q * H)
+    parents = _grown(41, B, Q)
+    out, lse = torch.full((B, Q, H, 512), 7.0, dtype=torch.bfloat16, device=DEV), torch.full((B, Q, H), 7.0, device=DEV)
+    got = _lib.sd_latent_attention_tree(q, cache, ln, _i32(parents), 512, pages=pages, scale=0.06, rows=_i32(rows), out=out, lse=lse)
+    seqs = sorted({0, 1, 5, 7, 14, 21, B // 2, B - 2, B - 1} & set(range(B)))
+    _check(q, cache, lens, parents, 512, pages, rows, 0.06, got, "bf16", seqs=seqs, heads=[0, H - 1])
+    for b in range(B):
+        n = min(max(rows[b], 0), Q)
+        assert (out[b, n:] == 7).all() and (lse[b, n:] == 7).all() and torch.isfinite(out[b, :n].float()).all()
+
+
+def test_many_rows_in_a_graph_and_on_two_streams():
+    """Replays see new queries, lengths and trees; a workspace holds nothing of the call before."""
+    B, Q, H, dc, t = 3, 24, 32, 512, "bf16"
+    lens = [900, 333, 1500]
+    q, cache, ln, pages = chain._case(B, Q, H, dc, 64, lens, t, 44, page=48)
+    pages = _roomy(pages, 48, B, Q * H)
+    parents = _i32(_grown(6, B, Q))
+    ws = torch.empty(_lib.sd_latent_attention_tree_workspace(B, Q, H, dc, 64), dtype=torch.uint8, device=DEV)
+    other = torch.empty_like(ws)
+    outs = [torch.zeros(B, Q, H, dc, dtype=TYPES[t], device=DEV) for _ in range(3)]
+    lses = [torch.zeros(B, Q, H, device=DEV) for _ in range(3)]
+
+    def call(k, w):
+        return _lib.sd_latent_attention_tree(q, cache, ln, parents, dc, pages=pages, scale=0.05, out=outs[k], lse=lses[k], ws=w)
+
+    call(0, ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(0, ws)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for i in range(4):
+        ws.fill_(0xA5)
+        torch.cuda.synchronize()
+        graph.replay()
+        for k, (s, w) in enumerate(zip(streams, (ws, other))):
+            if k == 0:
+                torch.cuda.synchronize()
+                w.fill_(0xFF)
+            s.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(s):
+                call(1 + k, w)
+        torch.cuda.synchronize()
+        for k in (1, 2):
+            assert torch.equal(outs[0], outs[k]) and torch.equal(lses[0], lses[k]), (i, k)
+        _check(q, cache, ln.tolist(), parents.tolist(), dc, pages, None, 0.05, (outs[0], lses[0]), t, heads=[i, H - 1])
+        q.copy_(q.flip(1))
+        ln.copy_(_i32([[40, 1400, 24], [700, 701, 24 + i], [1500, 333, 64]][i % 3]).clamp(max=pages.shape[1] * 48))
+        ln.clamp_(max=_i32(lens))
+        parents.copy_(_i32(_grown(7 + i, B, Q)))

@@ -374,3 +374,28 @@ def test_more_children_than_nodes_are_all(draws):
         got = _lib.sd_verify_tree(draft, target, tokens, _i32(trees), draws=DRAWS[draws], uniforms=un, max_children=most)
         assert all(torch.equal(got[k], want[k]) for k in want)
     _check(draft, target, tokens, trees, un, want, draws)
+
+
+@pytest.mark.parametrize("draws", list(DRAWS))
+def test_stages_in_a_graph(draws):
+    B, Q, V, wide = 24, 32, 60001, 4
+    draft, target, tokens, trees, un = _inputs(B, Q, V, wide, draws, "bf16", 120, near=2.0)
+    ws = torch.empty(_lib.sd_verify_tree_workspace(B, Q, V), dtype=torch.uint8, device=DEV)
+    parents, kw = _i32(trees), dict(draws=DRAWS[draws], max_children=wide)
+    _lib.sd_verify_tree(draft, target, tokens, parents, uniforms=un, ws=ws, **kw)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        kept = _lib.sd_verify_tree(draft, target, tokens, parents, uniforms=un, ws=ws, **kw)
+    for i in range(4):
+        ws.fill_(0xA5 if i % 2 else 0xFF)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        want = _lib.sd_verify_tree(draft, target, tokens, parents, uniforms=un, **kw)
+        for key in want:
+            assert torch.equal(want[key], kept[key]), (i, key)
+        if i < 2:
+            _check(draft, target, tokens, parents.tolist(), un, kept, draws, wide=wide, seqs=[i, 11])
+        un.copy_(un.flip(0))
+        parents.copy_(parents.flip(0))
