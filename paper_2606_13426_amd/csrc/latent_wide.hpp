@@ -21,8 +21,8 @@
 // tile is of no use once its S is made: half of the tile's P takes its place (so d_rope is 64 here, and
 // d_latent 512).
 //
-// What bounds it, on MI355X: the matrix cores at the clock that they leave.  A tile takes 1.83 to 2.1 us
-// (1.25 to 1.09 PFLOP/s; the library's product of 8192^3 reaches 1.23), and 2.0 to 2.25 with the
+// What bounds it, on MI355X: the rate of matrix instructions that the card sustains.  A tile takes 1.83 to 2.1 us
+// (1.25 to 1.09 PFLOP/s; the library's product of 8192^3 reaches 1.23), and no less (2.0 to 2.25) with the
 // exponentials, the reads of K or V or the tile loads left out.  Beside the tiles a workgroup's Q (147 KB) and
 // its O (262 KB where it is a part) cost as much as 16 tiles, which the dealing of the tiles counts (kWideFixedTiles),
 // and the join of the parts of cut blocks 15 to 25 us: 8 trees of 32 nodes, 128 heads, up to 6000 tokens
