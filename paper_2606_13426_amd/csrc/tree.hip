@@ -338,44 +338,56 @@ __device__ __forceinline__ void node_step(const VerifyTreeArgs& a, const Tree& w
 
 // A step of every open node that the walk may come to and that lies at most `deep` steps below the root.  A node is out once another child of its parent is accepted or it is rejected.
 // That may happen while this runs, and a workgroup that sees it leaves its slice out: then the node's
-// count of slices never fills, and it stays open.
+// count of slices never fills, and it stays open.  A workgroup's wavefronts have to agree on its nodes, as they meet in
+// barriers at each: the first one reads the states, once, and hands the list to all.  (What else they read of a node on it
+// stays as it is in this launch: it changes when the last of the node's slices is counted, and this workgroup's is one.)
 template <class T, int E, int SUMS>
 __global__ __launch_bounds__(kThreads) void tree_step_kernel(VerifyTreeArgs a, Tree w, int S, int R, int deep, Scale c, double inv_t) {
+  __shared__ uint64_t list_s, kids_s[kNodes];
   const int slice = blockIdx.x % S, lane = threadIdx.x & 63;
   const int64_t id = blockIdx.x / S;
   const int b = (int)(id / R), worker = (int)(id % R);
   const Node* nodes = w.nodes + (int64_t)b * a.Q;
-  const int state = lane < a.Q ? get(&nodes[lane].state) : kNone;
-  const uint64_t kids_of = lane < a.Q ? nodes[lane].kids : 0;
-  uint64_t open = kids_of;  // the children of node `lane` that are not out
-  if (decided(state) != kOpen) open = decided(state) == kNone ? 0ull : 1ull << (decided(state) - 1);
-  else
-    for (int k = state >> 8; k > 0; --k) open &= open - 1;
-  auto of = [](uint64_t v, int i) {
-    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, i) |
-           (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), i) << 32;
-  };
-  auto state_of = [&](int i) { return __builtin_amdgcn_readlane(state, i); };
-  const uint64_t inner = __ballot(open != 0);
-  uint64_t alive = 1, todo = inner & 1;  // (a parent comes before its children)
-  int depth = 0;
-  while (todo) {
-    const int i = __ffsll((unsigned long long)todo) - 1, below = __builtin_amdgcn_readlane(depth, i) + 1;
-    const uint64_t more = below <= deep ? of(open, i) : 0;
-    alive |= more;
-    if (more >> lane & 1u) depth = below;
-    todo = (todo & (todo - 1)) | (more & inner);
+  if (threadIdx.x < 64) {
+    const int state = lane < a.Q ? get(&nodes[lane].state) : kNone;
+    const uint64_t kids_of = lane < a.Q ? nodes[lane].kids : 0;
+    uint64_t open = kids_of;  // the children of node `lane` that are not out
+    if (decided(state) != kOpen) open = decided(state) == kNone ? 0ull : 1ull << (decided(state) - 1);
+    else
+      for (int k = state >> 8; k > 0; --k) open &= open - 1;
+    auto of = [](uint64_t v, int i) {
+      return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, i) |
+             (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), i) << 32;
+    };
+    const uint64_t inner = __ballot(open != 0);
+    uint64_t alive = 1, todo = inner & 1;  // (a parent comes before its children)
+    int depth = 0;
+    while (todo) {
+      const int i = __ffsll((unsigned long long)todo) - 1, below = __builtin_amdgcn_readlane(depth, i) + 1;
+      const uint64_t more = below <= deep ? of(open, i) : 0;
+      alive |= more;
+      if (more >> lane & 1u) depth = below;
+      todo = (todo & (todo - 1)) | (more & inner);
+    }
+    // (a node's workgroup is told by its place among all nodes with children, which does not change)
+    const uint64_t kids = __ballot(kids_of != 0);
+    const bool here = decided(state) == kOpen && kids_of != 0 && __popcll(kids & ((1ull << lane) - 1ull)) % R == worker;
+    // (of the laws' own sums: nodes that have none yet)
+    const uint64_t mine = __ballot(here && !(SUMS == kLaws && state >> 8)) & alive;
+    kids_s[lane] = kids_of;
+    if (lane == 0) list_s = mine;
   }
-  // (a node's workgroup is told by its place among all nodes with children, which does not change)
-  const uint64_t kids = __ballot(kids_of != 0);
-  for (uint64_t mine = __ballot(decided(state) == kOpen) & kids & alive; mine; mine &= mine - 1) {
+  __syncthreads();
+  auto uniform = [](uint64_t v) {
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)v) |
+           (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(v >> 32)) << 32;
+  };
+  for (uint64_t mine = uniform(list_s); mine; mine &= mine - 1) {
     const int i = __ffsll((unsigned long long)mine) - 1;
-    if (__popcll(kids & ((1ull << i) - 1ull)) % R != worker) continue;
     Node v{};
     if (SUMS == kLaws) {  // (nothing more is known of it yet)
-      if (state_of(i) >> 8) continue;
       v.S = v.rest = 1.0;
-      v.kids = of(kids_of, i);
+      v.kids = uniform(kids_s[i]);
     } else {
       v = nodes[i];
       if (SUMS == kExcess && !v.steps) continue;

@@ -399,3 +399,18 @@ def test_stages_in_a_graph(draws):
             _check(draft, target, tokens, parents.tolist(), un, kept, draws, wide=wide, seqs=[i, 11])
         un.copy_(un.flip(0))
         parents.copy_(parents.flip(0))
+
+
+@pytest.mark.parametrize("draws", list(DRAWS))
+def test_equal_calls_have_equal_bits_where_nodes_are_decided_meanwhile(draws):
+    """More workgroups than the card holds at once, trees with many inner nodes for each: some start while a node of their
+    tree is being decided."""
+    B, Q, V, wide = 32, 48, 100003, 4
+    draft, target, tokens, trees, un = _inputs(B, Q, V, wide, draws, "bf16", 130, near=1.5)
+    assert all(len(set(t[1:])) > 9 for t in trees)
+    call = lambda: _lib.sd_verify_tree(draft, target, tokens, _i32(trees), draws=DRAWS[draws], max_children=wide, uniforms=un)  # noqa: E731
+    got = call()
+    _check(draft, target, tokens, trees, un, got, draws, wide=wide, seqs=range(0, B, 8))
+    for _ in range(20):
+        again = call()
+        assert all(torch.equal(got[k], again[k]) for k in got)
