@@ -356,6 +356,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
     for (int s = 0; s < kAhead; ++s) kread(s);
     const u32x4 zero{0u, 0u, 0u, 0u};
     each<16>([&](auto blk) { acc_zero<decltype(blk)::value>(zero); });
+    // the first tile's weights take the place of its rotary parts, which all wavefronts have read now
+    lds_barrier();
     // wait states for a read of the last results behind a branch
     __builtin_amdgcn_sched_barrier(0);
     asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 7");
