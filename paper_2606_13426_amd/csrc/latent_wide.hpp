@@ -89,6 +89,8 @@ __device__ __forceinline__ float acc_read() {
 // (In the kernel of few rows the first gives 1 to 9 % and takes from a chain of nodes that its sums are
 // the chain form's bit by bit: not there.)
 constexpr int kWideFixedTiles = 8;
+// How many of a block's first `rows` rows are w, w + 4, w + 8 and so on: a wavefront's at the output.
+__host__ __device__ constexpr int rows_of_wave(int rows, int w) { return rows > w ? (rows - w + 3) / 4 : 0; }
 template <class T>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) void latent_wide_kernel(Args a) {
   constexpr int DC = 512, C = (DC + kRope) / 8, TK = 32, kFixed = kWideFixedTiles, kRing = 4, TW = TK / 4, NL = TW * C / 64, KS = C / 2;
@@ -589,7 +591,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
       to = reinterpret_cast<uint64_t>(a.out + (int64_t)b * a.os + (int64_t)i * a.orow + (int64_t)h * a.oh);
       if (hf == 0 && a.lse) a.lse[((int64_t)b * a.Q + i) * a.H + h] = (ref + __builtin_amdgcn_logf(sum)) * kLn2;
     }
-    const int rows_here = whole ? max(min((rlast - r0 - w) / 4 + 1, kWideRows / 4), 0) : kWideRows / 4;
+    const int rows_here = whole ? rows_of_wave(rlast - r0 + 1, w) : kWideRows / 4;
     // O goes by way of the ring, in whole lines: half of the columns at a time, [128 rows][256] in pieces of 16 bytes
     // that are permuted by the row; piece 16 w + p is columns 128 w + 64 half + 4 p ..
     each<2>([&](auto which) {

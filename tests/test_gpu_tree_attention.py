@@ -304,3 +304,26 @@ def test_many_rows_in_a_graph_and_on_two_streams():
         ln.copy_(_i32([[40, 1400, 24], [700, 701, 24 + i], [1500, 333, 64]][i % 3]).clamp(max=pages.shape[1] * 48))
         ln.clamp_(max=_i32(lens))
         parents.copy_(_i32(_grown(7 + i, B, Q)))
+
+
+@pytest.mark.parametrize("t", list(TYPES))
+@pytest.mark.parametrize("lens", [(40, 64), (300, 61), (64, 7000)])
+@pytest.mark.parametrize("Q,H,rows", [(55, 7, (55, 37)), (64, 2, (64, 1)), (43, 3, (43, 1)), (3, 43, (3, 3)), (2, 65, (2, 1)), (1, 131, (1, 1)),
+                                      (64, 3, (43, 64))])
+def test_many_rows_that_leave_one_to_three_in_a_block(Q, H, rows, lens, t):
+    """A block's last rows are fewer than the wavefronts that store them; whole blocks (one tile) and cut ones."""
+    B = 2
+    q, cache, ln, pages = chain._case(B, Q, H, 512, 64, list(lens), t, 7 * Q + H, 16)
+    pages = _roomy(pages, 16, B, Q * H)
+    parents = _grown(B + Q, B, Q)
+    out, lse = torch.full((B, Q, H, 528), 7.0, dtype=TYPES[t], device=DEV), torch.full((B, Q, H), 7.0, device=DEV)
+    _lib.sd_profile_enable(True)
+    got = _lib.sd_latent_attention_tree(q, cache, ln, _i32(parents), 512, pages=pages, scale=0.06, out=out[..., 8:520], lse=lse,
+                                        rows=_i32(list(rows)))
+    torch.cuda.synchronize()
+    _lib.sd_profile_enable(False)
+    assert "latent_wide" in _lib.sd_profile_read()
+    _check(q, cache, list(lens), parents, 512, pages, list(rows), 0.06, got, t, heads=None if H < 8 else [0, H // 2, H - 1])
+    assert (out[..., :8] == 7).all() and (out[..., 520:] == 7).all()
+    for b in range(B):
+        assert (out[b, rows[b]:] == 7).all() and (lse[b, rows[b]:] == 7).all()
