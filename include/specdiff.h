@@ -671,7 +671,7 @@ sd_status sd_verify_tree(int32_t B, int32_t Q, int32_t V, sd_tree_draws draws, s
  * cache [layers][n_pages][page_size][d] of 16-bit `type`, layers layer_stride elements
  * apart, one page table for all; d a multiple of 8 in [8, 576]; strides multiples of 8
  * elements, 16-byte addresses.  path [B][Q], tau, lens, rows (NULL: Q) [B]; new_lens [B],
- * nullable, may not overlap lens.  No workspace. */
+ * nullable, may not overlap lens, rows, tau or path.  No workspace. */
 sd_status sd_latent_keep(int32_t layers, int32_t B, int32_t Q, int32_t d, sd_type type, void* cache,
                          int64_t layer_stride, int64_t page_stride, int64_t token_stride,
                          int32_t n_pages, int32_t page_size, const int32_t* pages,

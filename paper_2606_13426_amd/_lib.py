@@ -801,7 +801,7 @@ def sd_latent_keep(cache, lens, tau, path, pages=None, rows=None, new_lens=None)
     """cache [n_pages][page_size][d] or [layers][n_pages][page_size][d] of a 16-bit type (d contiguous); lens, tau [B],
     path [B][Q] (sd_verify_tree's), rows [B] (None: Q each), pages [B][max_pages] (None: page b is sequence b) int32.
 
-    Returns new_lens [B] int32 (None: a new tensor; not lens itself).
+    Returns new_lens [B] int32 (None: a new tensor; none of lens, rows, tau or path).
     """
     import torch
     name, i32 = "sd_latent_keep", torch.int32

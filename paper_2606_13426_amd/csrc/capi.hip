@@ -1461,9 +1461,13 @@ sd_status sd_latent_keep(int32_t layers, int32_t B, int32_t Q, int32_t d, sd_typ
                                apart(sd_stride_h{layer_stride, page_stride, token_stride}, layers, n_pages, page_size, d)),
                "sd_latent_keep: layer stride must be a multiple of 8 elements that leaves no two vectors in one place");
   SD_CHECK_ARG(aligned(cache, 16), "sd_latent_keep: cache must be 16-byte aligned");
-  SD_CHECK_ARG(!new_lens || (uintptr_t)(new_lens + B) <= (uintptr_t)lens || (uintptr_t)(lens + B) <= (uintptr_t)new_lens,
-               "sd_latent_keep: new_lens overlaps lens");
   SD_CHECK_ARG((int64_t)B * Q < ((int64_t)1 << 31) && keep_groups(layers, B) <= kMaxGroups, "sd_latent_keep: too many rows for one call");
+  // (the first layer's wavefronts write it while those of other layers still read)
+  auto apart_from_new = [&](const int32_t* p, int64_t n) {
+    return !new_lens || !p || (uintptr_t)(new_lens + B) <= (uintptr_t)p || (uintptr_t)(p + n) <= (uintptr_t)new_lens;
+  };
+  SD_CHECK_ARG(apart_from_new(lens, B) && apart_from_new(rows, B) && apart_from_new(tau, B) && apart_from_new(path, (int64_t)B * Q),
+               "sd_latent_keep: new_lens overlaps lens, rows, tau or path");
   a.layers = layers;
   a.B = B;
   a.Q = Q;

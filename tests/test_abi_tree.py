@@ -147,3 +147,11 @@ def test_the_binding_refuses_logits_whose_rows_are_not_contiguous():
         _lib.sd_verify_tree(x.transpose(1, 2), x.transpose(1, 2), i, i, uniforms=torch.zeros(2, 3, dtype=torch.float64))
     with pytest.raises(_lib.SpecDiffError, match="contiguous rows"):
         _lib.sd_verify_tree(x.transpose(1, 2), torch.zeros(2, 3, 10), i, i, uniforms=torch.zeros(2, 3, dtype=torch.float64))
+
+
+@pytest.mark.parametrize("kw", [dict(tau=P), dict(rows=P), dict(path=P), dict(path=ctypes.c_void_p(256 - 4 * 7)), dict(tau=ctypes.c_void_p(252)),
+                                dict(rows=ctypes.c_void_p(260))])
+def test_latent_keep_refuses_new_lengths_over_what_other_layers_read(lib, kw):
+    """B = 2, Q = 4: eight bytes of new lengths at 256, the other arrays elsewhere but for one."""
+    far = {k: ctypes.c_void_p(4096 * (i + 1)) for i, k in enumerate(("lens", "rows", "tau", "path"))}
+    _refused(_keep(lib, **{**far, **kw, "new_lens": P}), "overlaps")
