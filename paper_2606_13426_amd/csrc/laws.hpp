@@ -14,7 +14,7 @@ using namespace logits;
 
 // What a slice says of its part of a row.
 struct Part {
-  double S, U;  // sums against the slice's own maximum
+  double S, U;  // sums against the slice's own maximum m: of the weights w, and of w (x - m), which log-probabilities need
   float m;      // -inf: nothing but -inf in it
   float pad;
 };
@@ -68,7 +68,8 @@ __device__ __forceinline__ double weight_or_tiny(float x, float m, Scale c) {
   return pow2(fmax((double)x - (double)m, c.low), c.c);
 }
 
-// The same without U and in float64 throughout: verification divides differences of two laws by one another.
+// The maximum of a workgroup's slice x and the weights' sum against it (NaN where a value is NaN or +inf; U is 0, verification has no
+// use for it), in float64 throughout: verification divides differences of two laws by one another.
 template <class T, int E>
 __device__ __forceinline__ Part slice_sums64(const float (&x)[E], Scale c, double* red, float* redm) {
   const int t = threadIdx.x, w = t >> 6;
