@@ -638,8 +638,9 @@ typedef enum { SD_TREE_IID = 0, SD_TREE_DISTINCT = 1, SD_TREE_GIVEN = 2 } sd_tre
  * S_k = sum_x max(0, q_i - a_k p_i), a_{k+1} = a_k + S_k (DISTINCT: S_k over the mass
  * that the tries have left of p_i), so a try costs one sum over the vocabulary.
  * A log-ratio log q_i - log p_i below 2^-44 is 0.
- * max_children in [1, Q]: at most so many children of a node are tried (the calls'
- * number grows with it).
+ * max_children in [1, Q]: at most so many children of a node are tried.  The kernels'
+ * number grows with it (but for SD_TREE_GIVEN), whatever the trees have: Q where they have
+ * 4 at most costs 64 nodes 4 to 5 us for every child that there is not.
  * tau[b] = 1 + accepted drafts; path[b][0..tau-1] their nodes, the root first, -1
  * behind; accept[b][i] (nullable) = min(1, h) of the nodes that were tried, -1 of others.
  * A draft outside [0, V), of target probability 0, a sibling's token once more

@@ -753,7 +753,9 @@ def sd_verify_tree(draft, target, tokens, parents, rows=None, draws=SD_TREE_IID,
                    seed=0, temperature=1.0, ws=None, out=None):
     """draft (None with SD_TREE_GIVEN) and target [B][Q][V] logits of one type (rows contiguous); tokens, parents
     [B][Q], rows [B] (None: Q each) int32; uniforms [B][Q] float64, or rnd [B] int32/uint32 and the seed.
-    max_children: how many children of a node are tried at most (None, Q or more: all; each one more is one more kernel).
+    max_children: how many children of a node are tried at most (None, Q or more: all).  Each one more is one more kernel but with
+    SD_TREE_GIVEN, whether a node has so many or not: a caller says what its trees have (trees of 64 nodes with up to 4
+    children, independent draws, 4 / None: one over 32000 tokens 40 / 254 us, 32 over 131072 197 / 479 us).
 
     Returns dict of device tensors tau, token [B], path [B][Q] int32, accept [B][Q] float32.
     """

@@ -13,9 +13,9 @@
 // vector is overwritten before it was read.
 //
 // What bounds them, on MI355X: memory, behind three or four trips that a token's place takes (lengths, parents,
-// page).  Append: 10766 tokens of 32 heads 24 us, 5.4 TB/s; 64 trees of up to 24 nodes, 128 heads 12.3 us, 3.4
-// TB/s (with the vectors asked for before the angles 12.6); one token 3.2.  Keep: 61 layers of 64
-// sequences of up to 24 nodes 11.2 us (13.2 where a wavefront took 64 pieces of every vector); one 3.5.
+// page).  Append: 10766 tokens of 32 heads 24 us, 5.4 TB/s; 64 trees of up to 24 nodes, 128 heads 12.2 us, 3.4
+// TB/s (with the vectors asked for before the angles 12.6); one token 3.4.  Keep: 61 layers of 64
+// sequences of up to 24 nodes 10.9 us (13.2 where a wavefront took 64 pieces of every vector); one 4.1.
 #include "common.hpp"
 
 namespace sd {

@@ -93,11 +93,11 @@ inline Plan plan(int B, int Q, int H, int capacity) {
 // The kernel of 128 rows a workgroup (latent_wide.hpp), for trees: by its tiles of 128 rows and 64 tokens, 12 a
 // compute unit where sequences are cut (its parts to join are twice as large), 2 where there is a block of rows for
 // most compute units and mostly done whole.  In us (all kernels), at most 64 rows a workgroup / 128:
-//   1 tree of 64 nodes, 16 heads, 6400 tokens, 3.1 tiles a unit:  48 / 56    25600, 12.5: 95 / 88     100000, 49: 290 / 225
-//   64 trees of 16 nodes, 16 heads, 1600 tokens, 12.5:            92 / 104   3200, 25:    160 / 160   6400, 50:   300 / 255
-//   24 trees of 20 nodes, 32 heads, 400 tokens, 3.3:              62 / 68    1600, 11.7:  104 / 102   6400, 47:   300 / 244
-//   8 trees of 32 nodes, 128 heads (256 blocks), 100 tokens, 2:   66 / 49    6400, 100:   596 / 395
-//   30 trees of up to 46 nodes, 16 heads (180 blocks), up to 383 tokens, 4.2:  68 / 57
+//   1 tree of 64 nodes, 16 heads, 6400 tokens, 3.1 tiles a unit:  53 / 59    25600, 12.5: 99 / 93     100000, 49: 293 / 227
+//   64 trees of 16 nodes, 16 heads, 1600 tokens, 12.5:            94 / 108   3200, 25:    161 / 161   6400, 50:   304 / 263
+//   24 trees of 20 nodes, 32 heads (120 blocks), 400 tokens, 3.3: 63 / 57    1600, 11.7:  107 / 103   6400, 47:   303 / 259
+//   8 trees of 32 nodes, 128 heads (256 blocks), 100 tokens, 2:   64 / 50    6400, 100:   575 / 423
+//   30 trees of up to 46 nodes, 16 heads (180 blocks), up to 383 tokens, 4.2:  66 / 57
 constexpr int kWideRows = 128, kWideR = kWideRows / 16;
 inline bool wide_fits(int64_t rows, int dc, int dr) { return rows >= kWideRows && dc == 512 && dr == kRope; }
 inline Plan tree_plan(int B, int Q, int H, int dc, int dr, int capacity) {

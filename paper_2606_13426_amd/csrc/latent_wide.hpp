@@ -26,7 +26,10 @@
 // exponentials, the reads of K or V or the tile loads left out.  Beside the tiles a workgroup's Q (147 KB) and
 // its O (262 KB where it is a part) cost as much as 16 tiles, which the dealing of the tiles counts (kWideFixedTiles),
 // and the join of the parts of cut blocks 15 to 25 us: 8 trees of 32 nodes, 128 heads, up to 6000 tokens
-// 250 + 24 us (405 + 17 with 64 rows a workgroup), 1 of 64 nodes, 16 heads, 100000 tokens 215 + 15 (287 + 10).
+// 241 + 24 us (399 + 17 with 64 rows a workgroup), 1 of 64 nodes, 16 heads, 100000 tokens 212 + 15 (282 + 10); in a long row of
+// calls, on a warm card, 268 + 26 and 249 + 17.
+//
+// The weights P are rounded to the operands' type, half a step each, as in latent.hpp; S, maxima, sums and O are float32.
 #pragma once
 
 #include "latent.hpp"
@@ -80,12 +83,12 @@ __device__ __forceinline__ float acc_read() {
 // A run of tiles starts with Q and ends with its part of O, whatever its length.  So where the list of tiles is
 // dealt out, every block of rows has in front of its tiles a place as long as these take: a workgroup that comes
 // into the next block gets fewer tiles.  In tiles of 64 tokens; in us (both kernels) with 0 / 4 / 8 / 12:
-//   24 trees of 20 nodes, 32 heads, up to 5003: 183 / 152 / 143 / 144    8 of 32, 128 heads, up to 6000: 326 / 287 / 274 / 280
-//   1 of 64, 16 heads, 100000: 270 / 252 / 250 / 253                     64 of 16, 16 heads, up to 6400: 222 / 204 / 186 / 191
+//   24 trees of 20 nodes, 32 heads, up to 5003: 181 / 166 / 155 / 164    8 of 32, 128 heads, up to 6000: 293 / 273 / 264 / 273
+//   1 of 64, 16 heads, 100000: 240 / 222 / 227 / 233                     64 of 16, 16 heads, up to 6400: 195 / 179 / 172 / 178
 // And where the longest block is no longer than a workgroup's share, and as many blocks as a workgroup gets at most take no
 // longer than a share with a cut block's cost, none is cut: 8 trees of 32 nodes, 128 heads, up to 400 tokens 77 / 62,
-// 30 of 46, 16 heads, up to 383 tokens 65 / 57, 48 of 64, 16 heads, 300 tokens 113 / 105 (with longer ones
-// uncut too, 8 of 32, 128 heads, up to 1600 117 / 130).
+// 30 of 46, 16 heads, up to 383 tokens 64 / 57, 48 of 64, 16 heads, 300 tokens 114 / 109 (with longer ones
+// uncut too, 8 of 32, 128 heads, up to 1600 117 / 122).
 // (In the kernel of few rows the first gives 1 to 9 % and takes from a chain of nodes that its sums are
 // the chain form's bit by bit: not there.)
 constexpr int kWideFixedTiles = 8;

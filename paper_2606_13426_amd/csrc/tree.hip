@@ -21,9 +21,9 @@
 // compared with a uniform.
 //
 // What bounds it: float64 exponentials, 16 products each (1.2e12 a second reached), where laws are summed, and for
-// small calls launches and each one's trips to memory (5 us for the trees, 7 to 10 a step, 12 the draw).  1 tree
-// of 12 over 32000 36 us, 24 of 24 over 50001 (given) 46, 32 of 32 over 131072 (distinct) 141 (in graphs): 194 with
-// every node's laws at once.
+// small calls launches and each one's trips to memory (3 to 6 us for the trees, 4 to 14 a later step, 10 to 20 the draw).  In
+// us, a call among others / in a graph of its own: 1 tree of 12 over 32000 28 to 30 / 36, 24 of 24 over 50001 (given) 41 /
+// 44, 32 of 32 over 131072 (distinct) 144 to 155 / 139 (190 with every node's laws at once).
 #include "common.hpp"
 #include "laws.hpp"
 #include "logits.hpp"
@@ -670,10 +670,14 @@ inline int many(int Q) { return Q > 1 ? Q / 2 : 1; }
 inline int few(int Q) { return Q > 4 ? 4 : Q > 1 ? Q - 1 : 1; }
 // Whether the root's law comes first, then its children's that are left, then the rest's: two launches more, and
 // most nodes out before they are summed.  A chain's next node is never out before the last one is summed: there the
-// stages go to depths 1, 3, 7 and so on.  In us, at once / in stages, by B Q V: 32000 x 12 36 / 51; 2^24 51 / 59,
-// 91 / 90; 2^25 93 / 95, 100 / 98; 46 x 2^20 132 / 121, 132 / 133; 2^26 127 / 115; 70 x 2^20 (given)
-// 82 / 70; 2^27 194 / 141; 2^29 (given) 450 / 116.  Chains: 20 x 2^20 (18 nodes) 87 / 92; 2^25 (64) 130 / 63;
-// 51 x 2^20 (32) 139 / 144; 91 x 2^20 (26) 195 / 145, with children of the root and the rest alone 174.
+// stages go to depths 1, 3, 7 and so on.  In us (graphs), at once / in stages, trees x nodes x vocabulary:
+//   1 x 12 x 32000 36 / 51     4 x 32 x 131072 49 / 60    16 x 12 x 131072 90 / 89   32 x 32 x 32000 98 / 96
+//   8 x 32 x 131072 89 / 92    64 x 16 x 50001 132 / 132  32 x 12 x 131072 129 / 120 16 x 32 x 131072 124 / 115
+//   32 x 32 x 131072 190 / 139
+//   given: 24 x 24 x 50001 44 / 51   8 x 32 x 131072 45 / 48   16 x 24 x 131072 56 / 58   64 x 24 x 50001 80 / 70
+//   64 x 64 x 131072 386 / 115
+//   chains: 20 x 18 x 60620 81 / 91   4 x 64 x 131072 114 / 61   32 x 32 x 52733 130 / 138   25 x 26 x 147437 183 / 145 (an
+//   earlier form with children of the root and the rest alone: 174)
 inline bool in_stages(const VerifyTreeArgs& a) {
   return (int64_t)a.B * a.Q * a.V >= (a.max_children == 1 ? 24ll << 20 : 40ll << 20);
 }
